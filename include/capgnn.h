@@ -480,6 +480,68 @@ int capgnn_sigmoid_bce(int64_t n, int C, const float *Z, int64_t ldz, const uint
                        const uint8_t *mask, double loss_norm, float *loss_dev, void *dZ, int64_t lddz,
                        int dz_dtype, void *ws, size_t ws_bytes, void *stream);
 
+/* ------------------------------------------------------------------------------------------
+ * What a classifier answers with, and what it learns from another one's answers.  Rows of logits Z: device [n x ldz] of
+ * z_dtype (C classes; rows need no alignment beyond their elements'), divided by `temperature` (finite, > 0) before the softmax.
+ * p_i = softmax(Z_i / temperature).  A logit of -infinity bars its class: p = 0, nothing is added to the entropy and no gradient
+ * flows through it.  A row whose classes are all barred is empty.  A NaN or +infinity makes the row's numbers NaN, no other row's.
+ * mask: device uint8[n] or NULL: rows with 0 are never read.  dZ may be Z itself if type and pitch are the same too (each
+ * logit is then replaced by its gradient); else they must not overlap.  No result depends on the order of atomic operations.
+ * Asynchronous on `stream`, which belongs to the current device; nothing is allocated, so calls can be recorded into HIP graphs
+ * (calls that may overlap in time need a workspace each).
+ * ---------------------------------------------------------------------------------------- */
+#define CAPGNN_TOP_MAX 64      /* most likely classes of a row that one call returns          */
+#define CAPGNN_GIVEN_MAX 256   /* classes given per row (m), classes of a teacher (k)         */
+
+/* Log-probabilities of given classes, entropy and the most likely classes of every row:
+ *   logp[i,a]  = ln p_i[ids[i,a]], a < m <= CAPGNN_GIVEN_MAX; 0 where ids[i,a] is outside [0,C) (a row with fewer classes than
+ *                columns).  ids: device int32 [n x ldi], any order, the same class any number of times; logp: device float [n x ldp].
+ *   entropy[i] = -sum_j p_ij ln p_ij; device float[n] or NULL.
+ *   stats[i]   = { max_j Z_ij, ln sum_j exp((Z_ij - max) / temperature) }: what the backward pass reads; the row's log normaliser is
+ *                stats[i][0] / temperature + stats[i][1].  device float [n x 2] or NULL.
+ *   top_ids[i,0:k], top_logp[i,0:k] = the k <= min(C, CAPGNN_TOP_MAX) classes of the largest logits, largest first, and their
+ *                log-probabilities; equal logits in ascending class order; a NaN counts as larger than everything.  device
+ *                int32 / float [n x ldt]; either may be NULL, both only when k is 0.
+ * An empty row gives log-probabilities of -infinity, entropy 0 and stats { -infinity, -infinity }; a masked-out row gives 0
+ * everywhere and top_ids of -1.  Sums are formed in float.
+ * ws: capgnn_logprobs_workspace_bytes(n, C, k) (a few long rows are split over workgroups; 0 bytes: ws may be NULL).
+ * Errors: EINVAL, ENOMEM (workspace too small), EHIP. */
+size_t capgnn_logprobs_workspace_bytes(int64_t n, int C, int k);
+int capgnn_logprobs(int64_t n, int C, const void *Z, int64_t ldz, int z_dtype, float temperature, const uint8_t *mask,
+                    const int32_t *ids, int64_t ldi, int m, float *logp, int64_t ldp, float *entropy, float *stats,
+                    int k, int32_t *top_ids, float *top_logp, int64_t ldt, void *ws, size_t ws_bytes, void *stream);
+
+/* Its gradient.  dlogp: device float [n x lddp], gradient w.r.t. logp (NULL with m = 0); dentropy: device float[n], gradient w.r.t.
+ * entropy, or NULL.  stats, and entropy where there is dentropy: as capgnn_logprobs left them for the same Z and temperature.
+ *   dZ_ij = ( sum_{a: ids[i,a] = j} dlogp[i,a] - p_ij ( G_i + dentropy[i] (ln p_ij + entropy[i]) ) ) / temperature,
+ * G_i = sum of dlogp[i,a] over the ids inside [0,C).  A class given several times gets the sum, added in the order of a.  Masked-out and
+ * empty rows: 0.  dZ: device [n x lddz] of dz_dtype, rounded once.  (The gradient of a top class's log-probability: pass top_ids as ids.) */
+int capgnn_logprobs_bwd(int64_t n, int C, const void *Z, int64_t ldz, int z_dtype, float temperature, const uint8_t *mask,
+                        const float *stats, const float *entropy, const int32_t *ids, int64_t ldi, int m, const float *dlogp,
+                        int64_t lddp, const float *dentropy, void *dZ, int64_t lddz, int dz_dtype, void *stream);
+
+/* Distillation from a teacher's top logits: the divergence of a row's p from the teacher's distribution q over the classes
+ * teacher_ids[i,0:k] (1 <= k <= CAPGNN_GIVEN_MAX; device int32 / float [n x ldt], e.g. top_ids / top_logp of capgnn_logprobs), and its gradient.
+ *   rest = 0: q_a = exp(v_a / temperature) / sum_b exp(v_b / temperature), v = teacher_val[i,:], logits or log-probabilities alike:
+ *             the teacher's mass is taken to lie on its k classes.
+ *             row_loss[i] = sum_a q_a (ln q_a - ln p_i[t_a])
+ *   rest = 1: v are log-probabilities at this temperature, q_a = exp(v_a), and what is left, r = 1 - sum_a q_a (less than 2^-20 is
+ *             rounding and counts as 0), is one more outcome, "none of the k classes", which the row gives P = sum of its other p:
+ *             row_loss[i] = sum_a q_a (ln q_a - ln p_i[t_a]) + r (ln r - ln P).
+ * loss = weight / norm * sum over masked rows of row_loss; norm = loss_norm, or the number of masked rows (at least 1) when
+ * loss_norm <= 0.  (The usual weight is temperature^2.)  dZ = gradient of that loss (0 in masked-out rows); added to what dZ holds when
+ * accumulate != 0 (a loss on labels next to this one; dZ must not be Z then).
+ * Entries with teacher_ids outside [0,C) or a value of -infinity are none (lists of different lengths); a class listed twice is an
+ * outcome with the sum of its q.  A row without any entry left, and an empty row, adds 0 to loss and gradient; one that gives
+ * a listed class with q > 0 probability 0 has an infinite loss and a finite gradient.
+ * loss_dev: device float[1]; row_loss: device float[n] or NULL (0 in masked-out rows); dZ: device [n x lddz] of dz_dtype or NULL.
+ * ws: capgnn_distill_workspace_bytes(n, C).  Errors: EINVAL, ENOMEM, EHIP. */
+size_t capgnn_distill_workspace_bytes(int64_t n, int C);
+int capgnn_distill(int64_t n, int C, const void *Z, int64_t ldz, int z_dtype, const int32_t *teacher_ids, const float *teacher_val,
+                   int64_t ldt, int k, int rest, float temperature, const uint8_t *mask, double loss_norm, float weight,
+                   float *loss_dev, float *row_loss, void *dZ, int64_t lddz, int dz_dtype, int accumulate, void *ws,
+                   size_t ws_bytes, void *stream);
+
 #define CAPGNN_MAX_RECORDS 96
 #define CAPGNN_K_GATHER_HIT   1
 #define CAPGNN_K_GATHER_MISS  2

@@ -345,6 +345,91 @@ def softmax_ce(Z, y, mask=None, norm: float = 0.0):
     return float(loss), dZ
 
 
+def row_softmax(Z, temperature: float = 1.0):
+    """ln p, p, max, ln sum exp((Z - max) / temperature) of every row in float64; barred classes (-inf) have p = 0; a row of barred
+    classes only has ln p = -inf everywhere."""
+    Z = _f64(Z)
+    top = Z.max(1)
+    ref = np.where(np.isneginf(top), 0.0, top)
+    with np.errstate(divide="ignore", over="ignore", invalid="ignore"):
+        d = (Z - ref[:, None]) / temperature
+        ln_s = np.log(np.exp(d).sum(1))
+        lp = np.where(np.isneginf(ln_s)[:, None], -np.inf, d - ln_s[:, None])
+        return lp, np.exp(lp), top, ln_s
+
+
+def logprobs(Z, ids, k: int, temperature: float = 1.0, mask=None):
+    """dict(logp, entropy, stats, top_ids, top_logp): capgnn_logprobs, from the definitions.  The classes of a row in the order of the
+    answer: NaN first, then by value, equal values in ascending class order."""
+    Z = _f64(Z)
+    n, C = Z.shape
+    on = np.ones(n, bool) if mask is None else np.asarray(mask).astype(bool)
+    lp, p, top, ln_s = row_softmax(np.where(on[:, None], Z, 0.0), temperature)
+    ids = np.asarray(ids, np.int64).reshape(n, -1)
+    ok = (ids >= 0) & (ids < C)
+    logp = np.where(ok, np.take_along_axis(lp, np.where(ok, ids, 0), 1), 0.0)
+    with np.errstate(invalid="ignore"):
+        ent = -np.where(p == 0.0, 0.0, p * lp).sum(1)
+    order = np.argsort(np.where(np.isnan(Z), -np.inf, -np.where(np.isnan(Z), 0.0, Z) + 0.0), axis=1, kind="stable") if not np.isposinf(Z).any() else \
+        np.array([sorted(range(C), key=lambda j: (0 if np.isnan(r[j]) else 1, 0.0 if np.isnan(r[j]) else -r[j], j)) for r in Z]).reshape(n, C)
+    order = order[:, :k]
+    res = {"logp": logp, "entropy": ent, "stats": np.stack([top, ln_s], 1), "top_ids": order,
+           "top_logp": np.take_along_axis(lp, order, 1)}
+    for key, v in res.items():
+        v[~on] = -1 if key == "top_ids" else 0
+    return res
+
+
+def logprobs_bwd(Z, ids, dlogp, dentropy=None, temperature: float = 1.0, mask=None):
+    """Gradient of sum(dlogp * logp) + sum(dentropy * entropy) w.r.t. Z, by the chain rule of the two definitions."""
+    Z = _f64(Z)
+    n, C = Z.shape
+    on = np.ones(n, bool) if mask is None else np.asarray(mask).astype(bool)
+    lp, p, top, ln_s = row_softmax(np.where(on[:, None], Z, 0.0), temperature)
+    onto = np.zeros((n, C))
+    for i in range(n):
+        for c, g in zip(np.asarray(ids)[i], _f64(dlogp)[i]):
+            if 0 <= c < C:
+                onto[i, c] += g
+    dZ = onto - p * onto.sum(1, keepdims=True)
+    if dentropy is not None:
+        with np.errstate(invalid="ignore"):
+            plp = np.where(p == 0.0, 0.0, p * lp)
+        dZ -= _f64(dentropy)[:, None] * (plp - p * plp.sum(1, keepdims=True))
+    dZ /= temperature
+    dZ[~on | np.isneginf(ln_s)] = 0.0
+    return dZ
+
+
+def distill(Z, t_ids, t_val, rest: bool = False, temperature: float = 1.0, mask=None, norm: float = 0.0, weight: float = 1.0):
+    """(loss, row_loss, dZ, extras) of capgnn_distill from its definition; extras: the teacher's q per class, its remainder r, P, p."""
+    Z, t_val = _f64(Z), _f64(t_val)
+    n, C = Z.shape
+    on = np.ones(n, bool) if mask is None else np.asarray(mask).astype(bool)
+    if norm <= 0.0:
+        norm = float(max(int(on.sum()), 1))
+    lp, p, top, ln_s = row_softmax(np.where(on[:, None], Z, 0.0), temperature)
+    row, dZ, q, rs, Ps = np.zeros(n), np.zeros((n, C)), np.zeros((n, C)), np.zeros(n), np.ones(n)
+    for i in np.flatnonzero(on & ~np.isneginf(ln_s)):
+        entries = [(int(c), v) for c, v in zip(np.asarray(t_ids)[i], t_val[i]) if 0 <= c < C and v != -np.inf]
+        if not entries:
+            continue
+        v = np.array([e[1] for e in entries])
+        w = np.exp(v) if rest else np.exp((v - v.max()) / temperature) / np.exp((v - v.max()) / temperature).sum()
+        for (c, _), x in zip(entries, w):
+            q[i, c] += x
+        listed = np.zeros(C, bool)
+        listed[[c for c, _ in entries]] = True
+        r = 1.0 - w.sum() if rest else 0.0
+        rs[i] = r = 0.0 if r < 2.0 ** -20 else r
+        Ps[i] = P = p[i, ~listed].sum()
+        with np.errstate(divide="ignore", invalid="ignore"):
+            row[i] = np.where(q[i] == 0.0, 0.0, q[i] * (np.log(q[i]) - lp[i])).sum() + (r * (np.log(r) - np.log(P)) if r > 0.0 else 0.0)
+            outside = np.where(listed | (p[i] == 0.0), 0.0, p[i] / P) if r > 0.0 else 0.0
+        dZ[i] = p[i] * (w.sum() + r) - q[i] - r * outside
+    return weight / norm * float(row.sum()), row, weight / (norm * temperature) * dZ, {"q": q, "r": rs, "P": Ps, "p": p, "lp": lp, "norm": norm}
+
+
 def sigmoid_bce(Z, Y, mask=None, norm: float = 0.0):
     """Binary cross-entropy on logits, the loss of the multi-label tasks (evaluation setup): per element
     -[y log s(z) + (1-y) log(1-s(z))] with s the logistic function, written in the overflow-free form

@@ -123,6 +123,14 @@ SIGNATURES = {
     "capgnn_softmax_ce": (_i32, [_i64, _i32, _vp, _i64, _vp, _vp, C.c_double, _vp, _vp, _i64, _i32, _vp, _sz, _vp]),
     "capgnn_softmax_ce_static": (_i32, [_i64, _i32, _vp, _i64, _vp, _vp, C.c_double, _vp, _vp, _i64, _i32, _vp]),
     "capgnn_sigmoid_bce": (_i32, [_i64, _i32, _vp, _i64, _vp, _i64, _vp, C.c_double, _vp, _vp, _i64, _i32, _vp, _sz, _vp]),
+    "capgnn_logprobs_workspace_bytes": (_sz, [_i64, _i32, _i32]),
+    "capgnn_logprobs": (_i32, [_i64, _i32, _vp, _i64, _i32, C.c_float, _vp, _vp, _i64, _i32, _vp, _i64, _vp, _vp, _i32, _vp, _vp,
+                               _i64, _vp, _sz, _vp]),
+    "capgnn_logprobs_bwd": (_i32, [_i64, _i32, _vp, _i64, _i32, C.c_float, _vp, _vp, _vp, _vp, _i64, _i32, _vp, _i64, _vp, _vp, _i64,
+                                   _i32, _vp]),
+    "capgnn_distill_workspace_bytes": (_sz, [_i64, _i32]),
+    "capgnn_distill": (_i32, [_i64, _i32, _vp, _i64, _i32, _vp, _vp, _i64, _i32, _i32, C.c_float, _vp, C.c_double, C.c_float, _vp, _vp,
+                              _vp, _i64, _i32, _i32, _vp, _sz, _vp]),
     "capgnn_epoch_multilabel": (_i32, [_vp, _vp, C.POINTER(Layer), _i32, _vp, _i64, _vp, _i64, _vp, C.c_double, _vp,
                                        C.POINTER(_vp), C.POINTER(_vp), C.POINTER(_vp), C.c_float, C.POINTER(C.c_float),
                                        C.POINTER(EpochTimes), _vp, _sz, _vp, _vp]),
@@ -503,6 +511,39 @@ def sigmoid_bce(n: int, n_classes: int, Z, ldz: int, targets, ldt: int, mask, lo
                 dz_dtype: int, ws, ws_bytes: int, stream=None):
     _check(lib().capgnn_sigmoid_bce(n, n_classes, _p(Z), ldz, _p(targets), ldt, _p(mask), loss_norm, _p(loss_dev), _p(dZ),
                                     lddz, dz_dtype, _p(ws), ws_bytes, _stream(stream)))
+
+
+TOP_MAX, GIVEN_MAX = 64, 256
+
+
+def logprobs_workspace_bytes(n: int, n_classes: int, k: int) -> int:
+    return int(lib().capgnn_logprobs_workspace_bytes(n, n_classes, k))
+
+
+def logprobs(n: int, n_classes: int, Z, ldz: int, z_dtype: int, temperature: float, mask, ids, ldi: int, m: int, logp, ldp: int,
+             entropy, stats, k: int, top_ids, top_logp, ldt: int, ws, ws_bytes: int, stream=None):
+    """Log-probabilities of given classes, entropy, statistics for the backward pass and the k most likely classes of every row."""
+    _check(lib().capgnn_logprobs(n, n_classes, _p(Z), ldz, z_dtype, temperature, _p(mask), _p(ids), ldi, m, _p(logp), ldp, _p(entropy),
+                                 _p(stats), k, _p(top_ids), _p(top_logp), ldt, _p(ws), ws_bytes, _stream(stream)))
+
+
+def logprobs_bwd(n: int, n_classes: int, Z, ldz: int, z_dtype: int, temperature: float, mask, stats, entropy, ids, ldi: int, m: int,
+                 dlogp, lddp: int, dentropy, dZ, lddz: int, dz_dtype: int, stream=None):
+    _check(lib().capgnn_logprobs_bwd(n, n_classes, _p(Z), ldz, z_dtype, temperature, _p(mask), _p(stats), _p(entropy), _p(ids), ldi, m,
+                                     _p(dlogp), lddp, _p(dentropy), _p(dZ), lddz, dz_dtype, _stream(stream)))
+
+
+def distill_workspace_bytes(n: int, n_classes: int) -> int:
+    return int(lib().capgnn_distill_workspace_bytes(n, n_classes))
+
+
+def distill(n: int, n_classes: int, Z, ldz: int, z_dtype: int, teacher_ids, teacher_val, ldt: int, k: int, rest: int,
+            temperature: float, mask, loss_norm: float, weight: float, loss_dev, row_loss, dZ, lddz: int, dz_dtype: int,
+            accumulate: int, ws, ws_bytes: int, stream=None):
+    """Divergence from a teacher's top logits (rest = 1: the teacher's remaining probability is one more outcome) and its gradient."""
+    _check(lib().capgnn_distill(n, n_classes, _p(Z), ldz, z_dtype, _p(teacher_ids), _p(teacher_val), ldt, k, rest, temperature, _p(mask),
+                                loss_norm, weight, _p(loss_dev), _p(row_loss), _p(dZ), lddz, dz_dtype, accumulate, _p(ws), ws_bytes,
+                                _stream(stream)))
 
 
 def gin_operator(n_loc: int, n_halo: int, rowptr, col, eps: float):

@@ -1,5 +1,6 @@
 // Small VALU kernels around the layer: sigma' masking + bias gradient, softmax cross-entropy, SGD step.
 #include "common.h"
+#include "softrow.h"
 
 #include <mutex>
 
@@ -839,6 +840,19 @@ static int loss_launch(LossArgs a, bool bce, double loss_norm, float times, floa
     }
     hipLaunchKernelGGL(loss_final_kernel, dim3(1 + (dbias ? (a.C + 31) / 32 : 0)), dim3(1024), 0, st, blocks, a.part, a.norm_val,
                        (a.norm_dev || a.norm_out) ? norm_dev : nullptr, loss_dev, a.colpart, a.C, dbias);
+    CG_HIP(hipGetLastError());
+    return CAPGNN_OK;
+}
+
+// norm_dev[0] = max(number of masked rows, 1); scratch: LOSS_PARTS doubles
+int launch_mask_count(int64_t n, const uint8_t *mask, float *norm_dev, double *scratch, hipStream_t stream) {
+    if (n <= COUNT_SMALL_N) {
+        hipLaunchKernelGGL(count_small_kernel, dim3(1), dim3(1024), 0, stream, n, mask, 1.f, norm_dev);
+    } else {
+        const int parts = static_cast<int>(std::min<int64_t>((n + 4095) / 4096, LOSS_PARTS));
+        hipLaunchKernelGGL(count_mask_kernel, dim3(parts), dim3(1024), 0, stream, n, mask, scratch, static_cast<uint16_t *>(nullptr));
+        hipLaunchKernelGGL(count_final_kernel, dim3(1), dim3(LOSS_PARTS), 0, stream, parts, scratch, 1.f, norm_dev);
+    }
     CG_HIP(hipGetLastError());
     return CAPGNN_OK;
 }
