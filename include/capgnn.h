@@ -485,7 +485,7 @@ int capgnn_sigmoid_bce(int64_t n, int C, const float *Z, int64_t ldz, const uint
  * z_dtype (C classes; rows need no alignment beyond their elements'), divided by `temperature` (finite, > 0) before the softmax.
  * p_i = softmax(Z_i / temperature).  A logit of -infinity bars its class: p = 0, nothing is added to the entropy and no gradient
  * flows through it.  A row whose classes are all barred is empty.  A NaN or +infinity makes the row's numbers NaN, no other row's.
- * mask: device uint8[n] or NULL: rows with 0 are never read.  dZ may be Z itself if type and pitch are the same too (each
+ * mask: device uint8[n] or NULL: rows with 0 are left out, whatever they hold.  dZ may be Z itself if type and pitch are the same too (each
  * logit is then replaced by its gradient); else they must not overlap.  No result depends on the order of atomic operations.
  * Asynchronous on `stream`, which belongs to the current device; nothing is allocated, so calls can be recorded into HIP graphs
  * (calls that may overlap in time need a workspace each).

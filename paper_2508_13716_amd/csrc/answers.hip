@@ -18,63 +18,488 @@ struct AnswerArgs {
     int32_t *top_ids; float *top_logp; int64_t ldt;
 };
 
-// One workgroup per row: the largest logit, then the sums, then the k largest one after another.
-template <bool BF16>
-__global__ __launch_bounds__(256) void answers_kernel(AnswerArgs a) {
-    __shared__ float red[4];
-    __shared__ unsigned long long redk[4];
-    for (int64_t row = blockIdx.x; row < a.n; row += gridDim.x) {
-        const char *z = a.Z + row * a.ldz * (BF16 ? 2 : 4);
+__device__ __forceinline__ void masked_out_row(const AnswerArgs &a, int64_t row, int threads) {
+    for (int i = threadIdx.x; i < a.m; i += threads) a.logp[row * a.ldp + i] = 0.f;
+    for (int i = threadIdx.x; i < a.k; i += threads) {
+        if (a.top_ids) a.top_ids[row * a.ldt + i] = -1;
+        if (a.top_logp) a.top_logp[row * a.ldt + i] = 0.f;
+    }
+    if (threadIdx.x == 0) {
+        if (a.entropy) a.entropy[row] = 0.f;
+        if (a.stats) a.stats[2 * row] = a.stats[2 * row + 1] = 0.f;
+    }
+}
+
+// What a row's sums come to.
+struct RowEnd {
+    float m0, ln_s, inv_T;
+    bool empty;
+    __device__ RowEnd(float m, float s, float inv_t) : m0(safe_max(m)), ln_s(s == 0.f ? -INFINITY : logf(s)), inv_T(inv_t), empty(s == 0.f) {}
+    __device__ float logp(float z) const { return empty ? -INFINITY : (z - m0) * inv_T - ln_s; }
+    // sum of p u, u = log2 of the exponentials: entropy = ln s - ln 2 * (sum of e u) / s
+    __device__ float entropy(float s, float e1) const { return empty ? 0.f : ln_s - e1 / s * 0.69314718f; }
+};
+
+// ------------------------------------------------------------------ the k largest of a stream of logits
+// A workgroup walks a row tile by tile and keeps the keys (logit, class) that may still be among the k largest in LDS, together with a
+// threshold: of at least k logits it is known that they are no smaller.  A tile's thread maxima give the first one: the k-th largest of
+// them is exceeded by hardly more than k logits of the tile (64 largest of 16384: 73 on average).  What passes the threshold is appended;
+// the list is ranked, each key by counting the larger ones, when it is half full and at the end.  Keys are distinct, so the
+// result does not depend on the order in which threads append.  A tile that passes more than the list holds is tried again
+// with its own maxima, then with its exact k-th largest key (equal logits, values in order): slower, never wrong.
+template <int THREADS> struct TopLds {
+    static constexpr int CAP = THREADS == 64 ? 512 : 1024;
+    unsigned long long key[CAP], best[CAPGNN_TOP_MAX];
+    uint32_t maxima[THREADS];
+    int count[3];
+    uint32_t bound;
+    int red[THREADS / 64];
+};
+
+// the float just below every logit of order o and more; NaN (no logit is <= it) where there is none
+__device__ __forceinline__ float just_below(uint32_t o) {
+    uint32_t b = o - 1u;
+    if (b == 0x7fffffffu) b = 0x7ffffffeu;      // below both zeros
+    return o <= 0x007fffffu ? __uint_as_float(0x7fc00000u) : order_logit(b);
+}
+
+template <int THREADS> struct Top {
+    static constexpr int CAP = TopLds<THREADS>::CAP;
+    TopLds<THREADS> &l;
+    int k, kept = 0, turn = 0;
+    float below = __uint_as_float(0x7fc00000u);         // a logit is a candidate unless it is <= this
+
+    __device__ Top(TopLds<THREADS> &lds, int k_) : l(lds), k(k_) {
+        if (threadIdx.x < 3) l.count[threadIdx.x] = 0;
+        __syncthreads();
+    }
+
+    __device__ void raise(uint32_t order, bool inclusive) {
+        const float f = inclusive ? just_below(order) : order_logit(order);
+        if (f == f && !(f <= below)) below = f;         // (from NaN to anything, to NaN never)
+    }
+
+    // the k-th largest of the threads' maxima (k <= THREADS)
+    __device__ uint32_t kth_maximum(float tmax) {
+        const uint32_t mine = logit_order(tmax);
+        l.maxima[threadIdx.x] = mine;
+        __syncthreads();
+        int larger = 0;
+        const uint4 *q = reinterpret_cast<const uint4 *>(l.maxima);
+#pragma unroll 4
+        for (int i = 0; i < THREADS / 4; ++i) {
+            const uint4 v = q[i];
+            const int t = threadIdx.x - 4 * i;
+            larger += (v.x > mine || (v.x == mine && t > 0)) + (v.y > mine || (v.y == mine && t > 1)) +
+                      (v.z > mine || (v.z == mine && t > 2)) + (v.w > mine || (v.w == mine && t > 3));
+        }
+        if (larger == k - 1) l.bound = mine;
+        __syncthreads();
+        const uint32_t r = l.bound;
+        __syncthreads();
+        return r;
+    }
+
+    // ranks the kept keys: the k largest are left, in descending order
+    __device__ void rank() {
+        const int n = kept;
+        if (threadIdx.x == 0 && (n & 1)) l.key[n] = 0;          // a pair is read at a time
+        __syncthreads();
+        const ulonglong2 *q = reinterpret_cast<const ulonglong2 *>(l.key);
+#pragma unroll 1
+        for (int i = threadIdx.x; i < n; i += THREADS) {
+            const unsigned long long own = l.key[i];
+            int larger = 0;
+#pragma unroll 4
+            for (int j = 0; j < (n + 1) / 2; ++j) {
+                const ulonglong2 v = q[j];
+                larger += (v.x > own) + (v.y > own);
+            }
+            if (larger < k) l.best[larger] = own;
+        }
+        __syncthreads();
+        kept = n < k ? n : k;
+        if (static_cast<int>(threadIdx.x) < kept) l.key[threadIdx.x] = l.best[threadIdx.x];
+        if (kept == k) raise(static_cast<uint32_t>(l.best[k - 1] >> 32), false);
+        __syncthreads();
+    }
+
+    // what the threads have appended since the last barrier; false if the list does not hold it
+    __device__ bool settle(int *added) {
+        __syncthreads();
+        const int c = l.count[turn];
+        // three counters in turn: this one is cleared before the next barrier, and used again after it
+        if (threadIdx.x == 0) l.count[(turn + 2) % 3] = 0;
+        turn = (turn + 1) % 3;
+        *added = c;
+        return kept + c <= CAP;
+    }
+
+    __device__ void append(float z, int j) {
+        const int p = kept + atomicAdd(&l.count[turn], 1);
+        if (p < CAP) l.key[p] = logit_key(z, j);
+    }
+
+    // the tile of NV vectors a thread, as the row's scan has read them; classes [from, end) are in the tile
+    template <bool BF16, int NV>
+    __device__ void tile(raw16 (&r)[NV], const float (&vmax)[NV], float tmax, const char *z, int from, int end) {
+        typedef Raw<BF16> R;
+        if (kept == 0 && end - from > CAP / 2) raise(kth_maximum(tmax), true);
+        int added;
+#pragma unroll 1
+        for (int attempt = 0; attempt < 2; ++attempt) {
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+                if (!__any(!(vmax[i] <= below))) continue;
+                const int own = from + (i * THREADS + static_cast<int>(threadIdx.x)) * R::V;
+                int j = own + R::V <= end ? own : end - R::V;
+                raw16 t = r[i];
+#pragma unroll 1
+                for (int word = 0; word < 4; ++word) {          // (rolled: 64 appends in a row cost 140 registers)
+                    const float x = R::get(t, 0);
+                    if (!(x <= below) && j >= own) append(x, j);
+                    ++j;
+                    if constexpr (BF16) {
+                        const float y = R::get(t, 1);
+                        if (!(y <= below) && j >= own) append(y, j);
+                        ++j;
+                    }
+                    t = raw16{t[1], t[2], t[3], t[0]};
+                }
+            }
+            if (settle(&added)) {
+                kept += added;
+                if (kept > CAP / 2) rank();
+                return;
+            }
+            if (attempt == 0) raise(kth_maximum(tmax), true);
+        }
+        // the tile's exact k-th largest key, bit by bit: order T, classes below J
+        const int want = end - from < k ? end - from : k;
+        auto count = [&](auto in) {
+            int c = 0;
+#pragma unroll 1
+            for (int j = from + threadIdx.x; j < end; j += THREADS) c += in(logit_order(ld_logit<BF16>(z, j)), j);
+            return group_all<THREADS>(c, l.red, OpSum());
+        };
+        uint32_t T = 0;
+        int J = 0;
+        for (int bit = 31; bit >= 0; --bit) {
+            const uint32_t t = T | 1u << bit;
+            if (count([&](uint32_t o, int) { return o >= t; }) >= want) T = t;
+        }
+        const int above = count([&](uint32_t o, int) { return o > T; });
+        for (int bit = 30; bit >= 0; --bit) {
+            const int t = J | 1 << bit;
+            if (count([&](uint32_t o, int j) { return o == T && j < t; }) <= want - above) J = t;
+        }
+#pragma unroll 1
+        for (int j = from + threadIdx.x; j < end; j += THREADS) {
+            const float x = ld_logit<BF16>(z, j);
+            const uint32_t o = logit_order(x);
+            if (o > T || (o == T && j < J)) append(x, j);
+        }
+        settle(&added);
+        kept += added;
+        rank();
+    }
+};
+
+// One workgroup per row, or per part of a row (parts > 1): running maximum and sums in every thread, one pass over the logits.
+constexpr int ANSWER_VECTORS = 8;       // 16-byte loads that a thread has in flight
+
+struct AnswerParts {
+    int parts;                      // of a row
+    int64_t chunk;                  // classes of one
+    float4 *sums;                   // [n][parts]: maximum, sum, sum of e u
+    unsigned long long *keys;       // [n][parts][k], 0 = none
+};
+
+template <bool BF16, int THREADS, bool ENT>
+__global__ __launch_bounds__(THREADS) void answers_rows_kernel(AnswerArgs a, AnswerParts w) {
+    typedef Raw<BF16> R;
+    constexpr int NV = ANSWER_VECTORS, TILE = THREADS * NV * R::V;
+    __shared__ __align__(16) TopLds<THREADS> lds;
+    __shared__ float red[THREADS / 64];
+    for (int64_t job = blockIdx.x; job < a.n * w.parts; job += gridDim.x) {
+        const int64_t row = w.parts > 1 ? job / w.parts : job;
+        const int part = w.parts > 1 ? static_cast<int>(job % w.parts) : 0;
         if (a.mask && !a.mask[row]) {
-            for (int i = threadIdx.x; i < a.m; i += 256) a.logp[row * a.ldp + i] = 0.f;
-            for (int i = threadIdx.x; i < a.k; i += 256) {
-                if (a.top_ids) a.top_ids[row * a.ldt + i] = -1;
-                if (a.top_logp) a.top_logp[row * a.ldt + i] = 0.f;
-            }
-            if (threadIdx.x == 0) {
-                if (a.entropy) a.entropy[row] = 0.f;
-                if (a.stats) a.stats[2 * row] = a.stats[2 * row + 1] = 0.f;
-            }
+            if (part == 0) masked_out_row(a, row, THREADS);
             continue;
         }
-        float m = -INFINITY;
-        for (int j = threadIdx.x; j < a.C; j += 256) m = max_of(m, ld_logit<BF16>(z, j));
-        m = group_all<256>(m, red, OpMax());
-        const float m0 = safe_max(m);
-        float s = 0.f, e1 = 0.f;
-        for (int j = threadIdx.x; j < a.C; j += 256) {
-            const float d = ld_logit<BF16>(z, j) - m0, u = d * a.t.L, e = exp2_raw(u);
-            s += e;
-            e1 = fmaf(e, fmaxf(u, -160.f), e1);
-        }
-        s = group_all<256>(s, red, OpSum());
-        e1 = group_all<256>(e1, red, OpSum());
-        const bool empty = s == 0.f;
-        const float ln_s = empty ? -INFINITY : logf(s);
-        auto logp_of = [&](float v) { return empty ? -INFINITY : (v - m0) * a.t.inv_T - ln_s; };
-        if (threadIdx.x == 0) {
-            if (a.entropy) a.entropy[row] = empty ? 0.f : ln_s - e1 / s * 0.69314718f;
-            if (a.stats) { a.stats[2 * row] = m; a.stats[2 * row + 1] = ln_s; }
-        }
-        for (int i = threadIdx.x; i < a.m; i += 256) {
-            const int c = a.ids[row * a.ldi + i];
-            a.logp[row * a.ldp + i] = c >= 0 && c < a.C ? logp_of(ld_logit<BF16>(z, c)) : 0.f;
-        }
-        unsigned long long last = ~0ull;
-        for (int i = 0; i < a.k; ++i) {
-            unsigned long long best = 0;
-            for (int j = threadIdx.x; j < a.C; j += 256) {
-                const unsigned long long key = logit_key(ld_logit<BF16>(z, j), j);
-                if (key < last && key > best) best = key;
+        const char *z = a.Z + row * a.ldz * (BF16 ? 2 : 4);
+        const int lo = static_cast<int>(part * w.chunk);
+        const int hi = static_cast<int>(lo + w.chunk < a.C ? lo + w.chunk : a.C);
+        Top<THREADS> top(lds, a.k);
+        float m = -INFINITY, s = 0.f, e1 = 0.f;
+        for (int t0 = lo; t0 < hi; t0 += TILE) {
+            raw16 r[NV];
+            float vmax[NV], tmax = -INFINITY;
+            int start;
+#pragma unroll
+            for (int i = 0; i < NV; ++i)
+                if (t0 + i * THREADS * R::V < hi) r[i] = R::load_until(z, t0 + (i * THREADS + static_cast<int>(threadIdx.x)) * R::V, hi, &start);
+                else r[i] = raw16{R::BARRED, R::BARRED, R::BARRED, R::BARRED};
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+                vmax[i] = R::get(r[i], 0);
+                if (t0 + i * THREADS * R::V >= hi) continue;          // (the same for all threads)
+#pragma unroll
+                for (int e = 1; e < R::V; ++e) vmax[i] = max_of(vmax[i], R::get(r[i], e));
+                tmax = max_of(tmax, vmax[i]);
             }
-            best = group_all<256>(best, redk, OpMaxKey());
-            last = best;
+            const float m_new = max_of(m, tmax), ref = safe_max(m_new);
+            const float du = (m - ref) * a.t.L, f = exp2_raw(du);
+            if constexpr (ENT) e1 = f * fmaf(s, fmaxf(du, -160.f), e1);
+            s *= f;
+            m = m_new;
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+                if (t0 + i * THREADS * R::V >= hi) continue;
+                forget(r[i]);
+#pragma unroll
+                for (int e = 0; e < R::V; ++e) {
+                    const float u = (R::get(r[i], e) - ref) * a.t.L, x = exp2_raw(u);
+                    s += x;
+                    if constexpr (ENT) e1 = fmaf(x, fmaxf(u, -160.f), e1);
+                }
+            }
+            if (a.k) top.template tile<BF16>(r, vmax, tmax, z, t0, hi - t0 < TILE ? hi : t0 + TILE);
+        }
+        // a thread's sums, taken from its own maximum to the row's
+        const float M = group_all<THREADS>(m, red, OpMax()), ref = safe_max(M);
+        const float du = (m - ref) * a.t.L, f = exp2_raw(du);
+        if constexpr (ENT) e1 = group_all<THREADS>(f * fmaf(s, fmaxf(du, -160.f), e1), red, OpSum());
+        s = group_all<THREADS>(s * f, red, OpSum());
+        if (a.k) top.rank();
+        if (w.parts > 1) {
+            if (threadIdx.x == 0) w.sums[job] = make_float4(M, s, e1, 0.f);
+            for (int i = threadIdx.x; i < a.k; i += THREADS) w.keys[job * a.k + i] = i < top.kept ? lds.key[i] : 0;
+        } else {
+            const RowEnd end(M, s, a.t.inv_T);
             if (threadIdx.x == 0) {
-                if (a.top_ids) a.top_ids[row * a.ldt + i] = static_cast<int32_t>(0xffffffffu - static_cast<uint32_t>(best));
-                if (a.top_logp) a.top_logp[row * a.ldt + i] = logp_of(order_logit(static_cast<uint32_t>(best >> 32)));
+                if (a.entropy) a.entropy[row] = end.entropy(s, e1);
+                if (a.stats) { a.stats[2 * row] = M; a.stats[2 * row + 1] = end.ln_s; }
             }
+            for (int i = threadIdx.x; i < a.m; i += THREADS) {
+                const int c = a.ids[row * a.ldi + i];
+                a.logp[row * a.ldp + i] = c >= 0 && c < a.C ? end.logp(ld_logit<BF16>(z, c)) : 0.f;
+            }
+            for (int i = threadIdx.x; i < a.k; i += THREADS) {
+                const unsigned long long key = lds.key[i];
+                if (a.top_ids) a.top_ids[row * a.ldt + i] = static_cast<int32_t>(0xffffffffu - static_cast<uint32_t>(key));
+                if (a.top_logp) a.top_logp[row * a.ldt + i] = end.logp(order_logit(static_cast<uint32_t>(key >> 32)));
+            }
+        }
+        __syncthreads();
+    }
+}
+
+// ------------------------------------------------------------------ few classes (NARROW_C) and at most NARROW_TOP top ones
+// Pass 1 keeps the k largest logits of a lane sorted, one median of three per place and logit; pass 2 forms the sums and notes the classes
+// that reach the k-th largest, of those equal to it only as many as are wanted; the noted ones rank one another.
+constexpr int NARROW_TOP = 8;
+template <bool BF16, bool ENT, bool TOP>
+__global__ __launch_bounds__(64 * NARROW_WAVES) void answers_narrow_kernel(AnswerArgs a, NarrowShape s) {
+    extern __shared__ __align__(16) char lds_all[];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const size_t per_wave = s.lds_wave + 64 * NARROW_TOP;
+    float *tile = reinterpret_cast<float *>(lds_all + wave * per_wave);
+    uint8_t *noted = reinterpret_cast<uint8_t *>(lds_all + wave * per_wave + s.lds_wave);
+    const int G = 1 << s.lg, sub = lane & (G - 1), C = s.C;
+    const float *z = tile + (lane >> s.lg) * s.pitch;
+    const int64_t step = static_cast<int64_t>(gridDim.x) * NARROW_WAVES * s.rows;
+    int64_t row0 = (static_cast<int64_t>(blockIdx.x) * NARROW_WAVES + wave) * s.rows;
+    NarrowLoad<BF16> next;
+    if (row0 < a.n) next.fetch(s, a.Z, a.ldz, a.n, row0, lane);
+    for (; row0 < a.n; row0 += step) {
+        next.put(s, tile, lane);
+        wave_sync();
+        if (row0 + step < a.n) next.fetch(s, a.Z, a.ldz, a.n, row0 + step, lane);
+        const int64_t row = row0 + (lane >> s.lg);
+        const bool in = row < a.n, on = in && (!a.mask || a.mask[row]);
+        float v[NARROW_TOP], m = -INFINITY;
+        if constexpr (TOP) {
+#pragma unroll
+            for (int i = 0; i < NARROW_TOP; ++i) v[i] = -INFINITY;
+            auto insert = [&](float x) {
+#pragma unroll
+                for (int i = NARROW_TOP - 1; i > 0; --i) v[i] = __builtin_amdgcn_fmed3f(v[i - 1], v[i], x);
+                v[0] = max_of(v[0], x);
+            };
+            for (int j = sub; j < C; j += G) insert(z[j]);
+            for (int off = 1; off < G; off <<= 1) {
+                float o[NARROW_TOP];
+#pragma unroll
+                for (int i = 0; i < NARROW_TOP; ++i) o[i] = __shfl_xor(v[i], off);
+#pragma unroll
+                for (int i = 0; i < NARROW_TOP; ++i) insert(o[i]);
+            }
+            m = v[0];
+        } else {
+            for (int j = sub; j < C; j += G) m = max_of(m, z[j]);
+            for (int off = 1; off < G; off <<= 1) m = max_of(m, __shfl_xor(m, off));
+        }
+        float kth = 0.f;
+        int equals = 0, hits = 0;           // how many of the k largest equal the k-th; classes noted by this lane
+        if constexpr (TOP) {
+#pragma unroll
+            for (int i = 0; i < NARROW_TOP; ++i) if (i == a.k - 1) kth = v[i];
+#pragma unroll
+            for (int i = 0; i < NARROW_TOP; ++i) equals += i < a.k && v[i] == kth;
+        }
+        const float ref = safe_max(m);
+        float sum = 0.f, e1 = 0.f;
+        int wanted = equals;
+        for (int j = sub; j < C; j += G) {
+            const float x = z[j], u = (x - ref) * a.t.L, e = exp2_raw(u);
+            sum += e;
+            if constexpr (ENT) e1 = fmaf(e, fmaxf(u, -160.f), e1);
+            if constexpr (TOP) {
+                if (x > kth || (x == kth && wanted > 0)) {
+                    wanted -= x == kth;
+                    if (hits < NARROW_TOP) noted[lane * NARROW_TOP + hits] = static_cast<uint8_t>(j);
+                    ++hits;
+                }
+            }
+        }
+        for (int off = 1; off < G; off <<= 1) {
+            sum += __shfl_xor(sum, off);
+            if constexpr (ENT) e1 += __shfl_xor(e1, off);
+        }
+        const RowEnd end(m, sum, a.t.inv_T);
+        if (in && sub == 0) {
+            if (a.entropy) a.entropy[row] = on ? end.entropy(sum, e1) : 0.f;
+            if (a.stats) { a.stats[2 * row] = on ? m : 0.f; a.stats[2 * row + 1] = on ? end.ln_s : 0.f; }
+        }
+        if (in)
+            for (int i = sub; i < a.m; i += G) {
+                const int c = on ? a.ids[row * a.ldi + i] : -1;
+                a.logp[row * a.ldp + i] = c >= 0 && c < C ? end.logp(z[c]) : 0.f;
+            }
+        if constexpr (TOP) {
+            auto give = [&](int place, int c) {
+                if (a.top_ids) a.top_ids[row * a.ldt + place] = c;
+                if (a.top_logp) a.top_logp[row * a.ldt + place] = end.logp(z[c]);
+            };
+            wave_sync();
+            if (in && !on) {
+                for (int i = sub; i < a.k; i += G) {
+                    if (a.top_ids) a.top_ids[row * a.ldt + i] = -1;
+                    if (a.top_logp) a.top_logp[row * a.ldt + i] = 0.f;
+                }
+            }
+            const bool plain = sum == sum;
+            const int first = lane & ~(G - 1);
+            int of_lane[4];         // classes noted by each lane of the row
+#pragma unroll
+            for (int g = 0; g < 4; ++g) of_lane[g] = g < G ? __shfl(hits, first + g) : 0;
+            if (on && plain) {
+                for (int i = 0; i < hits; ++i) {
+                    const int c = noted[lane * NARROW_TOP + i];
+                    const float x = z[c];
+                    int place = 0;
+#pragma unroll
+                    for (int g = 0; g < 4; ++g)
+                        for (int b = 0; b < of_lane[g]; ++b) {
+                            const int cb = noted[(first + g) * NARROW_TOP + b];
+                            const float y = z[cb];
+                            place += y > x || (y == x && cb < c);
+                        }
+                    if (place < a.k) give(place, c);
+                }
+            }
+            // a row with NaN: its classes one after another, by key
+            if (__any(on && !plain)) {
+                unsigned long long last = ~0ull;
+                for (int i = 0; i < a.k; ++i) {
+                    unsigned long long best = 0;
+                    for (int j = sub; j < C; j += G) {
+                        const unsigned long long key = logit_key(z[j], j);
+                        if (key < last && key > best) best = key;
+                    }
+                    for (int off = 1; off < G; off <<= 1) best = OpMaxKey()(best, __shfl_xor(best, off));
+                    last = best;
+                    if (on && !plain && sub == 0) give(i, static_cast<int>(0xffffffffu - static_cast<uint32_t>(best)));
+                }
+            }
+        }
+        wave_sync();
+    }
+}
+
+// The parts of a row put together: sums from the parts' maxima to the row's, and the k largest of the parts' k largest.
+constexpr int ANSWER_PARTS = 64;
+template <bool BF16>
+__global__ __launch_bounds__(256) void answers_join_kernel(AnswerArgs a, AnswerParts w) {
+    constexpr int OWN = ANSWER_PARTS * CAPGNN_TOP_MAX / 256;
+    __shared__ __align__(16) TopLds<256> lds;
+    __shared__ float red[4];
+    for (int64_t row = blockIdx.x; row < a.n; row += gridDim.x) {
+        if (a.mask && !a.mask[row]) continue;
+        const char *z = a.Z + row * a.ldz * (BF16 ? 2 : 4);
+        const int i = threadIdx.x;
+        unsigned long long own[OWN], best = 0;
+#pragma unroll
+        for (int o = 0; o < OWN; ++o) {
+            own[o] = i + o * 256 < w.parts * a.k ? w.keys[row * w.parts * a.k + i + o * 256] : 0;
+            best = own[o] > best ? own[o] : best;
+        }
+        const float4 p = i < w.parts ? w.sums[row * w.parts + i] : make_float4(-INFINITY, 0.f, 0.f, 0.f);
+        const float M = group_all<256>(p.x, red, OpMax());
+        const float du = (p.x - safe_max(M)) * a.t.L, f = exp2_raw(du);
+        const float s = group_all<256>(p.y * f, red, OpSum());
+        const float e1 = group_all<256>(f * fmaf(p.y, fmaxf(du, -160.f), p.z), red, OpSum());
+        const RowEnd end(M, s, a.t.inv_T);
+        if (i == 0) {
+            if (a.entropy) a.entropy[row] = end.entropy(s, e1);
+            if (a.stats) { a.stats[2 * row] = M; a.stats[2 * row + 1] = end.ln_s; }
+        }
+        if (i < a.m) {
+            const int c = a.ids[row * a.ldi + i];
+            a.logp[row * a.ldp + i] = c >= 0 && c < a.C ? end.logp(ld_logit<BF16>(z, c)) : 0.f;
+        }
+        if (a.k) {
+            // keys at least as large as the k-th largest of the threads' maxima: k threads have them, OWN at most each
+            Top<256> top(lds, a.k);
+            unsigned long long bound = 1;
+            if (w.parts * a.k > 256) {
+                lds.key[i] = best;
+                if (i == 0) lds.key[256] = 1;
+                __syncthreads();
+                int larger = 0;
+                const ulonglong2 *q = reinterpret_cast<const ulonglong2 *>(lds.key);
+                for (int j = 0; j < 128; ++j) larger += (q[j].x > best) + (q[j].y > best);
+                if (larger == a.k - 1 && best) lds.key[256] = best;
+                __syncthreads();
+                bound = lds.key[256];
+                __syncthreads();
+            }
+#pragma unroll
+            for (int o = 0; o < OWN; ++o)
+                if (own[o] >= bound) lds.key[atomicAdd(&lds.count[0], 1)] = own[o];
+            __syncthreads();
+            top.kept = lds.count[0];
+            top.rank();
+            if (i < a.k) {
+                const unsigned long long key = lds.key[i];
+                if (a.top_ids) a.top_ids[row * a.ldt + i] = static_cast<int32_t>(0xffffffffu - static_cast<uint32_t>(key));
+                if (a.top_logp) a.top_logp[row * a.ldt + i] = end.logp(order_logit(static_cast<uint32_t>(key >> 32)));
+            }
+            __syncthreads();
         }
     }
+}
+
+// Few rows are cut into parts, about a thousand workgroups in all and at least ANSWER_PART_LEAST classes each.
+constexpr int ANSWER_PART_LEAST = 2048, ANSWER_WORKGROUPS = 1024;
+static int answer_parts(int64_t n, int C, int64_t *chunk) {
+    int64_t parts = std::min<int64_t>(std::min<int64_t>(ANSWER_PARTS, ANSWER_WORKGROUPS / std::max<int64_t>(n, 1)), C / ANSWER_PART_LEAST);
+    if (parts <= 1) { *chunk = C; return 1; }
+    *chunk = (C + parts - 1) / parts;
+    *chunk = (*chunk + 511) / 512 * 512;
+    return static_cast<int>((C + *chunk - 1) / *chunk);
 }
 
 struct AnswerGradArgs {
@@ -146,13 +571,20 @@ __global__ __launch_bounds__(256) void answers_grad_kernel(AnswerGradArgs a) {
 
 using namespace capgnn;
 
-extern "C" size_t capgnn_logprobs_workspace_bytes(int64_t n, int C, int k) { (void)n; (void)C; (void)k; return 0; }
+extern "C" size_t capgnn_logprobs_workspace_bytes(int64_t n, int C, int k) {
+    if (n <= 0 || C <= 0 || k < 0) return 0;
+    int64_t chunk;
+    const int parts = answer_parts(n, C, &chunk);
+    if (parts == 1) return 0;
+    return align_up(sizeof(float4) * n * parts, 256) + align_up(sizeof(unsigned long long) * n * parts * k, 256);
+}
 
 extern "C" int capgnn_logprobs(int64_t n, int C, const void *Z, int64_t ldz, int z_dtype, float temperature, const uint8_t *mask,
                                const int32_t *ids, int64_t ldi, int m, float *logp, int64_t ldp, float *entropy, float *stats,
                                int k, int32_t *top_ids, float *top_logp, int64_t ldt, void *ws, size_t ws_bytes, void *stream) {
     if (z_dtype != CAPGNN_F32 && z_dtype != CAPGNN_BF16) CG_FAIL(CAPGNN_EINVAL, "logprobs: unknown z_dtype");
     if (n < 0 || C <= 0) CG_FAIL(CAPGNN_EINVAL, "logprobs: bad sizes");
+    if (C > CLASSES_MOST) CG_FAIL(CAPGNN_EUNSUPPORTED, "logprobs: more than 2^30 classes");
     if (m < 0 || m > CAPGNN_GIVEN_MAX) CG_FAIL(CAPGNN_EINVAL, "logprobs: m = %d, 0 to %d classes can be given per row", m, CAPGNN_GIVEN_MAX);
     if (k < 0 || k > CAPGNN_TOP_MAX || k > C) CG_FAIL(CAPGNN_EINVAL, "logprobs: k = %d, 0 to min(C, %d) expected", k, CAPGNN_TOP_MAX);
     if (!good_temperature(temperature)) CG_FAIL(CAPGNN_EINVAL, "logprobs: the temperature must be positive and finite");
@@ -166,9 +598,41 @@ extern "C" int capgnn_logprobs(int64_t n, int C, const void *Z, int64_t ldz, int
     hipStream_t st = static_cast<hipStream_t>(stream);
     AnswerArgs a{n, C, static_cast<const char *>(Z), ldz, temp_scale(temperature), mask, ids, ldi, m, logp, ldp, entropy, stats, k, top_ids,
                  top_logp, ldt};
-    const unsigned grid = static_cast<unsigned>(std::min<int64_t>(n, 1 << 20));
-    if (z_dtype == CAPGNN_BF16) hipLaunchKernelGGL(answers_kernel<true>, dim3(grid), dim3(256), 0, st, a);
-    else hipLaunchKernelGGL(answers_kernel<false>, dim3(grid), dim3(256), 0, st, a);
+    const bool bf16 = z_dtype == CAPGNN_BF16;
+    if (C <= NARROW_C && k <= NARROW_TOP) {
+        const NarrowShape s = narrow_shape(C, z_dtype);
+        const size_t lds = NARROW_WAVES * (s.lds_wave + 64 * NARROW_TOP);
+        auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(narrow_grid(s, n, lds)), dim3(64 * NARROW_WAVES), lds, st, a, s); };
+        if (bf16) {
+            if (entropy) k ? go(answers_narrow_kernel<true, true, true>) : go(answers_narrow_kernel<true, true, false>);
+            else k ? go(answers_narrow_kernel<true, false, true>) : go(answers_narrow_kernel<true, false, false>);
+        } else {
+            if (entropy) k ? go(answers_narrow_kernel<false, true, true>) : go(answers_narrow_kernel<false, true, false>);
+            else k ? go(answers_narrow_kernel<false, false, true>) : go(answers_narrow_kernel<false, false, false>);
+        }
+        CG_HIP(hipGetLastError());
+        return CAPGNN_OK;
+    }
+    AnswerParts w{};
+    w.parts = answer_parts(n, C, &w.chunk);
+    w.sums = static_cast<float4 *>(ws);
+    w.keys = reinterpret_cast<unsigned long long *>(static_cast<char *>(ws) + align_up(sizeof(float4) * n * w.parts, 256));
+    // a wave alone walks rows of one tile (no barriers between waves), a workgroup of four longer ones
+    const bool wave = C <= 64 * ANSWER_VECTORS * (bf16 ? 8 : 4);
+    const unsigned grid = static_cast<unsigned>(std::min<int64_t>(n * w.parts, 1 << 24));
+    auto go = [&](auto kernel, int threads) { hipLaunchKernelGGL(kernel, dim3(grid), dim3(threads), 0, st, a, w); };
+    if (bf16) {
+        if (wave) entropy ? go(answers_rows_kernel<true, 64, true>, 64) : go(answers_rows_kernel<true, 64, false>, 64);
+        else entropy ? go(answers_rows_kernel<true, 256, true>, 256) : go(answers_rows_kernel<true, 256, false>, 256);
+    } else {
+        if (wave) entropy ? go(answers_rows_kernel<false, 64, true>, 64) : go(answers_rows_kernel<false, 64, false>, 64);
+        else entropy ? go(answers_rows_kernel<false, 256, true>, 256) : go(answers_rows_kernel<false, 256, false>, 256);
+    }
+    if (w.parts > 1) {
+        const unsigned rows = static_cast<unsigned>(n);
+        if (bf16) hipLaunchKernelGGL(answers_join_kernel<true>, dim3(rows), dim3(256), 0, st, a, w);
+        else hipLaunchKernelGGL(answers_join_kernel<false>, dim3(rows), dim3(256), 0, st, a, w);
+    }
     CG_HIP(hipGetLastError());
     return CAPGNN_OK;
 }

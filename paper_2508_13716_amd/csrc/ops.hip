@@ -1,6 +1,5 @@
 // Small VALU kernels around the layer: sigma' masking + bias gradient, softmax cross-entropy, SGD step.
 #include "common.h"
-#include "softrow.h"
 
 #include <mutex>
 
@@ -844,7 +843,6 @@ static int loss_launch(LossArgs a, bool bce, double loss_norm, float times, floa
     return CAPGNN_OK;
 }
 
-// norm_dev[0] = max(number of masked rows, 1); scratch: LOSS_PARTS doubles
 int launch_mask_count(int64_t n, const uint8_t *mask, float *norm_dev, double *scratch, hipStream_t stream) {
     if (n <= COUNT_SMALL_N) {
         hipLaunchKernelGGL(count_small_kernel, dim3(1), dim3(1024), 0, stream, n, mask, 1.f, norm_dev);

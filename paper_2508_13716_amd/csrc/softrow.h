@@ -50,8 +50,8 @@ __device__ __forceinline__ float exp_scaled(float d, const TempScale &t) {
     return e > 0.f ? fmaf(e, lost * 0.69314718f, e) : e;        // (d = -inf: lost is NaN, e is 0; a NaN d gives a NaN e)
 }
 
-// the larger of the two, a NaN never (the sum of the exponentials shows it)
-__device__ __forceinline__ float max_of(float a, float b) { return fmaxf(a, b); }
+// the larger of the two; NaN if either is (one instruction, as the maximum that skips NaN)
+__device__ __forceinline__ float max_of(float a, float b) { return __builtin_elementwise_maximum(a, b); }
 
 // the reference point of a row: 0 where every class is barred, so that -inf - -inf is never formed
 __device__ __forceinline__ float safe_max(float m) { return m == -INFINITY ? 0.f : m; }
@@ -70,6 +70,130 @@ __device__ __forceinline__ float order_logit(uint32_t o) {
 __device__ __forceinline__ uint64_t logit_key(float z, int k) {
     return static_cast<uint64_t>(logit_order(z)) << 32 | (0xffffffffu - static_cast<uint32_t>(k));
 }
+
+// 16 bytes of logits from any address that is aligned to its elements (one load instruction), V of them
+typedef uint32_t raw16 __attribute__((ext_vector_type(4)));
+typedef raw16 raw16_by2 __attribute__((aligned(2)));
+typedef raw16 raw16_by4 __attribute__((aligned(4)));
+template <bool BF16> struct Raw {
+    static constexpr int V = BF16 ? 8 : 4;
+    static constexpr uint32_t BARRED = BF16 ? 0xff80ff80u : 0xff800000u;
+
+    static __device__ __forceinline__ raw16 load(const char *p, int64_t j) {
+        if constexpr (BF16) return *reinterpret_cast<const raw16_by2 *>(p + j * 2);
+        else return *reinterpret_cast<const raw16_by4 *>(p + j * 4);
+    }
+    static __device__ __forceinline__ float get(raw16 r, int e) {
+        if constexpr (BF16) return __uint_as_float(e & 1 ? r[e / 2] & 0xffff0000u : r[e / 2] << 16);
+        else return __uint_as_float(r[e]);
+    }
+    // Logits [j, j + V) of a row of at least V that ends at `end`.  Where fewer are left the row's last V are read, and those before j are
+    // barred in the result (all of them for j >= end): what is returned starts at class `start`.
+    static __device__ __forceinline__ raw16 load_until(const char *p, int j, int end, int *start) {
+        const int from = j + V <= end ? j : end - V;
+        raw16 r = load(p, from);
+        *start = from;
+        if (__any(from != j)) {
+            const int out = j - from;
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {
+                if constexpr (BF16) r[w] = 2 * w + 1 < out ? BARRED : 2 * w < out ? (r[w] & 0xffff0000u) | (BARRED & 0xffffu) : r[w];
+                else r[w] = w < out ? BARRED : r[w];
+            }
+        }
+        return r;
+    }
+};
+
+// Rows of at most NARROW_C classes: a wave takes 64 / G of them at a time through LDS, G lanes a row with at most 64 classes each, so that a
+// row's sums need no or hardly any exchange between lanes (lane groups over registers spent four times the instructions at 47 classes:
+// 612000 rows were bound by them, not by memory).  The next rows' loads are under way while a wave works on its own.  A row starts
+// G * odd words after the one before it: lanes that read class k of their rows at once hit different banks.
+constexpr int NARROW_C = 256;
+constexpr int NARROW_WAVES = 2;     // of a workgroup; each works for itself
+struct NarrowShape {
+    int C, lg;              // G = 1 << lg
+    int rows, pitch;        // of a wave; words between rows in LDS
+    int pieces, magic;      // loads of a row (16 bytes, or one logit where a row is shorter than 16 bytes); item / pieces = item * magic >> 16
+    int items;              // rows * pieces <= 1024
+    size_t lds_wave;        // bytes, without extra
+};
+
+static inline NarrowShape narrow_shape(int C, int dtype) {
+    NarrowShape s;
+    const int V = dtype == CAPGNN_BF16 ? 8 : 4;
+    s.C = C;
+    s.lg = 0;
+    while ((64 << s.lg) < C) ++s.lg;
+    const int G = 1 << s.lg;
+    s.rows = 64 / G;
+    s.pitch = G * (((C + G - 1) / G) | 1);
+    s.pieces = C < V ? C : (C + V - 1) / V;
+    s.magic = (65536 + s.pieces - 1) / s.pieces;
+    s.items = s.rows * s.pieces;
+    s.lds_wave = static_cast<size_t>(s.rows) * s.pitch * sizeof(float);
+    return s;
+}
+
+// LDS written by other lanes of the wave may be read after this
+__device__ __forceinline__ void wave_sync() {
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
+// workgroups: as many as the chip holds at once (lds: bytes of one), or fewer
+static inline unsigned narrow_grid(const NarrowShape &s, int64_t n, size_t lds) {
+    const int64_t held = static_cast<int64_t>(160 * 1024 / lds) < 8 ? static_cast<int64_t>(160 * 1024 / lds) : 8;
+    const int64_t needed = (n + NARROW_WAVES * s.rows - 1) / (NARROW_WAVES * s.rows);
+    return static_cast<unsigned>(needed < NUM_CU * held ? needed : NUM_CU * held);
+}
+
+template <bool BF16> struct NarrowLoad {
+    static constexpr int MOST = 16;
+    raw16 q[MOST];
+
+    // rows [row0, row0 + s.rows), those beyond the last one again the last one
+    __device__ __forceinline__ void fetch(const NarrowShape &s, const char *Z, int64_t ldz, int64_t n, int64_t row0, int lane) {
+        typedef Raw<BF16> R;
+#pragma unroll
+        for (int i = 0; i < MOST; ++i) {
+            const int item = i * 64 + lane;
+            if (i * 64 >= s.items) break;               // (the same for all lanes)
+            if (item < s.items) {
+                const int r = item * s.magic >> 16, v = item - r * s.pieces;
+                int64_t row = row0 + r;
+                row = row < n ? row : n - 1;
+                const char *p = Z + row * ldz * (BF16 ? 2 : 4);
+                if (s.C < R::V) q[i][0] = __float_as_uint(ld_logit<BF16>(p, v));
+                else q[i] = R::load(p, v * R::V + R::V <= s.C ? v * R::V : s.C - R::V);
+            }
+        }
+    }
+
+    __device__ __forceinline__ void put(const NarrowShape &s, float *lds, int lane) {
+        typedef Raw<BF16> R;
+#pragma unroll
+        for (int i = 0; i < MOST; ++i) {
+            const int item = i * 64 + lane;
+            if (i * 64 >= s.items) break;
+            if (item < s.items) {
+                const int r = item * s.magic >> 16, v = item - r * s.pieces;
+                float *row = lds + r * s.pitch;
+                if (s.C < R::V) {
+                    row[v] = __uint_as_float(q[i][0]);
+                } else {
+                    const int j = v * R::V + R::V <= s.C ? v * R::V : s.C - R::V;
+#pragma unroll
+                    for (int e = 0; e < R::V; ++e) row[j + e] = R::get(q[i], e);
+                }
+            }
+        }
+    }
+};
+
+// From here on the compiler knows nothing of r: what it has unpacked or derived from it before is not kept in registers for later.
+__device__ __forceinline__ void forget(raw16 &r) { asm volatile("" : "+v"(r)); }
 
 template <typename T, typename Op> __device__ __forceinline__ T wave_all(T v, Op op) {
 #pragma unroll
@@ -97,8 +221,7 @@ struct OpSum {
 };
 struct OpMaxKey { __device__ unsigned long long operator()(unsigned long long a, unsigned long long b) const { return a > b ? a : b; } };
 
-// The number of masked rows (at least 1) on the device: norm_dev[0].  scratch: 512 doubles.  In ops.hip.
-int launch_mask_count(int64_t n, const uint8_t *mask, float *norm_dev, double *scratch, hipStream_t stream);
+constexpr int CLASSES_MOST = 1 << 30;       // class numbers plus a tile stay ints
 
 static inline bool element_aligned(const void *p, int dtype) { return reinterpret_cast<uintptr_t>(p) % elem_bytes(dtype) == 0; }
 
