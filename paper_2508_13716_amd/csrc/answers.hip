@@ -2,6 +2,7 @@
 #include "softrow.h"
 
 #include <algorithm>
+#include <type_traits>
 
 namespace capgnn {
 
@@ -392,16 +393,16 @@ __global__ __launch_bounds__(64 * NARROW_WAVES) void answers_narrow_kernel(Answe
             }
             const bool plain = sum == sum;
             const int first = lane & ~(G - 1);
-            int of_lane[4];         // classes noted by each lane of the row
+            int of_lane[NARROW_G];          // classes noted by each lane of the row
 #pragma unroll
-            for (int g = 0; g < 4; ++g) of_lane[g] = g < G ? __shfl(hits, first + g) : 0;
+            for (int g = 0; g < NARROW_G; ++g) of_lane[g] = g < G ? __shfl(hits, first + g) : 0;
             if (on && plain) {
                 for (int i = 0; i < hits; ++i) {
                     const int c = noted[lane * NARROW_TOP + i];
                     const float x = z[c];
                     int place = 0;
 #pragma unroll
-                    for (int g = 0; g < 4; ++g)
+                    for (int g = 0; g < NARROW_G; ++g)
                         for (int b = 0; b < of_lane[g]; ++b) {
                             const int cb = noted[(first + g) * NARROW_TOP + b];
                             const float y = z[cb];
@@ -515,55 +516,140 @@ struct AnswerGradArgs {
     char *dZ; int64_t lddz;
 };
 
-// One workgroup per row: dz = -p (G + h (ln p + H)) everywhere, then the given classes get theirs from the thread that holds the first
-// mention of the class.
-template <bool BF16, bool DBF16>
-__global__ __launch_bounds__(256) void answers_grad_kernel(AnswerGradArgs a) {
+// What a row's logits are turned into their gradients with: dz = (-p (G + h (ln p + H)) + g) / T, g for the given classes.
+struct GradRow {
+    float m0, ln_s, inv_s, G, h, H;
+    bool none;                      // masked out, or no class allowed
+
+    __device__ __forceinline__ void read(const AnswerGradArgs &a, int64_t row, bool on) {
+        ln_s = on ? a.stats[2 * row + 1] : -INFINITY;
+        none = ln_s == -INFINITY;
+        m0 = none ? 0.f : a.stats[2 * row];
+        h = !none && a.dentropy ? a.dentropy[row] : 0.f;
+        H = !none && a.dentropy ? a.entropy[row] : 0.f;
+        inv_s = expf(-ln_s);
+    }
+    template <bool ENT> __device__ __forceinline__ float base(float z, const TempScale &t) const {
+        const float d = z - m0, p = exp_scaled(d, t) * inv_s;
+        float f = G;
+        if constexpr (ENT) f = p != 0.f ? fmaf(h, fmaf(d, t.inv_T, H - ln_s), G) : 0.f;
+        return -p * f;
+    }
+};
+
+// Workgroups of THREADS take CHUNK classes of a row each; the sums of the row come with the call.  The given classes' own terms follow
+// the rest of the chunk, behind a barrier, from the thread that holds the first mention of the class.
+constexpr int GRAD_VECTORS = 4;
+template <bool BF16, bool DBF16, int THREADS, bool ENT>
+__global__ __launch_bounds__(THREADS) void answers_grad_rows_kernel(AnswerGradArgs a, int chunks) {
+    typedef Raw<BF16> R;
+    constexpr int V = R::V, CHUNK = THREADS * GRAD_VECTORS * V, MOST = CAPGNN_GIVEN_MAX / THREADS;
     __shared__ int32_t id[CAPGNN_GIVEN_MAX];
     __shared__ float g[CAPGNN_GIVEN_MAX];
-    __shared__ float red[4];
-    for (int64_t row = blockIdx.x; row < a.n; row += gridDim.x) {
+    __shared__ float red[THREADS / 64];
+    for (int64_t job = blockIdx.x; job < a.n * chunks; job += gridDim.x) {
+        const int64_t row = chunks > 1 ? job / chunks : job;
+        const int lo = chunks > 1 ? static_cast<int>(job % chunks) * CHUNK : 0, hi = a.C - lo < CHUNK ? a.C : lo + CHUNK;
         const char *z = a.Z + row * a.ldz * (BF16 ? 2 : 4);
         char *dz = a.dZ + row * a.lddz * (DBF16 ? 2 : 4);
-        const bool on = !a.mask || a.mask[row];
-        const float ln_s = on ? a.stats[2 * row + 1] : 0.f;
-        if (!on || ln_s == -INFINITY) {
-            for (int j = threadIdx.x; j < a.C; j += 256) st_grad<DBF16>(dz, j, 0.f);
-            continue;
-        }
-        const float m0 = a.stats[2 * row], inv_s = expf(-ln_s);
-        const float h = a.dentropy ? a.dentropy[row] : 0.f, H = a.dentropy ? a.entropy[row] : 0.f;
-        float mine = 0.f, zc = 0.f;
-        int c = -1;
-        if (threadIdx.x < a.m) {
-            c = a.ids[row * a.ldi + threadIdx.x];
-            if (c < 0 || c >= a.C) c = -1;
-            mine = c >= 0 ? a.dlogp[row * a.lddp + threadIdx.x] : 0.f;
-            id[threadIdx.x] = c;
-            g[threadIdx.x] = mine;
-            if (c >= 0) zc = ld_logit<BF16>(z, c);
-        }
-        const float G = group_all<256>(mine, red, OpSum());
-        auto base = [&](float v) {
-            const float d = v - m0;
-            const float p = exp_scaled(d, a.t) * inv_s;
-            float f = G;
-            if (a.dentropy && p != 0.f) f = fmaf(h, d * a.t.inv_T - ln_s + H, G);
-            return -p * f;
-        };
-        for (int j = threadIdx.x; j < a.C; j += 256) st_grad<DBF16>(dz, j, base(ld_logit<BF16>(z, j)) * a.t.inv_T);
-        __syncthreads();
-        if (c >= 0) {
-            bool first = true;
-            float sum = 0.f;
-            for (int i = 0; i < a.m; ++i)
-                if (id[i] == c) {
-                    if (i < static_cast<int>(threadIdx.x)) first = false;
-                    sum += g[i];
+        GradRow w;
+        w.read(a, row, !a.mask || a.mask[row]);
+        raw16 r[GRAD_VECTORS];
+        int from = 0;
+        if (!w.none)
+#pragma unroll
+            for (int i = 0; i < GRAD_VECTORS; ++i)
+                if (lo + i * THREADS * V < hi) r[i] = R::load_until(z, lo + (i * THREADS + static_cast<int>(threadIdx.x)) * V, hi, &from);
+        int mine[MOST];
+        float zc[MOST], G = 0.f;
+#pragma unroll
+        for (int o = 0; o < MOST; ++o) {
+            const int i = threadIdx.x + o * THREADS;
+            mine[o] = -1;
+            if (o * THREADS >= a.m) break;
+            if (i < a.m && !w.none) {
+                const int c = a.ids[row * a.ldi + i];
+                const bool ok = c >= 0 && c < a.C;
+                const float gi = ok ? a.dlogp[row * a.lddp + i] : 0.f;
+                id[i] = ok ? c : -1;
+                g[i] = gi;
+                G += gi;
+                if (c >= lo && c < hi) {
+                    mine[o] = c;
+                    zc[o] = ld_logit<BF16>(z, c);
                 }
-            if (first) st_grad<DBF16>(dz, c, (base(zc) + sum) * a.t.inv_T);
+            }
         }
-        __syncthreads();
+        w.G = a.m ? group_all<THREADS>(G, red, OpSum()) : 0.f;
+#pragma unroll
+        for (int i = 0; i < GRAD_VECTORS; ++i) {
+            const int j = lo + (i * THREADS + static_cast<int>(threadIdx.x)) * V;
+            if (lo + i * THREADS * V >= hi) break;
+            if (j >= hi) continue;
+            float o[V];
+            const int shift = j + V <= hi ? 0 : j + V - hi;         // a row's last vector starts earlier than j by that
+#pragma unroll
+            for (int e = 0; e < V; ++e) o[e] = w.none ? 0.f : w.base<ENT>(R::get(r[i], e), a.t) * a.t.inv_T;
+            if (shift == 0) st_vector<DBF16>(dz, j, o);
+            else
+#pragma unroll
+                for (int e = 0; e < V; ++e) if (e >= shift) st_grad<DBF16>(dz, hi - V + e, o[e]);
+        }
+        if (a.m) {
+            __syncthreads();
+#pragma unroll
+            for (int o = 0; o < MOST; ++o) {
+                if (o * THREADS >= a.m) break;
+                const int at = threadIdx.x + o * THREADS, c = mine[o];
+                if (c < 0) continue;
+                bool first = true;
+                float sum = 0.f;
+                for (int i = 0; i < a.m; ++i)
+                    if (id[i] == c) {
+                        first = first && i >= at;
+                        sum += g[i];
+                    }
+                if (first) st_grad<DBF16>(dz, c, (w.base<ENT>(zc[o], a.t) + sum) * a.t.inv_T);
+            }
+            __syncthreads();
+        }
+    }
+}
+
+template <bool BF16, bool DBF16, bool ENT>
+__global__ __launch_bounds__(64 * NARROW_WAVES) void answers_grad_narrow_kernel(AnswerGradArgs a, NarrowShape s) {
+    extern __shared__ __align__(16) char lds_all[];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    float *tile = reinterpret_cast<float *>(lds_all + wave * s.lds_wave);
+    const int G = 1 << s.lg, sub = lane & (G - 1), C = s.C;
+    float *z = tile + (lane >> s.lg) * s.pitch;
+    const int64_t step = static_cast<int64_t>(gridDim.x) * NARROW_WAVES * s.rows;
+    int64_t row0 = (static_cast<int64_t>(blockIdx.x) * NARROW_WAVES + wave) * s.rows;
+    NarrowLoad<BF16> next;
+    if (row0 < a.n) next.fetch(s, a.Z, a.ldz, a.n, row0, lane);
+    for (; row0 < a.n; row0 += step) {
+        const int64_t row = row0 + (lane >> s.lg) < a.n ? row0 + (lane >> s.lg) : a.n - 1;
+        GradRow w;
+        w.read(a, row, !a.mask || a.mask[row]);
+        w.G = 0.f;
+        if (!w.none)
+            for (int i = 0; i < a.m; ++i) {
+                const int c = a.ids[row * a.ldi + i];
+                if (c >= 0 && c < C) w.G += a.dlogp[row * a.lddp + i];
+            }
+        next.put(s, tile, lane);
+        wave_sync();
+        if (row0 + step < a.n) next.fetch(s, a.Z, a.ldz, a.n, row0 + step, lane);
+        for (int j = sub; j < C; j += G) z[j] = w.none ? 0.f : w.base<ENT>(z[j], a.t) * a.t.inv_T;
+        wave_sync();
+        if (sub == 0 && !w.none)            // one lane a row: the same class may be given again
+            for (int i = 0; i < a.m; ++i) {
+                const int c = a.ids[row * a.ldi + i];
+                if (c >= 0 && c < C) z[c] = fmaf(a.dlogp[row * a.lddp + i], a.t.inv_T, z[c]);
+            }
+        wave_sync();
+        narrow_store<BF16, DBF16>(s, tile, a.dZ, a.lddz, a.n, row0, lane, false);
+        wave_sync();
     }
 }
 
@@ -643,6 +729,7 @@ extern "C" int capgnn_logprobs_bwd(int64_t n, int C, const void *Z, int64_t ldz,
     if ((z_dtype != CAPGNN_F32 && z_dtype != CAPGNN_BF16) || (dz_dtype != CAPGNN_F32 && dz_dtype != CAPGNN_BF16))
         CG_FAIL(CAPGNN_EINVAL, "logprobs_bwd: unknown z_dtype or dz_dtype");
     if (n < 0 || C <= 0) CG_FAIL(CAPGNN_EINVAL, "logprobs_bwd: bad sizes");
+    if (C > CLASSES_MOST) CG_FAIL(CAPGNN_EUNSUPPORTED, "logprobs_bwd: more than 2^30 classes");
     if (m < 0 || m > CAPGNN_GIVEN_MAX) CG_FAIL(CAPGNN_EINVAL, "logprobs_bwd: m = %d, 0 to %d classes can be given per row", m, CAPGNN_GIVEN_MAX);
     if (!good_temperature(temperature)) CG_FAIL(CAPGNN_EINVAL, "logprobs_bwd: the temperature must be positive and finite");
     if (n == 0) return CAPGNN_OK;
@@ -653,10 +740,33 @@ extern "C" int capgnn_logprobs_bwd(int64_t n, int C, const void *Z, int64_t ldz,
     hipStream_t st = static_cast<hipStream_t>(stream);
     AnswerGradArgs a{n, C, static_cast<const char *>(Z), ldz, temp_scale(temperature), mask, stats, entropy, ids, ldi, m, dlogp, lddp,
                      dentropy, static_cast<char *>(dZ), lddz};
-    const unsigned grid = static_cast<unsigned>(std::min<int64_t>(n, 1 << 20));
-    auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(grid), dim3(256), 0, st, a); };
-    if (z_dtype == CAPGNN_BF16) dz_dtype == CAPGNN_BF16 ? go(answers_grad_kernel<true, true>) : go(answers_grad_kernel<true, false>);
-    else dz_dtype == CAPGNN_BF16 ? go(answers_grad_kernel<false, true>) : go(answers_grad_kernel<false, false>);
+    const bool zb = z_dtype == CAPGNN_BF16, db = dz_dtype == CAPGNN_BF16, ent = dentropy != nullptr;
+    auto types = [&](auto f) {          // f(type of Z, type of dZ, with entropy), as compile-time truth values
+        using Y = std::true_type;
+        using N = std::false_type;
+        if (zb) {
+            if (db) ent ? f(Y(), Y(), Y()) : f(Y(), Y(), N());
+            else ent ? f(Y(), N(), Y()) : f(Y(), N(), N());
+        } else {
+            if (db) ent ? f(N(), Y(), Y()) : f(N(), Y(), N());
+            else ent ? f(N(), N(), Y()) : f(N(), N(), N());
+        }
+    };
+    if (C <= NARROW_C) {
+        const NarrowShape s = narrow_shape(C, z_dtype);
+        const size_t lds = NARROW_WAVES * s.lds_wave;
+        types([&](auto z, auto d, auto e) {
+            hipLaunchKernelGGL((answers_grad_narrow_kernel<z.value, d.value, e.value>), dim3(narrow_grid(s, n, lds)), dim3(64 * NARROW_WAVES), lds, st, a, s);
+        });
+    } else {
+        const int V = zb ? 8 : 4, threads = C <= 64 * GRAD_VECTORS * V ? 64 : 256;
+        const int chunks = (C + threads * GRAD_VECTORS * V - 1) / (threads * GRAD_VECTORS * V);
+        const unsigned grid = static_cast<unsigned>(std::min<int64_t>(n * chunks, 1 << 24));
+        types([&](auto z, auto d, auto e) {
+            if (threads == 64) hipLaunchKernelGGL((answers_grad_rows_kernel<z.value, d.value, 64, e.value>), dim3(grid), dim3(64), 0, st, a, chunks);
+            else hipLaunchKernelGGL((answers_grad_rows_kernel<z.value, d.value, 256, e.value>), dim3(grid), dim3(256), 0, st, a, chunks);
+        });
+    }
     CG_HIP(hipGetLastError());
     return CAPGNN_OK;
 }

@@ -29,14 +29,15 @@ template <bool BF16> __device__ __forceinline__ float ld_logit(const char *p, in
     else return reinterpret_cast<const float *>(p)[i];
 }
 
-__device__ __forceinline__ uint32_t bf16_bits(float v) {        // round to nearest even; NaN stays NaN
-    uint32_t u = __float_as_uint(v);
-    if ((u & 0x7fffffffu) > 0x7f800000u) return (u >> 16) | 0x40u;
-    return (u + 0x7fffu + ((u >> 16) & 1u)) >> 16;
+typedef __bf16 bf16_pair __attribute__((ext_vector_type(2)));
+typedef float float_pair __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ uint32_t bf16_two(float a, float b) {        // (one instruction)
+    const float_pair v = {a, b};
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, bf16_pair));
 }
 
 template <bool BF16> __device__ __forceinline__ void st_grad(char *p, int64_t i, float v) {
-    if constexpr (BF16) reinterpret_cast<uint16_t *>(p)[i] = static_cast<uint16_t>(bf16_bits(v));
+    if constexpr (BF16) reinterpret_cast<uint16_t *>(p)[i] = static_cast<uint16_t>(bf16_two(v, 0.f));
     else reinterpret_cast<float *>(p)[i] = v;
 }
 
@@ -48,6 +49,14 @@ __device__ __forceinline__ float exp_scaled(float d, const TempScale &t) {
     const float e = exp2_raw(u);
     const float lost = fmaf(d, t.L_lo, fmaf(d, t.L, -u));
     return e > 0.f ? fmaf(e, lost * 0.69314718f, e) : e;        // (d = -inf: lost is NaN, e is 0; a NaN d gives a NaN e)
+}
+
+// exp((a - b) / T), a <= b, without the rounding of a - b either (a teacher's probabilities: few, so the six operations more do not count)
+__device__ __forceinline__ float exp_difference(float a, float b, const TempScale &t) {
+    const float d = a - b, back = d - a, rest = (a - (d - back)) + (-b - back);
+    const float u = d * t.L, e = exp2_raw(u);
+    const float lost = fmaf(rest, t.L, fmaf(d, t.L_lo, fmaf(d, t.L, -u)));
+    return e > 0.f ? fmaf(e, lost * 0.69314718f, e) : e;
 }
 
 // the larger of the two; NaN if either is (one instruction, as the maximum that skips NaN)
@@ -105,17 +114,57 @@ template <bool BF16> struct Raw {
     }
 };
 
-// Rows of at most NARROW_C classes: a wave takes 64 / G of them at a time through LDS, G lanes a row with at most 64 classes each, so that a
-// row's sums need no or hardly any exchange between lanes (lane groups over registers spent four times the instructions at 47 classes:
+// V floats to the gradient row p, classes [j, j + V), in the widest stores there are; V is that of the logits' type
+typedef uint32_t raw8 __attribute__((ext_vector_type(2)));
+typedef raw8 raw8_by2 __attribute__((aligned(2)));
+template <bool DBF16, int V> __device__ __forceinline__ void st_vector(char *p, int j, const float (&g)[V]) {
+    if constexpr (DBF16) {
+        if constexpr (V == 8)
+            *reinterpret_cast<raw16_by2 *>(p + static_cast<int64_t>(j) * 2) =
+                raw16{bf16_two(g[0], g[1]), bf16_two(g[2], g[3]), bf16_two(g[4], g[5]), bf16_two(g[6], g[7])};
+        else
+            *reinterpret_cast<raw8_by2 *>(p + static_cast<int64_t>(j) * 2) = raw8{bf16_two(g[0], g[1]), bf16_two(g[2], g[3])};
+    } else {
+#pragma unroll
+        for (int h = 0; h < V; h += 4)
+            *reinterpret_cast<raw16_by4 *>(p + static_cast<int64_t>(j + h) * 4) =
+                raw16{__float_as_uint(g[h]), __float_as_uint(g[h + 1]), __float_as_uint(g[h + 2]), __float_as_uint(g[h + 3])};
+    }
+}
+template <bool DBF16, int V> __device__ __forceinline__ void ld_vector(const char *p, int j, float (&g)[V]) {
+    if constexpr (DBF16) {
+        raw16 r = {0, 0, 0, 0};
+        if constexpr (V == 8) {
+            r = *reinterpret_cast<const raw16_by2 *>(p + static_cast<int64_t>(j) * 2);
+        } else {
+            const raw8 q = *reinterpret_cast<const raw8_by2 *>(p + static_cast<int64_t>(j) * 2);
+            r[0] = q[0];
+            r[1] = q[1];
+        }
+#pragma unroll
+        for (int e = 0; e < V; ++e) g[e] = Raw<true>::get(r, e);
+    } else {
+#pragma unroll
+        for (int h = 0; h < V; h += 4) {
+            const raw16 r = *reinterpret_cast<const raw16_by4 *>(p + static_cast<int64_t>(j + h) * 4);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) g[h + e] = __uint_as_float(r[e]);
+        }
+    }
+}
+
+// Rows of at most NARROW_C classes: a wave takes 64 / G of them at a time through LDS, G lanes a row with at most 32 classes each, so that a
+// row's sums need hardly any exchange between lanes (lane groups over registers spent four times the instructions at 47 classes:
 // 612000 rows were bound by them, not by memory).  The next rows' loads are under way while a wave works on its own.  A row starts
-// G * odd words after the one before it: lanes that read class k of their rows at once hit different banks.
+// G * odd words after the one before it: lanes that read the same class of their rows at once hit different banks.
 constexpr int NARROW_C = 256;
+constexpr int NARROW_G = NARROW_C / 32;     // lanes of a row at most
 constexpr int NARROW_WAVES = 2;     // of a workgroup; each works for itself
 struct NarrowShape {
     int C, lg;              // G = 1 << lg
     int rows, pitch;        // of a wave; words between rows in LDS
     int pieces, magic;      // loads of a row (16 bytes, or one logit where a row is shorter than 16 bytes); item / pieces = item * magic >> 16
-    int items;              // rows * pieces <= 1024
+    int items;              // rows * pieces <= 64 * NarrowLoad::MOST
     size_t lds_wave;        // bytes, without extra
 };
 
@@ -124,7 +173,7 @@ static inline NarrowShape narrow_shape(int C, int dtype) {
     const int V = dtype == CAPGNN_BF16 ? 8 : 4;
     s.C = C;
     s.lg = 0;
-    while ((64 << s.lg) < C) ++s.lg;
+    while ((32 << s.lg) < C) ++s.lg;
     const int G = 1 << s.lg;
     s.rows = 64 / G;
     s.pitch = G * (((C + G - 1) / G) | 1);
@@ -150,7 +199,7 @@ static inline unsigned narrow_grid(const NarrowShape &s, int64_t n, size_t lds) 
 }
 
 template <bool BF16> struct NarrowLoad {
-    static constexpr int MOST = 16;
+    static constexpr int MOST = BF16 ? 7 : 8;       // (bf16: 4 of 16 bytes, or up to 7 of one logit)
     raw16 q[MOST];
 
     // rows [row0, row0 + s.rows), those beyond the last one again the last one
@@ -192,8 +241,45 @@ template <bool BF16> struct NarrowLoad {
     }
 };
 
-// From here on the compiler knows nothing of r: what it has unpacked or derived from it before is not kept in registers for later.
-__device__ __forceinline__ void forget(raw16 &r) { asm volatile("" : "+v"(r)); }
+// The wave's rows of gradients, from LDS as NarrowLoad put the logits there; add: to what dZ holds.
+template <bool BF16, bool DBF16>
+__device__ __forceinline__ void narrow_store(const NarrowShape &s, const float *lds, char *dZ, int64_t lddz, int64_t n, int64_t row0, int lane,
+                                             bool add) {
+    constexpr int V = Raw<BF16>::V;
+#pragma unroll
+    for (int i = 0; i < NarrowLoad<BF16>::MOST; ++i) {
+        const int item = i * 64 + lane;
+        if (i * 64 >= s.items) break;
+        const int r = item * s.magic >> 16, v = item - r * s.pieces;
+        if (item < s.items && row0 + r < n) {
+            char *p = dZ + (row0 + r) * lddz * (DBF16 ? 2 : 4);
+            const float *row = lds + r * s.pitch;
+            if (s.C < V || v * V + V > s.C) {           // one logit, or what is left of a row
+                const int j = s.C < V ? v : v * V, end = s.C < V ? v + 1 : s.C;
+                for (int k = j; k < end; ++k) st_grad<DBF16>(p, k, add ? ld_logit<DBF16>(p, k) + row[k] : row[k]);
+            } else {
+                float g[V];
+                if (add) ld_vector<DBF16>(p, v * V, g);
+#pragma unroll
+                for (int e = 0; e < V; ++e) g[e] = add ? g[e] + row[v * V + e] : row[v * V + e];
+                st_vector<DBF16>(p, v * V, g);
+            }
+        }
+    }
+}
+
+// From here on the compiler knows nothing of r: what it has unpacked or derived from it before is not kept in registers for later, and
+// work on one vector is not mixed with that on the next (which took twice the registers; other waves fill the gaps).
+__device__ __forceinline__ void forget(raw16 &r) {
+    __builtin_amdgcn_sched_barrier(0);
+    asm volatile("" : "+v"(r));
+}
+// The thread's number, of which the compiler knows nothing: addresses and conditions formed from it are not kept for the next use.
+__device__ __forceinline__ int thread_anew() {
+    int t = threadIdx.x;
+    asm volatile("" : "+v"(t));
+    return t;
+}
 
 template <typename T, typename Op> __device__ __forceinline__ T wave_all(T v, Op op) {
 #pragma unroll
@@ -222,6 +308,24 @@ struct OpSum {
 struct OpMaxKey { __device__ unsigned long long operator()(unsigned long long a, unsigned long long b) const { return a > b ? a : b; } };
 
 constexpr int CLASSES_MOST = 1 << 30;       // class numbers plus a tile stay ints
+
+// maximum and sum of exponentials of every thread, taken together: the same in every thread.  red: a pair per wave; a barrier has to
+// pass before it is used again.
+template <int THREADS> __device__ __forceinline__ void group_softmax(float &m, float &s, const TempScale &t, float2 *red) {
+    const float M = wave_all(m, OpMax());
+    s = wave_all(s * exp2_raw((m - safe_max(M)) * t.L), OpSum());
+    m = M;
+    if constexpr (THREADS > 64) {
+        if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = make_float2(m, s);
+        __syncthreads();
+#pragma unroll
+        for (int w = 0; w < THREADS / 64; ++w) m = max_of(m, red[w].x);
+        const float ref = safe_max(m);
+        s = 0.f;
+#pragma unroll
+        for (int w = 0; w < THREADS / 64; ++w) s += red[w].y * exp2_raw((red[w].x - ref) * t.L);
+    }
+}
 
 static inline bool element_aligned(const void *p, int dtype) { return reinterpret_cast<uintptr_t>(p) % elem_bytes(dtype) == 0; }
 
