@@ -42,19 +42,20 @@ struct RowEnd {
 };
 
 // ------------------------------------------------------------------ the k largest of a stream of logits
-// A workgroup walks a row tile by tile and keeps the keys (logit, class) that may still be among the k largest in LDS, together with a
-// threshold: of at least k logits it is known that they are no smaller.  A tile's thread maxima give the first one: the k-th largest of
-// them is exceeded by hardly more than k logits of the tile (64 largest of 16384: 73 on average).  What passes the threshold is appended;
-// the list is ranked, each key by counting the larger ones, when it is half full and at the end.  Keys are distinct, so the
-// result does not depend on the order in which threads append.  A tile that passes more than the list holds is tried again
-// with its own maxima, then with its exact k-th largest key (equal logits, values in order): slower, never wrong.
+// Every wave walks its share of a row and keeps the keys (logit, class) that may still be among the k largest in LDS, together with a
+// threshold: of at least k logits of the row it is known that they are no smaller.  The first tile's thread maxima give one for the whole
+// workgroup: the k-th largest of them is exceeded by hardly more than k logits of the tile (64 largest of 16384: 73 on average).  What
+// passes the threshold is appended; a wave's list that is half full is ranked, each key by counting the larger ones, and cut to k.
+// Keys are distinct, so the order of appending does not show.  A tile that passes more than the list holds is tried again with the
+// wave's own maxima, then with its exact k-th largest key (equal logits, values in order): slower, never wrong.  The waves meet
+// at the first threshold and at the end of the row only (a list for the workgroup, with an atomic counter and a barrier per tile:
+// 4096 x 131072 bf16, k = 64, 471 us).
 template <int THREADS> struct TopLds {
-    static constexpr int CAP = THREADS == 64 ? 512 : 1024;
-    unsigned long long key[CAP], best[CAPGNN_TOP_MAX];
+    static constexpr int WAVES = THREADS / 64, CAP = THREADS == 64 ? 512 : 256;
+    unsigned long long key[WAVES][CAP], best[WAVES][CAPGNN_TOP_MAX];
     uint32_t maxima[THREADS];
-    int count[3];
+    int kept[WAVES];
     uint32_t bound;
-    int red[THREADS / 64];
 };
 
 // the float just below every logit of order o and more; NaN (no logit is <= it) where there is none
@@ -64,125 +65,139 @@ __device__ __forceinline__ float just_below(uint32_t o) {
     return o <= 0x007fffffu ? __uint_as_float(0x7fc00000u) : order_logit(b);
 }
 
+// how many of n keys (n even, 16 bytes aligned) are larger
+__device__ __forceinline__ int larger_keys(const unsigned long long *key, int n, unsigned long long own) {
+    const ulonglong2 *q = reinterpret_cast<const ulonglong2 *>(key);
+    int larger = 0;
+#pragma unroll 4
+    for (int j = 0; j < n / 2; ++j) {
+        const ulonglong2 v = q[j];
+        larger += (v.x > own) + (v.y > own);
+    }
+    return larger;
+}
+
 template <int THREADS> struct Top {
-    static constexpr int CAP = TopLds<THREADS>::CAP;
+    static constexpr int CAP = TopLds<THREADS>::CAP, WAVES = THREADS / 64;
     TopLds<THREADS> &l;
-    int k, kept = 0, turn = 0;
+    int k, kept = 0;                                    // keys in the wave's list
     float below = __uint_as_float(0x7fc00000u);         // a logit is a candidate unless it is <= this
 
-    __device__ Top(TopLds<THREADS> &lds, int k_) : l(lds), k(k_) {
-        if (threadIdx.x < 3) l.count[threadIdx.x] = 0;
-        __syncthreads();
-    }
+    __device__ Top(TopLds<THREADS> &lds, int k_) : l(lds), k(k_) {}
+    static __device__ __forceinline__ int wave() { return THREADS == 64 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); }
+    static __device__ __forceinline__ int lane() { return threadIdx.x & 63; }
 
     __device__ void raise(uint32_t order, bool inclusive) {
         const float f = inclusive ? just_below(order) : order_logit(order);
         if (f == f && !(f <= below)) below = f;         // (from NaN to anything, to NaN never)
     }
 
-    // the k-th largest of the threads' maxima (k <= THREADS)
-    __device__ uint32_t kth_maximum(float tmax) {
-        const uint32_t mine = logit_order(tmax);
-        l.maxima[threadIdx.x] = mine;
-        __syncthreads();
+    // The k-th largest of N threads' maxima (k <= N), or hardly less: the last bits of the order are the thread's number, so that no two are
+    // equal and one comparison each ranks them.  N = THREADS: of the workgroup; 64: of the wave.
+    template <int N> __device__ uint32_t kth_maximum(float tmax) {
+        const int t = N == 64 ? lane() : threadIdx.x;
+        uint32_t *maxima = N == 64 ? l.maxima + wave() * 64 : l.maxima;
+        const uint32_t mine = (logit_order(tmax) & ~(N - 1u)) | t;
+        maxima[t] = mine;
+        N == 64 ? wave_sync() : __syncthreads();
         int larger = 0;
-        const uint4 *q = reinterpret_cast<const uint4 *>(l.maxima);
+        const uint4 *q = reinterpret_cast<const uint4 *>(maxima);
 #pragma unroll 4
-        for (int i = 0; i < THREADS / 4; ++i) {
+        for (int i = 0; i < N / 4; ++i) {
             const uint4 v = q[i];
-            const int t = threadIdx.x - 4 * i;
-            larger += (v.x > mine || (v.x == mine && t > 0)) + (v.y > mine || (v.y == mine && t > 1)) +
-                      (v.z > mine || (v.z == mine && t > 2)) + (v.w > mine || (v.w == mine && t > 3));
+            larger += v.x > mine;
+            larger += v.y > mine;
+            larger += v.z > mine;
+            larger += v.w > mine;
         }
-        if (larger == k - 1) l.bound = mine;
-        __syncthreads();
-        const uint32_t r = l.bound;
-        __syncthreads();
-        return r;
+        if constexpr (N == 64) {
+            const unsigned long long at = __ballot(larger == k - 1);
+            return __shfl(mine, __ffsll(at) - 1) & ~(N - 1u);
+        } else {
+            if (larger == k - 1) l.bound = mine & ~(N - 1u);
+            __syncthreads();
+            return l.bound;                             // (written once a row: a barrier lies before the next time)
+        }
     }
 
-    // ranks the kept keys: the k largest are left, in descending order
-    __device__ void rank() {
+    // cuts the wave's list to its k largest, in descending order
+    __device__ void cut() {
+        unsigned long long *key = l.key[wave()], *best = l.best[wave()];
         const int n = kept;
-        if (threadIdx.x == 0 && (n & 1)) l.key[n] = 0;          // a pair is read at a time
-        __syncthreads();
-        const ulonglong2 *q = reinterpret_cast<const ulonglong2 *>(l.key);
+        if (lane() == 0 && (n & 1)) key[n] = 0;
+        wave_sync();
 #pragma unroll 1
-        for (int i = threadIdx.x; i < n; i += THREADS) {
-            const unsigned long long own = l.key[i];
-            int larger = 0;
-#pragma unroll 4
-            for (int j = 0; j < (n + 1) / 2; ++j) {
-                const ulonglong2 v = q[j];
-                larger += (v.x > own) + (v.y > own);
-            }
-            if (larger < k) l.best[larger] = own;
+        for (int i = lane(); i < n; i += 64) {
+            const unsigned long long own = key[i];
+            const int at = larger_keys(key, n + 1 & ~1, own);
+            if (at < k) best[at] = own;
         }
-        __syncthreads();
+        wave_sync();
         kept = n < k ? n : k;
-        if (static_cast<int>(threadIdx.x) < kept) l.key[threadIdx.x] = l.best[threadIdx.x];
-        if (kept == k) raise(static_cast<uint32_t>(l.best[k - 1] >> 32), false);
-        __syncthreads();
+        if (lane() < kept) key[lane()] = best[lane()];
+        if (kept == k) raise(static_cast<uint32_t>(best[k - 1] >> 32), false);
+        wave_sync();
     }
 
-    // what the threads have appended since the last barrier; false if the list does not hold it
-    __device__ bool settle(int *added) {
-        __syncthreads();
-        const int c = l.count[turn];
-        // three counters in turn: this one is cleared before the next barrier, and used again after it
-        if (threadIdx.x == 0) l.count[(turn + 2) % 3] = 0;
-        turn = (turn + 1) % 3;
-        *added = c;
-        return kept + c <= CAP;
-    }
-
-    __device__ void append(float z, int j) {
-        const int p = kept + atomicAdd(&l.count[turn], 1);
-        if (p < CAP) l.key[p] = logit_key(z, j);
+    // one key of every lane that has one; false if the list does not hold them
+    __device__ bool append(bool has, float z, int j) {
+        const unsigned long long lanes = __ballot(has);
+        const int count = __popcll(lanes);
+        if (kept + count > CAP) return false;
+        const int at = kept + __builtin_amdgcn_mbcnt_hi(static_cast<uint32_t>(lanes >> 32), __builtin_amdgcn_mbcnt_lo(static_cast<uint32_t>(lanes), 0));
+        if (has) l.key[wave()][at] = logit_key(z, j);
+        kept += count;
+        return true;
     }
 
     // the tile of NV vectors a thread, as the row's scan has read them; classes [from, end) are in the tile
     template <bool BF16, int NV>
-    __device__ void tile(raw16 (&r)[NV], const float (&vmax)[NV], float tmax, const char *z, int from, int end) {
+    __device__ void tile(raw16 (&r)[NV], const float (&vmax)[NV], float tmax, const char *z, int from, int end, bool first) {
         typedef Raw<BF16> R;
-        if (kept == 0 && end - from > CAP / 2) raise(kth_maximum(tmax), true);
-        int added;
+        if (first && end - from > THREADS / 64 * CAP / 2) raise(kth_maximum<THREADS>(tmax), true);
+        const int before = kept;
 #pragma unroll 1
         for (int attempt = 0; attempt < 2; ++attempt) {
+            const int tid = thread_anew();
+            bool fits = true;
 #pragma unroll
             for (int i = 0; i < NV; ++i) {
-                if (!__any(!(vmax[i] <= below))) continue;
-                const int own = from + (i * THREADS + static_cast<int>(threadIdx.x)) * R::V;
-                int j = own + R::V <= end ? own : end - R::V;
-                raw16 t = r[i];
-#pragma unroll 1
-                for (int word = 0; word < 4; ++word) {          // (rolled: 64 appends in a row cost 140 registers)
-                    const float x = R::get(t, 0);
-                    if (!(x <= below) && j >= own) append(x, j);
-                    ++j;
-                    if constexpr (BF16) {
-                        const float y = R::get(t, 1);
-                        if (!(y <= below) && j >= own) append(y, j);
-                        ++j;
-                    }
-                    t = raw16{t[1], t[2], t[3], t[0]};
+                if (!fits || !__any(!(vmax[i] <= below))) continue;
+                forget(r[i]);
+                uint32_t passed = 0;
+#pragma unroll
+                for (int e = 0; e < R::V; ++e) passed |= !(R::get(r[i], e) <= below) ? 1u << e : 0u;
+                const int own = from + (i * THREADS + tid) * R::V, start = own + R::V <= end ? own : end - R::V;
+                passed = own < end ? passed & ~0u << (own - start) : 0u;        // (the row's last vectors start earlier)
+                while (fits && __any(passed != 0)) {
+                    const bool has = passed != 0;
+                    const int e = __ffs(passed) - 1;
+                    passed &= passed - 1;
+                    const int word = BF16 ? e >> 1 : e;
+                    const uint32_t lo = word & 1 ? r[i][1] : r[i][0], hi = word & 1 ? r[i][3] : r[i][2], w = word & 2 ? hi : lo;
+                    fits = append(has, __uint_as_float(!BF16 ? w : e & 1 ? w & 0xffff0000u : w << 16), start + e);
                 }
             }
-            if (settle(&added)) {
-                kept += added;
-                if (kept > CAP / 2) rank();
+            if (fits) {
+                if (kept > CAP / 2) cut();
                 return;
             }
-            if (attempt == 0) raise(kth_maximum(tmax), true);
+            kept = before;
+            if (attempt == 0) raise(kth_maximum<64>(tmax), true);
         }
-        // the tile's exact k-th largest key, bit by bit: order T, classes below J
-        const int want = end - from < k ? end - from : k;
+        // the exact k-th largest key of the wave's share, bit by bit: order T, classes below J
+        auto each = [&](auto f) {
+#pragma unroll 1
+            for (int v = from + static_cast<int>(threadIdx.x) * R::V; __any(v < end); v += THREADS * R::V)
+#pragma unroll 1
+                for (int e = 0; e < R::V; ++e) f(v + e < end ? ld_logit<BF16>(z, v + e) : 0.f, v + e, v + e < end);
+        };
         auto count = [&](auto in) {
             int c = 0;
-#pragma unroll 1
-            for (int j = from + threadIdx.x; j < end; j += THREADS) c += in(logit_order(ld_logit<BF16>(z, j)), j);
-            return group_all<THREADS>(c, l.red, OpSum());
+            each([&](float x, int j, bool there) { c += there && in(logit_order(x), j); });
+            return wave_all(c, OpSum());
         };
+        const int all = count([](uint32_t, int) { return true; }), want = all < k ? all : k;
         uint32_t T = 0;
         int J = 0;
         for (int bit = 31; bit >= 0; --bit) {
@@ -194,15 +209,38 @@ template <int THREADS> struct Top {
             const int t = J | 1 << bit;
             if (count([&](uint32_t o, int j) { return o == T && j < t; }) <= want - above) J = t;
         }
-#pragma unroll 1
-        for (int j = from + threadIdx.x; j < end; j += THREADS) {
-            const float x = ld_logit<BF16>(z, j);
+        each([&](float x, int j, bool there) {
             const uint32_t o = logit_order(x);
-            if (o > T || (o == T && j < J)) append(x, j);
+            append(there && (o > T || (o == T && j < J)), x, j);        // want <= k more: they fit behind at most CAP / 2
+        });
+        cut();
+    }
+
+    // The row's k largest in descending order, in l.best[0]; how many there are.  Barriers before and after.
+    __device__ int finish() {
+        if constexpr (WAVES == 1) {
+            cut();
+            return kept;
+        } else {
+            if (lane() == 0) {
+                l.kept[wave()] = kept;
+                if (kept & 1) l.key[wave()][kept] = 0;
+            }
+            __syncthreads();
+            int total = 0, n[WAVES];
+#pragma unroll
+            for (int w = 0; w < WAVES; ++w) { n[w] = l.kept[w]; total += n[w]; }
+#pragma unroll 1
+            for (int i = lane(); i < kept; i += 64) {
+                const unsigned long long own = l.key[wave()][i];
+                int at = 0;
+#pragma unroll 1
+                for (int w = 0; w < WAVES; ++w) at += larger_keys(l.key[w], l.kept[w] + 1 & ~1, own);
+                if (at < k) l.best[0][at] = own;
+            }
+            __syncthreads();
+            return total < k ? total : k;
         }
-        settle(&added);
-        kept += added;
-        rank();
     }
 };
 
@@ -217,7 +255,7 @@ struct AnswerParts {
 };
 
 template <bool BF16, int THREADS, bool ENT>
-__global__ __launch_bounds__(THREADS) void answers_rows_kernel(AnswerArgs a, AnswerParts w) {
+__global__ __launch_bounds__(THREADS) __attribute__((amdgpu_waves_per_eu(4))) void answers_rows_kernel(AnswerArgs a, AnswerParts w) {
     typedef Raw<BF16> R;
     constexpr int NV = ANSWER_VECTORS, TILE = THREADS * NV * R::V;
     __shared__ __align__(16) TopLds<THREADS> lds;
@@ -237,10 +275,11 @@ __global__ __launch_bounds__(THREADS) void answers_rows_kernel(AnswerArgs a, Ans
         for (int t0 = lo; t0 < hi; t0 += TILE) {
             raw16 r[NV];
             float vmax[NV], tmax = -INFINITY;
+            const int tid = thread_anew();
             int start;
 #pragma unroll
             for (int i = 0; i < NV; ++i)
-                if (t0 + i * THREADS * R::V < hi) r[i] = R::load_until(z, t0 + (i * THREADS + static_cast<int>(threadIdx.x)) * R::V, hi, &start);
+                if (t0 + i * THREADS * R::V < hi) r[i] = R::load_until(z, t0 + (i * THREADS + tid) * R::V, hi, &start);
                 else r[i] = raw16{R::BARRED, R::BARRED, R::BARRED, R::BARRED};
 #pragma unroll
             for (int i = 0; i < NV; ++i) {
@@ -266,17 +305,17 @@ __global__ __launch_bounds__(THREADS) void answers_rows_kernel(AnswerArgs a, Ans
                     if constexpr (ENT) e1 = fmaf(x, fmaxf(u, -160.f), e1);
                 }
             }
-            if (a.k) top.template tile<BF16>(r, vmax, tmax, z, t0, hi - t0 < TILE ? hi : t0 + TILE);
+            if (a.k) top.template tile<BF16>(r, vmax, tmax, z, t0, hi - t0 < TILE ? hi : t0 + TILE, t0 == lo);
         }
         // a thread's sums, taken from its own maximum to the row's
         const float M = group_all<THREADS>(m, red, OpMax()), ref = safe_max(M);
         const float du = (m - ref) * a.t.L, f = exp2_raw(du);
         if constexpr (ENT) e1 = group_all<THREADS>(f * fmaf(s, fmaxf(du, -160.f), e1), red, OpSum());
         s = group_all<THREADS>(s * f, red, OpSum());
-        if (a.k) top.rank();
+        const int found = a.k ? top.finish() : 0;
         if (w.parts > 1) {
             if (threadIdx.x == 0) w.sums[job] = make_float4(M, s, e1, 0.f);
-            for (int i = threadIdx.x; i < a.k; i += THREADS) w.keys[job * a.k + i] = i < top.kept ? lds.key[i] : 0;
+            for (int i = threadIdx.x; i < a.k; i += THREADS) w.keys[job * a.k + i] = i < found ? lds.best[0][i] : 0;
         } else {
             const RowEnd end(M, s, a.t.inv_T);
             if (threadIdx.x == 0) {
@@ -288,7 +327,7 @@ __global__ __launch_bounds__(THREADS) void answers_rows_kernel(AnswerArgs a, Ans
                 a.logp[row * a.ldp + i] = c >= 0 && c < a.C ? end.logp(ld_logit<BF16>(z, c)) : 0.f;
             }
             for (int i = threadIdx.x; i < a.k; i += THREADS) {
-                const unsigned long long key = lds.key[i];
+                const unsigned long long key = lds.best[0][i];
                 if (a.top_ids) a.top_ids[row * a.ldt + i] = static_cast<int32_t>(0xffffffffu - static_cast<uint32_t>(key));
                 if (a.top_logp) a.top_logp[row * a.ldt + i] = end.logp(order_logit(static_cast<uint32_t>(key >> 32)));
             }
@@ -435,7 +474,9 @@ constexpr int ANSWER_PARTS = 64;
 template <bool BF16>
 __global__ __launch_bounds__(256) void answers_join_kernel(AnswerArgs a, AnswerParts w) {
     constexpr int OWN = ANSWER_PARTS * CAPGNN_TOP_MAX / 256;
-    __shared__ __align__(16) TopLds<256> lds;
+    __shared__ __align__(16) unsigned long long key[ANSWER_PARTS * CAPGNN_TOP_MAX / 4], maxima[256], best_of[CAPGNN_TOP_MAX];
+    __shared__ unsigned long long shared_bound;
+    __shared__ int kept;
     __shared__ float red[4];
     for (int64_t row = blockIdx.x; row < a.n; row += gridDim.x) {
         if (a.mask && !a.mask[row]) continue;
@@ -463,30 +504,29 @@ __global__ __launch_bounds__(256) void answers_join_kernel(AnswerArgs a, AnswerP
         }
         if (a.k) {
             // keys at least as large as the k-th largest of the threads' maxima: k threads have them, OWN at most each
-            Top<256> top(lds, a.k);
-            unsigned long long bound = 1;
-            if (w.parts * a.k > 256) {
-                lds.key[i] = best;
-                if (i == 0) lds.key[256] = 1;
-                __syncthreads();
-                int larger = 0;
-                const ulonglong2 *q = reinterpret_cast<const ulonglong2 *>(lds.key);
-                for (int j = 0; j < 128; ++j) larger += (q[j].x > best) + (q[j].y > best);
-                if (larger == a.k - 1 && best) lds.key[256] = best;
-                __syncthreads();
-                bound = lds.key[256];
-                __syncthreads();
-            }
+            maxima[i] = best;
+            if (i == 0) { shared_bound = 1; kept = 0; }
+            __syncthreads();
+            if (w.parts * a.k > 256 && best && larger_keys(maxima, 256, best) == a.k - 1) shared_bound = best;
+            __syncthreads();
+            const unsigned long long bound = shared_bound;
 #pragma unroll
             for (int o = 0; o < OWN; ++o)
-                if (own[o] >= bound) lds.key[atomicAdd(&lds.count[0], 1)] = own[o];
+                if (own[o] >= bound) key[atomicAdd(&kept, 1)] = own[o];
             __syncthreads();
-            top.kept = lds.count[0];
-            top.rank();
+            const int n = kept;
+            if (i == 0 && (n & 1)) key[n] = 0;
+            __syncthreads();
+            for (int q = i; q < n; q += 256) {
+                const unsigned long long mine = key[q];
+                const int at = larger_keys(key, n + 1 & ~1, mine);
+                if (at < a.k) best_of[at] = mine;
+            }
+            __syncthreads();
             if (i < a.k) {
-                const unsigned long long key = lds.key[i];
-                if (a.top_ids) a.top_ids[row * a.ldt + i] = static_cast<int32_t>(0xffffffffu - static_cast<uint32_t>(key));
-                if (a.top_logp) a.top_logp[row * a.ldt + i] = end.logp(order_logit(static_cast<uint32_t>(key >> 32)));
+                const unsigned long long k1 = best_of[i];
+                if (a.top_ids) a.top_ids[row * a.ldt + i] = static_cast<int32_t>(0xffffffffu - static_cast<uint32_t>(k1));
+                if (a.top_logp) a.top_logp[row * a.ldt + i] = end.logp(order_logit(static_cast<uint32_t>(k1 >> 32)));
             }
             __syncthreads();
         }
