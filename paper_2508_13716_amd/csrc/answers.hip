@@ -53,6 +53,7 @@ struct RowEnd {
 template <int THREADS> struct TopLds {
     static constexpr int WAVES = THREADS / 64, CAP = THREADS == 64 ? 512 : 256;
     unsigned long long key[WAVES][CAP], best[WAVES][CAPGNN_TOP_MAX];
+    int32_t noted[WAVES][CAP];      // classes whose keys are not formed yet stand here, in their keys' places
     uint32_t maxima[THREADS];
     int kept[WAVES];
     uint32_t bound;
@@ -80,7 +81,8 @@ __device__ __forceinline__ int larger_keys(const unsigned long long *key, int n,
 template <int THREADS> struct Top {
     static constexpr int CAP = TopLds<THREADS>::CAP, WAVES = THREADS / 64;
     TopLds<THREADS> &l;
-    int k, kept = 0;                                    // keys in the wave's list
+    int k, kept = 0, formed = 0;                        // classes in the wave's list, of which so many have their keys
+    int again = -1;                                     // the first tile that has not been worked on
     float below = __uint_as_float(0x7fc00000u);         // a logit is a candidate unless it is <= this
 
     __device__ Top(TopLds<THREADS> &lds, int k_) : l(lds), k(k_) {}
@@ -120,8 +122,20 @@ template <int THREADS> struct Top {
         }
     }
 
+    // Only classes are noted during the scan, one read of their logits (out of the caches) forms the keys of many.
+    template <bool BF16> __device__ void form(const char *z) {
+        wave_sync();
+#pragma unroll 1
+        for (int i = formed + lane(); i < kept; i += 64) {
+            const int j = l.noted[wave()][i];
+            l.key[wave()][i] = logit_key(ld_logit<BF16>(z, j), j);
+        }
+        formed = kept;
+    }
+
     // cuts the wave's list to its k largest, in descending order
-    __device__ void cut() {
+    template <bool BF16> __device__ void cut(const char *z) {
+        form<BF16>(z);
         unsigned long long *key = l.key[wave()], *best = l.best[wave()];
         const int n = kept;
         if (lane() == 0 && (n & 1)) key[n] = 0;
@@ -133,19 +147,19 @@ template <int THREADS> struct Top {
             if (at < k) best[at] = own;
         }
         wave_sync();
-        kept = n < k ? n : k;
+        kept = formed = n < k ? n : k;
         if (lane() < kept) key[lane()] = best[lane()];
         if (kept == k) raise(static_cast<uint32_t>(best[k - 1] >> 32), false);
         wave_sync();
     }
 
-    // one key of every lane that has one; false if the list does not hold them
-    __device__ bool append(bool has, float z, int j) {
+    // one class of every lane that has one; false if the list does not hold them
+    __device__ bool append(bool has, int j) {
         const unsigned long long lanes = __ballot(has);
         const int count = __popcll(lanes);
         if (kept + count > CAP) return false;
         const int at = kept + __builtin_amdgcn_mbcnt_hi(static_cast<uint32_t>(lanes >> 32), __builtin_amdgcn_mbcnt_lo(static_cast<uint32_t>(lanes), 0));
-        if (has) l.key[wave()][at] = logit_key(z, j);
+        if (has) l.noted[wave()][at] = j;
         kept += count;
         return true;
     }
@@ -154,74 +168,96 @@ template <int THREADS> struct Top {
     template <bool BF16, int NV>
     __device__ void tile(raw16 (&r)[NV], const float (&vmax)[NV], float tmax, const char *z, int from, int end, bool first) {
         typedef Raw<BF16> R;
+        constexpr int V = R::V, HALF = NV * V / 2;
+        static_assert(HALF <= 32 && NV % 2 == 0, "a thread's logits of a tile are two words of bits");
         if (first && end - from > THREADS / 64 * CAP / 2) raise(kth_maximum<THREADS>(tmax), true);
+        if (again >= 0) return;
         const int before = kept;
 #pragma unroll 1
         for (int attempt = 0; attempt < 2; ++attempt) {
             const int tid = thread_anew();
-            bool fits = true;
+            uint32_t passed[2] = {0, 0};        // bit i * V + e of a half: class from + (i * THREADS + tid) * V + e
 #pragma unroll
             for (int i = 0; i < NV; ++i) {
-                if (!fits || !__any(!(vmax[i] <= below))) continue;
+                if (!__any(!(vmax[i] <= below))) continue;
                 forget(r[i]);
-                uint32_t passed = 0;
+                uint32_t p = 0;
 #pragma unroll
-                for (int e = 0; e < R::V; ++e) passed |= !(R::get(r[i], e) <= below) ? 1u << e : 0u;
-                const int own = from + (i * THREADS + tid) * R::V, start = own + R::V <= end ? own : end - R::V;
-                passed = own < end ? passed & ~0u << (own - start) : 0u;        // (the row's last vectors start earlier)
-                while (fits && __any(passed != 0)) {
-                    const bool has = passed != 0;
-                    const int e = __ffs(passed) - 1;
-                    passed &= passed - 1;
-                    const int word = BF16 ? e >> 1 : e;
-                    const uint32_t lo = word & 1 ? r[i][1] : r[i][0], hi = word & 1 ? r[i][3] : r[i][2], w = word & 2 ? hi : lo;
-                    fits = append(has, __uint_as_float(!BF16 ? w : e & 1 ? w & 0xffff0000u : w << 16), start + e);
-                }
+                for (int e = 0; e < V; ++e) p |= !(R::get(r[i], e) <= below) ? 1u << e : 0u;
+                const int own = from + (i * THREADS + tid) * V;
+                if (__any(own + V > end)) p = own >= end ? 0u : own + V > end ? p >> (own + V - end) : p;    // (the row's last vectors start earlier)
+                passed[2 * i / NV] |= p << i % (NV / 2) * V;
             }
+            bool fits = true;
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+                while (fits && __any(passed[h] != 0)) {
+                    const bool has = passed[h] != 0;
+                    const int b = __ffs(passed[h]) - 1;
+                    passed[h] &= passed[h] - 1;
+                    fits = append(has, from + ((h * (NV / 2) + b / V) * THREADS + tid) * V + b % V);
+                }
             if (fits) {
-                if (kept > CAP / 2) cut();
+                if (kept > CAP / 2) cut<BF16>(z);
                 return;
             }
             kept = before;
             if (attempt == 0) raise(kth_maximum<64>(tmax), true);
         }
-        // the exact k-th largest key of the wave's share, bit by bit: order T, classes below J
-        auto each = [&](auto f) {
+        again = from;
+    }
+
+    // The tiles from `again` on, out of memory (kept out of the scan, whose registers it would take): those with more candidates than the list
+    // holds by the exact k-th largest key of the wave's share, found bit by bit: order T, classes below J.
+    template <bool BF16, int NV> __device__ void rest(const char *z, int row_end) {
+        constexpr int V = Raw<BF16>::V, TILE = THREADS * NV * V;
 #pragma unroll 1
-            for (int v = from + static_cast<int>(threadIdx.x) * R::V; __any(v < end); v += THREADS * R::V)
+        for (int from = again; from < row_end; from += TILE) {
+            const int end = row_end - from < TILE ? row_end : from + TILE, mine = from + wave() * 64 * V;
+            auto each = [&](auto f) {
 #pragma unroll 1
-                for (int e = 0; e < R::V; ++e) f(v + e < end ? ld_logit<BF16>(z, v + e) : 0.f, v + e, v + e < end);
-        };
-        auto count = [&](auto in) {
-            int c = 0;
-            each([&](float x, int j, bool there) { c += there && in(logit_order(x), j); });
-            return wave_all(c, OpSum());
-        };
-        const int all = count([](uint32_t, int) { return true; }), want = all < k ? all : k;
-        uint32_t T = 0;
-        int J = 0;
-        for (int bit = 31; bit >= 0; --bit) {
-            const uint32_t t = T | 1u << bit;
-            if (count([&](uint32_t o, int) { return o >= t; }) >= want) T = t;
+                for (int q = lane(); q < NV * 64 * V; q += 64) {        // (whole waves)
+                    const int j = mine + q / (64 * V) * (THREADS * V) + q % (64 * V);
+                    f(j < end ? ld_logit<BF16>(z, j) : 0.f, j, j < end);
+                }
+            };
+            auto count = [&](auto in) {
+                int c = 0;
+                each([&](float x, int j, bool there) { c += there && in(x, j); });
+                return wave_all(c, OpSum());
+            };
+            const float limit = below;
+            const int all = count([&](float x, int) { return !(x <= limit); }), want = all < k ? all : k;
+            uint32_t T = 0;
+            int J = 0x7fffffff;
+            if (kept + all > CAP) {
+                J = 0;
+                for (int bit = 31; bit >= 0; --bit) {
+                    const uint32_t t = T | 1u << bit;
+                    if (count([&](float x, int) { return logit_order(x) >= t; }) >= want) T = t;
+                }
+                const int above = count([&](float x, int) { return logit_order(x) > T; });
+                for (int bit = 30; bit >= 0; --bit) {
+                    const int t = J | 1 << bit;
+                    if (count([&](float x, int j) { return logit_order(x) == T && j < t; }) <= want - above) J = t;
+                }
+            }
+            each([&](float x, int j, bool there) {
+                const uint32_t o = logit_order(x);
+                append(there && !(x <= limit) && (o > T || (o == T && j < J)), j);      // at most k, or all that the list holds
+            });
+            if (kept > CAP / 2 || kept + all > CAP) cut<BF16>(z);
         }
-        const int above = count([&](uint32_t o, int) { return o > T; });
-        for (int bit = 30; bit >= 0; --bit) {
-            const int t = J | 1 << bit;
-            if (count([&](uint32_t o, int j) { return o == T && j < t; }) <= want - above) J = t;
-        }
-        each([&](float x, int j, bool there) {
-            const uint32_t o = logit_order(x);
-            append(there && (o > T || (o == T && j < J)), x, j);        // want <= k more: they fit behind at most CAP / 2
-        });
-        cut();
     }
 
     // The row's k largest in descending order, in l.best[0]; how many there are.  Barriers before and after.
-    __device__ int finish() {
+    template <bool BF16, int NV> __device__ int finish(const char *z, int row_end) {
+        if (again >= 0) rest<BF16, NV>(z, row_end);
         if constexpr (WAVES == 1) {
-            cut();
+            cut<BF16>(z);
             return kept;
         } else {
+            form<BF16>(z);
             if (lane() == 0) {
                 l.kept[wave()] = kept;
                 if (kept & 1) l.key[wave()][kept] = 0;
@@ -312,7 +348,7 @@ __global__ __launch_bounds__(THREADS) __attribute__((amdgpu_waves_per_eu(4))) vo
         const float du = (m - ref) * a.t.L, f = exp2_raw(du);
         if constexpr (ENT) e1 = group_all<THREADS>(f * fmaf(s, fmaxf(du, -160.f), e1), red, OpSum());
         s = group_all<THREADS>(s * f, red, OpSum());
-        const int found = a.k ? top.finish() : 0;
+        const int found = a.k ? top.template finish<BF16, NV>(z, hi) : 0;
         if (w.parts > 1) {
             if (threadIdx.x == 0) w.sums[job] = make_float4(M, s, e1, 0.f);
             for (int i = threadIdx.x; i < a.k; i += THREADS) w.keys[job * a.k + i] = i < found ? lds.best[0][i] : 0;
