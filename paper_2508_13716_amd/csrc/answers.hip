@@ -373,28 +373,35 @@ __global__ __launch_bounds__(THREADS) __attribute__((amdgpu_waves_per_eu(4))) vo
 }
 
 // ------------------------------------------------------------------ few classes (NARROW_C) and at most NARROW_TOP top ones
-// Pass 1 keeps the k largest logits of a lane sorted, one median of three per place and logit; pass 2 forms the sums and notes the classes
-// that reach the k-th largest, of those equal to it only as many as are wanted; the noted ones rank one another.
+// Pass 1 keeps the k largest logits of a lane sorted, one median of three per place and logit (lanes of a row merge theirs); pass 2 forms the
+// sums, and a class that reaches the k-th largest finds its place among them as the number of those that are larger.  Rows with equal
+// logits among the k largest, or with NaN, are gone over once more by one lane, class by class.  The places of the wave's rows are
+// written out together.  (Ranking the classes found against one another, out of LDS: 612000 x 47, k = 5, 131 us.)
 constexpr int NARROW_TOP = 8;
 template <bool BF16, bool ENT, bool TOP>
-__global__ __launch_bounds__(64 * NARROW_WAVES) void answers_narrow_kernel(AnswerArgs a, NarrowShape s) {
+__global__ __launch_bounds__(64 * NARROW_WAVES) __attribute__((amdgpu_waves_per_eu(4))) void answers_narrow_kernel(AnswerArgs a, NarrowShape s) {
     extern __shared__ __align__(16) char lds_all[];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const size_t per_wave = s.lds_wave + 64 * NARROW_TOP;
+    const size_t per_wave = s.lds_wave + 64 * (sizeof(float2) + NARROW_TOP);
     float *tile = reinterpret_cast<float *>(lds_all + wave * per_wave);
-    uint8_t *noted = reinterpret_cast<uint8_t *>(lds_all + wave * per_wave + s.lds_wave);
-    const int G = 1 << s.lg, sub = lane & (G - 1), C = s.C;
-    const float *z = tile + (lane >> s.lg) * s.pitch;
+    float2 *ends = reinterpret_cast<float2 *>(lds_all + wave * per_wave + s.lds_wave);        // of every row: maximum, ln of the sum
+    uint8_t *places = reinterpret_cast<uint8_t *>(ends + 64);
+    const int G = 1 << s.lg, sub = lane & (G - 1), C = s.C, mine = lane >> s.lg;
+    const float *z = tile + mine * s.pitch;
+    uint8_t *place = places + mine * NARROW_TOP;
     const int64_t step = static_cast<int64_t>(gridDim.x) * NARROW_WAVES * s.rows;
     int64_t row0 = (static_cast<int64_t>(blockIdx.x) * NARROW_WAVES + wave) * s.rows;
+    const int magic = a.k ? (65536 + a.k - 1) / a.k : 0;
+    narrow_ends(s, tile, lane);
     NarrowLoad<BF16> next;
-    if (row0 < a.n) next.fetch(s, a.Z, a.ldz, a.n, row0, lane);
+    if (row0 < a.n) next.fetch(s, a.Z, a.ldz, a.n, row0);
     for (; row0 < a.n; row0 += step) {
-        next.put(s, tile, lane);
+        next.put(s, tile);
         wave_sync();
-        if (row0 + step < a.n) next.fetch(s, a.Z, a.ldz, a.n, row0 + step, lane);
-        const int64_t row = row0 + (lane >> s.lg);
+        if (row0 + step < a.n) next.fetch(s, a.Z, a.ldz, a.n, row0 + step);
+        const int64_t row = row0 + mine;
         const bool in = row < a.n, on = in && (!a.mask || a.mask[row]);
+        const int given = a.m && on && sub < a.m ? a.ids[row * a.ldi + sub] : -1;
         float v[NARROW_TOP], m = -INFINITY;
         if constexpr (TOP) {
 #pragma unroll
@@ -404,7 +411,13 @@ __global__ __launch_bounds__(64 * NARROW_WAVES) void answers_narrow_kernel(Answe
                 for (int i = NARROW_TOP - 1; i > 0; --i) v[i] = __builtin_amdgcn_fmed3f(v[i - 1], v[i], x);
                 v[0] = max_of(v[0], x);
             };
-            for (int j = sub; j < C; j += G) insert(z[j]);
+            for (int b = 0; b < s.each; b += NARROW_BATCH) {
+                float x[NARROW_BATCH];
+#pragma unroll
+                for (int i = 0; i < NARROW_BATCH; ++i) x[i] = z[sub + (b + i) * G];
+#pragma unroll
+                for (int i = 0; i < NARROW_BATCH; ++i) insert(x[i]);
+            }
             for (int off = 1; off < G; off <<= 1) {
                 float o[NARROW_TOP];
 #pragma unroll
@@ -414,91 +427,109 @@ __global__ __launch_bounds__(64 * NARROW_WAVES) void answers_narrow_kernel(Answe
             }
             m = v[0];
         } else {
-            for (int j = sub; j < C; j += G) m = max_of(m, z[j]);
+            for (int b = 0; b < s.each; b += NARROW_BATCH)
+#pragma unroll
+                for (int i = 0; i < NARROW_BATCH; ++i) m = max_of(m, z[sub + (b + i) * G]);
             for (int off = 1; off < G; off <<= 1) m = max_of(m, __shfl_xor(m, off));
         }
         float kth = 0.f;
-        int equals = 0, hits = 0;           // how many of the k largest equal the k-th; classes noted by this lane
+        bool twice = false;                 // two of the k largest, or one and the next, are equal
         if constexpr (TOP) {
 #pragma unroll
-            for (int i = 0; i < NARROW_TOP; ++i) if (i == a.k - 1) kth = v[i];
+            for (int i = 0; i < NARROW_TOP; ++i) {
+                if (i == a.k - 1) kth = v[i];
+                if (i > 0) twice = twice || (i < a.k && v[i] == v[i - 1]);
+            }
 #pragma unroll
-            for (int i = 0; i < NARROW_TOP; ++i) equals += i < a.k && v[i] == kth;
+            for (int i = 0; i < NARROW_TOP; ++i) if (i >= a.k) v[i] = -INFINITY;      // (no place of the k)
         }
         const float ref = safe_max(m);
         float sum = 0.f, e1 = 0.f;
-        int wanted = equals;
-        for (int j = sub; j < C; j += G) {
-            const float x = z[j], u = (x - ref) * a.t.L, e = exp2_raw(u);
-            sum += e;
-            if constexpr (ENT) e1 = fmaf(e, fmaxf(u, -160.f), e1);
-            if constexpr (TOP) {
-                if (x > kth || (x == kth && wanted > 0)) {
-                    wanted -= x == kth;
-                    if (hits < NARROW_TOP) noted[lane * NARROW_TOP + hits] = static_cast<uint8_t>(j);
-                    ++hits;
+        int reached = 0;                    // classes that reach the k-th largest
+        for (int b = 0; b < s.each; b += NARROW_BATCH) {
+            float x[NARROW_BATCH];
+#pragma unroll
+            for (int i = 0; i < NARROW_BATCH; ++i) x[i] = z[sub + (b + i) * G];
+#pragma unroll
+            for (int i = 0; i < NARROW_BATCH; ++i) {
+                const float u = (x[i] - ref) * a.t.L, e = exp2_raw(u);
+                sum += e;
+                if constexpr (ENT) e1 = fmaf(e, fmaxf(u, -160.f), e1);
+                if constexpr (TOP) {
+                    const int j = sub + (b + i) * G;
+                    if (x[i] >= kth && j < C) {
+                        int larger = 0;
+#pragma unroll
+                        for (int q = 0; q < NARROW_TOP; ++q) larger += v[q] > x[i];
+                        place[larger & (NARROW_TOP - 1)] = static_cast<uint8_t>(j);       // (8 only next to a NaN)
+                        ++reached;
+                    }
                 }
             }
         }
         for (int off = 1; off < G; off <<= 1) {
             sum += __shfl_xor(sum, off);
             if constexpr (ENT) e1 += __shfl_xor(e1, off);
+            if constexpr (TOP) reached += __shfl_xor(reached, off);
         }
         const RowEnd end(m, sum, a.t.inv_T);
         if (in && sub == 0) {
             if (a.entropy) a.entropy[row] = on ? end.entropy(sum, e1) : 0.f;
             if (a.stats) { a.stats[2 * row] = on ? m : 0.f; a.stats[2 * row + 1] = on ? end.ln_s : 0.f; }
         }
+        if (in && sub < a.m) a.logp[row * a.ldp + sub] = given >= 0 && given < C ? end.logp(z[given]) : 0.f;
         if (in)
-            for (int i = sub; i < a.m; i += G) {
+            for (int i = sub + G; i < a.m; i += G) {
                 const int c = on ? a.ids[row * a.ldi + i] : -1;
                 a.logp[row * a.ldp + i] = c >= 0 && c < C ? end.logp(z[c]) : 0.f;
             }
         if constexpr (TOP) {
-            auto give = [&](int place, int c) {
-                if (a.top_ids) a.top_ids[row * a.ldt + place] = c;
-                if (a.top_logp) a.top_logp[row * a.ldt + place] = end.logp(z[c]);
-            };
-            wave_sync();
-            if (in && !on) {
-                for (int i = sub; i < a.k; i += G) {
-                    if (a.top_ids) a.top_ids[row * a.ldt + i] = -1;
-                    if (a.top_logp) a.top_logp[row * a.ldt + i] = 0.f;
-                }
-            }
-            const bool plain = sum == sum;
-            const int first = lane & ~(G - 1);
-            int of_lane[NARROW_G];          // classes noted by each lane of the row
-#pragma unroll
-            for (int g = 0; g < NARROW_G; ++g) of_lane[g] = g < G ? __shfl(hits, first + g) : 0;
-            if (on && plain) {
-                for (int i = 0; i < hits; ++i) {
-                    const int c = noted[lane * NARROW_TOP + i];
-                    const float x = z[c];
-                    int place = 0;
-#pragma unroll
-                    for (int g = 0; g < NARROW_G; ++g)
-                        for (int b = 0; b < of_lane[g]; ++b) {
-                            const int cb = noted[(first + g) * NARROW_TOP + b];
-                            const float y = z[cb];
-                            place += y > x || (y == x && cb < c);
+            const bool nan = !(sum == sum), again = on && (twice || reached != a.k || nan);
+            if (sub == 0) ends[mine] = make_float2(on ? end.m0 : -INFINITY, end.ln_s);        // (-inf: a row that is masked out)
+            if (__any(again)) {
+                wave_sync();
+                if (again && sub == 0) {
+                    unsigned long long last = ~0ull;
+                    if (nan) {
+                        for (int i = 0; i < a.k; ++i) {
+                            unsigned long long best = 0;
+                            for (int j = 0; j < C; ++j) {
+                                const unsigned long long key = logit_key(z[j], j);
+                                if (key < last && key > best) best = key;
+                            }
+                            last = best;
+                            place[i] = static_cast<uint8_t>(0xffffffffu - static_cast<uint32_t>(best));
                         }
-                    if (place < a.k) give(place, c);
+                    } else {
+                        uint32_t taken = 0;         // equal logits: the first of their places that is open
+                        for (int b = 0; b < C; b += NARROW_BATCH) {
+                            float x[NARROW_BATCH];
+#pragma unroll
+                            for (int i = 0; i < NARROW_BATCH; ++i) x[i] = z[b + i < s.pitch ? b + i : s.pitch - 1];
+#pragma unroll
+                            for (int i = 0; i < NARROW_BATCH; ++i)
+                                if (x[i] >= kth && b + i < C) {
+                                    int larger = 0;
+#pragma unroll
+                                    for (int q = 0; q < NARROW_TOP; ++q) larger += v[q] > x[i];
+                                    const uint32_t open = ~taken & (~0u << larger) & ((1u << a.k) - 1u);
+                                    if (open) place[__ffs(open) - 1] = static_cast<uint8_t>(b + i);
+                                    taken |= open & (0u - open);
+                                }
+                        }
+                    }
                 }
             }
-            // a row with NaN: its classes one after another, by key
-            if (__any(on && !plain)) {
-                unsigned long long last = ~0ull;
-                for (int i = 0; i < a.k; ++i) {
-                    unsigned long long best = 0;
-                    for (int j = sub; j < C; j += G) {
-                        const unsigned long long key = logit_key(z[j], j);
-                        if (key < last && key > best) best = key;
-                    }
-                    for (int off = 1; off < G; off <<= 1) best = OpMaxKey()(best, __shfl_xor(best, off));
-                    last = best;
-                    if (on && !plain && sub == 0) give(i, static_cast<int>(0xffffffffu - static_cast<uint32_t>(best)));
-                }
+            wave_sync();
+            for (int i = lane; i < s.rows * a.k; i += 64) {
+                const int r = i * magic >> 16, p = i - r * a.k;
+                if (row0 + r >= a.n) break;
+                const float2 e = ends[r];
+                const bool there = e.x != -INFINITY;
+                const int c = places[r * NARROW_TOP + p];
+                if (a.top_ids) a.top_ids[(row0 + r) * a.ldt + p] = there ? c : -1;
+                if (a.top_logp)
+                    a.top_logp[(row0 + r) * a.ldt + p] = !there ? 0.f : e.y == -INFINITY ? -INFINITY : (tile[r * s.pitch + c] - e.x) * a.t.inv_T - e.y;
             }
         }
         wave_sync();
@@ -702,7 +733,7 @@ __global__ __launch_bounds__(64 * NARROW_WAVES) void answers_grad_narrow_kernel(
     const int64_t step = static_cast<int64_t>(gridDim.x) * NARROW_WAVES * s.rows;
     int64_t row0 = (static_cast<int64_t>(blockIdx.x) * NARROW_WAVES + wave) * s.rows;
     NarrowLoad<BF16> next;
-    if (row0 < a.n) next.fetch(s, a.Z, a.ldz, a.n, row0, lane);
+    if (row0 < a.n) next.fetch(s, a.Z, a.ldz, a.n, row0);
     for (; row0 < a.n; row0 += step) {
         const int64_t row = row0 + (lane >> s.lg) < a.n ? row0 + (lane >> s.lg) : a.n - 1;
         GradRow w;
@@ -713,9 +744,9 @@ __global__ __launch_bounds__(64 * NARROW_WAVES) void answers_grad_narrow_kernel(
                 const int c = a.ids[row * a.ldi + i];
                 if (c >= 0 && c < C) w.G += a.dlogp[row * a.lddp + i];
             }
-        next.put(s, tile, lane);
+        next.put(s, tile);
         wave_sync();
-        if (row0 + step < a.n) next.fetch(s, a.Z, a.ldz, a.n, row0 + step, lane);
+        if (row0 + step < a.n) next.fetch(s, a.Z, a.ldz, a.n, row0 + step);
         for (int j = sub; j < C; j += G) z[j] = w.none ? 0.f : w.base<ENT>(z[j], a.t) * a.t.inv_T;
         wave_sync();
         if (sub == 0 && !w.none)            // one lane a row: the same class may be given again
@@ -724,7 +755,7 @@ __global__ __launch_bounds__(64 * NARROW_WAVES) void answers_grad_narrow_kernel(
                 if (c >= 0 && c < C) z[c] = fmaf(a.dlogp[row * a.lddp + i], a.t.inv_T, z[c]);
             }
         wave_sync();
-        narrow_store<BF16, DBF16>(s, tile, a.dZ, a.lddz, a.n, row0, lane, false);
+        narrow_store<BF16, DBF16>(s, tile, a.dZ, a.lddz, a.n, row0, false);
         wave_sync();
     }
 }
@@ -763,7 +794,7 @@ extern "C" int capgnn_logprobs(int64_t n, int C, const void *Z, int64_t ldz, int
     const bool bf16 = z_dtype == CAPGNN_BF16;
     if (C <= NARROW_C && k <= NARROW_TOP) {
         const NarrowShape s = narrow_shape(C, z_dtype);
-        const size_t lds = NARROW_WAVES * (s.lds_wave + 64 * NARROW_TOP);
+        const size_t lds = NARROW_WAVES * (s.lds_wave + 64 * (sizeof(float2) + NARROW_TOP));
         auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(narrow_grid(s, n, lds)), dim3(64 * NARROW_WAVES), lds, st, a, s); };
         if (bf16) {
             if (entropy) k ? go(answers_narrow_kernel<true, true, true>) : go(answers_narrow_kernel<true, true, false>);

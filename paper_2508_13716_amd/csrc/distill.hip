@@ -1,498 +1,9 @@
-// Distillation from a teacher's top logits: the divergence of a row's softmax from the teacher's classes, and its gradient.
-#include "softrow.h"
+// capgnn_distill: checks, workspace, launches; the kernels without the teacher's remaining probability.
+#include "distill.h"
 
 #include <algorithm>
 
 namespace capgnn {
-
-struct DistillArgs {
-    int64_t n;
-    int C;
-    const char *Z; int64_t ldz;
-    TempScale t;
-    const uint8_t *mask;
-    const int32_t *t_ids; const float *t_val; int64_t ldt; int k, rest;
-    float weight;
-    float norm_val; const float *norm_dev;
-    double *part;                   // [gridDim.x]
-    float *row_loss;
-    char *dZ; int64_t lddz; int accumulate;
-};
-
-constexpr float REST_LEAST = 9.5367431640625e-7f;       // 2^-20
-
-// ------------------------------------------------------------------ the teacher of a row, in LDS; the first wave of a workgroup works on it
-struct Teacher {
-    static constexpr int OWN = CAPGNN_GIVEN_MAX / 64;       // entries of a lane: l, l + 64, ...
-    int32_t id[CAPGNN_GIVEN_MAX];   // class of every entry, -1: none
-    int32_t c[CAPGNN_GIVEN_MAX];    // the same at a class's first mention, else -1
-    float w[CAPGNN_GIVEN_MAX];      // probability of the entry
-    float q[CAPGNN_GIVEN_MAX];      // of the class in all
-    float z[CAPGNN_GIVEN_MAX];      // the row's logit of the class
-    float old[CAPGNN_GIVEN_MAX];    // what its gradient is added to
-    int entries;                    // that count
-    float mass;                     // Q + r
-    double r;                       // what the teacher leaves
-};
-
-// The bits of the listed classes, modulo the bits there are: set by the first wave between two barriers.
-struct Seen {
-    uint32_t *bits;
-    int most;               // a power of two, at least 256
-    __device__ __forceinline__ void set(int c) const { atomicOr(&bits[(c & (most - 1)) >> 5], 1u << (c & 31)); }
-    template <int V> __device__ __forceinline__ uint32_t vector(int j) const {     // classes [j, j + V), j a multiple of V
-        return bits[(j & (most - 1)) >> 5] >> (j & 31) & ((1u << V) - 1u);
-    }
-};
-
-// What the teacher leaves (rest) is the small difference of numbers near 1: its exponentials and their sum are doubles.  listed: where another
-// launch has left the logits of the entries' classes, or null.
-template <bool BF16>
-__device__ __forceinline__ void read_teacher(const DistillArgs &a, int64_t row, const char *z, const float *listed, Teacher &t) {
-    const int lane = threadIdx.x;
-    float top = -INFINITY, v[Teacher::OWN];
-    int entries = 0;
-#pragma unroll
-    for (int o = 0; o < Teacher::OWN; ++o) {
-        if (o * 64 >= a.k) break;
-        const int i = lane + o * 64;
-        v[o] = -INFINITY;
-        if (i < a.k) {
-            int c = a.t_ids[row * a.ldt + i];
-            v[o] = a.t_val[row * a.ldt + i];
-            if (c < 0 || c >= a.C || v[o] == -INFINITY) { c = -1; v[o] = -INFINITY; }
-            t.id[i] = c;
-            if (c >= 0) {
-                t.z[i] = listed ? listed[i] : ld_logit<BF16>(z, c);
-                top = max_of(top, v[o]);
-                ++entries;
-            }
-        }
-    }
-    entries = wave_all(entries, OpSum());
-    if (!a.rest) top = safe_max(wave_all(top, OpMax()));
-    double Q = 0.0, w[Teacher::OWN];
-#pragma unroll
-    for (int o = 0; o < Teacher::OWN; ++o) {
-        if (o * 64 >= a.k) break;
-        w[o] = a.rest ? exp(static_cast<double>(v[o])) : static_cast<double>(exp_difference(v[o], top, a.t));      // (none: 0)
-        Q += w[o];
-    }
-    Q = wave_all(Q, OpSum());
-    const double one = a.rest ? 1.0 : 1.0 / Q;
-#pragma unroll
-    for (int o = 0; o < Teacher::OWN; ++o) {
-        if (o * 64 >= a.k) break;
-        if (lane + o * 64 < a.k) t.w[lane + o * 64] = static_cast<float>(w[o] * one);
-    }
-    wave_sync();
-    // a class listed again: its first mention takes the sum
-#pragma unroll 1
-    for (int i = lane; i < a.k; i += 64) {
-        const int c = t.id[i];
-        float sum = 0.f;
-        bool first = c >= 0;
-        for (int b = 0; b < a.k; ++b)
-            if (t.id[b] == c) {
-                first = first && b >= i;
-                sum += t.w[b];
-            }
-        t.q[i] = sum;
-        t.c[i] = first ? c : -1;
-    }
-    double r = a.rest ? 1.0 - Q : 0.0;
-    if (r < REST_LEAST) r = 0.0;
-    if (lane == 0) {
-        t.entries = entries;
-        t.r = r;
-        t.mass = static_cast<float>(a.rest ? Q + r : 1.0 + 0.0 * Q);       // (a NaN among the values reaches every class)
-    }
-    wave_sync();
-}
-
-// Maximum and sum of a thread's logits of one tile, added to what it has (m, s).  With bits: only of classes that are not listed (what the row
-// gives to the others may be far below the rounding of a sum that holds the listed ones).
-template <bool BF16, int THREADS, int NV, bool REST>
-__device__ __forceinline__ void scan_tile(raw16 (&r)[NV], int t0, int hi, const DistillArgs &a, const Teacher &l, const Seen &seen, float &m, float &s) {
-    typedef Raw<BF16> R;
-    const int tid = thread_anew();
-    float tmax = -INFINITY;
-#pragma unroll
-    for (int i = 0; i < NV; ++i) {
-        if (t0 + i * THREADS * R::V >= hi) continue;
-#pragma unroll
-        for (int e = 0; e < R::V; ++e) tmax = max_of(tmax, R::get(r[i], e));
-    }
-    const float m_new = max_of(m, tmax), ref = safe_max(m_new);
-    s *= exp2_raw((m - ref) * a.t.L);
-    m = m_new;
-#pragma unroll
-    for (int i = 0; i < NV; ++i) {
-        if (t0 + i * THREADS * R::V >= hi) continue;
-        forget(r[i]);
-        uint32_t out = 0;
-        const int j = t0 + (i * THREADS + tid) * R::V;
-        if constexpr (REST) {
-            if (j < hi) out = seen.vector<R::V>(j);
-            if (__any(out != 0)) {
-                const int from = j + R::V <= hi ? j : hi - R::V;
-                if (a.C > seen.most && out) {           // some other class may have set the bit
-                    uint32_t sure = 0;
-                    for (int b = 0; b < a.k; ++b) {
-                        const int d = l.id[b] - j;
-                        if (d >= 0 && d < R::V) sure |= 1u << d;
-                    }
-                    out &= sure;
-                }
-                out <<= j < hi ? j - from : 0;
-#pragma unroll
-                for (int e = 0; e < R::V; ++e) {
-                    const float x = exp2_raw((R::get(r[i], e) - ref) * a.t.L);
-                    s += out >> e & 1u ? 0.f : x;
-                }
-                continue;
-            }
-        }
-#pragma unroll
-        for (int e = 0; e < R::V; ++e) s += exp2_raw((R::get(r[i], e) - ref) * a.t.L);
-    }
-}
-
-template <bool BF16, int THREADS, int NV>
-__device__ __forceinline__ void read_tile(raw16 (&r)[NV], const char *z, int t0, int hi) {
-    typedef Raw<BF16> R;
-    const int tid = thread_anew();
-    int from;
-#pragma unroll
-    for (int i = 0; i < NV; ++i) {
-        if (t0 + i * THREADS * R::V >= hi) continue;
-        r[i] = R::load_until(z, t0 + (i * THREADS + tid) * R::V, hi, &from);
-    }
-}
-
-// dz = p * factor for the tile's classes (p = exp(z - m0) * inv_s), added to dz's contents when add; barred classes get 0
-template <bool BF16, bool DBF16, int THREADS, int NV>
-__device__ __forceinline__ void grad_tile(raw16 (&r)[NV], char *dz, int t0, int hi, const TempScale &t, float m0, float inv_s, float factor, int add) {
-    typedef Raw<BF16> R;
-    constexpr int V = R::V;
-    const int tid = thread_anew();
-#pragma unroll
-    for (int i = 0; i < NV; ++i) {
-        if (t0 + i * THREADS * V >= hi) continue;
-        const int j = t0 + (i * THREADS + tid) * V;
-        if (j >= hi) continue;
-        forget(r[i]);
-        const int shift = j + V <= hi ? 0 : j + V - hi;         // a row's last vector starts earlier than j by that
-        float o[V], old[V];
-        if (add && shift == 0) ld_vector<DBF16>(dz, j, old);
-#pragma unroll
-        for (int e = 0; e < V; ++e) {
-            const float p = exp_scaled(R::get(r[i], e) - m0, t) * inv_s;
-            o[e] = p == 0.f ? 0.f : p * factor;
-        }
-        if (shift == 0) {
-            if (add)
-#pragma unroll
-                for (int e = 0; e < V; ++e) o[e] += old[e];
-            st_vector<DBF16>(dz, j, o);
-        } else {
-#pragma unroll
-            for (int e = 0; e < V; ++e)
-                if (e >= shift) st_grad<DBF16>(dz, hi - V + e, add ? o[e] + ld_logit<DBF16>(dz, hi - V + e) : o[e]);
-        }
-    }
-}
-
-// A row that adds nothing: zeros, unless they were to be added.
-template <bool BF16, bool DBF16, int THREADS>
-__device__ __forceinline__ void no_gradient(const DistillArgs &a, char *dz, int lo, int hi) {
-    constexpr int V = Raw<BF16>::V;
-    if (a.accumulate) return;
-    const float zero[V] = {};
-    int j = lo + static_cast<int>(threadIdx.x) * V;
-    for (; j + V <= hi; j += THREADS * V) st_vector<DBF16>(dz, j, zero);
-    for (; j < hi; ++j) st_grad<DBF16>(dz, j, 0.f);
-}
-
-// The divergence of one row, in the first wave (every lane); S the sum of all exponentials, others that of the classes not listed.
-__device__ __forceinline__ double divergence(const DistillArgs &a, const Teacher &t, float m0, float S, float others) {
-    const float ln_s = logf(S);
-    double kl = 0.0;
-#pragma unroll 1
-    for (int i = threadIdx.x; i < a.k; i += 64) {
-        const float q = t.q[i];
-        // (q d before 1/T: d / T may leave float's range)
-        if (t.c[i] >= 0 && q != 0.f) kl += static_cast<double>(fmaf(-q * (t.z[i] - m0), a.t.inv_T, q * (logf(q) + ln_s)));
-    }
-    kl = wave_all(kl, OpSum());
-    if (t.r > 0.0) kl += t.r * (log(t.r) - (log(static_cast<double>(others)) - log(static_cast<double>(S))));
-    return kl;
-}
-
-// Sum of the listed classes' exponentials: the first wave's.
-__device__ __forceinline__ float listed_sum(const DistillArgs &a, const Teacher &t, float m0) {
-    float e = 0.f;
-#pragma unroll 1
-    for (int i = threadIdx.x; i < a.k; i += 64)
-        if (t.c[i] >= 0) e += exp_scaled(t.z[i] - m0, a.t);
-    return wave_all(e, OpSum());
-}
-
-struct DistillParts {
-    int parts, chunk;       // of a row; classes of one
-    float2 *sums;           // [n][parts]: maximum, sum (rest: of the classes not listed)
-    float *listed;          // [n][GIVEN_MAX]: logits of the entries' classes (dZ may be Z: another part may have replaced them)
-    int seen;               // bits
-};
-
-// How much of the work on a row (or a part of it) a launch does
-enum DistillStage : int {
-    ROW_HELD,       // all of it, the row's logits in registers from the sums to the gradient
-    ROW_READ_TWICE, // all of it, longer rows: read again for the gradient (out of the caches where the rows under way fit)
-    PART_SUMS,      // maximum and sum of a part
-    PART_GRADIENT   // the parts' sums put together, gradient of a part
-};
-
-template <bool BF16, bool DBF16, int THREADS, int NV, bool REST, DistillStage STAGE>
-__global__ __launch_bounds__(THREADS) __attribute__((amdgpu_waves_per_eu(4))) void distill_rows_kernel(DistillArgs a, DistillParts w) {
-    typedef Raw<BF16> R;
-    constexpr int TILE = THREADS * NV * R::V;
-    constexpr bool PARTS = STAGE == PART_SUMS || STAGE == PART_GRADIENT;
-    extern __shared__ __align__(16) uint32_t seen_bits[];
-    __shared__ Teacher t;
-    __shared__ float2 red[THREADS / 64];
-    __shared__ float listed;
-    const Seen seen{seen_bits, w.seen};
-    const bool first_wave = threadIdx.x < 64;
-    const float norm = a.norm_dev ? a.norm_dev[0] : a.norm_val;
-    const float scale = a.weight / norm * a.t.inv_T;
-    double loss = 0.0;
-    for (int64_t job = blockIdx.x; job < a.n * (PARTS ? w.parts : 1); job += gridDim.x) {
-        const int64_t row = PARTS ? job / w.parts : job;
-        const int part = PARTS ? static_cast<int>(job % w.parts) : 0;
-        const int lo = PARTS ? part * w.chunk : 0, hi = PARTS && a.C - lo > w.chunk ? lo + w.chunk : a.C;
-        const char *z = a.Z + row * a.ldz * (BF16 ? 2 : 4);
-        char *dz = a.dZ ? a.dZ + row * a.lddz * (DBF16 ? 2 : 4) : nullptr;
-        if (a.mask && !a.mask[row]) {
-            if (STAGE != PART_SUMS) {
-                if (a.row_loss && part == 0 && threadIdx.x == 0) a.row_loss[row] = 0.f;
-                if (dz) no_gradient<BF16, DBF16, THREADS>(a, dz, lo, hi);
-            }
-            continue;
-        }
-        raw16 r[NV];
-        if (STAGE != PART_GRADIENT || dz) read_tile<BF16, THREADS, NV>(r, z, lo, hi);
-        if constexpr (REST && STAGE != PART_GRADIENT) {
-            for (int i = threadIdx.x; i < w.seen / 32; i += THREADS) seen_bits[i] = 0;
-            __syncthreads();
-        }
-        if (first_wave) {
-            float *left = STAGE == PART_SUMS || STAGE == PART_GRADIENT ? w.listed + row * CAPGNN_GIVEN_MAX : nullptr;
-            if (STAGE != PART_SUMS || REST || part == 0) read_teacher<BF16>(a, row, z, STAGE == PART_GRADIENT ? left : nullptr, t);
-            if constexpr (STAGE == PART_SUMS)
-                if (part == 0)
-                    for (int i = threadIdx.x; i < a.k; i += 64) left[i] = t.z[i];
-            if constexpr (REST && STAGE != PART_GRADIENT)
-                for (int i = threadIdx.x; i < a.k; i += 64)
-                    if (t.c[i] >= 0) seen.set(t.c[i]);
-        }
-        if constexpr (REST && STAGE != PART_GRADIENT) __syncthreads();
-        float m = -INFINITY, s = 0.f;
-        if constexpr (STAGE == PART_GRADIENT) {
-            for (int p = threadIdx.x & 63; p < w.parts; p += 64) {          // every wave for itself
-                const float2 v = w.sums[row * w.parts + p];
-                const float both = max_of(m, v.x), ref = safe_max(both);
-                s = s * exp2_raw((m - ref) * a.t.L) + v.y * exp2_raw((v.x - ref) * a.t.L);
-                m = both;
-            }
-            group_softmax<64>(m, s, a.t, red);
-        } else {
-            scan_tile<BF16, THREADS, NV, REST>(r, lo, hi, a, t, seen, m, s);
-            if constexpr (STAGE != ROW_HELD)
-#pragma unroll 1
-                for (int t0 = lo + TILE; t0 < hi; t0 += TILE) {
-                    read_tile<BF16, THREADS, NV>(r, z, t0, hi);
-                    scan_tile<BF16, THREADS, NV, REST>(r, t0, hi, a, t, seen, m, s);
-                }
-            group_softmax<THREADS>(m, s, a.t, red);
-        }
-        if constexpr (STAGE == PART_SUMS) {
-            if (threadIdx.x == 0) w.sums[job] = make_float2(m, s);
-            __syncthreads();
-            continue;
-        }
-        const float m0 = safe_max(m), others = s;
-        if (REST && first_wave) {
-            const float e = listed_sum(a, t, m0);
-            if (threadIdx.x == 0) listed = e;
-        }
-        __syncthreads();
-        const float S = REST ? others + listed : s;
-        if (t.entries == 0 || S == 0.f) {
-            if (a.row_loss && part == 0 && threadIdx.x == 0) a.row_loss[row] = 0.f;
-            if (dz) no_gradient<BF16, DBF16, THREADS>(a, dz, lo, hi);
-            __syncthreads();
-            continue;
-        }
-        if (first_wave && part == 0) {
-            const double kl = divergence(a, t, m0, S, others);
-            loss += kl;
-            if (a.row_loss && threadIdx.x == 0) a.row_loss[row] = static_cast<float>(kl);
-        }
-        if (dz) {
-            const float inv_s = 1.f / S, mass = t.mass * scale;
-            const float away = REST && t.r > 0.0 ? static_cast<float>(t.mass - t.r * (static_cast<double>(S) / others)) * scale : mass;
-            if (a.accumulate) {         // what the listed classes hold, before anything is written
-                if (first_wave)
-                    for (int i = threadIdx.x; i < a.k; i += 64)
-                        if (t.c[i] >= lo && t.c[i] < hi) t.old[i] = ld_logit<DBF16>(dz, t.c[i]);
-                __syncthreads();
-            }
-            if constexpr (STAGE == ROW_READ_TWICE) read_tile<BF16, THREADS, NV>(r, z, lo, hi);
-            grad_tile<BF16, DBF16, THREADS, NV>(r, dz, lo, hi, a.t, m0, inv_s, away, a.accumulate);
-            if constexpr (STAGE != ROW_HELD)
-#pragma unroll 1
-                for (int t0 = lo + TILE; t0 < hi; t0 += TILE) {
-                    read_tile<BF16, THREADS, NV>(r, z, t0, hi);
-                    grad_tile<BF16, DBF16, THREADS, NV>(r, dz, t0, hi, a.t, m0, inv_s, away, a.accumulate);
-                }
-            __syncthreads();
-            if (first_wave)
-                for (int i = threadIdx.x; i < a.k; i += 64) {
-                    const int c = t.c[i];
-                    if (c < lo || c >= hi) continue;
-                    const float g = fmaf(exp_scaled(t.z[i] - m0, a.t) * inv_s, mass, -t.q[i] * scale);
-                    st_grad<DBF16>(dz, c, a.accumulate ? t.old[i] + g : g);
-                }
-        }
-        __syncthreads();
-    }
-    if constexpr (STAGE != PART_SUMS)
-        if (threadIdx.x == 0) a.part[blockIdx.x] = loss;
-}
-
-// ------------------------------------------------------------------ few classes
-// As answers_grad_narrow_kernel, with a second row of LDS for the teacher's probabilities: -1 where a class is not listed, -2 once its gradient
-// is written.  One lane a row adds the teacher's entries up, and goes over them again at the end.
-template <bool BF16, bool DBF16, bool REST>
-__global__ __launch_bounds__(64 * NARROW_WAVES) void distill_narrow_kernel(DistillArgs a, NarrowShape s) {
-    extern __shared__ __align__(16) uint32_t seen_bits[];
-    __shared__ double red[NARROW_WAVES];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    float *tile = reinterpret_cast<float *>(reinterpret_cast<char *>(seen_bits) + wave * 2 * s.lds_wave);
-    const int G = 1 << s.lg, sub = lane & (G - 1), C = s.C;
-    float *z = tile + (lane >> s.lg) * s.pitch, *q = z + s.rows * s.pitch;
-    const float norm = a.norm_dev ? a.norm_dev[0] : a.norm_val;
-    const float scale = a.weight / norm * a.t.inv_T;
-    const int64_t step = static_cast<int64_t>(gridDim.x) * NARROW_WAVES * s.rows;
-    int64_t row0 = (static_cast<int64_t>(blockIdx.x) * NARROW_WAVES + wave) * s.rows;
-    double loss = 0.0;
-    NarrowLoad<BF16> next;
-    if (row0 < a.n) next.fetch(s, a.Z, a.ldz, a.n, row0, lane);
-    for (; row0 < a.n; row0 += step) {
-        const int64_t row = row0 + (lane >> s.lg);
-        const bool in = row < a.n, on = in && (!a.mask || a.mask[row]);
-        const int32_t *t_ids = a.t_ids + row * a.ldt;
-        const float *t_val = a.t_val + row * a.ldt;
-        next.put(s, tile, lane);
-        for (int j = sub; j < C; j += G) q[j] = -1.f;
-        wave_sync();
-        if (row0 + step < a.n) next.fetch(s, a.Z, a.ldz, a.n, row0 + step, lane);
-        double Q = 0.0;
-        int entries = 0;
-        if (on && sub == 0) {
-            auto valid = [&](int i, int &c, float &v) { c = t_ids[i]; v = t_val[i]; return c >= 0 && c < C && v != -INFINITY; };
-            int c;
-            float v, top = -INFINITY;
-            if (!REST) {
-                float sum = 0.f;
-                for (int i = 0; i < a.k; ++i) if (valid(i, c, v)) top = max_of(top, v);
-                for (int i = 0; i < a.k; ++i) if (valid(i, c, v)) sum += exp_difference(v, top, a.t);
-                Q = sum;
-            }
-            for (int i = 0; i < a.k; ++i)
-                if (valid(i, c, v)) {
-                    float p;
-                    if constexpr (REST) {
-                        const double w = exp(static_cast<double>(v));
-                        Q += w;
-                        p = static_cast<float>(w);
-                    } else {
-                        p = exp_difference(v, top, a.t) / static_cast<float>(Q);
-                    }
-                    const float had = q[c];
-                    q[c] = had < 0.f ? p : had + p;
-                    ++entries;
-                }
-        }
-        wave_sync();
-        float m = -INFINITY;
-        for (int j = sub; j < C; j += G) m = max_of(m, z[j]);
-        for (int off = 1; off < G; off <<= 1) m = max_of(m, __shfl_xor(m, off));
-        const float m0 = safe_max(m);
-        float others = 0.f, listed = 0.f;
-        for (int j = sub; j < C; j += G) {
-            const float e = exp2_raw((z[j] - m0) * a.t.L);
-            const bool in_list = REST && !(q[j] == -1.f);
-            others += in_list ? 0.f : e;
-            listed += in_list ? e : 0.f;
-        }
-        for (int off = 1; off < G; off <<= 1) {
-            others += __shfl_xor(others, off);
-            listed += __shfl_xor(listed, off);
-        }
-        const float S = others + listed;
-        for (int off = 1; off < G; off <<= 1) entries += __shfl_xor(entries, off);
-        const bool live = on && entries > 0 && S != 0.f;
-        const float ln_s = logf(S), inv_s = 1.f / S;
-        // (the first lane's: it alone has Q)
-        double r = REST ? 1.0 - Q : 0.0;
-        if (r < REST_LEAST) r = 0.0;
-        float mass = static_cast<float>(REST ? Q + r : 1.0 + 0.0 * Q) * scale;
-        float away = REST && r > 0.0 ? static_cast<float>(Q + r - r * (static_cast<double>(S) / others)) * scale : mass;
-        away = __shfl(away, lane & ~(G - 1));
-        if (sub == 0) {
-            double kl = 0.0;
-            if (live) {
-                for (int i = 0; i < a.k; ++i) {
-                    const int c = t_ids[i];
-                    if (c < 0 || c >= C || t_val[i] == -INFINITY) continue;
-                    const float p = q[c];
-                    if (p == -2.f) continue;
-                    const float d = z[c] - m0;
-                    if (p != 0.f) kl += static_cast<double>(fmaf(-p * d, a.t.inv_T, p * (logf(p) + ln_s)));
-                    z[c] = fmaf(exp_scaled(d, a.t) * inv_s, mass, -p * scale);
-                    q[c] = -2.f;
-                }
-                if (REST && r > 0.0) kl += r * (log(r) - (log(static_cast<double>(others)) - log(static_cast<double>(S))));
-                loss += kl;
-            }
-            if (in && a.row_loss) a.row_loss[row] = static_cast<float>(kl);
-        }
-        wave_sync();
-        if (a.dZ) {
-            const float none = a.accumulate ? -0.f : 0.f;       // (adding -0 leaves everything as it is)
-            for (int j = sub; j < C; j += G) {
-                if (!live) {
-                    z[j] = none;
-                } else if (q[j] == -1.f) {
-                    const float p = exp_scaled(z[j] - m0, a.t) * inv_s;
-                    z[j] = p == 0.f ? none : p * away;
-                }
-            }
-            wave_sync();
-            narrow_store<BF16, DBF16>(s, tile, a.dZ, a.lddz, a.n, row0, lane, a.accumulate);
-        }
-        wave_sync();
-    }
-    loss = wave_all(loss, OpSum());
-    if (lane == 0) red[wave] = loss;
-    __syncthreads();
-    if (threadIdx.x == 0) {
-        for (int w = 1; w < NARROW_WAVES; ++w) loss += red[w];
-        a.part[blockIdx.x] = loss;
-    }
-}
 
 // loss = weight / norm * sum of part
 __global__ __launch_bounds__(256) void distill_final_kernel(int parts, const double *part, float weight, float norm_val, const float *norm_dev,
@@ -505,7 +16,6 @@ __global__ __launch_bounds__(256) void distill_final_kernel(int parts, const dou
 }
 
 constexpr size_t DISTILL_HEADER = 8192;     // [0] the normaliser, [256 ..] counts of the mask
-constexpr int DISTILL_GROUPS = 8192;        // workgroups that leave a sum of the loss, at most
 
 // Few long rows are cut into parts, about a thousand workgroups in all and at least DISTILL_PART_LEAST classes each.
 constexpr int DISTILL_PART_LEAST = 2048, DISTILL_WORKGROUPS = 1024;
@@ -515,37 +25,6 @@ static int distill_parts(int64_t n, int C, int *chunk) {
     const int64_t c = ((C + parts - 1) / parts + 511) / 512 * 512;
     *chunk = static_cast<int>(c);
     return static_cast<int>((C + c - 1) / c);
-}
-
-template <bool BF16, bool DBF16, bool REST>
-static void launch_distill(const DistillArgs &a, DistillParts w, int *groups, hipStream_t st) {
-    constexpr int V = Raw<BF16>::V;
-    if (a.C <= NARROW_C) {
-        const NarrowShape s = narrow_shape(a.C, BF16 ? CAPGNN_BF16 : CAPGNN_F32);
-        const size_t lds = NARROW_WAVES * 2 * s.lds_wave;
-        *groups = static_cast<int>(narrow_grid(s, a.n, lds));
-        hipLaunchKernelGGL((distill_narrow_kernel<BF16, DBF16, REST>), dim3(*groups), dim3(64 * NARROW_WAVES), lds, st, a, s);
-        return;
-    }
-    w.seen = 256;
-    while (w.seen < a.C && w.seen < 1 << 18) w.seen *= 2;
-    const size_t lds = REST ? w.seen / 8 : 0;
-    *groups = static_cast<int>(std::min<int64_t>(a.n * w.parts, DISTILL_GROUPS));
-    auto go = [&](auto kernel, int threads, size_t bytes) { hipLaunchKernelGGL(kernel, dim3(*groups), dim3(threads), bytes, st, a, w); };
-    if (w.parts > 1) {
-        go(distill_rows_kernel<BF16, DBF16, 256, 8, REST, PART_SUMS>, 256, lds);
-        go(distill_rows_kernel<BF16, DBF16, 256, 8, REST, PART_GRADIENT>, 256, 0);
-    } else if (a.C <= 64 * 8 * V) {
-        go(distill_rows_kernel<BF16, DBF16, 64, 8, REST, ROW_HELD>, 64, lds);
-    } else if (a.C <= 256 * 8 * V) {
-        go(distill_rows_kernel<BF16, DBF16, 256, 8, REST, ROW_HELD>, 256, lds);
-    } else if (a.C <= 512 * 16 * V) {
-        go(distill_rows_kernel<BF16, DBF16, 512, 16, REST, ROW_HELD>, 512, lds);
-    } else if (a.C <= 1024 * 16 * V) {
-        go(distill_rows_kernel<BF16, DBF16, 1024, 16, REST, ROW_HELD>, 1024, lds);
-    } else {
-        go(distill_rows_kernel<BF16, DBF16, 512, 8, REST, ROW_READ_TWICE>, 512, lds);
-    }
 }
 
 }  // namespace capgnn
@@ -601,10 +80,7 @@ extern "C" int capgnn_distill(int64_t n, int C, const void *Z, int64_t ldz, int 
     int groups = 0;
     if (n > 0) {
         const bool zb = z_dtype == CAPGNN_BF16, db = dz_dtype == CAPGNN_BF16;
-        auto run = rest ? (zb ? (db ? launch_distill<true, true, true> : launch_distill<true, false, true>)
-                              : (db ? launch_distill<false, true, true> : launch_distill<false, false, true>))
-                        : (zb ? (db ? launch_distill<true, true, false> : launch_distill<true, false, false>)
-                              : (db ? launch_distill<false, true, false> : launch_distill<false, false, false>));
+        const DistillLaunch run = rest ? distill_launch_rest(zb, db) : distill_launch_of<false>(zb, db);
         run(a, p, &groups, st);
     }
     hipLaunchKernelGGL(distill_final_kernel, dim3(1), dim3(256), 0, st, groups, a.part, weight, a.norm_val, a.norm_dev, loss_dev);

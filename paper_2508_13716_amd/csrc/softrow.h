@@ -96,12 +96,24 @@ template <bool BF16> struct Raw {
         if constexpr (BF16) return __uint_as_float(e & 1 ? r[e / 2] & 0xffff0000u : r[e / 2] << 16);
         else return __uint_as_float(r[e]);
     }
-    // Logits [j, j + V) of a row of at least V that ends at `end`.  Where fewer are left the row's last V are read, and those before j are
-    // barred in the result (all of them for j >= end): what is returned starts at class `start`.
-    static __device__ __forceinline__ raw16 load_until(const char *p, int j, int end, int *start) {
+    // Logits [j, j + V) of a row that ends at `end`.  Where fewer are left the row's last V are read, and those before j are
+    // barred in the result (all of them for j >= end): what is returned starts at class `start`.  SHORT: the row may have fewer than V.
+    template <bool SHORT = false> static __device__ __forceinline__ raw16 load_until(const char *p, int j, int end, int *start) {
         const int from = j + V <= end ? j : end - V;
-        raw16 r = load(p, from);
+        raw16 r;
         *start = from;
+        if (SHORT && from < 0) {
+            r = raw16{BARRED, BARRED, BARRED, BARRED};
+            for (int k = 0; k < end; ++k) {
+                const uint32_t b = __float_as_uint(ld_logit<BF16>(p, k));
+                const int e = k - from, w = BF16 ? e / 2 : e;
+                const uint32_t mask = !BF16 ? 0xffffffffu : e & 1 ? 0xffff0000u : 0xffffu, v = BF16 && !(e & 1) ? b >> 16 : b;
+#pragma unroll
+                for (int q = 0; q < 4; ++q) if (q == w) r[q] = (r[q] & ~mask) | (v & mask);
+            }
+        } else {
+            r = load(p, from);
+        }
         if (__any(from != j)) {
             const int out = j - from;
 #pragma unroll
@@ -153,16 +165,32 @@ template <bool DBF16, int V> __device__ __forceinline__ void ld_vector(const cha
     }
 }
 
+// From here on the compiler knows nothing of r: what it has unpacked or derived from it before is not kept in registers for later, and
+// work on one vector is not mixed with that on the next (which took twice the registers; other waves fill the gaps).
+__device__ __forceinline__ void forget(raw16 &r) {
+    __builtin_amdgcn_sched_barrier(0);
+    asm volatile("" : "+v"(r));
+}
+// The thread's number, of which the compiler knows nothing: addresses and conditions formed from it are not kept for the next use.
+__device__ __forceinline__ int thread_anew() {
+    int t = threadIdx.x;
+    asm volatile("" : "+v"(t));
+    return t;
+}
+
 // Rows of at most NARROW_C classes: a wave takes 64 / G of them at a time through LDS, G lanes a row with at most 32 classes each, so that a
 // row's sums need hardly any exchange between lanes (lane groups over registers spent four times the instructions at 47 classes:
 // 612000 rows were bound by them, not by memory).  The next rows' loads are under way while a wave works on its own.  A row starts
-// G * odd words after the one before it: lanes that read the same class of their rows at once hit different banks.
+// G * odd words after the one before it: lanes that read the same class of their rows at once hit different banks.  A lane reads its
+// classes NARROW_BATCH at a time; what is behind a row's end holds -inf (narrow_ends).
 constexpr int NARROW_C = 256;
 constexpr int NARROW_G = NARROW_C / 32;     // lanes of a row at most
+constexpr int NARROW_BATCH = 8;
 constexpr int NARROW_WAVES = 2;     // of a workgroup; each works for itself
 struct NarrowShape {
     int C, lg;              // G = 1 << lg
     int rows, pitch;        // of a wave; words between rows in LDS
+    int each;               // classes of a lane, whole batches
     int pieces, magic;      // loads of a row (16 bytes, or one logit where a row is shorter than 16 bytes); item / pieces = item * magic >> 16
     int items;              // rows * pieces <= 64 * NarrowLoad::MOST
     size_t lds_wave;        // bytes, without extra
@@ -176,7 +204,8 @@ static inline NarrowShape narrow_shape(int C, int dtype) {
     while ((32 << s.lg) < C) ++s.lg;
     const int G = 1 << s.lg;
     s.rows = 64 / G;
-    s.pitch = G * (((C + G - 1) / G) | 1);
+    s.each = ((C + G - 1) / G + NARROW_BATCH - 1) / NARROW_BATCH * NARROW_BATCH;
+    s.pitch = G * (s.each | 1);
     s.pieces = C < V ? C : (C + V - 1) / V;
     s.magic = (65536 + s.pieces - 1) / s.pieces;
     s.items = s.rows * s.pieces;
@@ -193,9 +222,15 @@ __device__ __forceinline__ void wave_sync() {
 
 // workgroups: as many as the chip holds at once (lds: bytes of one), or fewer
 static inline unsigned narrow_grid(const NarrowShape &s, int64_t n, size_t lds) {
-    const int64_t held = static_cast<int64_t>(160 * 1024 / lds) < 8 ? static_cast<int64_t>(160 * 1024 / lds) : 8;
+    const int64_t held = static_cast<int64_t>(160 * 1024 / lds) < 10 ? static_cast<int64_t>(160 * 1024 / lds) : 10;
     const int64_t needed = (n + NARROW_WAVES * s.rows - 1) / (NARROW_WAVES * s.rows);
     return static_cast<unsigned>(needed < NUM_CU * held ? needed : NUM_CU * held);
+}
+
+// -inf behind the ends of the wave's rows; nothing writes there afterwards
+__device__ __forceinline__ void narrow_ends(const NarrowShape &s, float *lds, int lane) {
+    const int behind = s.pitch - s.C;
+    for (int i = lane; i < s.rows * behind; i += 64) lds[i / behind * s.pitch + s.C + i % behind] = -INFINITY;
 }
 
 template <bool BF16> struct NarrowLoad {
@@ -203,8 +238,9 @@ template <bool BF16> struct NarrowLoad {
     raw16 q[MOST];
 
     // rows [row0, row0 + s.rows), those beyond the last one again the last one
-    __device__ __forceinline__ void fetch(const NarrowShape &s, const char *Z, int64_t ldz, int64_t n, int64_t row0, int lane) {
+    __device__ __forceinline__ void fetch(const NarrowShape &s, const char *Z, int64_t ldz, int64_t n, int64_t row0) {
         typedef Raw<BF16> R;
+        const int lane = thread_anew() & 63;
 #pragma unroll
         for (int i = 0; i < MOST; ++i) {
             const int item = i * 64 + lane;
@@ -220,8 +256,9 @@ template <bool BF16> struct NarrowLoad {
         }
     }
 
-    __device__ __forceinline__ void put(const NarrowShape &s, float *lds, int lane) {
+    __device__ __forceinline__ void put(const NarrowShape &s, float *lds) {
         typedef Raw<BF16> R;
+        const int lane = thread_anew() & 63;
 #pragma unroll
         for (int i = 0; i < MOST; ++i) {
             const int item = i * 64 + lane;
@@ -243,9 +280,9 @@ template <bool BF16> struct NarrowLoad {
 
 // The wave's rows of gradients, from LDS as NarrowLoad put the logits there; add: to what dZ holds.
 template <bool BF16, bool DBF16>
-__device__ __forceinline__ void narrow_store(const NarrowShape &s, const float *lds, char *dZ, int64_t lddz, int64_t n, int64_t row0, int lane,
-                                             bool add) {
+__device__ __forceinline__ void narrow_store(const NarrowShape &s, const float *lds, char *dZ, int64_t lddz, int64_t n, int64_t row0, bool add) {
     constexpr int V = Raw<BF16>::V;
+    const int lane = thread_anew() & 63;
 #pragma unroll
     for (int i = 0; i < NarrowLoad<BF16>::MOST; ++i) {
         const int item = i * 64 + lane;
@@ -268,17 +305,12 @@ __device__ __forceinline__ void narrow_store(const NarrowShape &s, const float *
     }
 }
 
-// From here on the compiler knows nothing of r: what it has unpacked or derived from it before is not kept in registers for later, and
-// work on one vector is not mixed with that on the next (which took twice the registers; other waves fill the gaps).
-__device__ __forceinline__ void forget(raw16 &r) {
-    __builtin_amdgcn_sched_barrier(0);
-    asm volatile("" : "+v"(r));
-}
-// The thread's number, of which the compiler knows nothing: addresses and conditions formed from it are not kept for the next use.
-__device__ __forceinline__ int thread_anew() {
-    int t = threadIdx.x;
-    asm volatile("" : "+v"(t));
-    return t;
+// The same for a value that all threads have: what one pass over a row's vectors has found out about their number is not carried into the next
+// (code for every number of vectors: a kilobyte of scratch memory a thread).
+__device__ __forceinline__ int uniform_anew(int x) {
+    x = __builtin_amdgcn_readfirstlane(x);
+    asm volatile("" : "+s"(x));
+    return x;
 }
 
 template <typename T, typename Op> __device__ __forceinline__ T wave_all(T v, Op op) {
