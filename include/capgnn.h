@@ -482,7 +482,7 @@ int capgnn_sigmoid_bce(int64_t n, int C, const float *Z, int64_t ldz, const uint
 
 /* ------------------------------------------------------------------------------------------
  * What a classifier answers with, and what it learns from another one's answers.  Rows of logits Z: device [n x ldz] of
- * z_dtype (C classes; rows need no alignment beyond their elements'), divided by `temperature` (finite, > 0) before the softmax.
+ * z_dtype (C classes; rows need no alignment beyond their elements'), divided by `temperature` (2^-64 to 2^64) before the softmax.
  * p_i = softmax(Z_i / temperature).  A logit of -infinity bars its class: p = 0, nothing is added to the entropy and no gradient
  * flows through it.  A row whose classes are all barred is empty.  A NaN or +infinity makes the row's numbers NaN, no other row's.
  * mask: device uint8[n] or NULL: rows with 0 are left out, whatever they hold.  dZ may be Z itself if type and pitch are the same too (each

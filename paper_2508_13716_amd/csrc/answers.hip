@@ -636,11 +636,9 @@ struct GradRow {
         H = !none && a.dentropy ? a.entropy[row] : 0.f;
         inv_s = expf(-ln_s);
     }
-    template <bool ENT> __device__ __forceinline__ float base(float z, const TempScale &t) const {
-        const float d = z - m0, p = exp_scaled(d, t) * inv_s;
-        float f = G;
-        if constexpr (ENT) f = p != 0.f ? fmaf(h, fmaf(d, t.inv_T, H - ln_s), G) : 0.f;
-        return -p * f;
+    template <bool ENT, bool EXACT = true> __device__ __forceinline__ float base(float z, const TempScale &t) const {
+        const float d = difference(z, m0, t), p = exp_scaled<EXACT>(d, t) * inv_s;
+        return -p * (ENT ? fmaf(h, fmaf(d, t.inv_T, H - ln_s), G) : G);
     }
 };
 
@@ -696,7 +694,7 @@ __global__ __launch_bounds__(THREADS) void answers_grad_rows_kernel(AnswerGradAr
             float o[V];
             const int shift = j + V <= hi ? 0 : j + V - hi;         // a row's last vector starts earlier than j by that
 #pragma unroll
-            for (int e = 0; e < V; ++e) o[e] = w.none ? 0.f : w.base<ENT>(R::get(r[i], e), a.t) * a.t.inv_T;
+            for (int e = 0; e < V; ++e) o[e] = w.none ? 0.f : w.base<ENT, !DBF16>(R::get(r[i], e), a.t) * a.t.inv_T;
             if (shift == 0) st_vector<DBF16>(dz, j, o);
             else
 #pragma unroll
@@ -747,7 +745,7 @@ __global__ __launch_bounds__(64 * NARROW_WAVES) void answers_grad_narrow_kernel(
         next.put(s, tile);
         wave_sync();
         if (row0 + step < a.n) next.fetch(s, a.Z, a.ldz, a.n, row0 + step);
-        for (int j = sub; j < C; j += G) z[j] = w.none ? 0.f : w.base<ENT>(z[j], a.t) * a.t.inv_T;
+        for (int j = sub; j < C; j += G) z[j] = w.none ? 0.f : w.base<ENT, !DBF16>(z[j], a.t) * a.t.inv_T;
         wave_sync();
         if (sub == 0 && !w.none)            // one lane a row: the same class may be given again
             for (int i = 0; i < a.m; ++i) {
@@ -780,7 +778,7 @@ extern "C" int capgnn_logprobs(int64_t n, int C, const void *Z, int64_t ldz, int
     if (C > CLASSES_MOST) CG_FAIL(CAPGNN_EUNSUPPORTED, "logprobs: more than 2^30 classes");
     if (m < 0 || m > CAPGNN_GIVEN_MAX) CG_FAIL(CAPGNN_EINVAL, "logprobs: m = %d, 0 to %d classes can be given per row", m, CAPGNN_GIVEN_MAX);
     if (k < 0 || k > CAPGNN_TOP_MAX || k > C) CG_FAIL(CAPGNN_EINVAL, "logprobs: k = %d, 0 to min(C, %d) expected", k, CAPGNN_TOP_MAX);
-    if (!good_temperature(temperature)) CG_FAIL(CAPGNN_EINVAL, "logprobs: the temperature must be positive and finite");
+    if (!good_temperature(temperature)) CG_FAIL(CAPGNN_EINVAL, "logprobs: the temperature must lie between 2^-64 and 2^64");
     if (n == 0) return CAPGNN_OK;
     if (!Z || (m > 0 && (!ids || !logp)) || (k > 0 && !top_ids && !top_logp)) CG_FAIL(CAPGNN_EINVAL, "logprobs: NULL operand");
     if (ldz < C || (m > 0 && (ldi < m || ldp < m)) || (k > 0 && ldt < k)) CG_FAIL(CAPGNN_EINVAL, "logprobs: leading dimension smaller than the row");
@@ -838,7 +836,7 @@ extern "C" int capgnn_logprobs_bwd(int64_t n, int C, const void *Z, int64_t ldz,
     if (n < 0 || C <= 0) CG_FAIL(CAPGNN_EINVAL, "logprobs_bwd: bad sizes");
     if (C > CLASSES_MOST) CG_FAIL(CAPGNN_EUNSUPPORTED, "logprobs_bwd: more than 2^30 classes");
     if (m < 0 || m > CAPGNN_GIVEN_MAX) CG_FAIL(CAPGNN_EINVAL, "logprobs_bwd: m = %d, 0 to %d classes can be given per row", m, CAPGNN_GIVEN_MAX);
-    if (!good_temperature(temperature)) CG_FAIL(CAPGNN_EINVAL, "logprobs_bwd: the temperature must be positive and finite");
+    if (!good_temperature(temperature)) CG_FAIL(CAPGNN_EINVAL, "logprobs_bwd: the temperature must lie between 2^-64 and 2^64");
     if (n == 0) return CAPGNN_OK;
     if (!Z || !stats || !dZ || (m > 0 && (!ids || !dlogp)) || (dentropy && !entropy)) CG_FAIL(CAPGNN_EINVAL, "logprobs_bwd: NULL operand");
     if (ldz < C || lddz < C || (m > 0 && (ldi < m || lddp < m))) CG_FAIL(CAPGNN_EINVAL, "logprobs_bwd: leading dimension smaller than the row");

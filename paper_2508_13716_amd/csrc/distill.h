@@ -176,9 +176,9 @@ __device__ __forceinline__ void read_tile(raw16 (&r)[NV], const char *z, int t0,
     }
 }
 
-// dz = p * factor for the tile's classes (p = exp(z - m0) * inv_s), added to dz's contents when add; barred classes get 0
+// dz = exp((z - m0) / T) * factor for the tile's classes, added to dz's contents when add
 template <bool BF16, bool DBF16, int THREADS, int NV>
-__device__ __forceinline__ void grad_tile(raw16 (&r)[NV], char *dz, int t0, int hi, const TempScale &t, float m0, float inv_s, float factor, int add) {
+__device__ __forceinline__ void grad_tile(raw16 (&r)[NV], char *dz, int t0, int hi, const TempScale &t, float m0, float factor, int add) {
     typedef Raw<BF16> R;
     constexpr int V = R::V;
     const int tid = thread_anew();
@@ -194,8 +194,7 @@ __device__ __forceinline__ void grad_tile(raw16 (&r)[NV], char *dz, int t0, int 
         if (add && shift == 0) ld_vector<DBF16>(dz, j, old);
 #pragma unroll
         for (int e = 0; e < V; ++e) {
-            const float p = exp_scaled(R::get(r[i], e) - m0, t) * inv_s;
-            o[e] = p == 0.f ? 0.f : p * factor;
+            o[e] = exp_scaled<!DBF16>(difference(R::get(r[i], e), m0, t), t) * factor;
         }
         if (shift == 0) {
             if (add)
@@ -241,7 +240,7 @@ __device__ __forceinline__ float listed_sum(const DistillArgs &a, const Teacher 
     float e = 0.f;
 #pragma unroll 1
     for (int i = threadIdx.x; i < a.k; i += 64)
-        if (t.c[i] >= 0) e += exp_scaled(t.z[i] - m0, a.t);
+        if (t.c[i] >= 0) e += exp_scaled(difference(t.z[i], m0, a.t), a.t);
     return wave_all(e, OpSum());
 }
 
@@ -348,7 +347,8 @@ __global__ __launch_bounds__(THREADS) __attribute__((amdgpu_waves_per_eu(4))) vo
         }
         if (dz) {
             const float inv_s = 1.f / S, mass = t.mass * scale;
-            const float away = REST && t.r > 0.0 ? static_cast<float>(t.mass - t.r * (static_cast<double>(S) / others)) * scale : mass;
+            // (others = 0: every class that is not listed has p = 0)
+            const float away = !REST || t.r == 0.0 ? mass : others == 0.f ? 0.f : static_cast<float>(t.mass - t.r * (static_cast<double>(S) / others)) * scale;
             if (a.accumulate) {         // what the listed classes hold, before anything is written
                 if (first_wave)
                     for (int i = threadIdx.x; i < a.k; i += 64)
@@ -357,18 +357,18 @@ __global__ __launch_bounds__(THREADS) __attribute__((amdgpu_waves_per_eu(4))) vo
             }
             // a longer row: its last tile is still there, the others come again, the latest first
             int t0 = STAGE == ROW_READ_TWICE ? lo + (hi - lo - 1) / TILE * TILE : lo;
-            grad_tile<BF16, DBF16, THREADS, NV>(r, dz, t0, hi, a.t, m0, inv_s, away, a.accumulate);
+            grad_tile<BF16, DBF16, THREADS, NV>(r, dz, t0, hi, a.t, m0, away * inv_s, a.accumulate);
             if constexpr (STAGE == ROW_READ_TWICE) {
 #pragma unroll 1
                 for (t0 -= TILE; t0 >= lo; t0 -= TILE) {
                     read_tile<BF16, THREADS, NV>(r, z, t0, hi);
-                    grad_tile<BF16, DBF16, THREADS, NV>(r, dz, t0, hi, a.t, m0, inv_s, away, a.accumulate);
+                    grad_tile<BF16, DBF16, THREADS, NV>(r, dz, t0, hi, a.t, m0, away * inv_s, a.accumulate);
                 }
             } else if constexpr (STAGE == PART_GRADIENT) {
 #pragma unroll 1
                 for (t0 += TILE; t0 < hi; t0 += TILE) {
                     read_tile<BF16, THREADS, NV>(r, z, t0, hi);
-                    grad_tile<BF16, DBF16, THREADS, NV>(r, dz, t0, hi, a.t, m0, inv_s, away, a.accumulate);
+                    grad_tile<BF16, DBF16, THREADS, NV>(r, dz, t0, hi, a.t, m0, away * inv_s, a.accumulate);
                 }
             }
             __syncthreads();
@@ -376,7 +376,7 @@ __global__ __launch_bounds__(THREADS) __attribute__((amdgpu_waves_per_eu(4))) vo
                 for (int i = threadIdx.x; i < a.k; i += 64) {
                     const int c = t.c[i];
                     if (c < lo || c >= hi) continue;
-                    const float g = fmaf(exp_scaled(t.z[i] - m0, a.t) * inv_s, mass, -t.q[i] * scale);
+                    const float g = fmaf(exp_scaled(difference(t.z[i], m0, a.t), a.t) * inv_s, mass, -t.q[i] * scale);
                     st_grad<DBF16>(dz, c, a.accumulate ? t.old[i] + g : g);
                 }
         }
@@ -507,7 +507,8 @@ __global__ __launch_bounds__(64 * NARROW_WAVES) __attribute__((amdgpu_waves_per_
         double r = REST ? 1.0 - Q : 0.0;
         if (r < REST_LEAST) r = 0.0;
         const float mass = static_cast<float>(REST ? Q + r : 1.0 + 0.0 * Q) * scale;
-        const float away = REST && r > 0.0 ? static_cast<float>(Q + r - r * (static_cast<double>(S) / others)) * scale : mass;
+        const float away = !REST || r == 0.0 ? mass : others == 0.f ? 0.f : static_cast<float>(Q + r - r * (static_cast<double>(S) / others)) * scale;
+        const float factor = away * inv_s;
         double kl = 0.0;
         if (live) {
             for (int i = sub; i < k; i += G) {
@@ -515,7 +516,7 @@ __global__ __launch_bounds__(64 * NARROW_WAVES) __attribute__((amdgpu_waves_per_
                 if (j < 0) continue;
                 const float p = q[j], d = z[j] - m0;
                 if (p != 0.f) kl += static_cast<double>(fmaf(-p * d, a.t.inv_T, p * (logf(p) + ln_s)));      // (q d before 1/T, as above)
-                z[j] = fmaf(exp_scaled(d, a.t) * inv_s, mass, -p * scale);
+                z[j] = fmaf(exp_scaled(difference(z[j], m0, a.t), a.t) * inv_s, mass, -p * scale);
             }
         }
         for (int off = 1; off < G; off <<= 1) kl += __shfl_xor(kl, off);
@@ -536,7 +537,7 @@ __global__ __launch_bounds__(64 * NARROW_WAVES) __attribute__((amdgpu_waves_per_
                 }
 #pragma unroll
                 for (int i = 0; i < NARROW_BATCH; ++i) {
-                    const float p = exp_scaled(x[i] - m0, a.t) * inv_s, g = p == 0.f ? none : p * away;
+                    const float g = exp_scaled<!DBF16>(difference(x[i], m0, a.t), a.t) * factor;
                     if ((!live || y[i] == -1.f) && sub + (b + i) * G < C) z[sub + (b + i) * G] = live ? g : none;
                 }
             }

@@ -48,7 +48,7 @@ extern "C" int capgnn_distill(int64_t n, int C, const void *Z, int64_t ldz, int 
     if (C > CLASSES_MOST) CG_FAIL(CAPGNN_EUNSUPPORTED, "distill: more than 2^30 classes");
     if (k < 1 || k > CAPGNN_GIVEN_MAX) CG_FAIL(CAPGNN_EINVAL, "distill: k = %d, 1 to %d classes of a teacher expected", k, CAPGNN_GIVEN_MAX);
     if (rest != 0 && rest != 1) CG_FAIL(CAPGNN_EINVAL, "distill: rest must be 0 or 1");
-    if (!good_temperature(temperature)) CG_FAIL(CAPGNN_EINVAL, "distill: the temperature must be positive and finite");
+    if (!good_temperature(temperature)) CG_FAIL(CAPGNN_EINVAL, "distill: the temperature must lie between 2^-64 and 2^64");
     if (!std::isfinite(weight) || loss_norm != loss_norm) CG_FAIL(CAPGNN_EINVAL, "distill: weight or loss_norm is not a number");
     if (!loss_dev) CG_FAIL(CAPGNN_EINVAL, "distill: NULL operand");
     if (n > 0 && (!Z || !teacher_ids || !teacher_val)) CG_FAIL(CAPGNN_EINVAL, "distill: NULL operand");

@@ -10,6 +10,7 @@ namespace capgnn {
 // exp(d / T) = 2^(d * L): L and what its rounding to float leaves of log2(e) / T
 struct TempScale {
     float L, L_lo, inv_T;
+    float least;            // differences below this are taken for it: exp is 0 and every product with them finite
 };
 
 static inline TempScale temp_scale(float temperature) {
@@ -18,11 +19,12 @@ static inline TempScale temp_scale(float temperature) {
     t.L = static_cast<float>(l);
     t.L_lo = static_cast<float>(l - static_cast<double>(t.L));
     t.inv_T = static_cast<float>(1.0 / static_cast<double>(temperature));
+    t.least = static_cast<float>(-1000.0 / l);
     return t;
 }
 
-// T > 0, finite, and 1/T a finite float too
-static inline bool good_temperature(float t) { return t > 1e-37f && t < 1e37f; }
+// 2^-64 to 2^64: everything formed from T and a difference of logits that matters stays a finite float
+static inline bool good_temperature(float t) { return t >= 5.421010862427522e-20f && t <= 1.8446744073709552e19f; }
 
 template <bool BF16> __device__ __forceinline__ float ld_logit(const char *p, int64_t i) {
     if constexpr (BF16) return __uint_as_float(static_cast<uint32_t>(reinterpret_cast<const uint16_t *>(p)[i]) << 16);
@@ -43,24 +45,26 @@ template <bool BF16> __device__ __forceinline__ void st_grad(char *p, int64_t i,
 
 __device__ __forceinline__ float exp2_raw(float x) { return __builtin_amdgcn_exp2f(x); }
 
-// exp(d / T), d <= 0.  The product d * L loses up to |d L| 2^-24 of the exponent: what it loses is put back to first order.
-__device__ __forceinline__ float exp_scaled(float d, const TempScale &t) {
-    const float u = d * t.L;
-    const float e = exp2_raw(u);
-    const float lost = fmaf(d, t.L_lo, fmaf(d, t.L, -u));
-    return e > 0.f ? fmaf(e, lost * 0.69314718f, e) : e;        // (d = -inf: lost is NaN, e is 0; a NaN d gives a NaN e)
-}
-
-// exp((a - b) / T), a <= b, without the rounding of a - b either (a teacher's probabilities: few, so the six operations more do not count)
-__device__ __forceinline__ float exp_difference(float a, float b, const TempScale &t) {
-    const float d = a - b, back = d - a, rest = (a - (d - back)) + (-b - back);
-    const float u = d * t.L, e = exp2_raw(u);
-    const float lost = fmaf(rest, t.L, fmaf(d, t.L_lo, fmaf(d, t.L, -u)));
-    return e > 0.f ? fmaf(e, lost * 0.69314718f, e) : e;
-}
-
 // the larger of the two; NaN if either is (one instruction, as the maximum that skips NaN)
 __device__ __forceinline__ float max_of(float a, float b) { return __builtin_elementwise_maximum(a, b); }
+
+// exp(d / T), d <= 0 and not below TempScale::least.  The product d * L loses up to |d L| 2^-24 of the exponent; EXACT puts what it loses back
+// to first order (float results; a bf16 result's rounding is thousands of times as large).
+template <bool EXACT = true> __device__ __forceinline__ float exp_scaled(float d, const TempScale &t) {
+    const float u = d * t.L, e = exp2_raw(u);
+    if constexpr (!EXACT) return e;
+    return fmaf(e, fmaf(d, t.L_lo, fmaf(d, t.L, -u)) * 0.69314718f, e);
+}
+__device__ __forceinline__ float difference(float z, float m0, const TempScale &t) { return max_of(z - m0, t.least); }
+
+// exp((a - b) / T), a <= b, without the rounding of a - b either (a teacher's probabilities: few, so the operations more do not count)
+__device__ __forceinline__ float exp_difference(float a, float b, const TempScale &t) {
+    const float d = a - b;
+    if (d < t.least) return 0.f;
+    const float back = d - a, rest = (a - (d - back)) + (-b - back);
+    const float u = d * t.L, e = exp2_raw(u);
+    return fmaf(e, fmaf(rest, t.L, fmaf(d, t.L_lo, fmaf(d, t.L, -u))) * 0.69314718f, e);
+}
 
 // the reference point of a row: 0 where every class is barred, so that -inf - -inf is never formed
 __device__ __forceinline__ float safe_max(float m) { return m == -INFINITY ? 0.f : m; }

@@ -34,7 +34,7 @@ def logprobs_args(**kw):
 
 @pytest.mark.parametrize("bad", [
     dict(n=-1), dict(n_classes=0), dict(n_classes=-3), dict(z_dtype=2), dict(ldz=9), dict(Z=None), dict(Z=FAKE + 2), dict(Z=FAKE + 1, z_dtype=B.BF16),
-    dict(temperature=0.0), dict(temperature=-1.0), dict(temperature=float("inf")), dict(temperature=float("nan")), dict(temperature=1e-39),
+    dict(temperature=0.0), dict(temperature=-1.0), dict(temperature=float("inf")), dict(temperature=float("nan")), dict(temperature=1e-39), dict(temperature=1e20),
     dict(m=-1), dict(m=257, ldi=257, ldp=257), dict(ldi=1), dict(ldp=1), dict(ids=None), dict(logp=None),
     dict(k=-1), dict(k=11, ldt=11), dict(k=65, ldt=65, n_classes=100, ldz=100), dict(ldt=2), dict(top_ids=None, top_logp=None)])
 def test_logprobs_refuses(bad):
