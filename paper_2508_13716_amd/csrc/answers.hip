@@ -315,7 +315,8 @@ __global__ __launch_bounds__(THREADS) __attribute__((amdgpu_waves_per_eu(4))) vo
             int start;
 #pragma unroll
             for (int i = 0; i < NV; ++i)
-                if (t0 + i * THREADS * R::V < hi) r[i] = R::load_until(z, t0 + (i * THREADS + tid) * R::V, hi, &start);
+                if (t0 + (i + 1) * THREADS * R::V <= hi) r[i] = R::load(z, t0 + (i * THREADS + tid) * R::V);
+                else if (t0 + i * THREADS * R::V < hi) r[i] = R::load_until(z, t0 + (i * THREADS + tid) * R::V, hi, &start);
                 else r[i] = raw16{R::BARRED, R::BARRED, R::BARRED, R::BARRED};
 #pragma unroll
             for (int i = 0; i < NV; ++i) {

@@ -172,7 +172,9 @@ __device__ __forceinline__ void read_tile(raw16 (&r)[NV], const char *z, int t0,
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
         if (t0 + i * THREADS * R::V >= hi) continue;
-        r[i] = R::template load_until<SHORT>(z, t0 + (i * THREADS + tid) * R::V, hi, &from);
+        const int j = t0 + (i * THREADS + tid) * R::V;
+        if (t0 + (i + 1) * THREADS * R::V <= hi) r[i] = R::load(z, j);
+        else r[i] = R::template load_until<SHORT>(z, j, hi, &from);
     }
 }
 
@@ -187,21 +189,20 @@ __device__ __forceinline__ void grad_tile(raw16 (&r)[NV], char *dz, int t0, int 
     for (int i = 0; i < NV; ++i) {
         if (t0 + i * THREADS * V >= hi) continue;
         const int j = t0 + (i * THREADS + tid) * V;
-        if (j >= hi) continue;
         forget(r[i]);
-        const int shift = j + V <= hi ? 0 : j + V - hi;         // a row's last vector starts earlier than j by that
-        float o[V], old[V];
-        if (add && shift == 0) ld_vector<DBF16>(dz, j, old);
+        float o[V];
 #pragma unroll
-        for (int e = 0; e < V; ++e) {
-            o[e] = exp_scaled<!DBF16>(difference(R::get(r[i], e), m0, t), t) * factor;
-        }
-        if (shift == 0) {
-            if (add)
+        for (int e = 0; e < V; ++e) o[e] = exp_scaled<!DBF16>(difference(R::get(r[i], e), m0, t), t) * factor;
+        if (t0 + (i + 1) * THREADS * V <= hi || j + V <= hi) {
+            if (add) {
+                float old[V];
+                ld_vector<DBF16>(dz, j, old);
 #pragma unroll
                 for (int e = 0; e < V; ++e) o[e] += old[e];
+            }
             st_vector<DBF16>(dz, j, o);
-        } else {
+        } else if (j < hi) {
+            const int shift = j + V - hi;           // a row's last vector starts earlier than j by that
 #pragma unroll
             for (int e = 0; e < V; ++e)
                 if (e >= shift) st_grad<DBF16>(dz, hi - V + e, add ? o[e] + ld_logit<DBF16>(dz, hi - V + e) : o[e]);
@@ -584,7 +585,7 @@ void launch_distill(const DistillArgs &a, DistillParts w, int *groups, hipStream
     } else if (a.C <= 512 * 16 * V) {
         go(distill_rows_kernel<BF16, DBF16, 512, 16, REST, ROW_HELD>, 512, lds);
     } else {
-        go(distill_rows_kernel<BF16, DBF16, 1024, 16, REST, ROW_READ_TWICE>, 1024, lds);
+        go(distill_rows_kernel<BF16, DBF16, 512, 16, REST, ROW_READ_TWICE>, 512, lds);
     }
 }
 

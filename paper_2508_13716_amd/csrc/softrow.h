@@ -92,9 +92,10 @@ template <bool BF16> struct Raw {
     static constexpr int V = BF16 ? 8 : 4;
     static constexpr uint32_t BARRED = BF16 ? 0xff80ff80u : 0xff800000u;
 
-    static __device__ __forceinline__ raw16 load(const char *p, int64_t j) {
-        if constexpr (BF16) return *reinterpret_cast<const raw16_by2 *>(p + j * 2);
-        else return *reinterpret_cast<const raw16_by4 *>(p + j * 4);
+    // j >= 0; a row has 2^30 classes at most: its bytes are counted in 32 bits, and the row's address may stay in scalar registers
+    static __device__ __forceinline__ raw16 load(const char *p, int j) {
+        if constexpr (BF16) return *reinterpret_cast<const raw16_by2 *>(p + static_cast<uint32_t>(j) * 2u);
+        else return *reinterpret_cast<const raw16_by4 *>(p + static_cast<uint32_t>(j) * 4u);
     }
     static __device__ __forceinline__ float get(raw16 r, int e) {
         if constexpr (BF16) return __uint_as_float(e & 1 ? r[e / 2] & 0xffff0000u : r[e / 2] << 16);
@@ -136,14 +137,14 @@ typedef raw8 raw8_by2 __attribute__((aligned(2)));
 template <bool DBF16, int V> __device__ __forceinline__ void st_vector(char *p, int j, const float (&g)[V]) {
     if constexpr (DBF16) {
         if constexpr (V == 8)
-            *reinterpret_cast<raw16_by2 *>(p + static_cast<int64_t>(j) * 2) =
+            *reinterpret_cast<raw16_by2 *>(p + static_cast<uint32_t>(j) * 2u) =
                 raw16{bf16_two(g[0], g[1]), bf16_two(g[2], g[3]), bf16_two(g[4], g[5]), bf16_two(g[6], g[7])};
         else
-            *reinterpret_cast<raw8_by2 *>(p + static_cast<int64_t>(j) * 2) = raw8{bf16_two(g[0], g[1]), bf16_two(g[2], g[3])};
+            *reinterpret_cast<raw8_by2 *>(p + static_cast<uint32_t>(j) * 2u) = raw8{bf16_two(g[0], g[1]), bf16_two(g[2], g[3])};
     } else {
 #pragma unroll
         for (int h = 0; h < V; h += 4)
-            *reinterpret_cast<raw16_by4 *>(p + static_cast<int64_t>(j + h) * 4) =
+            *reinterpret_cast<raw16_by4 *>(p + static_cast<uint32_t>(j + h) * 4u) =
                 raw16{__float_as_uint(g[h]), __float_as_uint(g[h + 1]), __float_as_uint(g[h + 2]), __float_as_uint(g[h + 3])};
     }
 }
@@ -151,9 +152,9 @@ template <bool DBF16, int V> __device__ __forceinline__ void ld_vector(const cha
     if constexpr (DBF16) {
         raw16 r = {0, 0, 0, 0};
         if constexpr (V == 8) {
-            r = *reinterpret_cast<const raw16_by2 *>(p + static_cast<int64_t>(j) * 2);
+            r = *reinterpret_cast<const raw16_by2 *>(p + static_cast<uint32_t>(j) * 2u);
         } else {
-            const raw8 q = *reinterpret_cast<const raw8_by2 *>(p + static_cast<int64_t>(j) * 2);
+            const raw8 q = *reinterpret_cast<const raw8_by2 *>(p + static_cast<uint32_t>(j) * 2u);
             r[0] = q[0];
             r[1] = q[1];
         }
@@ -162,7 +163,7 @@ template <bool DBF16, int V> __device__ __forceinline__ void ld_vector(const cha
     } else {
 #pragma unroll
         for (int h = 0; h < V; h += 4) {
-            const raw16 r = *reinterpret_cast<const raw16_by4 *>(p + static_cast<int64_t>(j + h) * 4);
+            const raw16 r = *reinterpret_cast<const raw16_by4 *>(p + static_cast<uint32_t>(j + h) * 4u);
 #pragma unroll
             for (int e = 0; e < 4; ++e) g[h + e] = __uint_as_float(r[e]);
         }
