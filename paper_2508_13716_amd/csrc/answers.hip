@@ -601,10 +601,10 @@ __global__ __launch_bounds__(256) void answers_join_kernel(AnswerArgs a, AnswerP
     }
 }
 
-// Few rows are cut into parts, about a thousand workgroups in all and at least ANSWER_PART_LEAST classes each.
+// Few rows are cut into parts, about a thousand workgroups in all and ANSWER_PART_LEAST classes or more each.
 constexpr int ANSWER_PART_LEAST = 2048, ANSWER_WORKGROUPS = 1024;
 static int answer_parts(int64_t n, int C, int64_t *chunk) {
-    int64_t parts = std::min<int64_t>(std::min<int64_t>(ANSWER_PARTS, ANSWER_WORKGROUPS / std::max<int64_t>(n, 1)), C / ANSWER_PART_LEAST);
+    int64_t parts = std::min<int64_t>(std::min<int64_t>(ANSWER_PARTS, ANSWER_WORKGROUPS / std::max<int64_t>(n, 1)), (C + ANSWER_PART_LEAST - 1) / ANSWER_PART_LEAST);
     if (parts <= 1) { *chunk = C; return 1; }
     *chunk = (C + parts - 1) / parts;
     *chunk = (*chunk + 511) / 512 * 512;
@@ -810,7 +810,7 @@ extern "C" int capgnn_logprobs(int64_t n, int C, const void *Z, int64_t ldz, int
     w.sums = static_cast<float4 *>(ws);
     w.keys = reinterpret_cast<unsigned long long *>(static_cast<char *>(ws) + align_up(sizeof(float4) * n * w.parts, 256));
     // a wave alone walks rows of one tile (no barriers between waves), a workgroup of four longer ones
-    const bool wave = C <= 64 * ANSWER_VECTORS * (bf16 ? 8 : 4);
+    const bool wave = w.chunk <= 64 * ANSWER_VECTORS * (bf16 ? 8 : 4);
     const unsigned grid = static_cast<unsigned>(std::min<int64_t>(n * w.parts, 1 << 24));
     auto go = [&](auto kernel, int threads) { hipLaunchKernelGGL(kernel, dim3(grid), dim3(threads), 0, st, a, w); };
     if (bf16) {

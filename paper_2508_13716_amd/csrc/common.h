@@ -256,8 +256,8 @@ struct SgdList {
     int count = 0;
 };
 int launch_sgd(const SgdList &all, float lr, hipStream_t stream);
-// norm_dev[0] = the number of masked rows, at least 1; scratch: 512 doubles
-int launch_mask_count(int64_t n, const uint8_t *mask, float *norm_dev, double *scratch, hipStream_t stream);
+// the number of masked rows as the sum of counts[0 .. *n_counts), 64 at most (device)
+int launch_mask_counts(int64_t n, const uint8_t *mask, double *counts, int *n_counts, hipStream_t stream);
 // the loss of an epoch on labels or targets, with what else can be had on the way (see ops.hip)
 int loss_epoch(int64_t n, int C, const float *Z, int64_t ldz, const int32_t *labels, const uint8_t *targets, int64_t ldt,
                const uint8_t *mask, double loss_norm, float *loss_dev, void *dZ, int64_t lddz, int dz_dtype, float *copy, float *dbias,

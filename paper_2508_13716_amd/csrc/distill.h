@@ -16,11 +16,19 @@ struct DistillArgs {
     const uint8_t *mask;
     const int32_t *t_ids; const float *t_val; int64_t ldt; int k, rest;
     float weight;
-    float norm_val; const float *norm_dev;
+    float norm_val; const double *counts; int n_counts;       // the normaliser, or the parts (64 at most) of the number of masked rows
     double *part;                   // [gridDim.x]
     float *row_loss;
     char *dZ; int64_t lddz; int accumulate;
 };
+
+// by every wave for itself
+__device__ __forceinline__ float distill_norm(const DistillArgs &a) {
+    if (!a.counts) return a.norm_val;
+    const int lane = threadIdx.x & 63;
+    const double c = wave_all(lane < a.n_counts ? a.counts[lane] : 0.0, OpSum());
+    return c > 0.0 ? static_cast<float>(c) : 1.f;
+}
 
 constexpr float REST_LEAST = 9.5367431640625e-7f;       // 2^-20
 
@@ -271,7 +279,7 @@ __global__ __launch_bounds__(THREADS) __attribute__((amdgpu_waves_per_eu(4))) vo
     __shared__ float listed;
     const Seen seen{seen_bits, w.seen};
     const bool first_wave = threadIdx.x < 64;
-    const float norm = a.norm_dev ? a.norm_dev[0] : a.norm_val;
+    const float norm = distill_norm(a);
     const float scale = a.weight / norm * a.t.inv_T;
     double loss = 0.0;
     for (int64_t job = blockIdx.x; job < a.n * (PARTS ? w.parts : 1); job += gridDim.x) {
@@ -388,22 +396,25 @@ __global__ __launch_bounds__(THREADS) __attribute__((amdgpu_waves_per_eu(4))) vo
 }
 
 // ------------------------------------------------------------------ few classes
-// As answers_grad_narrow_kernel, with a second set of rows in LDS for the teacher's probabilities by class, -1 where a class is not listed, and
-// the entries beside them.  The lanes of a row share its entries; adding them up by class is one lane's, since a class may be listed again.
-// (Entries read where they are used, by one lane a row: 612000 x 47, k = 8, 278 us.)
+// As answers_grad_narrow_kernel, the teacher's entries beside the rows in LDS, shared by the lanes of a row; each entry looks for other
+// mentions of its class.  rest: the listed classes' logits are taken out of the row before it is summed.
+// (Entries read where they are used, by one lane a row: 612000 x 47, k = 8, 278 us; the teacher's probabilities by class in a second set
+// of rows, which leaves LDS for ten waves per compute unit: 170 us.)
 constexpr int NARROW_ENTRIES = 16;      // of a lane
+static inline size_t distill_narrow_lds(const NarrowShape &s, int k) { return s.lds_wave + static_cast<size_t>(s.rows) * k * 3 * sizeof(float); }
+
 template <bool BF16, bool DBF16, bool REST>
 __global__ __launch_bounds__(64 * NARROW_WAVES) __attribute__((amdgpu_waves_per_eu(4))) void distill_narrow_kernel(DistillArgs a, NarrowShape s) {
     extern __shared__ __align__(16) uint32_t seen_bits[];
     __shared__ double red[NARROW_WAVES];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, k = a.k;
-    float *tile = reinterpret_cast<float *>(reinterpret_cast<char *>(seen_bits) + wave * (2 * s.lds_wave + s.rows * k * 2 * sizeof(float)));
-    float *tile_q = tile + s.rows * s.pitch, *tile_w = tile_q + s.rows * s.pitch;
-    int32_t *tile_id = reinterpret_cast<int32_t *>(tile_w + s.rows * k);
+    float *tile = reinterpret_cast<float *>(reinterpret_cast<char *>(seen_bits) + wave * (s.lds_wave + s.rows * k * 3 * sizeof(float)));
+    float *tile_w = tile + s.rows * s.pitch, *tile_q = tile_w + s.rows * k;
+    int32_t *tile_id = reinterpret_cast<int32_t *>(tile_q + s.rows * k);
     const int G = 1 << s.lg, sub = lane & (G - 1), C = s.C, mine = lane >> s.lg;
-    float *z = tile + mine * s.pitch, *q = tile_q + mine * s.pitch, *w = tile_w + mine * k;
+    float *z = tile + mine * s.pitch, *w = tile_w + mine * k, *q = tile_q + mine * k;
     int32_t *id = tile_id + mine * k;
-    const float norm = a.norm_dev ? a.norm_dev[0] : a.norm_val;
+    const float norm = distill_norm(a);
     const float scale = a.weight / norm * a.t.inv_T;
     const int magic = (65536 + k - 1) / k, items = s.rows * k;
     const int64_t step = static_cast<int64_t>(gridDim.x) * NARROW_WAVES * s.rows;
@@ -415,38 +426,37 @@ __global__ __launch_bounds__(64 * NARROW_WAVES) __attribute__((amdgpu_waves_per_
     for (; row0 < a.n; row0 += step) {
         const int64_t row = row0 + mine;
         const bool in = row < a.n, on = in && (!a.mask || a.mask[row]);
-        int32_t c[NARROW_ENTRIES];
-        float v[NARROW_ENTRIES];
-        const int anew = thread_anew() & 63;
+        {
+            int32_t c[NARROW_ENTRIES];
+            float v[NARROW_ENTRIES];
+            const int anew = thread_anew() & 63;
 #pragma unroll
-        for (int i = 0; i < NARROW_ENTRIES; ++i) {
-            const int item = i * 64 + anew;
-            if (i * 64 >= items) continue;              // (the same for all lanes)
-            const int r = item * magic >> 16;
-            const bool there = item < items && row0 + r < a.n;
-            const int64_t at = there ? (row0 + r) * a.ldt + (item - r * k) : 0;
-            c[i] = there ? a.t_ids[at] : -1;
-            v[i] = there ? a.t_val[at] : -INFINITY;
+            for (int i = 0; i < NARROW_ENTRIES; ++i) {
+                const int item = i * 64 + anew;
+                if (i * 64 >= items) continue;              // (the same for all lanes)
+                const int r = item * magic >> 16;
+                const bool there = item < items && row0 + r < a.n;
+                const int64_t at = there ? (row0 + r) * a.ldt + (item - r * k) : 0;
+                c[i] = there ? a.t_ids[at] : -1;
+                v[i] = there ? a.t_val[at] : -INFINITY;
+            }
+            next.put(s, tile);
+#pragma unroll
+            for (int i = 0; i < NARROW_ENTRIES; ++i) {
+                const int item = i * 64 + anew;
+                if (i * 64 >= items) continue;
+                if (item < items) {
+                    tile_id[item] = c[i] >= 0 && c[i] < C && v[i] != -INFINITY ? c[i] : -1;
+                    tile_w[item] = v[i];
+                }
+            }
         }
-        next.put(s, tile);
-        for (int b = 0; b < s.each; ++b) q[sub + b * G] = -1.f;
         wave_sync();
         if (row0 + step < a.n) next.fetch(s, a.Z, a.ldz, a.n, row0 + step);
         float m = -INFINITY;
         for (int b = 0; b < s.each; b += NARROW_BATCH)
 #pragma unroll
             for (int i = 0; i < NARROW_BATCH; ++i) m = max_of(m, z[sub + (b + i) * G]);
-        for (int off = 1; off < G; off <<= 1) m = max_of(m, __shfl_xor(m, off));
-#pragma unroll
-        for (int i = 0; i < NARROW_ENTRIES; ++i) {
-            const int item = i * 64 + anew;
-            if (i * 64 >= items) continue;
-            if (item < items) {
-                tile_id[item] = c[i] >= 0 && c[i] < C && v[i] != -INFINITY ? c[i] : -1;
-                tile_w[item] = v[i];
-            }
-        }
-        wave_sync();
         float top = -INFINITY;
         int entries = 0;
         for (int i = sub; i < k; i += G)
@@ -455,48 +465,58 @@ __global__ __launch_bounds__(64 * NARROW_WAVES) __attribute__((amdgpu_waves_per_
                 ++entries;
             }
         for (int off = 1; off < G; off <<= 1) {
+            m = max_of(m, __shfl_xor(m, off));
             top = max_of(top, __shfl_xor(top, off));
             entries += __shfl_xor(entries, off);
         }
         double Q = 0.0;
+        float sum = 0.f;
         for (int i = sub; i < k; i += G)
             if (id[i] >= 0) {
-                const double p = REST ? exp(static_cast<double>(w[i])) : static_cast<double>(exp_difference(w[i], top, a.t));
-                Q += p;
-                w[i] = static_cast<float>(p);
-            }
-        for (int off = 1; off < G; off <<= 1) Q += __shfl_xor(Q, off);
-        const float one = REST ? 1.f : static_cast<float>(1.0 / Q);
-        wave_sync();
-        if (on && sub == 0)
-            for (int i = 0; i < k; ++i) {
-                const int j = id[i];
-                if (j < 0) continue;
-                const float had = q[j], p = w[i] * one;
-                if (had < 0.f) {
-                    q[j] = p;
+                if constexpr (REST) {
+                    const double p = exp(static_cast<double>(w[i]));
+                    Q += p;
+                    w[i] = static_cast<float>(p);
                 } else {
-                    q[j] = had + p;
-                    id[i] = -1;             // the first mention stands for it
+                    const float p = exp_difference(w[i], top, a.t);
+                    sum += p;
+                    w[i] = p;
                 }
             }
+        for (int off = 1; off < G; off <<= 1) {
+            if constexpr (REST) Q += __shfl_xor(Q, off);
+            else sum += __shfl_xor(sum, off);
+        }
+        const float one = REST ? 1.f : 1.f / sum;
         wave_sync();
         const float m0 = safe_max(m);
-        float others = 0.f, listed = 0.f;
+        float listed = 0.f;
+        for (int i = sub; i < k; i += G) {          // q: of the class in all, at its first mention; -1 elsewhere
+            const int c = id[i];
+            float p = 0.f;
+            bool first = c >= 0;
+            for (int b = 0; b < k; ++b)
+                if (id[b] == c) {
+                    first = first && b >= i;
+                    p += w[b];
+                }
+            q[i] = first ? p * one : -1.f;
+            if (REST && first) listed += exp2_raw(difference(z[c], m0, a.t) * a.t.L);
+        }
+        wave_sync();
+        for (int i = sub; i < k; i += G) {          // w: the class's logit from here on
+            if (q[i] == -1.f) continue;
+            w[i] = z[id[i]];
+            if constexpr (REST) z[id[i]] = -INFINITY;
+        }
+        wave_sync();
+        float others = 0.f;
         for (int b = 0; b < s.each; b += NARROW_BATCH) {
-            float x[NARROW_BATCH], y[NARROW_BATCH];
+            float x[NARROW_BATCH];
 #pragma unroll
-            for (int i = 0; i < NARROW_BATCH; ++i) {
-                x[i] = z[sub + (b + i) * G];
-                if constexpr (REST) y[i] = q[sub + (b + i) * G];
-            }
+            for (int i = 0; i < NARROW_BATCH; ++i) x[i] = z[sub + (b + i) * G];
 #pragma unroll
-            for (int i = 0; i < NARROW_BATCH; ++i) {
-                const float e = exp2_raw((x[i] - m0) * a.t.L);
-                const bool in_list = REST && !(y[i] == -1.f);
-                others += in_list ? 0.f : e;
-                if constexpr (REST) listed += in_list ? e : 0.f;
-            }
+            for (int i = 0; i < NARROW_BATCH; ++i) others += exp2_raw((x[i] - m0) * a.t.L);
         }
         for (int off = 1; off < G; off <<= 1) {
             others += __shfl_xor(others, off);
@@ -505,21 +525,39 @@ __global__ __launch_bounds__(64 * NARROW_WAVES) __attribute__((amdgpu_waves_per_
         const float S = others + listed;
         const bool live = on && entries > 0 && S != 0.f;
         const float ln_s = logf(S), inv_s = 1.f / S;
-        double r = REST ? 1.0 - Q : 0.0;
-        if (r < REST_LEAST) r = 0.0;
-        const float mass = static_cast<float>(REST ? Q + r : 1.0 + 0.0 * Q) * scale;
-        const float away = !REST || r == 0.0 ? mass : others == 0.f ? 0.f : static_cast<float>(Q + r - r * (static_cast<double>(S) / others)) * scale;
-        const float factor = away * inv_s;
-        double kl = 0.0;
-        if (live) {
-            for (int i = sub; i < k; i += G) {
-                const int j = id[i];
-                if (j < 0) continue;
-                const float p = q[j], d = z[j] - m0;
-                if (p != 0.f) kl += static_cast<double>(fmaf(-p * d, a.t.inv_T, p * (logf(p) + ln_s)));      // (q d before 1/T, as above)
-                z[j] = fmaf(exp_scaled(difference(z[j], m0, a.t), a.t) * inv_s, mass, -p * scale);
+        float mass = scale, away = scale;
+        double r = 0.0;
+        if constexpr (REST) {
+            r = 1.0 - Q;
+            if (r < REST_LEAST) r = 0.0;
+            mass = static_cast<float>(Q + r) * scale;
+            // (others = 0: every class that is not listed has p = 0)
+            away = r == 0.0 ? mass : others == 0.f ? 0.f : static_cast<float>(Q + r - r * (static_cast<double>(S) / others)) * scale;
+        } else {
+            mass = away = (1.f + 0.f * sum) * scale;         // (a NaN among the teacher's values reaches every class)
+        }
+        if (a.dZ) {
+            const float none = a.accumulate ? -0.f : 0.f, factor = away * inv_s;       // (adding -0 leaves everything as it is)
+            for (int b = 0; b < s.each; b += NARROW_BATCH) {
+                float x[NARROW_BATCH];
+#pragma unroll
+                for (int i = 0; i < NARROW_BATCH; ++i) x[i] = z[sub + (b + i) * G];
+#pragma unroll
+                for (int i = 0; i < NARROW_BATCH; ++i) {
+                    const float g = exp_scaled<!DBF16>(difference(x[i], m0, a.t), a.t) * factor;
+                    if (sub + (b + i) * G < C) z[sub + (b + i) * G] = live ? g : none;
+                }
             }
         }
+        wave_sync();
+        double kl = 0.0;
+        if (live)
+            for (int i = sub; i < k; i += G) {
+                const float p = q[i], d = w[i] - m0;
+                if (p == -1.f) continue;
+                if (p != 0.f) kl += static_cast<double>(fmaf(-p * d, a.t.inv_T, p * (logf(p) + ln_s)));      // (q d before 1/T, as above)
+                z[id[i]] = fmaf(exp_scaled(difference(w[i], m0, a.t), a.t) * inv_s, mass, -p * scale);
+            }
         for (int off = 1; off < G; off <<= 1) kl += __shfl_xor(kl, off);
         if (sub == 0) {
             if (REST && live && r > 0.0) kl += r * (log(r) - (log(static_cast<double>(others)) - log(static_cast<double>(S))));
@@ -527,24 +565,7 @@ __global__ __launch_bounds__(64 * NARROW_WAVES) __attribute__((amdgpu_waves_per_
             if (in && a.row_loss) a.row_loss[row] = static_cast<float>(kl);
         }
         wave_sync();
-        if (a.dZ) {
-            const float none = a.accumulate ? -0.f : 0.f;       // (adding -0 leaves everything as it is)
-            for (int b = 0; b < s.each; b += NARROW_BATCH) {
-                float x[NARROW_BATCH], y[NARROW_BATCH];
-#pragma unroll
-                for (int i = 0; i < NARROW_BATCH; ++i) {
-                    x[i] = z[sub + (b + i) * G];
-                    y[i] = q[sub + (b + i) * G];
-                }
-#pragma unroll
-                for (int i = 0; i < NARROW_BATCH; ++i) {
-                    const float g = exp_scaled<!DBF16>(difference(x[i], m0, a.t), a.t) * factor;
-                    if ((!live || y[i] == -1.f) && sub + (b + i) * G < C) z[sub + (b + i) * G] = live ? g : none;
-                }
-            }
-            wave_sync();
-            narrow_store<BF16, DBF16>(s, tile, a.dZ, a.lddz, a.n, row0, a.accumulate);
-        }
+        if (a.dZ) narrow_store<BF16, DBF16>(s, tile, a.dZ, a.lddz, a.n, row0, a.accumulate);
         wave_sync();
     }
     loss = wave_all(loss, OpSum());
@@ -563,7 +584,7 @@ void launch_distill(const DistillArgs &a, DistillParts w, int *groups, hipStream
     constexpr int V = Raw<BF16>::V;
     const NarrowShape s = narrow_shape(a.C < NARROW_C ? a.C : NARROW_C, BF16 ? CAPGNN_BF16 : CAPGNN_F32);
     if (a.C <= NARROW_C && a.k <= NARROW_ENTRIES << s.lg) {
-        const size_t lds = NARROW_WAVES * (2 * s.lds_wave + s.rows * a.k * 2 * sizeof(float));
+        const size_t lds = NARROW_WAVES * distill_narrow_lds(s, a.k);
         *groups = static_cast<int>(narrow_grid(s, a.n, lds));
         hipLaunchKernelGGL((distill_narrow_kernel<BF16, DBF16, REST>), dim3(*groups), dim3(64 * NARROW_WAVES), lds, st, a, s);
         return;

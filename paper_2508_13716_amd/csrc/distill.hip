@@ -6,16 +6,22 @@
 namespace capgnn {
 
 // loss = weight / norm * sum of part
-__global__ __launch_bounds__(256) void distill_final_kernel(int parts, const double *part, float weight, float norm_val, const float *norm_dev,
-                                                            float *loss_out) {
-    __shared__ double red[4];
+__global__ __launch_bounds__(1024) void distill_final_kernel(DistillArgs a, int parts, float *loss_out) {
+    __shared__ double red[16];
     double c = 0.0;
-    for (int b = threadIdx.x; b < parts; b += 256) c += part[b];
-    c = group_all<256>(c, red, OpSum());
-    if (threadIdx.x == 0) loss_out[0] = static_cast<float>(c * weight / (norm_dev ? norm_dev[0] : norm_val));
+    for (int b = threadIdx.x; b < parts; b += 8 * 1024) {       // (eight loads in flight)
+        double v[8];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) v[u] = b + u * 1024 < parts ? a.part[b + u * 1024] : 0.0;
+#pragma unroll
+        for (int u = 0; u < 8; ++u) c += v[u];
+    }
+    const float norm = distill_norm(a);
+    c = group_all<1024>(c, red, OpSum());
+    if (threadIdx.x == 0) loss_out[0] = static_cast<float>(c * a.weight / norm);
 }
 
-constexpr size_t DISTILL_HEADER = 8192;     // [0] the normaliser, [256 ..] counts of the mask
+constexpr size_t DISTILL_HEADER = 8192;     // [256 ..] counts of the mask
 
 // Few long rows are cut into parts, about a thousand workgroups in all and at least DISTILL_PART_LEAST classes each.
 constexpr int DISTILL_PART_LEAST = 2048, DISTILL_WORKGROUPS = 1024;
@@ -70,8 +76,8 @@ extern "C" int capgnn_distill(int64_t n, int C, const void *Z, int64_t ldz, int 
     if (loss_norm > 0.0) a.norm_val = static_cast<float>(loss_norm);
     else if (n == 0 || !mask) a.norm_val = static_cast<float>(std::max<int64_t>(n, 1));
     else {
-        CG_TRY(launch_mask_count(n, mask, reinterpret_cast<float *>(w), reinterpret_cast<double *>(w + 256), st));
-        a.norm_dev = reinterpret_cast<const float *>(w);
+        a.counts = reinterpret_cast<const double *>(w + 256);
+        CG_TRY(launch_mask_counts(n, mask, reinterpret_cast<double *>(w + 256), &a.n_counts, st));
     }
     DistillParts p{};
     p.parts = distill_parts(n, C, &p.chunk);
@@ -83,7 +89,7 @@ extern "C" int capgnn_distill(int64_t n, int C, const void *Z, int64_t ldz, int 
         const DistillLaunch run = rest ? distill_launch_rest(zb, db) : distill_launch_of<false>(zb, db);
         run(a, p, &groups, st);
     }
-    hipLaunchKernelGGL(distill_final_kernel, dim3(1), dim3(256), 0, st, groups, a.part, weight, a.norm_val, a.norm_dev, loss_dev);
+    hipLaunchKernelGGL(distill_final_kernel, dim3(1), dim3(1024), 0, st, a, groups, loss_dev);
     CG_HIP(hipGetLastError());
     return CAPGNN_OK;
 }

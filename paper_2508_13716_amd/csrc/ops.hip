@@ -843,14 +843,9 @@ static int loss_launch(LossArgs a, bool bce, double loss_norm, float times, floa
     return CAPGNN_OK;
 }
 
-int launch_mask_count(int64_t n, const uint8_t *mask, float *norm_dev, double *scratch, hipStream_t stream) {
-    if (n <= COUNT_SMALL_N) {
-        hipLaunchKernelGGL(count_small_kernel, dim3(1), dim3(1024), 0, stream, n, mask, 1.f, norm_dev);
-    } else {
-        const int parts = static_cast<int>(std::min<int64_t>((n + 4095) / 4096, LOSS_PARTS));
-        hipLaunchKernelGGL(count_mask_kernel, dim3(parts), dim3(1024), 0, stream, n, mask, scratch, static_cast<uint16_t *>(nullptr));
-        hipLaunchKernelGGL(count_final_kernel, dim3(1), dim3(LOSS_PARTS), 0, stream, parts, scratch, 1.f, norm_dev);
-    }
+int launch_mask_counts(int64_t n, const uint8_t *mask, double *counts, int *n_counts, hipStream_t stream) {
+    *n_counts = static_cast<int>(std::min<int64_t>((n + 4095) / 4096, 64));
+    hipLaunchKernelGGL(count_mask_kernel, dim3(*n_counts), dim3(1024), 0, stream, n, mask, counts, static_cast<uint16_t *>(nullptr));
     CG_HIP(hipGetLastError());
     return CAPGNN_OK;
 }
