@@ -438,3 +438,174 @@ def test_distill_without_rows_leaves_a_loss_of_zero():
     B.distill(0, 4, None, 4, B.F32, None, None, 2, 2, 0, 1.0, None, 0.0, 1.0, loss, None, None, 4, B.F32, 0, ws, ws.numel(), stream=stream())
     torch.cuda.synchronize()
     assert float(loss) == 0.0
+
+
+# ----------------------------------------------------------------------------- together, as they are used
+def chain_on_gpu(Zt, Zs, y, k, T, rest, mask, ws, out, st):
+    """a teacher's top classes, a student's loss on labels and, next to it, on the teacher: one gradient"""
+    n, C = Zs.shape
+    B.logprobs(n, C, Zt, C, B.F32, T, None, None, 0, 0, None, 0, None, None, k, out["top"], out["top_logp"], k, ws["lp"], ws["lp"].numel(), stream=st)
+    B.softmax_ce(n, C, Zs, C, y, mask, 0.0, out["ce"], out["dZ"], C, B.F32, ws["ce"], ws["ce"].numel(), stream=st)
+    B.distill(n, C, Zs, C, B.F32, out["top"], out["top_logp"], k, k, rest, T, mask, 0.0, 0.5 * T * T, out["kd"], out["row"], out["dZ"], C, B.F32, 1,
+              ws["kd"], ws["kd"].numel(), stream=st)
+    B.logprobs(n, C, Zs, C, B.F32, 1.0, mask, y, 1, 1, out["logp"], 1, out["ent"], out["stats"], 0, None, None, 0, ws["lp"], ws["lp"].numel(), stream=st)
+    B.logprobs_bwd(n, C, Zs, C, B.F32, 1.0, mask, out["stats"], out["ent"], y, 1, 1, out["g"], 1, out["h"], out["dZ2"], C, B.F32, stream=st)
+
+
+def chain_buffers(n, C, k):
+    import torch
+    f = lambda *s: torch.full(s, 55.0, device="cuda")
+    size = lambda b: torch.empty(max(b, 256), dtype=torch.uint8, device="cuda")
+    out = dict(top=torch.empty(n, k, dtype=torch.int32, device="cuda"), top_logp=f(n, k), ce=f(1), kd=f(1), row=f(n), dZ=f(n, C), logp=f(n, 1), ent=f(n),
+               stats=f(n, 2), g=torch.linspace(-1, 1, n, device="cuda").view(n, 1).contiguous(), h=torch.linspace(1, -2, n, device="cuda"), dZ2=f(n, C))
+    ws = dict(lp=size(B.logprobs_workspace_bytes(n, C, k)), ce=size(B.loss_workspace_bytes(n)), kd=size(B.distill_workspace_bytes(n, C)))
+    return out, ws
+
+
+CHAIN = [(700, 47, 8), (130, 1500, 20), (6, 30_011, 64), (260, 12_000, 33)]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("rest", [0, 1])
+@pytest.mark.parametrize("n,C,k", CHAIN)
+def test_teacher_to_student_chain_vs_oracle(n, C, k, rest):
+    import torch
+    rng = np.random.default_rng(n)
+    T = 2.0
+    Zt = to_dtype(rng.standard_normal((n, C)) * 2, "f32")
+    Zs = to_dtype(Zt * 0.7 + rng.standard_normal((n, C)), "f32")
+    y, mask = rng.integers(0, C, n).astype(np.int32), (rng.random(n) < 0.6).astype(np.uint8)
+    dev = lambda x, t: torch.from_numpy(np.ascontiguousarray(x, t)).cuda()
+    out, ws = chain_buffers(n, C, k)
+    chain_on_gpu(dev(Zt, np.float32), dev(Zs, np.float32), dev(y, np.int32), k, T, rest, dev(mask, np.uint8), ws, out, stream())
+    torch.cuda.synchronize()
+    t = orc.logprobs(Zt, np.zeros((n, 0)), k, T)
+    np.testing.assert_array_equal(out["top"].cpu().numpy(), t["top_ids"])
+    val = out["top_logp"].cpu().numpy()              # what the student is given
+    ce, dce = orc.softmax_ce(Zs, y, mask)
+    kd, row, dkd, ex = orc.distill(Zs, t["top_ids"], val, bool(rest), T, mask, 0.0, 0.5 * T * T)
+    row_tol, dz_tol = distill_tol(Zs, ex, row, dkd, T, C, k, 0.5 * T * T, "f32")
+    check("row", out["row"].cpu().numpy(), row, row_tol)
+    # softmax_ce's own gradient: a probability with the sum's error, expf and three roundings, twice for the sum of the two
+    p = np.exp(orc.row_softmax(Zs)[0])
+    check("dZ", out["dZ"].cpu().numpy(), dce + dkd, dz_tol + mask[:, None] * (p * 2 * sum_err(C) + 8 * EPS * (np.arange(C) == y[:, None])) / max(mask.sum(), 1) +
+          2 * EPS * np.abs(dce + dkd))
+    g, h = np.linspace(-1, 1, n), np.linspace(1, -2, n)
+    g, h = out["g"].cpu().numpy().astype(np.float64), out["h"].cpu().numpy().astype(np.float64)
+    ref = orc.logprobs(Zs, y[:, None], 0, 1.0, mask)
+    dref = orc.logprobs_bwd(Zs, y[:, None], g, h, 1.0, mask)
+    check("dZ2", out["dZ2"].cpu().numpy(), dref, bwd_tol(Zs, ref, dref, y[:, None], g, h, 1.0, C, "f32"))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("n,C,k", CHAIN)
+def test_chain_recorded_and_replayed_gives_the_eager_bits(n, C, k):
+    import torch
+    rng = np.random.default_rng(C)
+    st = torch.cuda.Stream()
+    y, mask = rng.integers(0, C, n).astype(np.int32), (rng.random(n) < 0.6).astype(np.uint8)
+    dev = lambda x: torch.from_numpy(np.ascontiguousarray(x)).cuda()
+    y, mask = dev(y), dev(mask)
+    Zt, Zs = torch.empty(n, C, device="cuda"), torch.empty(n, C, device="cuda")
+    out, ws = chain_buffers(n, C, k)
+    eager, ews = chain_buffers(n, C, k)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=st):
+        chain_on_gpu(Zt, Zs, y, k, 1.5, 1, mask, ws, out, torch.cuda.current_stream())
+    for replay in range(4):
+        Zt.copy_(dev((rng.standard_normal((n, C)) * 2).astype(np.float32)))
+        Zs.copy_(dev(rng.standard_normal((n, C)).astype(np.float32)))
+        chain_on_gpu(Zt, Zs, y, k, 1.5, 1, mask, ews, eager, torch.cuda.current_stream())
+        torch.cuda.synchronize()
+        for w in ws.values():
+            w.fill_(replay * 37 + 1)                 # a workspace's contents do not matter
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        for key in out:
+            a, b = out[key].cpu().numpy(), eager[key].cpu().numpy()
+            assert np.array_equal(a, b, equal_nan=True), (replay, key)
+
+
+@pytest.mark.gpu
+def test_two_streams_with_a_workspace_each():
+    import torch
+    n, C, k = 5, 60_001, 17
+    rng = np.random.default_rng(1)
+    sets = []
+    for i in range(2):
+        st = torch.cuda.Stream()
+        Zt, Zs = (torch.from_numpy(rng.standard_normal((n, C)).astype(np.float32)).cuda() for _ in range(2))
+        y = torch.from_numpy(rng.integers(0, C, n).astype(np.int32)).cuda()
+        sets.append((Zt, Zs, y, st, *chain_buffers(n, C, k)))
+    alone = []
+    for Zt, Zs, y, st, out, ws in sets:
+        o, w = chain_buffers(n, C, k)
+        chain_on_gpu(Zt, Zs, y, k, 1.0, 1, None, w, o, torch.cuda.current_stream())
+        alone.append(o)
+    torch.cuda.synchronize()
+    for _ in range(3):
+        for Zt, Zs, y, st, out, ws in sets:
+            chain_on_gpu(Zt, Zs, y, k, 1.0, 1, None, ws, out, st)
+    torch.cuda.synchronize()
+    for (_, _, _, _, out, _), o in zip(sets, alone):
+        for key in out:
+            assert torch.equal(out[key], o[key]), key
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("C", [40, 3000, 20_000])
+def test_rows_far_apart(C):
+    """row offsets beyond 2^31 elements and 2^32 bytes"""
+    import torch
+    n, ld, k = 3, (1 << 30) + 40_007, 5
+    rng = np.random.default_rng(C)
+    Z = to_dtype(rng.standard_normal((n, C)) * 2, "bf16")
+    big = torch.empty((n - 1) * ld + C, dtype=torch.bfloat16, device="cuda")
+    rows = torch.as_strided(big, (n, C), (ld, 1))
+    rows.copy_(torch.from_numpy(Z).to(torch.bfloat16).cuda())
+    ids = np.tile(np.array([[0, C - 1]], np.int32), (n, 1))
+    res = run_logprobs(rows, C, "bf16", 1.0, None, ids, k)
+    ref = orc.logprobs(Z, ids, k)
+    check_logprobs(res, ref, Z, C, 1.0)
+    tids, val = teacher_of(Z, 4, 0, 1.0, rng)
+    _, ref_row, dref, ex = orc.distill(Z, tids, val)
+    row_tol, dz_tol = distill_tol(Z, ex, ref_row, dref, 1.0, C, 4, 1.0, "bf16")
+    got = run_distill(rows, C, "bf16", "bf16", 1.0, None, tids, val, 0, 0.0, 1.0, 0, in_place=True)
+    check("row_loss", got[1], ref_row, row_tol)
+    check("dZ", got[2], dref, dz_tol)
+    rows.copy_(torch.from_numpy(Z).to(torch.bfloat16).cuda())
+    g, h = rng.standard_normal((n, 2)), rng.standard_normal(n)
+    g, h = to_dtype(g, "f32"), to_dtype(h, "f32")
+    dref = orc.logprobs_bwd(Z, ids, g, h)
+    got = run_bwd(rows, C, "bf16", "bf16", 1.0, None, ref, ids, g, h, 0, in_place=True)
+    check("dZ", got, dref, bwd_tol(Z, ref, dref, ids, g, h, 1.0, C, "bf16"))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("n,C", [(3, 11), (2, 700), (2, 9000)])
+def test_gradients_are_the_difference_quotients_of_the_kernels_own_values(n, C):
+    """a step of 2^-5 each way along random directions, values as double sums of the row losses / log-probabilities; a third derivative of at
+    most ~1 times step^2 / 6, and the float values' rounding over the step, bound the difference"""
+    import torch
+    rng = np.random.default_rng(C)
+    Z, D = rng.standard_normal((n, C)), rng.standard_normal((n, C))
+    D /= np.abs(D).max()
+    step = 2.0 ** -5
+    ids, val = teacher_of(Z, 3, 1, 1.0, rng)
+    given_ids, g, h = rng.integers(0, C, (n, 2)).astype(np.int32), rng.standard_normal((n, 2)), rng.standard_normal(n)
+
+    def values(x):
+        x = to_dtype(x, "f32")
+        _, row, dz = run_distill(device(x, "f32", C), C, "f32", "f32", 1.0, None, ids, val, 1, 1.0, 1.0, C)
+        r = run_logprobs(device(x, "f32", C), C, "f32", 1.0, None, given_ids, 0)
+        return row.astype(np.float64).sum(), (g * r["logp"]).sum() + (h * r["entropy"]).sum(), dz[:, :C], r
+
+    _, _, dz, r = values(Z)
+    dlp = run_bwd(device(to_dtype(Z, "f32"), "f32", C), C, "f32", "f32", 1.0, None, r, given_ids, g, h, C)[:, :C]
+    up, down = values(Z + step * D), values(Z - step * D)
+    for i, grad in ((0, dz), (1, dlp)):
+        quotient, slope = (up[i] - down[i]) / (2 * step), (grad.astype(np.float64) * D).sum()
+        weight = n * (2.0 + (np.abs(g).sum() + 12 * np.abs(h).sum() if i else 0.0))
+        assert abs(quotient - slope) <= weight * (step ** 2 + sum_err(C) * 20 / step), (quotient, slope)
