@@ -593,6 +593,20 @@ int capgnn_epoch_multilabel(const capgnn_graph *g, capgnn_cache *c, const capgnn
                             float *loss_out, capgnn_epoch_times *times,
                             void *ws, size_t ws_bytes, void *stream, void *side_stream);
 
+/* The same epoch for a student: the loss is capgnn_distill on a teacher's top classes (of every local vertex) instead of the cross-entropy
+ * on labels; loss_norm and mask as there.  Everything else as capgnn_epoch. */
+typedef struct {
+    const int32_t *ids;      /* device int32 [n_loc x ld]: the teacher's classes of every local vertex    */
+    const float *val;        /* device float [n_loc x ld]: their logits or log-probabilities              */
+    int64_t ld;
+    int k, rest;
+    float temperature, weight;
+} capgnn_teacher;
+int capgnn_epoch_distill(const capgnn_graph *g, capgnn_cache *c, const capgnn_layer *layers, int L, void *X0, int64_t ld0,
+                         const capgnn_teacher *teacher, const uint8_t *mask, double loss_norm, float *logits, float **dW,
+                         float **dW_self, float **dbias, float lr, float *loss_out, capgnn_epoch_times *times, void *ws,
+                         size_t ws_bytes, void *stream, void *side_stream);
+
 /* Where capgnn_epoch leaves the output of hidden layer l (0 <= l < L-1) inside ws: *ptr = device
  * address of H_l ([n_loc x *ld] of the layers' dtype), valid until ws is reused.  Same arguments as
  * capgnn_epoch_workspace_bytes; no GPU work.  For callers that want the embeddings, and for tests. */

@@ -524,7 +524,7 @@ def epoch(g: Graph, layers: List[Layer], X0_local, halo_tables: Sequence[Optiona
 
     halo_tables[l] is the logical [n_halo, f_in(l)] cache table feeding layer l (None when the
     partition has no halo).  loss_kind "ce": labels are class indices (single-label tasks); "bce": labels is the
-    [n_loc, classes] 0/1 target matrix (multi-label tasks).  Returns dict(loss, logits, dW, dW_self, db, dX_halo,
+    [n_loc, classes] 0/1 target matrix (multi-label tasks); "distill": labels is distill's keyword arguments.  Returns dict(loss, logits, dW, dW_self, db, dX_halo,
     new_W ...) and the intermediate quantities of every layer l: X[l] its input [local rows; halo rows], M[l] the
     aggregated input, hidden[l] = Z_l, dH[l] the loss gradient with respect to its output, dZ[l] = dH[l] (.) sigma'(Z_l).
     """
@@ -543,7 +543,10 @@ def epoch(g: Graph, layers: List[Layer], X0_local, halo_tables: Sequence[Optiona
         Xs.append(X)
         saves.append(sv)
     logits = H
-    loss, dH = (softmax_ce if loss_kind == "ce" else sigmoid_bce)(logits, labels, mask, loss_norm)
+    if loss_kind == "distill":
+        loss, _, dH, _ = distill(logits, mask=mask, norm=loss_norm, **labels)
+    else:
+        loss, dH = (softmax_ce if loss_kind == "ce" else sigmoid_bce)(logits, labels, mask, loss_norm)
     res = {"loss": loss, "logits": logits, "dW": [None] * len(layers), "dW_self": [None] * len(layers),
            "db": [None] * len(layers), "dX_halo": [None] * len(layers), "hidden": [s["Z"] for s in saves],
            "X": Xs, "M": [s["M"] for s in saves], "dH": [None] * len(layers), "dZ": [None] * len(layers)}

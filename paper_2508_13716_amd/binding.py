@@ -41,6 +41,11 @@ class Layer(C.Structure):
                 ("bias", C.c_void_p)]
 
 
+class Teacher(C.Structure):
+    _fields_ = [("ids", C.c_void_p), ("val", C.c_void_p), ("ld", C.c_int64), ("k", C.c_int), ("rest", C.c_int),
+                ("temperature", C.c_float), ("weight", C.c_float)]
+
+
 class RapaDevice(C.Structure):
     _fields_ = [("t_spmm", C.c_double), ("t_mm", C.c_double), ("f_h2d", C.c_double), ("f_d2h", C.c_double),
                 ("f_idt", C.c_double), ("mem_bytes", C.c_double)]
@@ -134,6 +139,9 @@ SIGNATURES = {
     "capgnn_epoch_multilabel": (_i32, [_vp, _vp, C.POINTER(Layer), _i32, _vp, _i64, _vp, _i64, _vp, C.c_double, _vp,
                                        C.POINTER(_vp), C.POINTER(_vp), C.POINTER(_vp), C.c_float, C.POINTER(C.c_float),
                                        C.POINTER(EpochTimes), _vp, _sz, _vp, _vp]),
+    "capgnn_epoch_distill": (_i32, [_vp, _vp, C.POINTER(Layer), _i32, _vp, _i64, C.POINTER(Teacher), _vp, C.c_double, _vp,
+                                    C.POINTER(_vp), C.POINTER(_vp), C.POINTER(_vp), C.c_float, C.POINTER(C.c_float),
+                                    C.POINTER(EpochTimes), _vp, _sz, _vp, _vp]),
     "capgnn_epoch_workspace_bytes": (_sz, [_vp, _vp, C.POINTER(Layer), _i32]),
     "capgnn_epoch_activation": (_i32, [_vp, _vp, C.POINTER(Layer), _i32, _i32, _vp, C.POINTER(_vp), C.POINTER(_i64)]),
     "capgnn_epoch": (_i32, [_vp, _vp, C.POINTER(Layer), _i32, _vp, _i64, _vp, _vp, C.c_double, _vp, C.POINTER(_vp),
@@ -546,6 +554,11 @@ def distill(n: int, n_classes: int, Z, ldz: int, z_dtype: int, teacher_ids, teac
                                 _stream(stream)))
 
 
+def make_teacher(ids, val, ld: int, k: int, rest: int, temperature: float, weight: float) -> Teacher:
+    """What a student's epoch learns from: the teacher's k classes of every local vertex (keep the tensors alive)."""
+    return Teacher(_p(ids), _p(val), ld, k, rest, temperature, weight)
+
+
 def gin_operator(n_loc: int, n_halo: int, rowptr, col, eps: float):
     """(rowptr, col, edge_val) of the GIN aggregation operator: unit entries plus a diagonal of 1 + eps."""
     rowptr = np.ascontiguousarray(rowptr, np.int64)
@@ -607,8 +620,10 @@ class EpochGraph:
 
 def epoch(g: Graph, c: Optional[Cache], layers: List[Layer], X0, ld0: int, labels, mask, loss_norm: float, logits,
           dW: Sequence, dW_self: Optional[Sequence], dbias: Sequence, lr: float, ws, ws_bytes: int, stream=None,
-          side_stream=None, want_loss: bool = True, want_times: bool = False, targets=None, ldt: int = 0):
-    """One epoch; with `targets` (device uint8 [n_loc x ldt]) the multi-label entry point runs and `labels` is unused."""
+          side_stream=None, want_loss: bool = True, want_times: bool = False, targets=None, ldt: int = 0,
+          teacher: Optional[Teacher] = None):
+    """One epoch; with `targets` (device uint8 [n_loc x ldt]) the multi-label entry point runs, with `teacher` (make_teacher) the student's, and
+    `labels` is unused."""
     L = len(layers)
     arr = (Layer * L)(*layers)
     pw = (C.c_void_p * L)(*[_p(t) for t in dW])
@@ -618,7 +633,9 @@ def epoch(g: Graph, c: Optional[Cache], layers: List[Layer], X0, ld0: int, label
     times = EpochTimes() if want_times else None
     tail = (_p(mask), loss_norm, _p(logits), pw, ps, pb, lr, C.byref(loss) if want_loss else None,
             C.byref(times) if times is not None else None, _p(ws), ws_bytes, _stream(stream), _stream(side_stream))
-    if targets is not None:
+    if teacher is not None:
+        _check(lib().capgnn_epoch_distill(g.h, c.h if c is not None else None, arr, L, _p(X0), ld0, C.byref(teacher), *tail))
+    elif targets is not None:
         _check(lib().capgnn_epoch_multilabel(g.h, c.h if c is not None else None, arr, L, _p(X0), ld0, _p(targets), ldt, *tail))
     else:
         _check(lib().capgnn_epoch(g.h, c.h if c is not None else None, arr, L, _p(X0), ld0, _p(labels), *tail))

@@ -258,6 +258,10 @@ struct SgdList {
 int launch_sgd(const SgdList &all, float lr, hipStream_t stream);
 // the number of masked rows as the sum of counts[0 .. *n_counts), 64 at most (device)
 int launch_mask_counts(int64_t n, const uint8_t *mask, double *counts, int *n_counts, hipStream_t stream);
+// what capgnn_distill checks of its arguments, the workspace apart
+int distill_check(int64_t n, int C, const void *Z, int64_t ldz, int z_dtype, const int32_t *teacher_ids, const float *teacher_val, int64_t ldt,
+                  int k, int rest, float temperature, double loss_norm, float weight, const float *loss_dev, const void *dZ, int64_t lddz,
+                  int dz_dtype, int accumulate);
 // the loss of an epoch on labels or targets, with what else can be had on the way (see ops.hip)
 int loss_epoch(int64_t n, int C, const float *Z, int64_t ldz, const int32_t *labels, const uint8_t *targets, int64_t ldt,
                const uint8_t *mask, double loss_norm, float *loss_dev, void *dZ, int64_t lddz, int dz_dtype, float *copy, float *dbias,

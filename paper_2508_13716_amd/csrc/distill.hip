@@ -44,10 +44,9 @@ extern "C" size_t capgnn_distill_workspace_bytes(int64_t n, int C) {
     return DISTILL_HEADER + sizeof(double) * DISTILL_GROUPS + (parts > 1 ? align_up((sizeof(float2) * parts + sizeof(float) * CAPGNN_GIVEN_MAX) * static_cast<size_t>(n), 256) : 0);
 }
 
-extern "C" int capgnn_distill(int64_t n, int C, const void *Z, int64_t ldz, int z_dtype, const int32_t *teacher_ids,
-                              const float *teacher_val, int64_t ldt, int k, int rest, float temperature, const uint8_t *mask,
-                              double loss_norm, float weight, float *loss_dev, float *row_loss, void *dZ, int64_t lddz, int dz_dtype,
-                              int accumulate, void *ws, size_t ws_bytes, void *stream) {
+int capgnn::distill_check(int64_t n, int C, const void *Z, int64_t ldz, int z_dtype, const int32_t *teacher_ids, const float *teacher_val,
+                          int64_t ldt, int k, int rest, float temperature, double loss_norm, float weight, const float *loss_dev,
+                          const void *dZ, int64_t lddz, int dz_dtype, int accumulate) {
     if ((z_dtype != CAPGNN_F32 && z_dtype != CAPGNN_BF16) || (dz_dtype != CAPGNN_F32 && dz_dtype != CAPGNN_BF16))
         CG_FAIL(CAPGNN_EINVAL, "distill: unknown z_dtype or dz_dtype");
     if (n < 0 || C <= 0) CG_FAIL(CAPGNN_EINVAL, "distill: bad sizes");
@@ -62,6 +61,15 @@ extern "C" int capgnn_distill(int64_t n, int C, const void *Z, int64_t ldz, int 
     if (!element_aligned(Z, z_dtype) || (dZ && !element_aligned(dZ, dz_dtype))) CG_FAIL(CAPGNN_EINVAL, "distill: Z or dZ is not aligned to its elements");
     if (n > 0 && dZ == Z && (lddz != ldz || dz_dtype != z_dtype || accumulate))
         CG_FAIL(CAPGNN_EINVAL, "distill: dZ may be Z only with the same type and pitch, and not to accumulate");
+    return CAPGNN_OK;
+}
+
+extern "C" int capgnn_distill(int64_t n, int C, const void *Z, int64_t ldz, int z_dtype, const int32_t *teacher_ids,
+                              const float *teacher_val, int64_t ldt, int k, int rest, float temperature, const uint8_t *mask,
+                              double loss_norm, float weight, float *loss_dev, float *row_loss, void *dZ, int64_t lddz, int dz_dtype,
+                              int accumulate, void *ws, size_t ws_bytes, void *stream) {
+    CG_TRY(distill_check(n, C, Z, ldz, z_dtype, teacher_ids, teacher_val, ldt, k, rest, temperature, loss_norm, weight, loss_dev, dZ, lddz,
+                         dz_dtype, accumulate));
     const size_t need = capgnn_distill_workspace_bytes(n, C);
     if (!ws || ws_bytes < need) CG_FAIL(CAPGNN_ENOMEM, "distill: workspace of %zu bytes needed, %zu given", need, ws ? ws_bytes : size_t(0));
     if (reinterpret_cast<uintptr_t>(ws) & 255u) CG_FAIL(CAPGNN_EINVAL, "distill: workspace must be 256-byte aligned");

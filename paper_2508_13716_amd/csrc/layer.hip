@@ -409,7 +409,7 @@ static int plan_epoch(const capgnn_graph *g, const capgnn_cache *c, const capgnn
     p->grad_off[1] = take(static_cast<size_t>(g->n_loc) * max_w * sizeof(float));
     p->layer_ws_bytes = lws;
     p->layer_ws_off = take(lws);
-    p->loss_ws_off = take(loss_epoch_ws_bytes(g->n_loc, layers[L - 1].f_out));
+    p->loss_ws_off = take(std::max(loss_epoch_ws_bytes(g->n_loc, layers[L - 1].f_out), capgnn_distill_workspace_bytes(g->n_loc, layers[L - 1].f_out)));
     p->loss_val_off = take(256);
     // few bytes of parts: their sums wait for the epoch's last launch, so each layer keeps its own
     p->later_off.assign(L, 0); p->later_bytes.assign(L, 0);
@@ -518,7 +518,6 @@ extern "C" int capgnn_epoch_activation(const capgnn_graph *g, const capgnn_cache
     return CAPGNN_OK;
 }
 
-// labels (class indices, softmax cross-entropy) or targets (0/1 matrix, binary cross-entropy): exactly one is given
 // The events that order the two streams of an epoch.  An eager epoch uses the cache's own; an epoch that is being
 // recorded into a HIP graph brings a set of its own (an event last recorded during a capture must not be waited for
 // outside it) and sets `capture`.
@@ -569,13 +568,14 @@ struct LossLine {
     float host() const { return *static_cast<const volatile float *>(g->loss_host + i * capgnn_graph::LOSS_STRIDE); }
 };
 
+// labels (class indices, softmax cross-entropy), targets (0/1 matrix, binary cross-entropy) or a teacher: exactly one is given
 static int epoch_impl(const capgnn_graph *g, capgnn_cache *c, const capgnn_layer *layers, int L, void *X0,
                       int64_t ld0, const int32_t *labels, const uint8_t *targets, int64_t ldt, const uint8_t *mask,
                       double loss_norm, float *logits, float **dW, float **dW_self, float **dbias, float lr, float *loss_out,
                       capgnn_epoch_times *times, void *ws, size_t ws_bytes, void *stream, void *side_stream,
-                      const EpochEvents *own_events = nullptr, float *loss_copy = nullptr) {
+                      const EpochEvents *own_events = nullptr, float *loss_copy = nullptr, const capgnn_teacher *teacher = nullptr) {
     CG_TRY(check_epoch_args(g, c, layers, L));
-    if (!X0 || (!labels && !targets) || !dW || !dbias) CG_FAIL(CAPGNN_EINVAL, "epoch: NULL argument");
+    if (!X0 || (!labels && !targets && !teacher) || !dW || !dbias) CG_FAIL(CAPGNN_EINVAL, "epoch: NULL argument");
     if (targets && ldt < layers[L - 1].f_out) CG_FAIL(CAPGNN_EINVAL, "epoch: ldt smaller than the number of classes");
     if (ld0 < layers[0].f_in) CG_FAIL(CAPGNN_EINVAL, "epoch: ld0 smaller than the input width");
     const int dt = layers[0].dtype, es = elem_bytes(dt);
@@ -591,6 +591,9 @@ static int epoch_impl(const capgnn_graph *g, capgnn_cache *c, const capgnn_layer
     const int C = layers[L - 1].f_out;
     float *Z = reinterpret_cast<float *>(w + p.logits_off);   // padded pitch keeps the vector paths usable
     const int64_t ldz = p.ldz;
+    if (teacher)
+        CG_TRY(distill_check(g->n_loc, C, Z, ldz, CAPGNN_F32, teacher->ids, teacher->val, teacher->ld, teacher->k, teacher->rest,
+                             teacher->temperature, loss_norm, teacher->weight, Z, nullptr, 0, CAPGNN_F32, 0));
     void *staging = (c && c->miss_mode != CAPGNN_MISS_ZEROCOPY) ? w + p.staging_off : nullptr;
     g_rec.reset(times != nullptr);
     hipEvent_t ev_t0 = nullptr, ev_t1 = nullptr;
@@ -710,19 +713,27 @@ static int epoch_impl(const capgnn_graph *g, capgnn_cache *c, const capgnn_layer
         void *dz = dt == CAPGNN_BF16 ? static_cast<void *>(w + p.dz32_off) : static_cast<void *>(w + p.grad_off[cur]);
         const int64_t lddz = dt == CAPGNN_BF16 ? ldz : p.ld_grad;
         const int dzt = dt == CAPGNN_BF16 ? CAPGNN_F32 : dt;
-        // the kernel reads every logit anyway: it also writes the caller's dense copy, sums the columns of dZ for the last bias
-        // and scales the rows of dZ when the last layer's transposed aggregation gathers them
-        const bool linear = layers[L - 1].act == CAPGNN_ACT_NONE && g->n_loc > 0;
-        fuse.ready = linear;
-        fuse.dbias_done = linear && dbias[L - 1] && loss_sums_columns(C);
-        const bool scale = linear && scaled_dz(g, &layers[L - 1], p.order[L - 1]);
-        if (scale && dbias[L - 1] && !fuse.dbias_done) fuse.ready = false;       // the pass that sums the columns scales the rows
-        // rows outside the loss have no gradient: the aggregation that gathers dZ itself need not read them
-        const bool skip = mask && dzt == CAPGNN_F32 && p.order[L - 1] == CAPGNN_XFORM_FIRST && spmm_uses_live(g->bwd, C, lddz);
-        CG_TRY(loss_epoch(g->n_loc, C, Z, ldz, labels, targets, ldt, mask, loss_norm, loss_dev, dz, lddz, dzt, logits,
-                          fuse.dbias_done ? dbias[L - 1] : nullptr, scale && fuse.ready ? g->bwd.in_scale : nullptr,
-                          skip ? &fuse.live : nullptr, w + p.loss_ws_off,
-                          loss_epoch_ws_bytes(g->n_loc, C), st, later));
+        if (teacher) {          // the layer's backward pass masks, sums and scales the gradient itself
+            CG_TRY(capgnn_distill(g->n_loc, C, Z, ldz, CAPGNN_F32, teacher->ids, teacher->val, teacher->ld, teacher->k, teacher->rest,
+                                  teacher->temperature, mask, loss_norm, teacher->weight, loss_dev, nullptr, dz, lddz, dzt, 0,
+                                  w + p.loss_ws_off, capgnn_distill_workspace_bytes(g->n_loc, C), st));
+            if (logits && g->n_loc > 0)
+                CG_HIP(hipMemcpy2DAsync(logits, C * sizeof(float), Z, ldz * sizeof(float), C * sizeof(float), g->n_loc, hipMemcpyDeviceToDevice, st));
+        } else {
+            // the kernel reads every logit anyway: it also writes the caller's dense copy, sums the columns of dZ for the last bias
+            // and scales the rows of dZ when the last layer's transposed aggregation gathers them
+            const bool linear = layers[L - 1].act == CAPGNN_ACT_NONE && g->n_loc > 0;
+            fuse.ready = linear;
+            fuse.dbias_done = linear && dbias[L - 1] && loss_sums_columns(C);
+            const bool scale = linear && scaled_dz(g, &layers[L - 1], p.order[L - 1]);
+            if (scale && dbias[L - 1] && !fuse.dbias_done) fuse.ready = false;       // the pass that sums the columns scales the rows
+            // rows outside the loss have no gradient: the aggregation that gathers dZ itself need not read them
+            const bool skip = mask && dzt == CAPGNN_F32 && p.order[L - 1] == CAPGNN_XFORM_FIRST && spmm_uses_live(g->bwd, C, lddz);
+            CG_TRY(loss_epoch(g->n_loc, C, Z, ldz, labels, targets, ldt, mask, loss_norm, loss_dev, dz, lddz, dzt, logits,
+                              fuse.dbias_done ? dbias[L - 1] : nullptr, scale && fuse.ready ? g->bwd.in_scale : nullptr,
+                              skip ? &fuse.live : nullptr, w + p.loss_ws_off,
+                              loss_epoch_ws_bytes(g->n_loc, C), st, later));
+        }
         if (finish.count && loss_out && line.take()) loss_copy = line.dev();      // (an epoch with a copy on the device asks for none on the host)
         if (finish.count) finish.task[0].out2 = loss_copy;       // (the first task is the loss)
     }
@@ -819,6 +830,15 @@ extern "C" int capgnn_epoch_multilabel(const capgnn_graph *g, capgnn_cache *c, c
     if (!targets) CG_FAIL(CAPGNN_EINVAL, "epoch_multilabel: targets is NULL");
     return epoch_impl(g, c, layers, L, X0, ld0, nullptr, targets, ldt, mask, loss_norm, logits, dW, dW_self, dbias, lr,
                       loss_out, times, ws, ws_bytes, stream, side_stream);
+}
+
+extern "C" int capgnn_epoch_distill(const capgnn_graph *g, capgnn_cache *c, const capgnn_layer *layers, int L, void *X0, int64_t ld0,
+                                    const capgnn_teacher *teacher, const uint8_t *mask, double loss_norm, float *logits, float **dW,
+                                    float **dW_self, float **dbias, float lr, float *loss_out, capgnn_epoch_times *times, void *ws,
+                                    size_t ws_bytes, void *stream, void *side_stream) {
+    if (!teacher) CG_FAIL(CAPGNN_EINVAL, "epoch_distill: teacher is NULL");
+    return epoch_impl(g, c, layers, L, X0, ld0, nullptr, nullptr, 0, mask, loss_norm, logits, dW, dW_self, dbias, lr, loss_out, times, ws,
+                      ws_bytes, stream, side_stream, nullptr, nullptr, teacher);
 }
 
 // ---- the epoch as a HIP graph: one launch per epoch instead of one per kernel

@@ -166,12 +166,12 @@ class DeviceProblem:
     def resolved_orders(self) -> List[int]:
         return [B.layer_order(self.graph, l, i > 0) for i, l in enumerate(self.layers)]
 
-    def run_epoch(self, lr: float = 0.0, want_loss: bool = True, want_times: bool = False, mask=True):
+    def run_epoch(self, lr: float = 0.0, want_loss: bool = True, want_times: bool = False, mask=True, teacher=None):
         return B.epoch(self.graph, self.cache, self.layers, self.X0, self.ld0, self.labels,
                        self.mask if mask else None, 0.0, self.logits, self.dW,
                        self.dW_self if any(t is not None for t in self.dW_self) else None, self.dbias, lr,
                        self.ws, self.ws_bytes, self.stream, self.side, want_loss=want_loss, want_times=want_times,
-                       targets=self.targets, ldt=0 if self.targets is None else self.targets.shape[1])
+                       targets=self.targets, ldt=0 if self.targets is None else self.targets.shape[1], teacher=teacher)
 
     def capture_epoch(self, lr: float = 0.0, mask=True, two_streams: bool = False):
         """The epoch as a HIP graph on this problem's buffers; returns (graph, device float the replays write the loss to).

@@ -1,0 +1,90 @@
+"""capgnn_epoch_distill: a student's epoch on a teacher's top classes, against the oracle's epoch and against its parts called one by one."""
+import numpy as np
+import pytest
+
+from paper_2508_13716_amd import binding as B
+from paper_2508_13716_amd import synth
+
+
+def config(kind, dtype, dims, seed=3):
+    return synth.Config(f"student-{kind}-{dtype}", kind, 2500, 2000, 30_000, dims, dtype, 0.5, max_deg=300, seed=synth.BASE_SEED * 10 + seed)
+
+
+def teacher_for(prob, k, T, rest, seed):
+    """a teacher's answers over the local vertices: noise around a preferred class, its k best"""
+    from oracle import oracle as orc
+    rng = np.random.default_rng(seed)
+    n, C = prob.part.n_loc, prob.cfg.dims[-1]
+    z = rng.standard_normal((n, C)) * 1.5
+    z[np.arange(n), prob.labels] += 3.0
+    r = orc.logprobs(z, np.zeros((n, 0)), k, T)
+    return r["top_ids"].astype(np.int32), r["top_logp"].astype(np.float32)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("kind,dtype,dims", [("gcn", "f32", [96, 64, 24]), ("sage", "f32", [40, 32, 32, 300]), ("gcn", "bf16", [64, 64, 47]),
+                                             ("sage", "bf16", [64, 32, 8])])
+@pytest.mark.parametrize("rest", [0, 1])
+def test_epoch_distill_vs_oracle(orc, kind, dtype, dims, rest):
+    import torch
+    from paper_2508_13716_amd import harness as H
+    from tests import oracle_side as O
+    from tests.gpu_compare import TOL, compare_epoch
+    env = dict(torch=torch, B=B, H=H, O=O, orc=orc)
+    T, k = 2.0, min(8, dims[-1])
+    prob = H.make_problem(config(kind, dtype, dims), mask_frac=0.5)
+    ids, val = teacher_for(prob, k, T, rest, 1)
+    g, layers = O.oracle_graph(prob.part, kind, 0.0), O.oracle_layers(prob)
+    ref = orc.epoch(g, layers, O.widen(prob.X0), [O.widen(t) for t in prob.tables],
+                    dict(t_ids=ids, t_val=val, rest=bool(rest), temperature=T, weight=T * T), prob.mask, 0.0, 0.0, loss_kind="distill")
+    idd, vd = torch.from_numpy(ids).cuda(), torch.from_numpy(val).cuda()
+    for orders in (None, [B.AGG_FIRST] * (len(dims) - 1), [B.XFORM_FIRST] * (len(dims) - 1)):
+        dp = H.DeviceProblem(prob, orders=orders)
+        teacher = B.make_teacher(idd, vd, k, k, rest, T, T * T)
+        for rep in range(2):
+            loss, times = dp.run_epoch(teacher=teacher, want_times=rep == 1)
+            compare_epoch(env, prob, dp, ref, loss, TOL[dtype], f"{prob.cfg.name} rest={rest} orders={orders} rep={rep}")
+        dp.close()
+
+
+@pytest.mark.gpu
+def test_epoch_distill_steps_the_weights_and_labels_epochs_keep_their_bits(orc):
+    import torch
+    from paper_2508_13716_amd import harness as H
+    prob = H.make_problem(config("gcn", "f32", [48, 32, 12], 5), mask_frac=0.7)
+    dp = H.DeviceProblem(prob)
+    loss0, _ = dp.run_epoch()
+    before = dp.results()
+    ids, val = teacher_for(prob, 4, 1.0, 0, 2)
+    idd, vd = torch.from_numpy(ids).cuda(), torch.from_numpy(val).cuda()
+    teacher = B.make_teacher(idd, vd, 4, 4, 0, 1.0, 1.0)
+    W = [w.clone() for w in dp.W]
+    dp.run_epoch(teacher=teacher, lr=0.0)
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(W, dp.W))
+    loss1, _ = dp.run_epoch()                       # an epoch on labels, before and after a student's on the same workspace
+    after = dp.results()
+    assert loss0 == loss1 and all(np.array_equal(a, b) for a, b in zip(before["dW"], after["dW"]))
+    dp.run_epoch(teacher=teacher, lr=0.25)
+    torch.cuda.synchronize()
+    for w0, w1, d in zip(W, dp.W, dp.dW):
+        assert torch.equal(w1, w0 - 0.25 * d) or torch.allclose(w1, w0 - 0.25 * d, rtol=2 ** -22, atol=1e-9)
+    dp.close()
+
+
+@pytest.mark.gpu
+def test_epoch_distill_refuses(orc):
+    import torch
+    from paper_2508_13716_amd import harness as H
+    prob = H.make_problem(config("gcn", "f32", [16, 8], 6))
+    dp = H.DeviceProblem(prob)
+    n = prob.part.n_loc
+    ids, val = torch.zeros((n, 4), dtype=torch.int32, device="cuda"), torch.zeros((n, 4), device="cuda")
+    for bad in (dict(k=0), dict(k=5), dict(rest=2), dict(temperature=0.0), dict(weight=float("nan")), dict(ids=None), dict(val=None), dict(k=300, ld=300)):
+        a = dict(ids=ids, val=val, ld=4, k=4, rest=0, temperature=1.0, weight=1.0)
+        a.update(bad)
+        with pytest.raises(B.CapgnnError) as e:
+            dp.run_epoch(teacher=B.make_teacher(**a))
+        assert e.value.code == B.EINVAL
+    dp.run_epoch(teacher=B.make_teacher(ids, val, 4, 4, 0, 1.0, 1.0))
+    dp.close()
