@@ -382,7 +382,7 @@ constexpr int NARROW_TOP = 8;
 template <bool BF16, bool ENT, bool TOP>
 __global__ __launch_bounds__(64 * NARROW_WAVES) __attribute__((amdgpu_waves_per_eu(4))) void answers_narrow_kernel(AnswerArgs a, NarrowShape s) {
     extern __shared__ __align__(16) char lds_all[];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const size_t per_wave = s.lds_wave + 64 * (sizeof(float2) + NARROW_TOP);
     float *tile = reinterpret_cast<float *>(lds_all + wave * per_wave);
     float2 *ends = reinterpret_cast<float2 *>(lds_all + wave * per_wave + s.lds_wave);        // of every row: maximum, ln of the sum
@@ -725,7 +725,7 @@ __global__ __launch_bounds__(THREADS) void answers_grad_rows_kernel(AnswerGradAr
 template <bool BF16, bool DBF16, bool ENT>
 __global__ __launch_bounds__(64 * NARROW_WAVES) void answers_grad_narrow_kernel(AnswerGradArgs a, NarrowShape s) {
     extern __shared__ __align__(16) char lds_all[];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     float *tile = reinterpret_cast<float *>(lds_all + wave * s.lds_wave);
     const int G = 1 << s.lg, sub = lane & (G - 1), C = s.C;
     float *z = tile + (lane >> s.lg) * s.pitch;

@@ -35,7 +35,7 @@ constexpr float REST_LEAST = 9.5367431640625e-7f;       // 2^-20
 // ------------------------------------------------------------------ the teacher of a row, in LDS; the first wave of a workgroup works on it
 struct Teacher {
     static constexpr int OWN = CAPGNN_GIVEN_MAX / 64;       // entries of a lane: l, l + 64, ...
-    int32_t id[CAPGNN_GIVEN_MAX];   // class of every entry, -1: none
+    alignas(16) int32_t id[CAPGNN_GIVEN_MAX];   // class of every entry, -1: none
     int32_t c[CAPGNN_GIVEN_MAX];    // the same at a class's first mention, else -1
     float w[CAPGNN_GIVEN_MAX];      // probability of the entry
     float q[CAPGNN_GIVEN_MAX];      // of the class in all
@@ -97,19 +97,30 @@ __device__ __forceinline__ void read_teacher(const DistillArgs &a, int64_t row, 
         if (lane + o * 64 < a.k) t.w[lane + o * 64] = static_cast<float>(w[o] * one);
     }
     wave_sync();
-    // a class listed again: its first mention takes the sum
+    // a class listed again: its first mention takes the sum (ids four at a time; the sums only where there are some)
 #pragma unroll 1
-    for (int i = lane; i < a.k; i += 64) {
-        const int c = t.id[i];
-        float sum = 0.f;
-        bool first = c >= 0;
-        for (int b = 0; b < a.k; ++b)
-            if (t.id[b] == c) {
-                first = first && b >= i;
-                sum += t.w[b];
+    for (int i = lane; i < (a.k + 63 & ~63); i += 64) {
+        const int c = i < a.k ? t.id[i] : -1;
+        int same = 0, before = 0;
+        for (int b = 0; b < a.k; b += 4) {
+            const int4 v = *reinterpret_cast<const int4 *>(&t.id[b]);
+            const int there[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                const bool hit = there[u] == c && b + u < a.k;
+                same += hit;
+                before += hit && b + u < i;
             }
-        t.q[i] = sum;
-        t.c[i] = first ? c : -1;
+        }
+        float sum = i < a.k ? t.w[i] : 0.f;
+        if (__any(c >= 0 && same > 1)) {
+            sum = 0.f;
+            for (int b = 0; b < a.k; ++b) sum += t.id[b] == c ? t.w[b] : 0.f;
+        }
+        if (i < a.k) {
+            t.q[i] = sum;
+            t.c[i] = c >= 0 && before == 0 ? c : -1;
+        }
     }
     double r = a.rest ? 1.0 - Q : 0.0;
     if (r < REST_LEAST) r = 0.0;
@@ -240,7 +251,7 @@ __device__ __forceinline__ double divergence(const DistillArgs &a, const Teacher
         if (t.c[i] >= 0 && q != 0.f) kl += static_cast<double>(fmaf(-q * (t.z[i] - m0), a.t.inv_T, q * (logf(q) + ln_s)));
     }
     kl = wave_all(kl, OpSum());
-    if (t.r > 0.0) kl += t.r * (log(t.r) - (log(static_cast<double>(others)) - log(static_cast<double>(S))));
+    if (t.r > 0.0) kl += t.r * (logf(static_cast<float>(t.r)) - (logf(others) - ln_s));
     return kl;
 }
 
@@ -407,7 +418,7 @@ template <bool BF16, bool DBF16, bool REST>
 __global__ __launch_bounds__(64 * NARROW_WAVES) __attribute__((amdgpu_waves_per_eu(4))) void distill_narrow_kernel(DistillArgs a, NarrowShape s) {
     extern __shared__ __align__(16) uint32_t seen_bits[];
     __shared__ double red[NARROW_WAVES];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, k = a.k;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), k = a.k;
     float *tile = reinterpret_cast<float *>(reinterpret_cast<char *>(seen_bits) + wave * (s.lds_wave + s.rows * k * 3 * sizeof(float)));
     float *tile_w = tile + s.rows * s.pitch, *tile_q = tile_w + s.rows * k;
     int32_t *tile_id = reinterpret_cast<int32_t *>(tile_q + s.rows * k);
@@ -416,7 +427,7 @@ __global__ __launch_bounds__(64 * NARROW_WAVES) __attribute__((amdgpu_waves_per_
     int32_t *id = tile_id + mine * k;
     const float norm = distill_norm(a);
     const float scale = a.weight / norm * a.t.inv_T;
-    const int magic = (65536 + k - 1) / k, items = s.rows * k;
+    const int magic = ((1 << 20) + k - 1) / k, items = s.rows * k;        // item / k = item * magic >> 20 for item < 1024, k <= 128
     const int64_t step = static_cast<int64_t>(gridDim.x) * NARROW_WAVES * s.rows;
     int64_t row0 = (static_cast<int64_t>(blockIdx.x) * NARROW_WAVES + wave) * s.rows;
     double loss = 0.0;
@@ -429,16 +440,26 @@ __global__ __launch_bounds__(64 * NARROW_WAVES) __attribute__((amdgpu_waves_per_
         {
             int32_t c[NARROW_ENTRIES];
             float v[NARROW_ENTRIES];
-            const int anew = thread_anew() & 63;
+            const int anew = thread_anew() & 63, last = static_cast<int>(a.n - row0 < s.rows ? a.n - row0 : s.rows) - 1;
+            const int32_t *t_ids = a.t_ids + row0 * a.ldt;
+            const float *t_val = a.t_val + row0 * a.ldt;
+            const bool near = a.ldt < 1 << 22;
+            const uint32_t ldt = static_cast<uint32_t>(a.ldt);
 #pragma unroll
             for (int i = 0; i < NARROW_ENTRIES; ++i) {
                 const int item = i * 64 + anew;
                 if (i * 64 >= items) continue;              // (the same for all lanes)
-                const int r = item * magic >> 16;
-                const bool there = item < items && row0 + r < a.n;
-                const int64_t at = there ? (row0 + r) * a.ldt + (item - r * k) : 0;
-                c[i] = there ? a.t_ids[at] : -1;
-                v[i] = there ? a.t_val[at] : -INFINITY;
+                int r = item * magic >> 20;
+                const int e = item - __mul24(r, k);
+                r = r < last ? r : last;                    // (rows and entries beyond the last ones again those)
+                if (near) {
+                    const uint32_t at = __umul24(r, ldt) + e;
+                    c[i] = t_ids[at];
+                    v[i] = t_val[at];
+                } else {
+                    c[i] = t_ids[r * a.ldt + e];
+                    v[i] = t_val[r * a.ldt + e];
+                }
             }
             next.put(s, tile);
 #pragma unroll
@@ -495,11 +516,12 @@ __global__ __launch_bounds__(64 * NARROW_WAVES) __attribute__((amdgpu_waves_per_
             const int c = id[i];
             float p = 0.f;
             bool first = c >= 0;
-            for (int b = 0; b < k; ++b)
-                if (id[b] == c) {
-                    first = first && b >= i;
-                    p += w[b];
-                }
+#pragma unroll 4
+            for (int b = 0; b < k; ++b) {
+                const bool hit = id[b] == c;
+                first = first && !(hit && b < i);
+                p += hit ? w[b] : 0.f;
+            }
             q[i] = first ? p * one : -1.f;
             if (REST && first) listed += exp2_raw(difference(z[c], m0, a.t) * a.t.L);
         }
@@ -560,7 +582,7 @@ __global__ __launch_bounds__(64 * NARROW_WAVES) __attribute__((amdgpu_waves_per_
             }
         for (int off = 1; off < G; off <<= 1) kl += __shfl_xor(kl, off);
         if (sub == 0) {
-            if (REST && live && r > 0.0) kl += r * (log(r) - (log(static_cast<double>(others)) - log(static_cast<double>(S))));
+            if (REST && live && r > 0.0) kl += r * (logf(static_cast<float>(r)) - (logf(others) - ln_s));
             loss += kl;
             if (in && a.row_loss) a.row_loss[row] = static_cast<float>(kl);
         }

@@ -238,25 +238,33 @@ __device__ __forceinline__ void narrow_ends(const NarrowShape &s, float *lds, in
     for (int i = lane; i < s.rows * behind; i += 64) lds[i / behind * s.pitch + s.C + i % behind] = -INFINITY;
 }
 
+// rows so near to one another that a wave's offsets are products of 24-bit numbers (one instruction; a 64-bit product takes many)
+__device__ __forceinline__ bool narrow_near(int64_t pitch_bytes) { return pitch_bytes < 1 << 24; }
+
 template <bool BF16> struct NarrowLoad {
     static constexpr int MOST = BF16 ? 7 : 8;       // (bf16: 4 of 16 bytes, or up to 7 of one logit)
     raw16 q[MOST];
 
-    // rows [row0, row0 + s.rows), those beyond the last one again the last one
+    // rows [row0, row0 + s.rows) from row0 < n on, those beyond the last one again the last one; row0: the same for all lanes
     __device__ __forceinline__ void fetch(const NarrowShape &s, const char *Z, int64_t ldz, int64_t n, int64_t row0) {
         typedef Raw<BF16> R;
-        const int lane = thread_anew() & 63;
+        constexpr int ES = BF16 ? 2 : 4;
+        const int lane = thread_anew() & 63, last = static_cast<int>(n - row0 < s.rows ? n - row0 : s.rows) - 1;
+        const char *rows = Z + row0 * ldz * ES;
+        const bool near = narrow_near(ldz * ES);
+        const uint32_t pitch = static_cast<uint32_t>(ldz * ES);
 #pragma unroll
         for (int i = 0; i < MOST; ++i) {
             const int item = i * 64 + lane;
             if (i * 64 >= s.items) break;               // (the same for all lanes)
             if (item < s.items) {
-                const int r = item * s.magic >> 16, v = item - r * s.pieces;
-                int64_t row = row0 + r;
-                row = row < n ? row : n - 1;
-                const char *p = Z + row * ldz * (BF16 ? 2 : 4);
-                if (s.C < R::V) q[i][0] = __float_as_uint(ld_logit<BF16>(p, v));
-                else q[i] = R::load(p, v * R::V + R::V <= s.C ? v * R::V : s.C - R::V);
+                int r = item * s.magic >> 16;
+                const int v = item - __mul24(r, s.pieces);
+                r = r < last ? r : last;
+                const int j = s.C < R::V ? v : v * R::V + R::V <= s.C ? v * R::V : s.C - R::V;
+                const char *p = near ? rows + __umul24(r, pitch) : rows + r * ldz * ES;
+                if (s.C < R::V) q[i][0] = __float_as_uint(ld_logit<BF16>(p, j));
+                else q[i] = R::load(p, j);
             }
         }
     }
@@ -269,8 +277,8 @@ template <bool BF16> struct NarrowLoad {
             const int item = i * 64 + lane;
             if (i * 64 >= s.items) break;
             if (item < s.items) {
-                const int r = item * s.magic >> 16, v = item - r * s.pieces;
-                float *row = lds + r * s.pitch;
+                const int r = item * s.magic >> 16, v = item - __mul24(r, s.pieces);
+                float *row = lds + __mul24(r, s.pitch);
                 if (s.C < R::V) {
                     row[v] = __uint_as_float(q[i][0]);
                 } else {
@@ -286,16 +294,19 @@ template <bool BF16> struct NarrowLoad {
 // The wave's rows of gradients, from LDS as NarrowLoad put the logits there; add: to what dZ holds.
 template <bool BF16, bool DBF16>
 __device__ __forceinline__ void narrow_store(const NarrowShape &s, const float *lds, char *dZ, int64_t lddz, int64_t n, int64_t row0, bool add) {
-    constexpr int V = Raw<BF16>::V;
-    const int lane = thread_anew() & 63;
+    constexpr int V = Raw<BF16>::V, ES = DBF16 ? 2 : 4;
+    const int lane = thread_anew() & 63, there = static_cast<int>(n - row0 < s.rows ? n - row0 : s.rows);
+    char *rows = dZ + row0 * lddz * ES;
+    const bool near = narrow_near(lddz * ES);
+    const uint32_t pitch = static_cast<uint32_t>(lddz * ES);
 #pragma unroll
     for (int i = 0; i < NarrowLoad<BF16>::MOST; ++i) {
         const int item = i * 64 + lane;
         if (i * 64 >= s.items) break;
-        const int r = item * s.magic >> 16, v = item - r * s.pieces;
-        if (item < s.items && row0 + r < n) {
-            char *p = dZ + (row0 + r) * lddz * (DBF16 ? 2 : 4);
-            const float *row = lds + r * s.pitch;
+        const int r = item * s.magic >> 16, v = item - __mul24(r, s.pieces);
+        if (item < s.items && r < there) {
+            char *p = near ? rows + __umul24(r, pitch) : rows + r * lddz * ES;
+            const float *row = lds + __mul24(r, s.pitch);
             if (s.C < V || v * V + V > s.C) {           // one logit, or what is left of a row
                 const int j = s.C < V ? v : v * V, end = s.C < V ? v + 1 : s.C;
                 for (int k = j; k < end; ++k) st_grad<DBF16>(p, k, add ? ld_logit<DBF16>(p, k) + row[k] : row[k]);

@@ -413,6 +413,30 @@ def test_distill_vs_oracle(n, C, pad, T, dtype, dz_dtype):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("rest", [0, 1])
+@pytest.mark.parametrize("n,C,k", [(67, 200, 127), (50, 256, 113), (131, 90, 63), (90, 129, 99), (200, 33, 31), (301, 20, 16), (140, 3, 16), (140, 3, 17),
+                                   (70, 7, 150), (45, 200, 129), (40, 400, 256)])
+def test_distill_lists_of_many_lengths(n, C, k, rest):
+    """as many entries as a lane of few classes takes, one more, odd numbers of them, more than there are classes"""
+    rng = np.random.default_rng(C + k)
+    for dtype in ("f32", "bf16"):
+        Z = hard_rows(n, C, dtype, C + k)
+        ids, val = teacher_of(Z, min(C, k), rest, 1.0, rng)
+        if k > C:                                    # behind the classes: nothing, and classes again with little mass
+            more = rng.integers(-1, C, (n, k - C)).astype(np.int32)
+            ids, val = np.concatenate([ids, more], 1), np.concatenate([val - 0.5, np.full((n, k - C), -9.0, np.float32)], 1).astype(np.float32)
+        perm = rng.permutation(k)
+        ids, val = ids[:, perm], val[:, perm]
+        mask = (rng.random(n) < 0.8).astype(np.uint8)
+        with np.errstate(divide="ignore", invalid="ignore"):
+            ref_loss, ref_row, dref, ex = orc.distill(Z, ids, val, bool(rest), 1.0, mask)
+            row_tol, dz_tol = distill_tol(Z, ex, ref_row, dref, 1.0, C, k, 1.0, dtype)
+        loss, row, dZ = run_distill(device(Z, dtype, C + 1), C, dtype, dtype, 1.0, mask, ids, val, rest, 0.0, 1.0, C + 3)
+        check("row_loss", row, ref_row, row_tol)
+        check("dZ", dZ[:, :C], dref, dz_tol)
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("C", [30, 700, 9000, 150_000])
 def test_distill_student_sure_of_the_listed_classes(C):
     """P far below the rounding of a sum that holds the listed classes: it has to be formed without them"""
