@@ -46,8 +46,9 @@ struct RowEnd {
 // threshold: of at least k logits of the row it is known that they are no smaller.  The first tile's thread maxima give one for the whole
 // workgroup: the k-th largest of them is exceeded by hardly more than k logits of the tile (64 largest of 16384: 73 on average).  What
 // passes the threshold is appended; a wave's list that is half full is ranked, each key by counting the larger ones, and cut to k.
-// Keys are distinct, so the order of appending does not show.  A tile that passes more than the list holds is tried again with the
-// wave's own maxima, then with its exact k-th largest key (equal logits, values in order): slower, never wrong.  The waves meet
+// Keys are distinct, so the order of appending does not show.  A wave alone has 64 maxima, of which the 64th largest is passed by 260 of 4096
+// logits and sometimes twice as many: for k > 32 it takes the k-th largest of its 512 vectors' maxima.  A tile that passes more than
+// the list holds is tried again with those, then with its exact k-th largest key (equal logits): slower, never wrong.  The waves meet
 // at the first threshold and at the end of the row only (a list for the workgroup, with an atomic counter and a barrier per tile:
 // 4096 x 131072 bf16, k = 64, 471 us).
 template <int THREADS> struct TopLds {
@@ -133,6 +134,22 @@ template <int THREADS> struct Top {
         formed = kept;
     }
 
+    // The same of the maxima of the wave's NV vectors of every lane, bit by bit: seldom more than a few logits behind the exact k-th largest.
+    template <int NV> __device__ uint32_t kth_vector(const float (&vmax)[NV]) {
+        uint32_t o[NV], T = 0;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) o[i] = logit_order(vmax[i]);
+#pragma unroll 1
+        for (int bit = 31; bit >= 0; --bit) {
+            const uint32_t t = T | 1u << bit;
+            int c = 0;
+#pragma unroll
+            for (int i = 0; i < NV; ++i) c += __popcll(__ballot(o[i] >= t));
+            if (c >= k) T = t;
+        }
+        return T;
+    }
+
     // cuts the wave's list to its k largest, in descending order
     template <bool BF16> __device__ void cut(const char *z) {
         form<BF16>(z);
@@ -170,7 +187,7 @@ template <int THREADS> struct Top {
         typedef Raw<BF16> R;
         constexpr int V = R::V, HALF = NV * V / 2;
         static_assert(HALF <= 32 && NV % 2 == 0, "a thread's logits of a tile are two words of bits");
-        if (first && end - from > THREADS / 64 * CAP / 2) raise(kth_maximum<THREADS>(tmax), true);
+        if (first && end - from > THREADS / 64 * CAP / 2) raise(THREADS == 64 && k > 32 ? kth_vector<NV>(vmax) : kth_maximum<THREADS>(tmax), true);
         if (again >= 0) return;
         const int before = kept;
 #pragma unroll 1
@@ -202,7 +219,7 @@ template <int THREADS> struct Top {
                 return;
             }
             kept = before;
-            if (attempt == 0) raise(kth_maximum<64>(tmax), true);
+            if (attempt == 0) raise(kth_vector<NV>(vmax), true);
         }
         again = from;
     }
@@ -602,7 +619,7 @@ __global__ __launch_bounds__(256) void answers_join_kernel(AnswerArgs a, AnswerP
 }
 
 // Few rows are cut into parts, about a thousand workgroups in all and ANSWER_PART_LEAST classes or more each.
-constexpr int ANSWER_PART_LEAST = 2048, ANSWER_WORKGROUPS = 1024;
+constexpr int ANSWER_PART_LEAST = 2048, ANSWER_WORKGROUPS = 1024, ANSWER_WAVE_C = 16384;
 static int answer_parts(int64_t n, int C, int64_t *chunk) {
     int64_t parts = std::min<int64_t>(std::min<int64_t>(ANSWER_PARTS, ANSWER_WORKGROUPS / std::max<int64_t>(n, 1)), (C + ANSWER_PART_LEAST - 1) / ANSWER_PART_LEAST);
     if (parts <= 1) { *chunk = C; return 1; }
@@ -809,8 +826,10 @@ extern "C" int capgnn_logprobs(int64_t n, int C, const void *Z, int64_t ldz, int
     w.parts = answer_parts(n, C, &w.chunk);
     w.sums = static_cast<float4 *>(ws);
     w.keys = reinterpret_cast<unsigned long long *>(static_cast<char *>(ws) + align_up(sizeof(float4) * n * w.parts, 256));
-    // a wave alone walks rows of one tile (no barriers between waves), a workgroup of four longer ones
-    const bool wave = w.chunk <= 64 * ANSWER_VECTORS * (bf16 ? 8 : 4);
+    // A wave alone walks rows of one tile and, where there are enough rows for two waves on every SIMD, rows up to ANSWER_WAVE_C classes, half as many for long lists (no meeting
+    // of waves: 3001 x 10007 bf16, k = 10, 40 us by workgroups of four waves, 23 by waves; 8000 x 5000 fp32 82 and 36; but 600 x 10007
+    // fp32 15 and 19, and from 33000 classes on no difference; k = 64: 8000 x 5000 fp32 95 and 72, 2500 x 16384 bf16 41 and 70).
+    const bool wave = w.chunk <= 64 * ANSWER_VECTORS * (bf16 ? 8 : 4) || (n >= 2048 && C <= (k > 32 ? ANSWER_WAVE_C / 2 : ANSWER_WAVE_C));
     const unsigned grid = static_cast<unsigned>(std::min<int64_t>(n * w.parts, 1 << 24));
     auto go = [&](auto kernel, int threads) { hipLaunchKernelGGL(kernel, dim3(grid), dim3(threads), 0, st, a, w); };
     if (bf16) {

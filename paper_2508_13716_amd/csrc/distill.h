@@ -623,12 +623,12 @@ void launch_distill(const DistillArgs &a, DistillParts w, int *groups, hipStream
         go(distill_rows_kernel<BF16, DBF16, 64, 8, REST, ROW_HELD>, 64, lds);
     } else if (a.C <= 256 * 8 * V) {
         go(distill_rows_kernel<BF16, DBF16, 256, 8, REST, ROW_HELD>, 256, lds);
-    } else if (a.C <= 256 * 16 * V) {
-        go(distill_rows_kernel<BF16, DBF16, 256, 16, REST, ROW_HELD>, 256, lds);
+    } else if (a.C <= 256 * 12 * V) {
+        go(distill_rows_kernel<BF16, DBF16, 256, 12, REST, ROW_HELD>, 256, lds);
     } else if (a.C <= 512 * 16 * V) {
         go(distill_rows_kernel<BF16, DBF16, 512, 16, REST, ROW_HELD>, 512, lds);
     } else {
-        go(distill_rows_kernel<BF16, DBF16, 512, 16, REST, ROW_READ_TWICE>, 512, lds);
+        go(distill_rows_kernel<BF16, DBF16, 512, 12, REST, ROW_READ_TWICE>, 512, lds);
     }
 }
 
