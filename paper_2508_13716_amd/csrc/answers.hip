@@ -463,7 +463,7 @@ __global__ __launch_bounds__(64 * NARROW_WAVES) __attribute__((amdgpu_waves_per_
         }
         const float ref = safe_max(m);
         float sum = 0.f, e1 = 0.f;
-        int reached = 0;                    // classes that reach the k-th largest
+        uint32_t hits = 0;                  // the lane's classes that reach the k-th largest, a bit each
         for (int b = 0; b < s.each; b += NARROW_BATCH) {
             float x[NARROW_BATCH];
 #pragma unroll
@@ -473,16 +473,22 @@ __global__ __launch_bounds__(64 * NARROW_WAVES) __attribute__((amdgpu_waves_per_
                 const float u = (x[i] - ref) * a.t.L, e = exp2_raw(u);
                 sum += e;
                 if constexpr (ENT) e1 = fmaf(e, fmaxf(u, -160.f), e1);
-                if constexpr (TOP) {
-                    const int j = sub + (b + i) * G;
-                    if (x[i] >= kth && j < C) {
-                        int larger = 0;
+                if constexpr (TOP) hits |= x[i] >= kth ? 1u << (b + i) : 0u;
+            }
+        }
+        int reached = 0;
+        if constexpr (TOP) {
+            const int own = (C - sub + G - 1) >> s.lg;          // (behind the row's end: -inf, which a k-th largest may be as well)
+            hits &= own < 32 ? (1u << own) - 1u : ~0u;
+            reached = __popc(hits);
+            while (__any(hits != 0)) {
+                const int i = __ffs(hits) - 1;
+                const float x = z[i < 0 ? sub : sub + i * G];
+                int larger = 0;
 #pragma unroll
-                        for (int q = 0; q < NARROW_TOP; ++q) larger += v[q] > x[i];
-                        place[larger & (NARROW_TOP - 1)] = static_cast<uint8_t>(j);       // (8 only next to a NaN)
-                        ++reached;
-                    }
-                }
+                for (int q = 0; q < NARROW_TOP; ++q) larger += v[q] > x;
+                if (hits) place[larger & (NARROW_TOP - 1)] = static_cast<uint8_t>(sub + i * G);         // (8 only next to a NaN)
+                hits &= hits - 1;
             }
         }
         for (int off = 1; off < G; off <<= 1) {

@@ -412,19 +412,20 @@ __global__ __launch_bounds__(THREADS) __attribute__((amdgpu_waves_per_eu(4))) vo
 // (Entries read where they are used, by one lane a row: 612000 x 47, k = 8, 278 us; the teacher's probabilities by class in a second set
 // of rows, which leaves LDS for ten waves per compute unit: 170 us.)
 constexpr int NARROW_ENTRIES = 16;      // of a lane
-static inline size_t distill_narrow_lds(const NarrowShape &s, int k) { return s.lds_wave + static_cast<size_t>(s.rows) * k * 3 * sizeof(float); }
+// (an odd number of words between rows: their lanes hit different banks)
+static inline size_t distill_narrow_lds(const NarrowShape &s, int k) { return s.lds_wave + static_cast<size_t>(s.rows) * (k | 1) * 3 * sizeof(float); }
 
 template <bool BF16, bool DBF16, bool REST>
 __global__ __launch_bounds__(64 * NARROW_WAVES) __attribute__((amdgpu_waves_per_eu(4))) void distill_narrow_kernel(DistillArgs a, NarrowShape s) {
     extern __shared__ __align__(16) uint32_t seen_bits[];
     __shared__ double red[NARROW_WAVES];
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), k = a.k;
-    float *tile = reinterpret_cast<float *>(reinterpret_cast<char *>(seen_bits) + wave * (s.lds_wave + s.rows * k * 3 * sizeof(float)));
-    float *tile_w = tile + s.rows * s.pitch, *tile_q = tile_w + s.rows * k;
-    int32_t *tile_id = reinterpret_cast<int32_t *>(tile_q + s.rows * k);
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), k = a.k, kp = k | 1;
+    float *tile = reinterpret_cast<float *>(reinterpret_cast<char *>(seen_bits) + wave * (s.lds_wave + s.rows * kp * 3 * sizeof(float)));
+    float *tile_w = tile + s.rows * s.pitch, *tile_q = tile_w + s.rows * kp;
+    int32_t *tile_id = reinterpret_cast<int32_t *>(tile_q + s.rows * kp);
     const int G = 1 << s.lg, sub = lane & (G - 1), C = s.C, mine = lane >> s.lg;
-    float *z = tile + mine * s.pitch, *w = tile_w + mine * k, *q = tile_q + mine * k;
-    int32_t *id = tile_id + mine * k;
+    float *z = tile + mine * s.pitch, *w = tile_w + mine * kp, *q = tile_q + mine * kp;
+    int32_t *id = tile_id + mine * kp;
     const float norm = distill_norm(a);
     const float scale = a.weight / norm * a.t.inv_T;
     const int magic = ((1 << 20) + k - 1) / k, items = s.rows * k;        // item / k = item * magic >> 20 for item < 1024, k <= 128
@@ -467,8 +468,9 @@ __global__ __launch_bounds__(64 * NARROW_WAVES) __attribute__((amdgpu_waves_per_
                 const int item = i * 64 + anew;
                 if (i * 64 >= items) continue;
                 if (item < items) {
-                    tile_id[item] = c[i] >= 0 && c[i] < C && v[i] != -INFINITY ? c[i] : -1;
-                    tile_w[item] = v[i];
+                    const int at = item + (kp - k) * (item * magic >> 20);
+                    tile_id[at] = c[i] >= 0 && c[i] < C && v[i] != -INFINITY ? c[i] : -1;
+                    tile_w[at] = v[i];
                 }
             }
         }

@@ -307,15 +307,16 @@ __device__ __forceinline__ void narrow_store(const NarrowShape &s, const float *
         if (item < s.items && r < there) {
             char *p = near ? rows + __umul24(r, pitch) : rows + r * lddz * ES;
             const float *row = lds + __mul24(r, s.pitch);
-            if (s.C < V || v * V + V > s.C) {           // one logit, or what is left of a row
+            if (s.C < V || (add && v * V + V > s.C)) {          // one logit, or what is left of a row
                 const int j = s.C < V ? v : v * V, end = s.C < V ? v + 1 : s.C;
                 for (int k = j; k < end; ++k) st_grad<DBF16>(p, k, add ? ld_logit<DBF16>(p, k) + row[k] : row[k]);
             } else {
+                const int j = v * V + V <= s.C ? v * V : s.C - V;        // (a row's last piece: some of what its neighbour writes, too)
                 float g[V];
-                if (add) ld_vector<DBF16>(p, v * V, g);
+                if (add) ld_vector<DBF16>(p, j, g);
 #pragma unroll
-                for (int e = 0; e < V; ++e) g[e] = add ? g[e] + row[v * V + e] : row[v * V + e];
-                st_vector<DBF16>(p, v * V, g);
+                for (int e = 0; e < V; ++e) g[e] = add ? g[e] + row[j + e] : row[j + e];
+                st_vector<DBF16>(p, j, g);
             }
         }
     }
