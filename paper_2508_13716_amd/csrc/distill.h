@@ -419,7 +419,7 @@ template <bool BF16, bool DBF16, bool REST>
 __global__ __launch_bounds__(64 * NARROW_WAVES) __attribute__((amdgpu_waves_per_eu(4))) void distill_narrow_kernel(DistillArgs a, NarrowShape s) {
     extern __shared__ __align__(16) uint32_t seen_bits[];
     __shared__ double red[NARROW_WAVES];
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), k = a.k, kp = k | 1;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), k = a.k, kp = k | 1, all_items = s.rows * k;
     float *tile = reinterpret_cast<float *>(reinterpret_cast<char *>(seen_bits) + wave * (s.lds_wave + s.rows * kp * 3 * sizeof(float)));
     float *tile_w = tile + s.rows * s.pitch, *tile_q = tile_w + s.rows * kp;
     int32_t *tile_id = reinterpret_cast<int32_t *>(tile_q + s.rows * kp);
@@ -428,7 +428,7 @@ __global__ __launch_bounds__(64 * NARROW_WAVES) __attribute__((amdgpu_waves_per_
     int32_t *id = tile_id + mine * kp;
     const float norm = distill_norm(a);
     const float scale = a.weight / norm * a.t.inv_T;
-    const int magic = ((1 << 20) + k - 1) / k, items = s.rows * k;        // item / k = item * magic >> 20 for item < 1024, k <= 128
+    const int magic = ((1 << 20) + k - 1) / k; // item / k = item * magic >> 20 for item < 1024, k <= 128
     const int64_t step = static_cast<int64_t>(gridDim.x) * NARROW_WAVES * s.rows;
     int64_t row0 = (static_cast<int64_t>(blockIdx.x) * NARROW_WAVES + wave) * s.rows;
     double loss = 0.0;
@@ -441,7 +441,7 @@ __global__ __launch_bounds__(64 * NARROW_WAVES) __attribute__((amdgpu_waves_per_
         {
             int32_t c[NARROW_ENTRIES];
             float v[NARROW_ENTRIES];
-            const int anew = thread_anew() & 63, last = static_cast<int>(a.n - row0 < s.rows ? a.n - row0 : s.rows) - 1;
+            const int items = uniform_anew(all_items), anew = thread_anew() & 63, last = static_cast<int>(a.n - row0 < s.rows ? a.n - row0 : s.rows) - 1;
             const int32_t *t_ids = a.t_ids + row0 * a.ldt;
             const float *t_val = a.t_val + row0 * a.ldt;
             const bool near = a.ldt < 1 << 22;

@@ -183,6 +183,14 @@ __device__ __forceinline__ int thread_anew() {
     return t;
 }
 
+// The same for a value that all threads have: what one pass over a row's vectors has found out about their number is not carried into the next
+// (code for every number of vectors, a kilobyte of scratch memory a thread; or a loop's conditions kept in spilled registers).
+__device__ __forceinline__ int uniform_anew(int x) {
+    x = __builtin_amdgcn_readfirstlane(x);
+    asm volatile("" : "+s"(x));
+    return x;
+}
+
 // Rows of at most NARROW_C classes: a wave takes 64 / G of them at a time through LDS, G lanes a row with at most 32 classes each, so that a
 // row's sums need hardly any exchange between lanes (lane groups over registers spent four times the instructions at 47 classes:
 // 612000 rows were bound by them, not by memory).  The next rows' loads are under way while a wave works on its own.  A row starts
@@ -253,11 +261,12 @@ template <bool BF16> struct NarrowLoad {
         const char *rows = Z + row0 * ldz * ES;
         const bool near = narrow_near(ldz * ES);
         const uint32_t pitch = static_cast<uint32_t>(ldz * ES);
+        const int items = uniform_anew(s.items);
 #pragma unroll
         for (int i = 0; i < MOST; ++i) {
             const int item = i * 64 + lane;
-            if (i * 64 >= s.items) break;               // (the same for all lanes)
-            if (item < s.items) {
+            if (i * 64 >= items) break;                 // (the same for all lanes)
+            if (item < items) {
                 int r = item * s.magic >> 16;
                 const int v = item - __mul24(r, s.pieces);
                 r = r < last ? r : last;
@@ -271,12 +280,12 @@ template <bool BF16> struct NarrowLoad {
 
     __device__ __forceinline__ void put(const NarrowShape &s, float *lds) {
         typedef Raw<BF16> R;
-        const int lane = thread_anew() & 63;
+        const int lane = thread_anew() & 63, items = uniform_anew(s.items);
 #pragma unroll
         for (int i = 0; i < MOST; ++i) {
             const int item = i * 64 + lane;
-            if (i * 64 >= s.items) break;
-            if (item < s.items) {
+            if (i * 64 >= items) break;
+            if (item < items) {
                 const int r = item * s.magic >> 16, v = item - __mul24(r, s.pieces);
                 float *row = lds + __mul24(r, s.pitch);
                 if (s.C < R::V) {
@@ -299,12 +308,13 @@ __device__ __forceinline__ void narrow_store(const NarrowShape &s, const float *
     char *rows = dZ + row0 * lddz * ES;
     const bool near = narrow_near(lddz * ES);
     const uint32_t pitch = static_cast<uint32_t>(lddz * ES);
+    const int items = uniform_anew(s.items);
 #pragma unroll
     for (int i = 0; i < NarrowLoad<BF16>::MOST; ++i) {
         const int item = i * 64 + lane;
-        if (i * 64 >= s.items) break;
+        if (i * 64 >= items) break;
         const int r = item * s.magic >> 16, v = item - __mul24(r, s.pieces);
-        if (item < s.items && r < there) {
+        if (item < items && r < there) {
             char *p = near ? rows + __umul24(r, pitch) : rows + r * lddz * ES;
             const float *row = lds + __mul24(r, s.pitch);
             if (s.C < V || (add && v * V + V > s.C)) {          // one logit, or what is left of a row
@@ -320,14 +330,6 @@ __device__ __forceinline__ void narrow_store(const NarrowShape &s, const float *
             }
         }
     }
-}
-
-// The same for a value that all threads have: what one pass over a row's vectors has found out about their number is not carried into the next
-// (code for every number of vectors: a kilobyte of scratch memory a thread).
-__device__ __forceinline__ int uniform_anew(int x) {
-    x = __builtin_amdgcn_readfirstlane(x);
-    asm volatile("" : "+s"(x));
-    return x;
 }
 
 template <typename T, typename Op> __device__ __forceinline__ T wave_all(T v, Op op) {
