@@ -225,7 +225,7 @@ template <int THREADS> struct Top {
     }
 
     // The tiles from `again` on, out of memory (kept out of the scan, whose registers it would take): those with more candidates than the list
-    // holds by the exact k-th largest key of the wave's share, found bit by bit: order T, classes below J.
+    // holds by the exact k-th largest key of the wave's share (4096 x 131072 equal logits, k = 64: 2.0 ms; random ones 0.31).
     template <bool BF16, int NV> __device__ void rest(const char *z, int row_end) {
         constexpr int V = Raw<BF16>::V, TILE = THREADS * NV * V;
 #pragma unroll 1
@@ -238,30 +238,49 @@ template <int THREADS> struct Top {
                     f(j < end ? ld_logit<BF16>(z, j) : 0.f, j, j < end);
                 }
             };
-            auto count = [&](auto in) {
+            auto count = [&](auto in) {             // (eight loads in flight)
                 int c = 0;
-                each([&](float x, int j, bool there) { c += there && in(x, j); });
+#pragma unroll 1
+                for (int q = lane(); q < NV * 64 * V; q += 8 * 64) {
+                    float x[8];
+                    int j[8];
+#pragma unroll
+                    for (int u = 0; u < 8; ++u) {
+                        j[u] = mine + (q + u * 64) / (64 * V) * (THREADS * V) + (q + u * 64) % (64 * V);
+                        x[u] = j[u] < end ? ld_logit<BF16>(z, j[u]) : 0.f;
+                    }
+#pragma unroll
+                    for (int u = 0; u < 8; ++u) c += j[u] < end && in(x[u], j[u]);
+                }
                 return wave_all(c, OpSum());
             };
             const float limit = below;
             const int all = count([&](float x, int) { return !(x <= limit); }), want = all < k ? all : k;
             uint32_t T = 0;
-            int J = 0x7fffffff;
+            int equal = all;                // how many of order T are wanted
             if (kept + all > CAP) {
-                J = 0;
-                for (int bit = 31; bit >= 0; --bit) {
-                    const uint32_t t = T | 1u << bit;
-                    if (count([&](float x, int) { return logit_order(x) >= t; }) >= want) T = t;
+                // the k-th largest of the lanes' maxima, if fewer than k are above it (many equal logits); else bit by bit
+                float most[1] = {-INFINITY};
+                each([&](float x, int, bool there) { if (there) most[0] = max_of(most[0], x); });
+                T = kth_vector<1>(most);
+                int above = count([&](float x, int) { return logit_order(x) > T; });
+                if (above >= want) {
+                    T = 0;
+                    for (int bit = 31; bit >= 0; --bit) {
+                        const uint32_t t = T | 1u << bit;
+                        if (count([&](float x, int) { return logit_order(x) >= t; }) >= want) T = t;
+                    }
+                    above = count([&](float x, int) { return logit_order(x) > T; });
                 }
-                const int above = count([&](float x, int) { return logit_order(x) > T; });
-                for (int bit = 30; bit >= 0; --bit) {
-                    const int t = J | 1 << bit;
-                    if (count([&](float x, int j) { return logit_order(x) == T && j < t; }) <= want - above) J = t;
-                }
+                equal = want - above;
             }
+            // classes come in ascending order: the first ones of order T are taken
             each([&](float x, int j, bool there) {
                 const uint32_t o = logit_order(x);
-                append(there && !(x <= limit) && (o > T || (o == T && j < J)), j);      // at most k, or all that the list holds
+                const unsigned long long same = __ballot(there && !(x <= limit) && o == T);
+                const int before = __builtin_amdgcn_mbcnt_hi(static_cast<uint32_t>(same >> 32), __builtin_amdgcn_mbcnt_lo(static_cast<uint32_t>(same), 0));
+                append(there && !(x <= limit) && (o > T || (o == T && before < equal)), j);      // k at most, or all, which the list holds
+                equal -= __popcll(same);
             });
             if (kept > CAP / 2 || kept + all > CAP) cut<BF16>(z);
         }
@@ -297,7 +316,10 @@ template <int THREADS> struct Top {
     }
 };
 
-// One workgroup per row, or per part of a row (parts > 1): running maximum and sums in every thread, one pass over the logits.
+// One workgroup (or wave) per row, or per part of a row (parts > 1): running maximum and sums in every thread, one pass over the logits, eight
+// 16-byte loads a thread in flight, which read -> sums -> threshold out of registers; sixteen waves on a compute unit cover one another's waits.
+// Bound by HBM: 4096 x 131072 bf16 without top classes 5.3 TB/s (200 us), with 8 of them 217, with 64 312 us, where the instructions of the
+// threshold and the ranking show (VALU issue about 60 % of the time).
 constexpr int ANSWER_VECTORS = 8;       // 16-byte loads that a thread has in flight
 
 struct AnswerParts {
@@ -394,7 +416,8 @@ __global__ __launch_bounds__(THREADS) __attribute__((amdgpu_waves_per_eu(4))) vo
 // Pass 1 keeps the k largest logits of a lane sorted, one median of three per place and logit (lanes of a row merge theirs); pass 2 forms the
 // sums, and a class that reaches the k-th largest finds its place among them as the number of those that are larger.  Rows with equal
 // logits among the k largest, or with NaN, are gone over once more by one lane, class by class.  The places of the wave's rows are
-// written out together.  (Ranking the classes found against one another, out of LDS: 612000 x 47, k = 5, 131 us.)
+// written out together.  612000 x 47, k = 5: 53 us, 2.8 TB/s, bound by instruction issue and LDS latency in about equal parts; without top
+// classes 28 us, 4.1 TB/s.  (Ranking the classes found against one another, out of LDS: 131 us.)
 constexpr int NARROW_TOP = 8;
 template <bool BF16, bool ENT, bool TOP>
 __global__ __launch_bounds__(64 * NARROW_WAVES) __attribute__((amdgpu_waves_per_eu(4))) void answers_narrow_kernel(AnswerArgs a, NarrowShape s) {
@@ -560,7 +583,8 @@ __global__ __launch_bounds__(64 * NARROW_WAVES) __attribute__((amdgpu_waves_per_
     }
 }
 
-// The parts of a row put together: sums from the parts' maxima to the row's, and the k largest of the parts' k largest.
+// The parts of a row put together: sums from the parts' maxima to the row's, and the k largest of the parts' k largest.  One row of 40000
+// classes, k = 20: 15 us in two launches, both latency (one workgroup a row: 60 us and more of one compute unit's loads).
 constexpr int ANSWER_PARTS = 64;
 template <bool BF16>
 __global__ __launch_bounds__(256) void answers_join_kernel(AnswerArgs a, AnswerParts w) {
@@ -667,7 +691,8 @@ struct GradRow {
 };
 
 // Workgroups of THREADS take CHUNK classes of a row each; the sums of the row come with the call.  The given classes' own terms follow
-// the rest of the chunk, behind a barrier, from the thread that holds the first mention of the class.
+// the rest of the chunk, behind a barrier, from the thread that holds the first mention of the class.  Bound by HBM: 4096 x 65536 bf16
+// 188 us, 5.7 TB/s read and written.
 constexpr int GRAD_VECTORS = 4;
 template <bool BF16, bool DBF16, int THREADS, bool ENT>
 __global__ __launch_bounds__(THREADS) void answers_grad_rows_kernel(AnswerGradArgs a, int chunks) {
@@ -745,6 +770,8 @@ __global__ __launch_bounds__(THREADS) void answers_grad_rows_kernel(AnswerGradAr
     }
 }
 
+// Few classes: the rows' gradients take their logits' places in LDS and leave in whole vectors.  60000 x 41: 9.3 us, of which a launch and its
+// way through Python are most (kernel 6-7 us).
 template <bool BF16, bool DBF16, bool ENT>
 __global__ __launch_bounds__(64 * NARROW_WAVES) void answers_grad_narrow_kernel(AnswerGradArgs a, NarrowShape s) {
     extern __shared__ __align__(16) char lds_all[];

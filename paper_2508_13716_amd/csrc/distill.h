@@ -279,6 +279,12 @@ enum DistillStage : int {
     PART_GRADIENT   // the parts' sums put together, gradient of a part
 };
 
+// One workgroup per row (or part): the first wave reads the teacher while all of them have the row's logits on their way; maximum and sums from
+// registers, one meeting, then the gradient from the same registers; the listed classes' own terms follow behind a barrier.  Bound by
+// HBM: 8192 x 64000 bf16 415 us (5.05 TB/s read and written).  Rows longer than the registers hold come out of the Infinity Cache a second
+// time, all but the last tile: 2048 x 131072 fp32 573 us for 2.1 GB (a second pass over everything: 650).  Rows of some ten thousand
+// classes are held up by the teacher's chain of dependent reads, four workgroups a compute unit: 2999 x 10007 fp32, k = 32, rest, 70 us.
+// At most 128 registers, for sixteen waves per compute unit: without that bound the compiler takes twice as many and has half the waves.
 template <bool BF16, bool DBF16, int THREADS, int NV, bool REST, DistillStage STAGE>
 __global__ __launch_bounds__(THREADS) __attribute__((amdgpu_waves_per_eu(4))) void distill_rows_kernel(DistillArgs a, DistillParts w) {
     typedef Raw<BF16> R;
@@ -409,8 +415,8 @@ __global__ __launch_bounds__(THREADS) __attribute__((amdgpu_waves_per_eu(4))) vo
 // ------------------------------------------------------------------ few classes
 // As answers_grad_narrow_kernel, the teacher's entries beside the rows in LDS, shared by the lanes of a row; each entry looks for other
 // mentions of its class.  rest: the listed classes' logits are taken out of the row before it is summed.
-// (Entries read where they are used, by one lane a row: 612000 x 47, k = 8, 278 us; the teacher's probabilities by class in a second set
-// of rows, which leaves LDS for ten waves per compute unit: 170 us.)
+// 612000 x 47, k = 8: 110 us, 2 TB/s, bound by instruction issue (53 us of it) and LDS latency.  (Entries read where they are used, by one lane
+// a row: 278 us; the teacher's probabilities by class in a second set of rows, which leaves LDS for ten waves per compute unit: 170 us.)
 constexpr int NARROW_ENTRIES = 16;      // of a lane
 // (an odd number of words between rows: their lanes hit different banks)
 static inline size_t distill_narrow_lds(const NarrowShape &s, int k) { return s.lds_wave + static_cast<size_t>(s.rows) * (k | 1) * 3 * sizeof(float); }
@@ -617,6 +623,8 @@ void launch_distill(const DistillArgs &a, DistillParts w, int *groups, hipStream
     while (w.seen < a.C && w.seen < 1 << 18) w.seen *= 2;
     const size_t lds = REST ? w.seen / 8 : 0;
     *groups = static_cast<int>(std::min<int64_t>(a.n * w.parts, DISTILL_GROUPS));
+    // The fewest threads that hold a row (more rows on a compute unit, whose chains overlap: 2999 x 10007 fp32 with 512 threads 102 us, with 256
+    // 72; 12 vectors a thread rather than 16 there, which spills: 63.6 and 62.1 us).
     auto go = [&](auto kernel, int threads, size_t bytes) { hipLaunchKernelGGL(kernel, dim3(*groups), dim3(threads), bytes, st, a, w); };
     if (w.parts > 1) {
         go(distill_rows_kernel<BF16, DBF16, 256, 8, REST, PART_SUMS>, 256, lds);

@@ -455,6 +455,24 @@ def test_distill_student_sure_of_the_listed_classes(C):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("rest", [0, 1])
+@pytest.mark.parametrize("n,C", [(9, 40), (9, 600), (9, 9000), (9, 80_000), (700, 70_000)])
+def test_distill_nan_stays_in_its_row(n, C, rest):
+    """a NaN or an infinite logit, a NaN among the teacher's values: that row's numbers are NaN, the others' what they are without"""
+    rng = np.random.default_rng(C)
+    Z = to_dtype(rng.standard_normal((n, C)), "f32")
+    ids, val = teacher_of(Z, 6, rest, 1.0, rng)
+    clean = run_distill(device(Z, "f32", C), C, "f32", "f32", 1.0, None, ids, val, rest, 3.0, 1.0, C)
+    Z[1, C // 2], Z[2, 0] = np.nan, np.inf
+    val[6, 3] = np.nan
+    loss, row, dZ = run_distill(device(Z, "f32", C), C, "f32", "f32", 1.0, None, ids, val, rest, 3.0, 1.0, C)
+    broken = np.zeros(n, bool)
+    broken[[1, 2, 6]] = True
+    assert np.isnan(loss) and np.isnan(row[broken]).all() and np.isnan(dZ[broken]).all()
+    assert np.array_equal(row[~broken], clean[1][~broken]) and np.array_equal(dZ[~broken], clean[2][~broken])
+
+
+@pytest.mark.gpu
 def test_distill_without_rows_leaves_a_loss_of_zero():
     import torch
     loss = torch.full((1,), 5.0, device="cuda")
