@@ -796,7 +796,16 @@ __global__ __launch_bounds__(64 * NARROW_WAVES) void answers_grad_narrow_kernel(
         next.put(s, tile);
         wave_sync();
         if (row0 + step < a.n) next.fetch(s, a.Z, a.ldz, a.n, row0 + step);
-        for (int j = sub; j < C; j += G) z[j] = w.none ? 0.f : w.base<ENT, !DBF16>(z[j], a.t) * a.t.inv_T;
+        for (int b = 0; b < s.each; b += NARROW_BATCH) {
+            float x[NARROW_BATCH];
+#pragma unroll
+            for (int i = 0; i < NARROW_BATCH; ++i) x[i] = z[sub + (b + i) * G];
+#pragma unroll
+            for (int i = 0; i < NARROW_BATCH; ++i) {
+                const float g = w.none ? 0.f : w.base<ENT, !DBF16>(x[i], a.t) * a.t.inv_T;
+                if (sub + (b + i) * G < C) z[sub + (b + i) * G] = g;
+            }
+        }
         wave_sync();
         if (sub == 0 && !w.none)            // one lane a row: the same class may be given again
             for (int i = 0; i < a.m; ++i) {

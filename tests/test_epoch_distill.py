@@ -4,6 +4,7 @@ import pytest
 
 from paper_2508_13716_amd import binding as B
 from paper_2508_13716_amd import synth
+from tests.test_answers import distill_tol
 
 
 def config(kind, dtype, dims, seed=3):
@@ -88,3 +89,32 @@ def test_epoch_distill_refuses(orc):
         assert e.value.code == B.EINVAL
     dp.run_epoch(teacher=B.make_teacher(ids, val, 4, 4, 0, 1.0, 1.0))
     dp.close()
+
+
+@pytest.mark.gpu
+def test_a_teachers_epoch_then_its_students(orc):
+    """the teacher's logits, its top classes, a student of other widths on the same vertices"""
+    import torch
+    from paper_2508_13716_amd import harness as H
+    from tests import oracle_side as O
+    teacher_dp = H.DeviceProblem(H.make_problem(config("gcn", "f32", [48, 64, 24], 7)))
+    prob = H.make_problem(config("gcn", "f32", [48, 16, 24], 7))
+    student = H.DeviceProblem(prob)
+    teacher_dp.run_epoch()
+    n, C, k, T = *teacher_dp.logits.shape, 8, 2.0
+    ws = torch.empty(max(B.logprobs_workspace_bytes(n, C, k), 256), dtype=torch.uint8, device="cuda")
+    ids, logp = torch.empty(n, k, dtype=torch.int32, device="cuda"), torch.empty(n, k, device="cuda")
+    torch.cuda.synchronize()
+    B.logprobs(n, C, teacher_dp.logits, C, B.F32, T, None, None, 0, 0, None, 0, None, None, k, ids, logp, k, ws, ws.numel(), stream=student.stream)
+    teacher = B.make_teacher(ids, logp, k, k, rest=1, temperature=T, weight=T * T)
+    loss, _ = student.run_epoch(lr=0.01, teacher=teacher)
+    got = student.results()
+    z = got["logits"].astype(np.float64)
+    ref_loss, row, dref, ex = orc.distill(z, ids.cpu().numpy(), logp.cpu().numpy(), True, T, prob.mask, 0.0, T * T)
+    # two nets that were not trained differ by 0.03 only: terms of the size of ln 24 cancel, so the loss is off by what its rows are, each within
+    # distill_tol (a share of the terms, not of their difference; 5e-6 of 1 each), and one rounding
+    row_tol, _ = distill_tol(z, ex, row, dref, T, C, k, T * T, "f32")
+    assert abs(loss - ref_loss) <= T * T / ex["norm"] * row_tol[prob.mask != 0].sum() + 2.0 ** -22 * abs(ref_loss)
+    assert O.normwise(got["db"][-1], dref.sum(0)) <= 1e-4
+    teacher_dp.close()
+    student.close()
