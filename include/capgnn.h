@@ -505,7 +505,7 @@ int capgnn_sigmoid_bce(int64_t n, int C, const float *Z, int64_t ldz, const uint
  * An empty row gives log-probabilities of -infinity, entropy 0 and stats { -infinity, -infinity }; a masked-out row gives 0
  * everywhere and top_ids of -1.  Sums are formed in float.
  * ws: capgnn_logprobs_workspace_bytes(n, C, k) (a few long rows are split over workgroups; 0 bytes: ws may be NULL).
- * Errors: EINVAL, ENOMEM (workspace too small), EHIP. */
+ * Errors: EINVAL, ENOMEM (workspace too small), EUNSUPPORTED (more than 2^30 classes; so in the calls below), EHIP. */
 size_t capgnn_logprobs_workspace_bytes(int64_t n, int C, int k);
 int capgnn_logprobs(int64_t n, int C, const void *Z, int64_t ldz, int z_dtype, float temperature, const uint8_t *mask,
                     const int32_t *ids, int64_t ldi, int m, float *logp, int64_t ldp, float *entropy, float *stats,

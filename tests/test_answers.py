@@ -85,6 +85,13 @@ def test_too_little_workspace_is_refused():
             refuse(B.EINVAL, B.logprobs, **dict(a, ws=FAKE + 8))
 
 
+def test_more_classes_than_offsets_hold_are_refused():
+    C = (1 << 30) + 1
+    refuse(B.EUNSUPPORTED, B.logprobs, **logprobs_args(n_classes=C, ldz=C))
+    refuse(B.EUNSUPPORTED, B.logprobs_bwd, **bwd_args(n_classes=C, ldz=C, lddz=C))
+    refuse(B.EUNSUPPORTED, B.distill, **distill_args(n_classes=C, ldz=C, lddz=C))
+
+
 def test_no_rows_is_no_work():
     B.logprobs(**logprobs_args(n=0, Z=None, ids=None, logp=None))
     B.logprobs_bwd(**bwd_args(n=0, Z=None, dZ=None, stats=None))
