@@ -676,12 +676,15 @@ struct GradRow {
     float m0, ln_s, inv_s, G, h, H;
     bool none;                      // masked out, or no class allowed
 
-    __device__ __forceinline__ void read(const AnswerGradArgs &a, int64_t row, bool on) {
-        ln_s = on ? a.stats[2 * row + 1] : -INFINITY;
-        none = ln_s == -INFINITY;
-        m0 = none ? 0.f : a.stats[2 * row];
-        h = !none && a.dentropy ? a.dentropy[row] : 0.f;
-        H = !none && a.dentropy ? a.entropy[row] : 0.f;
+    // (nothing is read under a condition on what was read before: one wait for all of it)
+    __device__ __forceinline__ void read(const AnswerGradArgs &a, int64_t row) {
+        const bool on = !a.mask || a.mask[row];
+        const float top = a.stats[2 * row], ln = a.stats[2 * row + 1], dh = a.dentropy ? a.dentropy[row] : 0.f, e = a.dentropy ? a.entropy[row] : 0.f;
+        none = !on || ln == -INFINITY;
+        ln_s = none ? 0.f : ln;
+        m0 = none ? 0.f : top;
+        h = none ? 0.f : dh;
+        H = none ? 0.f : e;
         inv_s = expf(-ln_s);
     }
     template <bool ENT, bool EXACT = true> __device__ __forceinline__ float base(float z, const TempScale &t) const {
@@ -707,10 +710,10 @@ __global__ __launch_bounds__(THREADS) void answers_grad_rows_kernel(AnswerGradAr
         const char *z = a.Z + row * a.ldz * (BF16 ? 2 : 4);
         char *dz = a.dZ + row * a.lddz * (DBF16 ? 2 : 4);
         GradRow w;
-        w.read(a, row, !a.mask || a.mask[row]);
+        w.read(a, row);
         raw16 r[GRAD_VECTORS];
         int from = 0;
-        if (!w.none)
+        if (!a.mask || a.mask[row])         // (before what the row's sums say)
 #pragma unroll
             for (int i = 0; i < GRAD_VECTORS; ++i)
                 if (lo + i * THREADS * V < hi) r[i] = R::load_until(z, lo + (i * THREADS + static_cast<int>(threadIdx.x)) * V, hi, &from);
@@ -721,10 +724,11 @@ __global__ __launch_bounds__(THREADS) void answers_grad_rows_kernel(AnswerGradAr
             const int i = threadIdx.x + o * THREADS;
             mine[o] = -1;
             if (o * THREADS >= a.m) break;
-            if (i < a.m && !w.none) {
-                const int c = a.ids[row * a.ldi + i];
+            if (i < a.m) {
+                const int c = w.none ? -1 : a.ids[row * a.ldi + i];
+                const float read = a.dlogp[row * a.lddp + i];
                 const bool ok = c >= 0 && c < a.C;
-                const float gi = ok ? a.dlogp[row * a.lddp + i] : 0.f;
+                const float gi = ok ? read : 0.f;
                 id[i] = ok ? c : -1;
                 g[i] = gi;
                 G += gi;
@@ -770,7 +774,7 @@ __global__ __launch_bounds__(THREADS) void answers_grad_rows_kernel(AnswerGradAr
     }
 }
 
-// Few classes: the rows' gradients take their logits' places in LDS and leave in whole vectors.  60000 x 41: 9.3 us, of which a launch and its
+// Few classes: the rows' gradients take their logits' places in LDS and leave in whole vectors.  60000 x 41: 9.4 us, of which a launch and its
 // way through Python are most (kernel 6-7 us).
 template <bool BF16, bool DBF16, bool ENT>
 __global__ __launch_bounds__(64 * NARROW_WAVES) void answers_grad_narrow_kernel(AnswerGradArgs a, NarrowShape s) {
@@ -786,13 +790,16 @@ __global__ __launch_bounds__(64 * NARROW_WAVES) void answers_grad_narrow_kernel(
     for (; row0 < a.n; row0 += step) {
         const int64_t row = row0 + (lane >> s.lg) < a.n ? row0 + (lane >> s.lg) : a.n - 1;
         GradRow w;
-        w.read(a, row, !a.mask || a.mask[row]);
-        w.G = 0.f;
-        if (!w.none)
-            for (int i = 0; i < a.m; ++i) {
-                const int c = a.ids[row * a.ldi + i];
-                if (c >= 0 && c < C) w.G += a.dlogp[row * a.lddp + i];
-            }
+        w.read(a, row);
+        int c0 = a.m ? a.ids[row * a.ldi] : -1;                 // the first class given (often the only one), and its gradient
+        const float g0 = a.m ? a.dlogp[row * a.lddp] : 0.f;
+        if (c0 >= C || w.none) c0 = -1;
+        w.G = c0 >= 0 ? g0 : 0.f;
+        for (int i = 1; i < a.m; ++i) {
+            const int c = a.ids[row * a.ldi + i];
+            const float g = a.dlogp[row * a.lddp + i];
+            if (c >= 0 && c < C) w.G += g;
+        }
         next.put(s, tile);
         wave_sync();
         if (row0 + step < a.n) next.fetch(s, a.Z, a.ldz, a.n, row0 + step);
@@ -807,11 +814,13 @@ __global__ __launch_bounds__(64 * NARROW_WAVES) void answers_grad_narrow_kernel(
             }
         }
         wave_sync();
-        if (sub == 0 && !w.none)            // one lane a row: the same class may be given again
-            for (int i = 0; i < a.m; ++i) {
+        if (sub == 0 && !w.none) {          // one lane a row: the same class may be given again
+            if (c0 >= 0) z[c0] = fmaf(g0, a.t.inv_T, z[c0]);
+            for (int i = 1; i < a.m; ++i) {
                 const int c = a.ids[row * a.ldi + i];
                 if (c >= 0 && c < C) z[c] = fmaf(a.dlogp[row * a.lddp + i], a.t.inv_T, z[c]);
             }
+        }
         wave_sync();
         narrow_store<BF16, DBF16>(s, tile, a.dZ, a.lddz, a.n, row0, false);
         wave_sync();
@@ -868,9 +877,10 @@ extern "C" int capgnn_logprobs(int64_t n, int C, const void *Z, int64_t ldz, int
     w.parts = answer_parts(n, C, &w.chunk);
     w.sums = static_cast<float4 *>(ws);
     w.keys = reinterpret_cast<unsigned long long *>(static_cast<char *>(ws) + align_up(sizeof(float4) * n * w.parts, 256));
-    // A wave alone walks rows of one tile and, where there are enough rows for two waves on every SIMD, rows up to ANSWER_WAVE_C classes, half as many for long lists (no meeting
-    // of waves: 3001 x 10007 bf16, k = 10, 40 us by workgroups of four waves, 23 by waves; 8000 x 5000 fp32 82 and 36; but 600 x 10007
-    // fp32 15 and 19, and from 33000 classes on no difference; k = 64: 8000 x 5000 fp32 95 and 72, 2500 x 16384 bf16 41 and 70).
+    // A wave alone walks rows of one tile and, where there are enough rows for two waves on every SIMD, rows up to ANSWER_WAVE_C classes, half
+    // as many for long lists (no meeting of waves: 3001 x 10007 bf16, k = 10, 40 us by workgroups of four waves, 23 by waves; 8000 x 5000
+    // fp32 82 and 36; but 600 x 10007 fp32 15 and 19, and from 33000 classes on no difference; k = 64: 8000 x 5000 fp32 95 and 72, 2500 x
+    // 16384 bf16 41 and 70).
     const bool wave = w.chunk <= 64 * ANSWER_VECTORS * (bf16 ? 8 : 4) || (n >= 2048 && C <= (k > 32 ? ANSWER_WAVE_C / 2 : ANSWER_WAVE_C));
     const unsigned grid = static_cast<unsigned>(std::min<int64_t>(n * w.parts, 1 << 24));
     auto go = [&](auto kernel, int threads) { hipLaunchKernelGGL(kernel, dim3(grid), dim3(threads), 0, st, a, w); };

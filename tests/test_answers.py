@@ -163,7 +163,7 @@ def stream():
     return torch.cuda.current_stream()
 
 
-def run_logprobs(Zd, C, dtype, T, mask, ids, k, ids_pad=1, m=None):
+def run_logprobs(Zd, C, dtype, T, mask, ids, k, ids_pad=1):
     import torch
     n, ld = Zd.shape[0], Zd.stride(0)
     m = ids.shape[1]
@@ -539,7 +539,6 @@ def test_teacher_to_student_chain_vs_oracle(n, C, k, rest):
     p = np.exp(orc.row_softmax(Zs)[0])
     check("dZ", out["dZ"].cpu().numpy(), dce + dkd, dz_tol + mask[:, None] * (p * 2 * sum_err(C) + 8 * EPS * (np.arange(C) == y[:, None])) / max(mask.sum(), 1) +
           2 * EPS * np.abs(dce + dkd))
-    g, h = np.linspace(-1, 1, n), np.linspace(1, -2, n)
     g, h = out["g"].cpu().numpy().astype(np.float64), out["h"].cpu().numpy().astype(np.float64)
     ref = orc.logprobs(Zs, y[:, None], 0, 1.0, mask)
     dref = orc.logprobs_bwd(Zs, y[:, None], g, h, 1.0, mask)
