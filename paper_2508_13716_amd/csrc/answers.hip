@@ -648,9 +648,14 @@ __global__ __launch_bounds__(256) void answers_join_kernel(AnswerArgs a, AnswerP
     }
 }
 
-// Few rows are cut into parts, about a thousand workgroups in all and ANSWER_PART_LEAST classes or more each.
+// Few long rows are cut into parts, about a thousand workgroups in all and ANSWER_PART_LEAST classes or more each; one workgroup a row is
+// as fast where the second launch costs what the parts save.  Parts against whole rows, us, k = 20: 1 x 24000 f32 15.7 / 14.5, 1 x 40000
+// f32 15.5 / 19.7, bf16 15.1 / 16.0, 1 x 150000 f32 18.5 / 57.9, 128 x 40000 f32 20.9 / 20.9, 128 x 65536 f32 21.8 / 34.2, 200 x 40000
+// f32 21.8 / 21.3, 200 x 65536 bf16 23.0 / 22.0, 300 x 9000 f32 19.0 / 12.4, 300 x 50000 f32 28.2 / 28.4.
 constexpr int ANSWER_PART_LEAST = 2048, ANSWER_WORKGROUPS = 1024, ANSWER_WAVE_C = 16384;
+constexpr int ANSWER_LONG = 32768, ANSWER_FEW = 256;
 static int answer_parts(int64_t n, int C, int64_t *chunk) {
+    if (C < ANSWER_LONG || C / ANSWER_FEW < n) { *chunk = C; return 1; }
     int64_t parts = std::min<int64_t>(std::min<int64_t>(ANSWER_PARTS, ANSWER_WORKGROUPS / std::max<int64_t>(n, 1)), (C + ANSWER_PART_LEAST - 1) / ANSWER_PART_LEAST);
     if (parts <= 1) { *chunk = C; return 1; }
     *chunk = (C + parts - 1) / parts;
@@ -936,6 +941,8 @@ extern "C" int capgnn_logprobs_bwd(int64_t n, int C, const void *Z, int64_t ldz,
             hipLaunchKernelGGL((answers_grad_narrow_kernel<z.value, d.value, e.value>), dim3(narrow_grid(s, n, lds)), dim3(64 * NARROW_WAVES), lds, st, a, s);
         });
     } else {
+        // One wave a row where it holds the row, 256 threads on longer ones: 50000 rows of 600 f32 49 us against 87 with 256 threads, 1000
+        // f32 87 / 116, 2000 bf16 84 / 114.
         const int V = zb ? 8 : 4, threads = C <= 64 * GRAD_VECTORS * V ? 64 : 256;
         const int chunks = (C + threads * GRAD_VECTORS * V - 1) / (threads * GRAD_VECTORS * V);
         const unsigned grid = static_cast<unsigned>(std::min<int64_t>(n * chunks, 1 << 24));

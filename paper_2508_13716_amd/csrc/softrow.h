@@ -196,6 +196,8 @@ __device__ __forceinline__ int uniform_anew(int x) {
 // 612000 rows were bound by them, not by memory).  The next rows' loads are under way while a wave works on its own.  A row starts
 // G * odd words after the one before it: lanes that read the same class of their rows at once hit different banks.  A lane reads its
 // classes NARROW_BATCH at a time; what is behind a row's end holds -inf (narrow_ends).
+// Up to NARROW_C classes it is the faster one throughout, against a wave a row, us: answers of 100000 rows of 100 f32 26 / 234, 200 f32
+// 50 / 494, 256 bf16 88 / 648; their gradient, 100 f32 22 / 169, 256 bf16 39 / 157; distillation, 100 f32 42 / 125, 200 f32 62 / 122.
 constexpr int NARROW_C = 256;
 constexpr int NARROW_G = NARROW_C / 32;     // lanes of a row at most
 constexpr int NARROW_BATCH = 8;
