@@ -240,19 +240,51 @@ __device__ __forceinline__ void no_gradient(const DistillArgs &a, char *dz, int 
     for (; j < hi; ++j) st_grad<DBF16>(dz, j, 0.f);
 }
 
-// The divergence of one row, in the first wave (every lane); S the sum of all exponentials, others that of the classes not listed.
-__device__ __forceinline__ double divergence(const DistillArgs &a, const Teacher &t, float m0, float S, float others) {
-    const float ln_s = logf(S);
+// A row's divergence with `rest`, sum q (ln q - d/T + ln S) over the listed classes d = z - m0 plus r (ln r + ln S - ln others), is the small
+// difference of its terms where the student is close to the teacher.  So ln others is taken out of all of them where the others have the
+// larger part: sum q (ln q - d/T + ln others) + ln(1 + listed / others) + r ln(1 - Q).  Every rounding then counts with a listed class's
+// q or p, and one of the others' sum with P - r, where logarithms of S, others and r by themselves left 1e-7 of a divergence of 1e-4.
+// d/T is taken from L as the exponentials have it, so that its rounding means another temperature, not another distribution.
+struct RestTerms {
+    float ln0;              // added to every listed class's ln q - d/T
+    double tail;            // the rest of the divergence; Q + r = mass
+};
+__device__ __forceinline__ RestTerms rest_terms(double r, float mass, float others, float listed) {
+    const bool near = others >= listed;
+    RestTerms w;
+    w.ln0 = logf(near ? others : others + listed);
+    w.tail = 0.0;
+    if (near) w.tail = static_cast<double>(log1pf(listed / others)) * (r > 0.0 ? 1.f : mass);
+    else if (r > 0.0) w.tail = r * (w.ln0 - logf(others));
+    if (r > 0.0) w.tail += r * (r > 0.5 ? log1pf(-static_cast<float>(1.0 - r)) : logf(static_cast<float>(r)));
+    return w;
+}
+__device__ __forceinline__ double rest_listed(float q, float z, float m0, const TempScale &t, float ln0) {
+    return q * (static_cast<double>(logf(q) + ln0) - (static_cast<double>(z) - m0) * (t.L * 0.6931471805599453094));
+}
+
+// The divergence of one row, in the first wave (every lane): others and listed are the sums of the exponentials (without REST others has all).
+template <bool REST>
+__device__ __forceinline__ double divergence(const DistillArgs &a, const Teacher &t, float m0, float others, float listed) {
     double kl = 0.0;
+    if constexpr (REST) {
+        const RestTerms w = rest_terms(t.r, t.mass, others, listed);
 #pragma unroll 1
-    for (int i = threadIdx.x; i < a.k; i += 64) {
-        const float q = t.q[i];
-        // (q d before 1/T: d / T may leave float's range)
-        if (t.c[i] >= 0 && q != 0.f) kl += static_cast<double>(fmaf(-q * (t.z[i] - m0), a.t.inv_T, q * (logf(q) + ln_s)));
+        for (int i = threadIdx.x; i < a.k; i += 64) {
+            const float q = t.q[i];
+            if (t.c[i] >= 0 && q != 0.f) kl += rest_listed(q, t.z[i], m0, a.t, w.ln0);
+        }
+        if (threadIdx.x == 0) kl += w.tail;
+    } else {
+        const float ln_s = logf(others);
+#pragma unroll 1
+        for (int i = threadIdx.x; i < a.k; i += 64) {
+            const float q = t.q[i];
+            // (q d before 1/T: d / T may leave float's range)
+            if (t.c[i] >= 0 && q != 0.f) kl += static_cast<double>(fmaf(-q * (t.z[i] - m0), a.t.inv_T, q * (logf(q) + ln_s)));
+        }
     }
-    kl = wave_all(kl, OpSum());
-    if (t.r > 0.0) kl += t.r * (logf(static_cast<float>(t.r)) - (logf(others) - ln_s));
-    return kl;
+    return wave_all(kl, OpSum());
 }
 
 // Sum of the listed classes' exponentials: the first wave's.
@@ -367,7 +399,7 @@ __global__ __launch_bounds__(THREADS) __attribute__((amdgpu_waves_per_eu(4))) vo
             continue;
         }
         if (first_wave && part == 0) {
-            const double kl = divergence(a, t, m0, S, others);
+            const double kl = divergence<REST>(a, t, m0, others, REST ? listed : 0.f);
             loss += kl;
             if (a.row_loss && threadIdx.x == 0) a.row_loss[row] = static_cast<float>(kl);
         }
@@ -554,7 +586,7 @@ __global__ __launch_bounds__(64 * NARROW_WAVES) __attribute__((amdgpu_waves_per_
         }
         const float S = others + listed;
         const bool live = on && entries > 0 && S != 0.f;
-        const float ln_s = logf(S), inv_s = 1.f / S;
+        const float inv_s = 1.f / S;
         float mass = scale, away = scale;
         double r = 0.0;
         if constexpr (REST) {
@@ -581,16 +613,20 @@ __global__ __launch_bounds__(64 * NARROW_WAVES) __attribute__((amdgpu_waves_per_
         }
         wave_sync();
         double kl = 0.0;
-        if (live)
+        if (live) {
+            const float ln_s = REST ? 0.f : logf(S);
+            RestTerms rest = {};
+            if constexpr (REST) rest = rest_terms(r, static_cast<float>(Q + r), others, listed);
+            if (sub == 0) kl = rest.tail;
             for (int i = sub; i < k; i += G) {
                 const float p = q[i], d = w[i] - m0;
                 if (p == -1.f) continue;
-                if (p != 0.f) kl += static_cast<double>(fmaf(-p * d, a.t.inv_T, p * (logf(p) + ln_s)));      // (q d before 1/T, as above)
+                if (p != 0.f) kl += REST ? rest_listed(p, w[i], m0, a.t, rest.ln0) : static_cast<double>(fmaf(-p * d, a.t.inv_T, p * (logf(p) + ln_s)));    // (as above)
                 z[id[i]] = fmaf(exp_scaled(difference(w[i], m0, a.t), a.t) * inv_s, mass, -p * scale);
             }
+        }
         for (int off = 1; off < G; off <<= 1) kl += __shfl_xor(kl, off);
         if (sub == 0) {
-            if (REST && live && r > 0.0) kl += r * (logf(static_cast<float>(r)) - (logf(others) - ln_s));
             loss += kl;
             if (in && a.row_loss) a.row_loss[row] = static_cast<float>(kl);
         }

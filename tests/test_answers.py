@@ -384,6 +384,30 @@ def distill_tol(Z, ex, row, dref, T, C, k, weight, dz_dtype):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("T", [1.0, 2.25, 3.0])
+@pytest.mark.parametrize("n,C,k", [(40, 200, 2), (30, 250, 1), (30, 2000, 4), (9, 5000, 8), (5, 40001, 8), (2, 131072, 20)])
+def test_small_divergences_keep_their_digits(n, C, k, T):
+    """A student close to its teacher, nearly all mass in what is not listed: the divergence is the small difference of terms that cancel.
+    The sum of the others counts with P - r, a listed exponential with p, a listed q with q; nothing counts with r."""
+    rng = np.random.default_rng(C + k)
+    Z = to_dtype(0.1 * rng.standard_normal((n, C)), "f32")
+    ids = np.stack([rng.permutation(C)[:k] for _ in range(n)]).astype(np.int32)
+    at = lambda v: np.take_along_axis(v, ids.astype(np.int64), 1)
+    val = (at(orc.row_softmax(Z, T)[0]) + 0.05 * rng.standard_normal((n, k))).astype(np.float32)
+    _, ref, _, ex = orc.distill(Z, ids, val, True, T)
+    u = 2.0 ** -24
+    x = (Z.max(1, keepdims=True) - Z) / T
+    p, q, lq, ln0 = at(ex["p"]), at(ex["q"]), -np.log(at(ex["q"])), np.log(C)
+    # q: its rounding and its exponential (2 u) times ln(q/p) + 1, the logarithms of q and of the others (each 2 u, their sum u); a listed
+    # exponential (x + 3) u, its sum, quotient and logarithm (k + 5) u; the logarithm of r 3 u of 1 - r; the others' sum: sum_err; another
+    # temperature: u times the derivative by it; row_loss: u
+    tol = (q * u * (2 * (1 + np.abs(np.log(q / p))) + 3 * (lq + ln0) + 3) + p * u * (at(x) + k + 8) + u * np.abs(q - p) * at(x)).sum(1)
+    tol += np.abs(ex["P"] - ex["r"]) * (sum_err(C) + u * x.max(1)) + u * ref + 1e-14
+    _, row, _ = run_distill(device(Z, "f32", C), C, "f32", "f32", T, None, ids, val, 1, 0.0, 1.0, C)
+    check("row_loss", row, ref, tol)
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("dtype,dz_dtype", [("f32", "f32"), ("bf16", "bf16"), ("f32", "bf16"), ("bf16", "f32")])
 @pytest.mark.parametrize("n,C,pad,T", SIZES)
 def test_distill_vs_oracle(n, C, pad, T, dtype, dz_dtype):
