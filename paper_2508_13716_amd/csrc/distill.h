@@ -32,6 +32,49 @@ __device__ __forceinline__ float distill_norm(const DistillArgs &a) {
 
 constexpr float REST_LEAST = 9.5367431640625e-7f;       // 2^-20
 
+// Exponential and logarithm in doubles, of a few numbers a row, to some 1e-14 (what they give is stored as a float): the series of exp on
+// |r| <= ln 2 / 2 and of 2 atanh((m - 1) / (m + 1)) on 1/sqrt 2 <= m <= sqrt 2, their coefficients read where they are used.  (As constants of
+// the program they are kept in registers across the loop over the rows, next to the logits: 16 to 53 of them in scratch memory.)
+static __constant__ double exp_terms[12] = {1.0 / 39916800, 1.0 / 3628800, 1.0 / 362880, 1.0 / 40320, 1.0 / 5040, 1.0 / 720, 1.0 / 120, 1.0 / 24, 1.0 / 6,
+                                            0.5, 1.4426950408889634074, 0.69314718055994530942};
+static __constant__ double log_terms[10] = {1.0 / 17, 1.0 / 15, 1.0 / 13, 1.0 / 11, 1.0 / 9, 1.0 / 7, 1.0 / 5, 1.0 / 3, 1.0, 0.69314718055994530942};
+__device__ __forceinline__ const double *terms_anew(const double *p) {
+    asm volatile("" : "+s"(p));
+    return p;
+}
+// x from -inf (0) to what a double holds; NaN stays
+__device__ __forceinline__ double exp_wide(double x) {
+    const double *c = terms_anew(exp_terms);
+    x = x < -800.0 ? -800.0 : x > 800.0 ? 800.0 : x;
+    const double n = rint(x * c[10]), r = fma(-n, c[11], x);
+    double e = c[0];
+#pragma unroll
+    for (int i = 1; i < 10; ++i) e = fma(e, r, c[i]);
+    e = fma(e, r, 1.0);
+    return ldexp(fma(e, r, 1.0), static_cast<int>(n));
+}
+__device__ __forceinline__ double inverse(double x) {
+    double y = __builtin_amdgcn_rcp(x);
+    y = fma(y, fma(-x, y, 1.0), y);
+    return fma(y, fma(-x, y, 1.0), y);
+}
+// x > 0 and finite; NaN stays
+__device__ __forceinline__ double log_wide(double x) {
+    const double *c = terms_anew(log_terms);
+    int n;
+    double m = frexp(x, &n);
+    if (m < 0.70710678118654752) { m += m; --n; }
+    const double t = (m - 1.0) * inverse(m + 1.0), t2 = t * t;
+    double l = c[0];
+#pragma unroll
+    for (int i = 1; i < 9; ++i) l = fma(l, t2, c[i]);
+    return fma(static_cast<double>(n), c[9], 2.0 * t * l);
+}
+
+// (z - m0) / T in doubles.  1 / T is taken from L as the float exponentials have it, so that its rounding means another temperature, not another
+// distribution.
+__device__ __forceinline__ double scaled(float z, float m0, const TempScale &t) { return (static_cast<double>(z) - m0) * (t.L * 0.6931471805599453094); }
+
 // ------------------------------------------------------------------ the teacher of a row, in LDS; the first wave of a workgroup works on it
 struct Teacher {
     static constexpr int OWN = CAPGNN_GIVEN_MAX / 64;       // entries of a lane: l, l + 64, ...
@@ -44,15 +87,31 @@ struct Teacher {
     int entries;                    // that count
     float mass;                     // Q + r
     double r;                       // what the teacher leaves
+    float top;                      // rest: largest of z, and the sum of the listed classes' exponentials from there
+    double sum;
 };
 
-// The bits of the listed classes, modulo the bits there are: set by the first wave between two barriers.
-struct Seen {
-    uint32_t *bits;
-    int most;               // a power of two, at least 256
-    __device__ __forceinline__ void set(int c) const { atomicOr(&bits[(c & (most - 1)) >> 5], 1u << (c & 31)); }
-    template <int V> __device__ __forceinline__ uint32_t vector(int j) const {     // classes [j, j + V), j a multiple of V
-        return bits[(j & (most - 1)) >> 5] >> (j & 31) & ((1u << V) - 1u);
+// A bit for every listed class: set by the first wave between two barriers.  The bits of a thread's classes of a tile lie together, one read of
+// LDS a tile.  Tiles beyond those there is room for share the bits of earlier ones.
+constexpr int SEEN_BYTES = 32768;
+template <bool BF16, int THREADS, int NV> struct Seen {
+    static constexpr int V = Raw<BF16>::V, STEP = THREADS * V, TILE = NV * STEP, W = NV * V <= 32 ? 1 : NV * V <= 64 ? 2 : 4;
+    static constexpr int MOST = SEEN_BYTES / (THREADS * W * 4);             // tiles
+    typedef uint32_t Words __attribute__((ext_vector_type(W)));
+    Words *own;             // [tiles][THREADS]
+    int tiles;
+    bool shared;            // the row (or part) has more tiles
+    static int tiles_for(int classes) { return std::min((classes + TILE - 1) / TILE, MOST); }
+    __device__ __forceinline__ Words *at(int tile) const { return own + (tile < tiles ? tile : tile % tiles) * THREADS; }
+    __device__ __forceinline__ void clear() const {
+        for (int t = 0; t < tiles; ++t) own[t * THREADS + threadIdx.x] = 0u;
+    }
+    __device__ __forceinline__ void set(int c) const {                      // c: from the row's (or part's) first class on
+        const int tile = c / TILE, in = c % TILE, bit = in / STEP * V + in % V;
+        atomicOr(reinterpret_cast<uint32_t *>(at(tile) + in % STEP / V) + bit / 32, 1u << bit % 32);
+    }
+    static __device__ __forceinline__ uint32_t vector(Words w, int i) {     // the i-th of the thread's vectors
+        return w[i * V / 32] >> (i * V % 32) & ((1u << V) - 1u);
     }
 };
 
@@ -61,33 +120,38 @@ struct Seen {
 template <bool BF16>
 __device__ __forceinline__ void read_teacher(const DistillArgs &a, int64_t row, const char *z, const float *listed, Teacher &t) {
     const int lane = threadIdx.x;
-    float top = -INFINITY, v[Teacher::OWN];
+    float top = -INFINITY, top_z = -INFINITY, v[Teacher::OWN], z_of[Teacher::OWN];
     int entries = 0;
 #pragma unroll
     for (int o = 0; o < Teacher::OWN; ++o) {
         if (o * 64 >= a.k) break;
         const int i = lane + o * 64;
-        v[o] = -INFINITY;
+        v[o] = z_of[o] = -INFINITY;
+        bool here = false;
         if (i < a.k) {
             int c = a.t_ids[row * a.ldt + i];
             v[o] = a.t_val[row * a.ldt + i];
             if (c < 0 || c >= a.C || v[o] == -INFINITY) { c = -1; v[o] = -INFINITY; }
             t.id[i] = c;
             if (c >= 0) {
-                t.z[i] = listed ? listed[i] : ld_logit<BF16>(z, c);
+                t.z[i] = z_of[o] = listed ? listed[i] : ld_logit<BF16>(z, c);
+                top_z = max_of(top_z, z_of[o]);
                 top = max_of(top, v[o]);
-                ++entries;
+                here = true;
             }
         }
+        entries += __popcll(__ballot(here));
     }
-    entries = wave_all(entries, OpSum());
-    if (!a.rest) top = safe_max(wave_all(top, OpMax()));
-    double Q = 0.0, w[Teacher::OWN];
+    if (a.rest) top_z = wave_all(top_z, OpMax());
+    else top = safe_max(wave_all(top, OpMax()));
+    const float ref_z = safe_max(top_z);
+    double Q = 0.0, listed_sum = 0.0, w[Teacher::OWN];
 #pragma unroll
     for (int o = 0; o < Teacher::OWN; ++o) {
         if (o * 64 >= a.k) break;
-        w[o] = a.rest ? exp(static_cast<double>(v[o])) : static_cast<double>(exp_difference(v[o], top, a.t));      // (none: 0)
+        w[o] = a.rest ? exp_wide(v[o]) : static_cast<double>(exp_difference(v[o], top, a.t));      // (none: 0)
         Q += w[o];
+        if (a.rest) listed_sum += exp_wide(scaled(z_of[o], ref_z, a.t));
     }
     Q = wave_all(Q, OpSum());
     const double one = a.rest ? 1.0 : 1.0 / Q;
@@ -120,11 +184,15 @@ __device__ __forceinline__ void read_teacher(const DistillArgs &a, int64_t row, 
         if (i < a.k) {
             t.q[i] = sum;
             t.c[i] = c >= 0 && before == 0 ? c : -1;
+            if (a.rest && c >= 0 && before > 0) listed_sum -= exp_wide(scaled(t.z[i], ref_z, a.t));        // (the very number that was added)
         }
     }
     double r = a.rest ? 1.0 - Q : 0.0;
     if (r < REST_LEAST) r = 0.0;
+    if (a.rest) listed_sum = wave_all(listed_sum, OpSum());
     if (lane == 0) {
+        t.top = top_z;
+        t.sum = listed_sum;
         t.entries = entries;
         t.r = r;
         t.mass = static_cast<float>(a.rest ? Q + r : 1.0 + 0.0 * Q);       // (a NaN among the values reaches every class)
@@ -132,17 +200,50 @@ __device__ __forceinline__ void read_teacher(const DistillArgs &a, int64_t row, 
     wave_sync();
 }
 
-// Maximum and sum of a thread's logits of one tile, added to what it has (m, s).  With bits: only of classes that are not listed (what the row
-// gives to the others may be far below the rounding of a sum that holds the listed ones).
+// Bars the logits of a vector whose bits are set in `out`.
+template <bool BF16> __device__ __forceinline__ void bar(raw16 &r, uint32_t out) {
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+        if constexpr (BF16) {
+            const uint32_t m = (out >> (2 * w) & 1u ? 0xffffu : 0u) | (out >> (2 * w + 1) & 1u ? 0xffff0000u : 0u);
+            r[w] = (r[w] & ~m) | (Raw<true>::BARRED & m);
+        } else {
+            r[w] = out >> w & 1u ? Raw<false>::BARRED : r[w];
+        }
+    }
+}
+
+// Maximum and sum of a thread's logits of one tile, added to what it has (m, s).  REST: of the classes that are not listed; the listed ones are
+// barred in r.  The others have a maximum of their own: what the row gives to them may be far below the rounding of a sum that holds the listed
+// ones, and (from a distance of 88 T on) below the least float as well.
 template <bool BF16, int THREADS, int NV, bool REST>
-__device__ __forceinline__ void scan_tile(raw16 (&r)[NV], int t0, int hi, const DistillArgs &a, const Teacher &l, const Seen &seen, float &m, float &s) {
+__device__ __forceinline__ void scan_tile(raw16 (&r)[NV], int t0, int hi, int tile, const DistillArgs &a, const Teacher &l,
+                                          const Seen<BF16, THREADS, NV> &seen, float &m, float &s) {
     typedef Raw<BF16> R;
+    typedef Seen<BF16, THREADS, NV> S;
     const int tid = thread_anew();
     hi = uniform_anew(hi);
     float tmax = -INFINITY;
+    typename S::Words listed = 0u;
+    if constexpr (REST) listed = seen.at(tile)[tid];
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
         if (t0 + i * THREADS * R::V >= hi) continue;
+        if constexpr (REST) {
+            uint32_t out = S::vector(listed, i);
+            if (__any(out != 0)) {
+                const int j = t0 + (i * THREADS + tid) * R::V, from = j + R::V <= hi ? j : hi - R::V;
+                if (seen.shared && out) {                  // some other class may have set the bit
+                    uint32_t sure = 0;
+                    for (int b = 0; b < a.k; ++b) {
+                        const int d = l.id[b] - j;
+                        if (d >= 0 && d < R::V) sure |= 1u << d;
+                    }
+                    out &= sure;
+                }
+                bar<BF16>(r[i], out << (j < hi ? j - from : 0));
+            }
+        }
 #pragma unroll
         for (int e = 0; e < R::V; ++e) tmax = max_of(tmax, R::get(r[i], e));
     }
@@ -153,35 +254,13 @@ __device__ __forceinline__ void scan_tile(raw16 (&r)[NV], int t0, int hi, const 
     for (int i = 0; i < NV; ++i) {
         if (t0 + i * THREADS * R::V >= hi) continue;
         forget(r[i]);
-        uint32_t out = 0;
-        const int j = t0 + (i * THREADS + tid) * R::V;
-        if constexpr (REST) {
-            if (j < hi) out = seen.vector<R::V>(j);
-            if (__any(out != 0)) {
-                const int from = j + R::V <= hi ? j : hi - R::V;
-                if (a.C > seen.most && out) {           // some other class may have set the bit
-                    uint32_t sure = 0;
-                    for (int b = 0; b < a.k; ++b) {
-                        const int d = l.id[b] - j;
-                        if (d >= 0 && d < R::V) sure |= 1u << d;
-                    }
-                    out &= sure;
-                }
-                out <<= j < hi ? j - from : 0;
-#pragma unroll
-                for (int e = 0; e < R::V; ++e) {
-                    const float x = exp2_raw((R::get(r[i], e) - ref) * a.t.L);
-                    s += out >> e & 1u ? 0.f : x;
-                }
-                continue;
-            }
-        }
 #pragma unroll
         for (int e = 0; e < R::V; ++e) s += exp2_raw((R::get(r[i], e) - ref) * a.t.L);
     }
 }
 
-// SHORT: the row may be shorter than a vector
+// SHORT: the row may be shorter than a vector.  Vectors behind the row's end are barred, not left as they were: registers without a value in some
+// of the rows are taken for carried on from row to row, next to their new values.
 template <bool BF16, int THREADS, int NV, bool SHORT = THREADS == 64>
 __device__ __forceinline__ void read_tile(raw16 (&r)[NV], const char *z, int t0, int hi) {
     typedef Raw<BF16> R;
@@ -190,14 +269,18 @@ __device__ __forceinline__ void read_tile(raw16 (&r)[NV], const char *z, int t0,
     int from;
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-        if (t0 + i * THREADS * R::V >= hi) continue;
+        if (t0 + i * THREADS * R::V >= hi) {
+            r[i] = raw16{R::BARRED, R::BARRED, R::BARRED, R::BARRED};
+            continue;
+        }
         const int j = t0 + (i * THREADS + tid) * R::V;
         if (t0 + (i + 1) * THREADS * R::V <= hi) r[i] = R::load(z, j);
         else r[i] = R::template load_until<SHORT>(z, j, hi, &from);
     }
 }
 
-// dz = exp((z - m0) / T) * factor for the tile's classes, added to dz's contents when add
+// dz = exp((z - m0) / T) * factor for the tile's classes, added to dz's contents when add.  (REST: m0 is the others' maximum, and what comes out for a
+// listed class, which may lie above it, is replaced.)
 template <bool BF16, bool DBF16, int THREADS, int NV>
 __device__ __forceinline__ void grad_tile(raw16 (&r)[NV], char *dz, int t0, int hi, const TempScale &t, float m0, float factor, int add) {
     typedef Raw<BF16> R;
@@ -240,43 +323,46 @@ __device__ __forceinline__ void no_gradient(const DistillArgs &a, char *dz, int 
     for (; j < hi; ++j) st_grad<DBF16>(dz, j, 0.f);
 }
 
-// A row's divergence with `rest`, sum q (ln q - d/T + ln S) over the listed classes d = z - m0 plus r (ln r + ln S - ln others), is the small
-// difference of its terms where the student is close to the teacher.  So ln others is taken out of all of them where the others have the
-// larger part: sum q (ln q - d/T + ln others) + ln(1 + listed / others) + r ln(1 - Q).  Every rounding then counts with a listed class's
-// q or p, and one of the others' sum with P - r, where logarithms of S, others and r by themselves left 1e-7 of a divergence of 1e-4.
-// d/T is taken from L as the exponentials have it, so that its rounding means another temperature, not another distribution.
-struct RestTerms {
-    float ln0;              // added to every listed class's ln q - d/T
-    double tail;            // the rest of the divergence; Q + r = mass
+// What the row gives to the classes that are not listed: P = exp((m - m0) / T) s / S, from their own maximum and sum (m, s), next to the listed
+// classes' (top, sum); m0: the larger maximum.  P may leave float's (and double's) range; its logarithm and the others' shares of it do not.
+struct RestSums {
+    double S, own;          // over all classes, from m0; 0 for an empty row; the others' part of it
+    float m0;
+    __device__ __forceinline__ RestSums(float m, float s, float top, double sum, const TempScale &t) {
+        const double e = m == top ? 1.0 : exp_wide(-fabs(scaled(m, top, t)));
+        m0 = safe_max(max_of(m, top));
+        own = m < top ? s * e : s;
+        S = own + (m < top ? sum : sum * e);
+    }
+    // dz of a class that is not listed is this by exp((z - m) / T): (P mass - r) / s; 0 where all of them are barred
+    __device__ __forceinline__ float factor(float s, double r, float mass, float scale) const {
+        return s == 0.f ? 0.f * mass : static_cast<float>((own * mass - r * S) * inverse(S * s)) * scale;
+    }
 };
-__device__ __forceinline__ RestTerms rest_terms(double r, float mass, float others, float listed) {
-    const bool near = others >= listed;
-    RestTerms w;
-    w.ln0 = logf(near ? others : others + listed);
-    w.tail = 0.0;
-    if (near) w.tail = static_cast<double>(log1pf(listed / others)) * (r > 0.0 ? 1.f : mass);
-    else if (r > 0.0) w.tail = r * (w.ln0 - logf(others));
-    if (r > 0.0) w.tail += r * (r > 0.5 ? log1pf(-static_cast<float>(1.0 - r)) : logf(static_cast<float>(r)));
-    return w;
-}
-__device__ __forceinline__ double rest_listed(float q, float z, float m0, const TempScale &t, float ln0) {
-    return q * (static_cast<double>(logf(q) + ln0) - (static_cast<double>(z) - m0) * (t.L * 0.6931471805599453094));
-}
 
-// The divergence of one row, in the first wave (every lane): others and listed are the sums of the exponentials (without REST others has all).
+// A row's divergence with `rest`, sum q (ln q - ln p) over the listed classes plus r (ln r - ln P), ln p = (z - m0) / T - ln S, is the small
+// difference of its terms where the student is close to the teacher.  Its terms are doubles; the roundings of the others' sum count with P - r.
+__device__ __forceinline__ double rest_listed(float q, float z, float m0, const TempScale &t, double ln_S) {
+    return q * (static_cast<double>(logf(q)) + ln_S - scaled(z, m0, t));
+}
+// r (ln r - ln P), from the logarithm of r S / s
+__device__ __forceinline__ double rest_others(float s, double r, double ln, double far) { return r > 0.0 ? s == 0.f ? INFINITY : r * (ln - far) : 0.0; }
+
+// The divergence of one row, in the first wave (every lane): s its sum, or (REST) that of the others; S of RestSums.
 template <bool REST>
-__device__ __forceinline__ double divergence(const DistillArgs &a, const Teacher &t, float m0, float others, float listed) {
+__device__ __forceinline__ double divergence(const DistillArgs &a, const Teacher &t, float m, float m0, float s, double S) {
     double kl = 0.0;
     if constexpr (REST) {
-        const RestTerms w = rest_terms(t.r, t.mass, others, listed);
+        // both logarithms at once, one in the even lanes, one in the odd ones
+        const double ln = log_wide(threadIdx.x & 1 ? t.r * S * inverse(s) : S), ln_S = __shfl(ln, 0);
 #pragma unroll 1
         for (int i = threadIdx.x; i < a.k; i += 64) {
             const float q = t.q[i];
-            if (t.c[i] >= 0 && q != 0.f) kl += rest_listed(q, t.z[i], m0, a.t, w.ln0);
+            if (t.c[i] >= 0 && q != 0.f) kl += rest_listed(q, t.z[i], m0, a.t, ln_S);
         }
-        if (threadIdx.x == 0) kl += w.tail;
+        if (threadIdx.x == 1) kl += rest_others(s, t.r, ln, scaled(m, m0, a.t));
     } else {
-        const float ln_s = logf(others);
+        const float ln_s = logf(s);
 #pragma unroll 1
         for (int i = threadIdx.x; i < a.k; i += 64) {
             const float q = t.q[i];
@@ -287,20 +373,11 @@ __device__ __forceinline__ double divergence(const DistillArgs &a, const Teacher
     return wave_all(kl, OpSum());
 }
 
-// Sum of the listed classes' exponentials: the first wave's.
-__device__ __forceinline__ float listed_sum(const DistillArgs &a, const Teacher &t, float m0) {
-    float e = 0.f;
-#pragma unroll 1
-    for (int i = threadIdx.x; i < a.k; i += 64)
-        if (t.c[i] >= 0) e += exp_scaled(difference(t.z[i], m0, a.t), a.t);
-    return wave_all(e, OpSum());
-}
-
 struct DistillParts {
     int parts, chunk;       // of a row; classes of one
     float2 *sums;           // [n][parts]: maximum, sum (rest: of the classes not listed)
     float *listed;          // [n][GIVEN_MAX]: logits of the entries' classes (dZ may be Z: another part may have replaced them)
-    int seen;               // bits
+    int seen;               // tiles with bits of their own (Seen)
 };
 
 // How much of the work on a row (or a part of it) a launch does
@@ -325,8 +402,8 @@ __global__ __launch_bounds__(THREADS) __attribute__((amdgpu_waves_per_eu(4))) vo
     extern __shared__ __align__(16) uint32_t seen_bits[];
     __shared__ Teacher t;
     __shared__ float2 red[THREADS / 64];
-    __shared__ float listed;
-    const Seen seen{seen_bits, w.seen};
+    typedef Seen<BF16, THREADS, NV> S;
+    const S seen{reinterpret_cast<typename S::Words *>(seen_bits), w.seen, (PARTS ? w.chunk : a.C) > w.seen * S::TILE};
     const bool first_wave = threadIdx.x < 64;
     const float norm = distill_norm(a);
     const float scale = a.weight / norm * a.t.inv_T;
@@ -345,9 +422,9 @@ __global__ __launch_bounds__(THREADS) __attribute__((amdgpu_waves_per_eu(4))) vo
             continue;
         }
         raw16 r[NV];
-        if (STAGE != PART_GRADIENT || dz) read_tile<BF16, THREADS, NV>(r, z, lo, hi);
+        read_tile<BF16, THREADS, NV>(r, z, lo, STAGE != PART_GRADIENT || dz ? hi : lo);
         if constexpr (REST && STAGE != PART_GRADIENT) {
-            for (int i = threadIdx.x; i < w.seen / 32; i += THREADS) seen_bits[i] = 0;
+            seen.clear();
             __syncthreads();
         }
         if (first_wave) {
@@ -358,7 +435,7 @@ __global__ __launch_bounds__(THREADS) __attribute__((amdgpu_waves_per_eu(4))) vo
                     for (int i = threadIdx.x; i < a.k; i += 64) left[i] = t.z[i];
             if constexpr (REST && STAGE != PART_GRADIENT)
                 for (int i = threadIdx.x; i < a.k; i += 64)
-                    if (t.c[i] >= 0) seen.set(t.c[i]);
+                    if (t.c[i] >= lo && t.c[i] < hi) seen.set(t.c[i] - lo);
         }
         if constexpr (REST && STAGE != PART_GRADIENT) __syncthreads();
         float m = -INFINITY, s = 0.f;
@@ -371,12 +448,12 @@ __global__ __launch_bounds__(THREADS) __attribute__((amdgpu_waves_per_eu(4))) vo
             }
             group_softmax<64>(m, s, a.t, red);
         } else {
-            scan_tile<BF16, THREADS, NV, REST>(r, lo, hi, a, t, seen, m, s);
+            scan_tile<BF16, THREADS, NV, REST>(r, lo, hi, 0, a, t, seen, m, s);
             if constexpr (STAGE != ROW_HELD)
 #pragma unroll 1
-                for (int t0 = lo + TILE; t0 < hi; t0 += TILE) {
+                for (int t0 = lo + TILE, tile = 1; t0 < hi; t0 += TILE, ++tile) {
                     read_tile<BF16, THREADS, NV>(r, z, t0, hi);
-                    scan_tile<BF16, THREADS, NV, REST>(r, t0, hi, a, t, seen, m, s);
+                    scan_tile<BF16, THREADS, NV, REST>(r, t0, hi, tile, a, t, seen, m, s);
                 }
             group_softmax<THREADS>(m, s, a.t, red);
         }
@@ -385,13 +462,10 @@ __global__ __launch_bounds__(THREADS) __attribute__((amdgpu_waves_per_eu(4))) vo
             __syncthreads();
             continue;
         }
-        const float m0 = safe_max(m), others = s;
-        if (REST && first_wave) {
-            const float e = listed_sum(a, t, m0);
-            if (threadIdx.x == 0) listed = e;
-        }
         __syncthreads();
-        const float S = REST ? others + listed : s;
+        const float ref = safe_max(m);          // REST: of the others
+        const RestSums rest(m, s, REST ? t.top : m, REST ? t.sum : 0.0, a.t);
+        const float m0 = REST ? rest.m0 : ref, S = REST ? static_cast<float>(rest.S) : s;
         if (t.entries == 0 || S == 0.f) {
             if (a.row_loss && part == 0 && threadIdx.x == 0) a.row_loss[row] = 0.f;
             if (dz) no_gradient<BF16, DBF16, THREADS>(a, dz, lo, hi);
@@ -399,14 +473,12 @@ __global__ __launch_bounds__(THREADS) __attribute__((amdgpu_waves_per_eu(4))) vo
             continue;
         }
         if (first_wave && part == 0) {
-            const double kl = divergence<REST>(a, t, m0, others, REST ? listed : 0.f);
+            const double kl = divergence<REST>(a, t, m, m0, s, rest.S);
             loss += kl;
             if (a.row_loss && threadIdx.x == 0) a.row_loss[row] = static_cast<float>(kl);
         }
         if (dz) {
-            const float inv_s = 1.f / S, mass = t.mass * scale;
-            // (others = 0: every class that is not listed has p = 0)
-            const float away = !REST || t.r == 0.0 ? mass : others == 0.f ? 0.f : static_cast<float>(t.mass - t.r * (static_cast<double>(S) / others)) * scale;
+            const float inv_s = 1.f / S, mass = t.mass * scale, away = REST ? rest.factor(s, t.r, t.mass, scale) : mass * inv_s;
             if (a.accumulate) {         // what the listed classes hold, before anything is written
                 if (first_wave)
                     for (int i = threadIdx.x; i < a.k; i += 64)
@@ -415,18 +487,18 @@ __global__ __launch_bounds__(THREADS) __attribute__((amdgpu_waves_per_eu(4))) vo
             }
             // a longer row: its last tile is still there, the others come again, the latest first
             int t0 = STAGE == ROW_READ_TWICE ? lo + (hi - lo - 1) / TILE * TILE : lo;
-            grad_tile<BF16, DBF16, THREADS, NV>(r, dz, t0, hi, a.t, m0, away * inv_s, a.accumulate);
+            grad_tile<BF16, DBF16, THREADS, NV>(r, dz, t0, hi, a.t, ref, away, a.accumulate);
             if constexpr (STAGE == ROW_READ_TWICE) {
 #pragma unroll 1
                 for (t0 -= TILE; t0 >= lo; t0 -= TILE) {
                     read_tile<BF16, THREADS, NV>(r, z, t0, hi);
-                    grad_tile<BF16, DBF16, THREADS, NV>(r, dz, t0, hi, a.t, m0, away * inv_s, a.accumulate);
+                    grad_tile<BF16, DBF16, THREADS, NV>(r, dz, t0, hi, a.t, ref, away, a.accumulate);
                 }
             } else if constexpr (STAGE == PART_GRADIENT) {
 #pragma unroll 1
                 for (t0 += TILE; t0 < hi; t0 += TILE) {
                     read_tile<BF16, THREADS, NV>(r, z, t0, hi);
-                    grad_tile<BF16, DBF16, THREADS, NV>(r, dz, t0, hi, a.t, m0, away * inv_s, a.accumulate);
+                    grad_tile<BF16, DBF16, THREADS, NV>(r, dz, t0, hi, a.t, ref, away, a.accumulate);
                 }
             }
             __syncthreads();
@@ -487,6 +559,8 @@ __global__ __launch_bounds__(64 * NARROW_WAVES) __attribute__((amdgpu_waves_per_
 #pragma unroll
             for (int i = 0; i < NARROW_ENTRIES; ++i) {
                 const int item = i * 64 + anew;
+                c[i] = -1;                                  // (as the vectors of read_tile)
+                v[i] = 0.f;
                 if (i * 64 >= items) continue;              // (the same for all lanes)
                 int r = item * magic >> 20;
                 const int e = item - __mul24(r, k);
@@ -514,19 +588,23 @@ __global__ __launch_bounds__(64 * NARROW_WAVES) __attribute__((amdgpu_waves_per_
         }
         wave_sync();
         if (row0 + step < a.n) next.fetch(s, a.Z, a.ldz, a.n, row0 + step);
-        float m = -INFINITY;
-        for (int b = 0; b < s.each; b += NARROW_BATCH)
+        // REST: the largest logit of the listed classes and, once these are barred, of the others; else the row's and the teacher's
+        auto largest = [&] {
+            float m = -INFINITY;
+            for (int b = 0; b < s.each; b += NARROW_BATCH)
 #pragma unroll
-            for (int i = 0; i < NARROW_BATCH; ++i) m = max_of(m, z[sub + (b + i) * G]);
-        float top = -INFINITY;
+                for (int i = 0; i < NARROW_BATCH; ++i) m = max_of(m, z[sub + (b + i) * G]);
+            return m;
+        };
+        float m = REST ? -INFINITY : largest(), top = -INFINITY;
         int entries = 0;
         for (int i = sub; i < k; i += G)
             if (id[i] >= 0) {
-                top = max_of(top, w[i]);
+                top = max_of(top, REST ? z[id[i]] : w[i]);
                 ++entries;
             }
         for (int off = 1; off < G; off <<= 1) {
-            m = max_of(m, __shfl_xor(m, off));
+            if constexpr (!REST) m = max_of(m, __shfl_xor(m, off));
             top = max_of(top, __shfl_xor(top, off));
             entries += __shfl_xor(entries, off);
         }
@@ -535,7 +613,7 @@ __global__ __launch_bounds__(64 * NARROW_WAVES) __attribute__((amdgpu_waves_per_
         for (int i = sub; i < k; i += G)
             if (id[i] >= 0) {
                 if constexpr (REST) {
-                    const double p = exp(static_cast<double>(w[i]));
+                    const double p = exp(static_cast<double>(w[i]));       // (the library's: reading coefficients for every entry takes longer)
                     Q += p;
                     w[i] = static_cast<float>(p);
                 } else {
@@ -550,8 +628,6 @@ __global__ __launch_bounds__(64 * NARROW_WAVES) __attribute__((amdgpu_waves_per_
         }
         const float one = REST ? 1.f : 1.f / sum;
         wave_sync();
-        const float m0 = safe_max(m);
-        float listed = 0.f;
         for (int i = sub; i < k; i += G) {          // q: of the class in all, at its first mention; -1 elsewhere
             const int c = id[i];
             float p = 0.f;
@@ -563,7 +639,6 @@ __global__ __launch_bounds__(64 * NARROW_WAVES) __attribute__((amdgpu_waves_per_
                 p += hit ? w[b] : 0.f;
             }
             q[i] = first ? p * one : -1.f;
-            if (REST && first) listed += exp2_raw(difference(z[c], m0, a.t) * a.t.L);
         }
         wave_sync();
         for (int i = sub; i < k; i += G) {          // w: the class's logit from here on
@@ -572,41 +647,56 @@ __global__ __launch_bounds__(64 * NARROW_WAVES) __attribute__((amdgpu_waves_per_
             if constexpr (REST) z[id[i]] = -INFINITY;
         }
         wave_sync();
+        if constexpr (REST) {
+            m = largest();
+            for (int off = 1; off < G; off <<= 1) m = max_of(m, __shfl_xor(m, off));
+        }
+        const float ref = safe_max(m), ref_z = safe_max(top);       // REST: of the others (as in scan_tile), of the listed classes
+        float m0 = ref;
+        double listed = 0.0;
         float others = 0.f;
+        if constexpr (REST)
+            for (int i = sub; i < k; i += G)
+                if (q[i] != -1.f) listed += exp(scaled(w[i], ref_z, a.t));
         for (int b = 0; b < s.each; b += NARROW_BATCH) {
             float x[NARROW_BATCH];
 #pragma unroll
             for (int i = 0; i < NARROW_BATCH; ++i) x[i] = z[sub + (b + i) * G];
 #pragma unroll
-            for (int i = 0; i < NARROW_BATCH; ++i) others += exp2_raw((x[i] - m0) * a.t.L);
+            for (int i = 0; i < NARROW_BATCH; ++i) others += exp2_raw((x[i] - ref) * a.t.L);
         }
         for (int off = 1; off < G; off <<= 1) {
             others += __shfl_xor(others, off);
             if constexpr (REST) listed += __shfl_xor(listed, off);
         }
-        const float S = others + listed;
+        float S = others, mass, away;
+        double ln_S = 0.0, tail = 0.0;
+        if constexpr (REST) {
+            double r = 1.0 - Q;
+            if (r < REST_LEAST) r = 0.0;
+            mass = static_cast<float>(Q + r);
+            const RestSums rest(m, others, top, listed, a.t);
+            m0 = rest.m0;
+            S = static_cast<float>(rest.S);
+            away = rest.factor(others, r, mass, scale);
+            mass *= scale;
+            ln_S = log_wide(rest.S);
+            tail = rest_others(others, r, log_wide(r * rest.S * inverse(others)), scaled(m, m0, a.t));
+        } else {
+            mass = (1.f + 0.f * sum) * scale;         // (a NaN among the teacher's values reaches every class)
+        }
         const bool live = on && entries > 0 && S != 0.f;
         const float inv_s = 1.f / S;
-        float mass = scale, away = scale;
-        double r = 0.0;
-        if constexpr (REST) {
-            r = 1.0 - Q;
-            if (r < REST_LEAST) r = 0.0;
-            mass = static_cast<float>(Q + r) * scale;
-            // (others = 0: every class that is not listed has p = 0)
-            away = r == 0.0 ? mass : others == 0.f ? 0.f : static_cast<float>(Q + r - r * (static_cast<double>(S) / others)) * scale;
-        } else {
-            mass = away = (1.f + 0.f * sum) * scale;         // (a NaN among the teacher's values reaches every class)
-        }
+        if constexpr (!REST) away = mass * inv_s;
         if (a.dZ) {
-            const float none = a.accumulate ? -0.f : 0.f, factor = away * inv_s;       // (adding -0 leaves everything as it is)
+            const float none = a.accumulate ? -0.f : 0.f;       // (adding -0 leaves everything as it is)
             for (int b = 0; b < s.each; b += NARROW_BATCH) {
                 float x[NARROW_BATCH];
 #pragma unroll
                 for (int i = 0; i < NARROW_BATCH; ++i) x[i] = z[sub + (b + i) * G];
 #pragma unroll
                 for (int i = 0; i < NARROW_BATCH; ++i) {
-                    const float g = exp_scaled<!DBF16>(difference(x[i], m0, a.t), a.t) * factor;
+                    const float g = exp_scaled<!DBF16>(difference(x[i], ref, a.t), a.t) * away;
                     if (sub + (b + i) * G < C) z[sub + (b + i) * G] = live ? g : none;
                 }
             }
@@ -615,13 +705,11 @@ __global__ __launch_bounds__(64 * NARROW_WAVES) __attribute__((amdgpu_waves_per_
         double kl = 0.0;
         if (live) {
             const float ln_s = REST ? 0.f : logf(S);
-            RestTerms rest = {};
-            if constexpr (REST) rest = rest_terms(r, static_cast<float>(Q + r), others, listed);
-            if (sub == 0) kl = rest.tail;
+            if (REST && sub == 0) kl = tail;
             for (int i = sub; i < k; i += G) {
                 const float p = q[i], d = w[i] - m0;
                 if (p == -1.f) continue;
-                if (p != 0.f) kl += REST ? rest_listed(p, w[i], m0, a.t, rest.ln0) : static_cast<double>(fmaf(-p * d, a.t.inv_T, p * (logf(p) + ln_s)));    // (as above)
+                if (p != 0.f) kl += REST ? rest_listed(p, w[i], m0, a.t, ln_S) : static_cast<double>(fmaf(-p * d, a.t.inv_T, p * (logf(p) + ln_s)));    // (as above)
                 z[id[i]] = fmaf(exp_scaled(difference(w[i], m0, a.t), a.t) * inv_s, mass, -p * scale);
             }
         }
@@ -655,26 +743,28 @@ void launch_distill(const DistillArgs &a, DistillParts w, int *groups, hipStream
         hipLaunchKernelGGL((distill_narrow_kernel<BF16, DBF16, REST>), dim3(*groups), dim3(64 * NARROW_WAVES), lds, st, a, s);
         return;
     }
-    w.seen = 256;
-    while (w.seen < a.C && w.seen < 1 << 18) w.seen *= 2;
-    const size_t lds = REST ? w.seen / 8 : 0;
     *groups = static_cast<int>(std::min<int64_t>(a.n * w.parts, DISTILL_GROUPS));
     // The fewest threads that hold a row (more rows on a compute unit, whose chains overlap: 2999 x 10007 fp32 with 512 threads 102 us, with 256
     // 72; 12 vectors a thread rather than 16 there, which spills: 63.6 and 62.1 us).
-    auto go = [&](auto kernel, int threads, size_t bytes) { hipLaunchKernelGGL(kernel, dim3(*groups), dim3(threads), bytes, st, a, w); };
+    auto go = [&](auto kernel, auto seen) {
+        typedef decltype(seen) S;
+        constexpr int threads = S::STEP / V;
+        w.seen = S::tiles_for(w.parts > 1 ? w.chunk : a.C);
+        hipLaunchKernelGGL(kernel, dim3(*groups), dim3(threads), REST ? w.seen * threads * sizeof(typename S::Words) : 0, st, a, w);
+    };
     if (w.parts > 1) {
-        go(distill_rows_kernel<BF16, DBF16, 256, 8, REST, PART_SUMS>, 256, lds);
-        go(distill_rows_kernel<BF16, DBF16, 256, 8, REST, PART_GRADIENT>, 256, 0);
+        go(distill_rows_kernel<BF16, DBF16, 256, 8, REST, PART_SUMS>, Seen<BF16, 256, 8>());
+        go(distill_rows_kernel<BF16, DBF16, 256, 8, REST, PART_GRADIENT>, Seen<BF16, 256, 8>());
     } else if (a.C <= 64 * 8 * V) {
-        go(distill_rows_kernel<BF16, DBF16, 64, 8, REST, ROW_HELD>, 64, lds);
+        go(distill_rows_kernel<BF16, DBF16, 64, 8, REST, ROW_HELD>, Seen<BF16, 64, 8>());
     } else if (a.C <= 256 * 8 * V) {
-        go(distill_rows_kernel<BF16, DBF16, 256, 8, REST, ROW_HELD>, 256, lds);
+        go(distill_rows_kernel<BF16, DBF16, 256, 8, REST, ROW_HELD>, Seen<BF16, 256, 8>());
     } else if (a.C <= 256 * 12 * V) {
-        go(distill_rows_kernel<BF16, DBF16, 256, 12, REST, ROW_HELD>, 256, lds);
+        go(distill_rows_kernel<BF16, DBF16, 256, 12, REST, ROW_HELD>, Seen<BF16, 256, 12>());
     } else if (a.C <= 512 * 16 * V) {
-        go(distill_rows_kernel<BF16, DBF16, 512, 16, REST, ROW_HELD>, 512, lds);
+        go(distill_rows_kernel<BF16, DBF16, 512, 16, REST, ROW_HELD>, Seen<BF16, 512, 16>());
     } else {
-        go(distill_rows_kernel<BF16, DBF16, 512, 12, REST, ROW_READ_TWICE>, 512, lds);
+        go(distill_rows_kernel<BF16, DBF16, 512, 12, REST, ROW_READ_TWICE>, Seen<BF16, 512, 12>());
     }
 }
 

@@ -334,10 +334,22 @@ __device__ __forceinline__ void narrow_store(const NarrowShape &s, const float *
     }
 }
 
-template <typename T, typename Op> __device__ __forceinline__ T wave_all(T v, Op op) {
+// v of the lane OFF before this one, round about in its 16 (no way through LDS)
+template <int OFF, typename T> __device__ __forceinline__ T lane_before(T v) {
+    static_assert(sizeof(T) % 4 == 0, "whole registers");
+    struct Words { int w[sizeof(T) / 4]; } x = __builtin_bit_cast(Words, v);
 #pragma unroll
-    for (int off = 32; off > 0; off >>= 1) v = op(v, __shfl_xor(v, off));
-    return v;
+    for (int &w : x.w) w = __builtin_amdgcn_update_dpp(w, w, 0x120 + OFF, 0xf, 0xf, false);
+    return __builtin_bit_cast(T, x);
+}
+// op over the wave, in pairs of lanes 32, 16, 8, 4, 2 and 1 apart.  (Lanes 16, 8, ... apart hold the same by then: the one before is as good.)
+template <typename T, typename Op> __device__ __forceinline__ T wave_all(T v, Op op) {
+    v = op(v, __shfl_xor(v, 32));
+    v = op(v, __shfl_xor(v, 16));
+    v = op(v, lane_before<8>(v));
+    v = op(v, lane_before<4>(v));
+    v = op(v, lane_before<2>(v));
+    return op(v, lane_before<1>(v));
 }
 
 // op over the workgroup, the same value in every thread; red: one T per wave.  Ends with a barrier before red may be used again.

@@ -1,0 +1,63 @@
+"""capgnn_distill with the teacher's remaining probability as one more outcome, where the classes that are not listed lie far from the row's
+maximum, where there are none, and where the student is close to its teacher; and the divergence of equal logits without it.
+
+EPS = 2^-24 is one float rounding; bounds are formed from the operations as in test_answers.py.
+"""
+import numpy as np
+import pytest
+
+from oracle import oracle as orc
+from tests.test_answers import EPS, check, device, distill_tol, run_distill, sum_err, to_dtype
+
+# (n, C, k, dtype): few classes, one to eight lanes a row; a wave, 256 and 512 threads a row; rows read twice; rows in parts
+KERNELS = [(5, 2, 1, "f32"), (70, 40, 4, "f32"), (33, 47, 8, "bf16"), (9, 256, 100, "f32"), (7, 200, 20, "bf16"), (5, 600, 6, "f32"), (4, 3000, 70, "bf16"),
+           (5, 7000, 8, "f32"), (3, 9001, 8, "bf16"), (3, 10_007, 8, "f32"), (2, 20_000, 8, "bf16"), (3, 30_001, 30, "f32"), (3, 40_003, 9, "bf16"),
+           (45, 44_001, 8, "f32"), (90, 70_001, 5, "bf16"), (3, 60_001, 8, "f32"), (2, 131_077, 8, "bf16")]
+
+
+def far_rows(n, C, k, dtype, T, gap, rng):
+    """logits whose k listed classes lie gap * T above the others, a fifth of which is barred"""
+    ids = np.stack([rng.permutation(C)[:k] for _ in range(n)]).astype(np.int32)
+    Z = rng.standard_normal((n, C)) * T
+    if C > 8:
+        Z[rng.random((n, C)) < 0.2] = -np.inf
+    np.put_along_axis(Z, ids.astype(np.int64), gap * T + rng.standard_normal((n, k)) * T, 1)
+    return to_dtype(Z, dtype), ids
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("gap,T", [(80.0, 1.0), (86.0, 1.0), (88.0, 0.5), (110.0, 2.0), (300.0, 1.0), (300.0, 0.125), (600.0, 0.5), (-120.0, 1.0)])
+@pytest.mark.parametrize("n,C,k,dtype", KERNELS)
+def test_others_far_from_the_listed_classes(n, C, k, dtype, gap, T):
+    """p of the others leaves float's range: ln P is linear in their distance all the same, and their share of what the teacher leaves stays"""
+    rng = np.random.default_rng(C + 1000 + int(gap))
+    Z, ids = far_rows(n, C, k, dtype, T, gap, rng)
+    q = 0.9 * rng.dirichlet(np.ones(k), n)
+    val = np.log(q).astype(np.float32)
+    val[0] += np.float32(np.log(1.0 / 0.9) - 1e-7)              # a row with hardly a remainder
+    with np.errstate(divide="ignore", invalid="ignore"):
+        ref_loss, ref_row, dref, ex = orc.distill(Z, ids, val, True, T, weight=T * T)
+        row_tol, dz_tol = distill_tol(Z, ex, ref_row, dref, T, C, k, T * T, dtype)
+    assert np.isfinite(ref_row).all() and (ex["r"][1:] > 0.05).all()
+    # the gap itself carries one rounding of each of its operations, with all of q or r
+    row_tol = row_tol + 4 * EPS * abs(gap)
+    loss, row, dZ = run_distill(device(Z, dtype, C), C, dtype, dtype, T, None, ids, val, 1, 0.0, T * T, C)
+    check("row_loss", row, ref_row, row_tol)
+    check("dZ", dZ, dref, dz_tol)
+    check("loss", loss, ref_loss, T * T / n * row_tol.sum() + 4 * EPS * abs(ref_loss))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("n,C,k,dtype", [c for c in KERNELS if c[1] > 8])
+def test_a_large_factor_next_to_far_others_leaves_barred_classes_alone(n, C, k, dtype):
+    """gradients of 2^40 and others of 2^-120: no product on the way leaves float's range, and a barred class keeps a gradient of 0"""
+    rng = np.random.default_rng(C)
+    Z, ids = far_rows(n, C, k, dtype, 1.0, 83.0, rng)
+    val = np.log(np.full((n, k), 0.9 / k)).astype(np.float32)
+    weight = 2.0 ** 40
+    ref_loss, ref_row, dref, ex = orc.distill(Z, ids, val, True, 1.0, norm=1.0, weight=weight)
+    row_tol, dz_tol = distill_tol(Z, ex, ref_row, dref, 1.0, C, k, weight, dtype)
+    loss, row, dZ = run_distill(device(Z, dtype, C), C, dtype, dtype, 1.0, None, ids, val, 1, 1.0, weight, C)
+    assert (dZ[np.isneginf(Z)] == 0.0).all()
+    check("row_loss", row, ref_row, row_tol + 4 * EPS * 83)
+    check("dZ", dZ, dref, dz_tol)
