@@ -534,6 +534,8 @@ int capgnn_logprobs_bwd(int64_t n, int C, const void *Z, int64_t ldz, int z_dtyp
  * Entries with teacher_ids outside [0,C) or a value of -infinity are none (lists of different lengths); a class listed twice is an
  * outcome with the sum of its q.  A row without any entry left, and an empty row, adds 0 to loss and gradient; one that gives
  * a listed class with q > 0 probability 0 has an infinite loss and a finite gradient.
+ * A student close to its teacher: with rest = 1 the sum of the classes that are not listed is a float, off by some 1e-7 of itself, and counts
+ * with P - r, so small divergences keep their digits; with rest = 0 the sum over all classes is the float, and ln of it counts with 1.
  * loss_dev: device float[1]; row_loss: device float[n] or NULL (0 in masked-out rows); dZ: device [n x lddz] of dz_dtype or NULL.
  * ws: capgnn_distill_workspace_bytes(n, C).  Errors: EINVAL, ENOMEM, EHIP. */
 size_t capgnn_distill_workspace_bytes(int64_t n, int C);

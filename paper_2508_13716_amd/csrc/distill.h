@@ -73,13 +73,18 @@ __device__ __forceinline__ double log_wide(double x) {
 
 // (z - m0) / T in doubles.  1 / T is taken from L as the float exponentials have it, so that its rounding means another temperature, not another
 // distribution.
-__device__ __forceinline__ double scaled(float z, float m0, const TempScale &t) { return (static_cast<double>(z) - m0) * (t.L * 0.6931471805599453094); }
+__device__ __forceinline__ double student_scale(const TempScale &t) { return t.L * 0.6931471805599453094; }
+__device__ __forceinline__ double scaled(float z, float m0, const TempScale &t) { return (static_cast<double>(z) - m0) * student_scale(t); }
+
+// 1 / T as exp_difference has it, for the teacher's values
+__device__ __forceinline__ double teacher_scale(const TempScale &t) { return (static_cast<double>(t.L) + t.L_lo) * 0.6931471805599453094; }
 
 // ------------------------------------------------------------------ the teacher of a row, in LDS; the first wave of a workgroup works on it
 struct Teacher {
     static constexpr int OWN = CAPGNN_GIVEN_MAX / 64;       // entries of a lane: l, l + 64, ...
     alignas(16) int32_t id[CAPGNN_GIVEN_MAX];   // class of every entry, -1: none
     int32_t c[CAPGNN_GIVEN_MAX];    // the same at a class's first mention, else -1
+    float v[CAPGNN_GIVEN_MAX];      // value of the entry
     float w[CAPGNN_GIVEN_MAX];      // probability of the entry
     float q[CAPGNN_GIVEN_MAX];      // of the class in all
     float z[CAPGNN_GIVEN_MAX];      // the row's logit of the class
@@ -88,7 +93,7 @@ struct Teacher {
     float mass;                     // Q + r
     double r;                       // what the teacher leaves
     float top;                      // rest: largest of z, and the sum of the listed classes' exponentials from there
-    double sum;
+    double sum;                     // else: the same of v
 };
 
 // A bit for every listed class: set by the first wave between two barriers.  The bits of a thread's classes of a tile lie together, one read of
@@ -133,6 +138,7 @@ __device__ __forceinline__ void read_teacher(const DistillArgs &a, int64_t row, 
             v[o] = a.t_val[row * a.ldt + i];
             if (c < 0 || c >= a.C || v[o] == -INFINITY) { c = -1; v[o] = -INFINITY; }
             t.id[i] = c;
+            t.v[i] = v[o];
             if (c >= 0) {
                 t.z[i] = z_of[o] = listed ? listed[i] : ld_logit<BF16>(z, c);
                 top_z = max_of(top_z, z_of[o]);
@@ -191,8 +197,8 @@ __device__ __forceinline__ void read_teacher(const DistillArgs &a, int64_t row, 
     if (r < REST_LEAST) r = 0.0;
     if (a.rest) listed_sum = wave_all(listed_sum, OpSum());
     if (lane == 0) {
-        t.top = top_z;
-        t.sum = listed_sum;
+        t.top = a.rest ? top_z : top;
+        t.sum = a.rest ? listed_sum : Q;
         t.entries = entries;
         t.r = r;
         t.mass = static_cast<float>(a.rest ? Q + r : 1.0 + 0.0 * Q);       // (a NaN among the values reaches every class)
@@ -340,36 +346,27 @@ struct RestSums {
     }
 };
 
-// A row's divergence with `rest`, sum q (ln q - ln p) over the listed classes plus r (ln r - ln P), ln p = (z - m0) / T - ln S, is the small
-// difference of its terms where the student is close to the teacher.  Its terms are doubles; the roundings of the others' sum count with P - r.
-__device__ __forceinline__ double rest_listed(float q, float z, float m0, const TempScale &t, double ln_S) {
-    return q * (static_cast<double>(logf(q)) + ln_S - scaled(z, m0, t));
-}
 // r (ln r - ln P), from the logarithm of r S / s
 __device__ __forceinline__ double rest_others(float s, double r, double ln, double far) { return r > 0.0 ? s == 0.f ? INFINITY : r * (ln - far) : 0.0; }
 
-// The divergence of one row, in the first wave (every lane): s its sum, or (REST) that of the others; S of RestSums.
+// The divergence of one row, sum q (ln q - ln p) over the listed classes, ln p = (z - m0) / T - ln S, and with REST r (ln r - ln P): in the first
+// wave (every lane); s is the row's sum, or (REST) that of the others, S over all.  It is the small difference of its terms where the student is
+// close to the teacher.  So they are doubles, ln q comes from the teacher's value (from q only where a class is listed again), and q's
+// rounding counts with ln q - ln p.  With REST the others' sum counts with P - r; without, the roundings of S stay, some 1e-7.
 template <bool REST>
 __device__ __forceinline__ double divergence(const DistillArgs &a, const Teacher &t, float m, float m0, float s, double S) {
+    // both logarithms at once, one in the even lanes, one in the odd ones: of S and r S / s, or of S / Z with Z the sum of the teacher's exponentials
+    const double ln = log_wide(!REST ? s * inverse(t.sum) : threadIdx.x & 1 ? t.r * S * inverse(s) : S), ln_S = REST ? __shfl(ln, 0) : ln;
     double kl = 0.0;
-    if constexpr (REST) {
-        // both logarithms at once, one in the even lanes, one in the odd ones
-        const double ln = log_wide(threadIdx.x & 1 ? t.r * S * inverse(s) : S), ln_S = __shfl(ln, 0);
 #pragma unroll 1
-        for (int i = threadIdx.x; i < a.k; i += 64) {
-            const float q = t.q[i];
-            if (t.c[i] >= 0 && q != 0.f) kl += rest_listed(q, t.z[i], m0, a.t, ln_S);
-        }
-        if (threadIdx.x == 1) kl += rest_others(s, t.r, ln, scaled(m, m0, a.t));
-    } else {
-        const float ln_s = logf(s);
-#pragma unroll 1
-        for (int i = threadIdx.x; i < a.k; i += 64) {
-            const float q = t.q[i];
-            // (q d before 1/T: d / T may leave float's range)
-            if (t.c[i] >= 0 && q != 0.f) kl += static_cast<double>(fmaf(-q * (t.z[i] - m0), a.t.inv_T, q * (logf(q) + ln_s)));
-        }
+    for (int i = threadIdx.x; i < a.k; i += 64) {
+        const float q = t.q[i];
+        if (t.c[i] < 0 || q == 0.f) continue;
+        double ln_q = REST ? static_cast<double>(t.v[i]) : (static_cast<double>(t.v[i]) - t.top) * teacher_scale(a.t);     // (without REST: and ln Z)
+        if (q != t.w[i]) ln_q = log_wide(REST ? q : q * t.sum);
+        kl += q * (ln_q + ln_S - scaled(t.z[i], m0, a.t));
     }
+    if (REST && threadIdx.x == 1) kl += rest_others(s, t.r, ln, scaled(m, m0, a.t));
     return wave_all(kl, OpSum());
 }
 
@@ -608,25 +605,19 @@ __global__ __launch_bounds__(64 * NARROW_WAVES) __attribute__((amdgpu_waves_per_
             top = max_of(top, __shfl_xor(top, off));
             entries += __shfl_xor(entries, off);
         }
-        double Q = 0.0;
-        float sum = 0.f;
+        // w: the entry's probability (without REST not divided by its sum Q yet), and the lane's part of sum q ln q from the very numbers
+        double Q = 0.0, kl = 0.0;
         for (int i = sub; i < k; i += G)
             if (id[i] >= 0) {
-                if constexpr (REST) {
-                    const double p = exp(static_cast<double>(w[i]));       // (the library's: reading coefficients for every entry takes longer)
-                    Q += p;
-                    w[i] = static_cast<float>(p);
-                } else {
-                    const float p = exp_difference(w[i], top, a.t);
-                    sum += p;
-                    w[i] = p;
-                }
+                const float v = w[i];
+                const double p = REST ? exp(static_cast<double>(v)) : static_cast<double>(exp_difference(v, top, a.t));     // (exp: coefficients read for every entry take longer)
+                const float held = static_cast<float>(p);
+                Q += p;
+                w[i] = held;
+                if (held != 0.f) kl += held * (REST ? static_cast<double>(v) : static_cast<double>(v) - top);
             }
-        for (int off = 1; off < G; off <<= 1) {
-            if constexpr (REST) Q += __shfl_xor(Q, off);
-            else sum += __shfl_xor(sum, off);
-        }
-        const float one = REST ? 1.f : 1.f / sum;
+        if constexpr (!REST) kl *= teacher_scale(a.t);
+        for (int off = 1; off < G; off <<= 1) Q += __shfl_xor(Q, off);
         wave_sync();
         for (int i = sub; i < k; i += G) {          // q: of the class in all, at its first mention; -1 elsewhere
             const int c = id[i];
@@ -638,7 +629,15 @@ __global__ __launch_bounds__(64 * NARROW_WAVES) __attribute__((amdgpu_waves_per_
                 first = first && !(hit && b < i);
                 p += hit ? w[b] : 0.f;
             }
-            q[i] = first ? p * one : -1.f;
+            q[i] = first ? p : -1.f;
+            if (c >= 0 && p != w[i]) {              // a class listed again: q ln q of the sum for that of its parts (a part that is the sum stays)
+                if (w[i] != 0.f) kl -= w[i] * log_wide(w[i]);
+                if (first) {
+                    bool there = false;
+                    for (int b = 0; b < k; ++b) there = there || (id[b] == c && w[b] == p);
+                    if (!there) kl += p * log_wide(p);
+                }
+            }
         }
         wave_sync();
         for (int i = sub; i < k; i += G) {          // w: the class's logit from here on
@@ -671,6 +670,7 @@ __global__ __launch_bounds__(64 * NARROW_WAVES) __attribute__((amdgpu_waves_per_
         }
         float S = others, mass, away;
         double ln_S = 0.0, tail = 0.0;
+        const float one = REST ? 1.f : static_cast<float>(inverse(Q));
         if constexpr (REST) {
             double r = 1.0 - Q;
             if (r < REST_LEAST) r = 0.0;
@@ -683,7 +683,8 @@ __global__ __launch_bounds__(64 * NARROW_WAVES) __attribute__((amdgpu_waves_per_
             ln_S = log_wide(rest.S);
             tail = rest_others(others, r, log_wide(r * rest.S * inverse(others)), scaled(m, m0, a.t));
         } else {
-            mass = (1.f + 0.f * sum) * scale;         // (a NaN among the teacher's values reaches every class)
+            ln_S = log_wide(S * inverse(Q));
+            mass = (1.f + 0.f * one) * scale;         // (a NaN among the teacher's values reaches every class)
         }
         const bool live = on && entries > 0 && S != 0.f;
         const float inv_s = 1.f / S;
@@ -702,16 +703,21 @@ __global__ __launch_bounds__(64 * NARROW_WAVES) __attribute__((amdgpu_waves_per_
             }
         }
         wave_sync();
-        double kl = 0.0;
         if (live) {
-            const float ln_s = REST ? 0.f : logf(S);
-            if (REST && sub == 0) kl = tail;
+            // as in divergence; kl has sum q ln q
+            double d = 0.0, all = 0.0;
             for (int i = sub; i < k; i += G) {
-                const float p = q[i], d = w[i] - m0;
+                const float p = q[i];
                 if (p == -1.f) continue;
-                if (p != 0.f) kl += REST ? rest_listed(p, w[i], m0, a.t, ln_S) : static_cast<double>(fmaf(-p * d, a.t.inv_T, p * (logf(p) + ln_s)));    // (as above)
-                z[id[i]] = fmaf(exp_scaled(difference(w[i], m0, a.t), a.t) * inv_s, mass, -p * scale);
+                if (p != 0.f) d += p * (static_cast<double>(w[i]) - m0);
+                if constexpr (REST) all += p;
+                z[id[i]] = fmaf(exp_scaled(difference(w[i], m0, a.t), a.t) * inv_s, mass, -p * (scale * one));
             }
+            d *= student_scale(a.t);
+            if constexpr (REST) kl += all * ln_S - d + (sub == 0 ? tail : 0.0);
+            else kl = (kl - d) * inverse(Q) + (sub == 0 ? ln_S : 0.0);
+        } else {
+            kl = 0.0;
         }
         for (int off = 1; off < G; off <<= 1) kl += __shfl_xor(kl, off);
         if (sub == 0) {

@@ -61,3 +61,49 @@ def test_a_large_factor_next_to_far_others_leaves_barred_classes_alone(n, C, k, 
     assert (dZ[np.isneginf(Z)] == 0.0).all()
     check("row_loss", row, ref_row, row_tol + 4 * EPS * 83)
     check("dZ", dZ, dref, dz_tol)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("noise", [0.02, 0.001])
+@pytest.mark.parametrize("T", [1.0, 2.25])
+@pytest.mark.parametrize("n,C,k,dtype", [(70, 40, 4, "f32"), (33, 47, 8, "bf16"), (9, 256, 100, "f32"), (9, 200, 20, "bf16"), (5, 600, 6, "f32"),
+                                         (4, 3000, 70, "bf16"), (5, 7000, 8, "f32"), (3, 10_007, 64, "f32"), (3, 30_001, 64, "f32"),
+                                         (45, 44_001, 64, "f32"), (3, 60_001, 64, "f32"), (2, 131_077, 64, "bf16")])
+def test_small_divergences_with_most_of_the_mass_listed(n, C, k, dtype, T, noise):
+    """A student close to its teacher, four fifths and more of both on the listed classes: the terms cancel to `noise` squared.  A listed
+    class's q counts with its own ln q - ln p, the others' sum with P - r, and another temperature (T's reciprocal is a float) with q - p."""
+    rng = np.random.default_rng(C + k)
+    Z = rng.standard_normal((n, C)) * T
+    ids = np.stack([rng.permutation(C)[:k] for _ in range(n)]).astype(np.int32)
+    np.put_along_axis(Z, ids.astype(np.int64), T * (np.log(C / k) + 3.0 + rng.standard_normal((n, k))), 1)
+    Z = to_dtype(Z, dtype)
+    at = lambda v: np.take_along_axis(v, ids.astype(np.int64), 1)
+    lp = at(orc.row_softmax(Z, T)[0])
+    P = 1.0 - np.exp(lp).sum(1, keepdims=True)
+    val = (lp + P * noise * (rng.standard_normal((n, k)) - 1.0)).astype(np.float32)
+    _, ref, dref, ex = orc.distill(Z, ids, val, True, T)
+    assert (ex["P"] < 0.5).all() and ref.max() < 3 * noise ** 2 and (ex["r"] > 2.0 ** -20).all()
+    x = (Z.max(1, keepdims=True) - Z) / T
+    p, q = at(ex["p"]), at(ex["q"])
+    tol = EPS * (q * np.abs(np.log(q / p)) + np.abs(q - p) * at(x)).sum(1)
+    tol += np.abs(ex["P"] - ex["r"]) * (sum_err(C) + EPS * x.max(1)) + 2 * EPS * ref + 1e-13
+    _, row, _ = run_distill(device(Z, dtype, C), C, dtype, dtype, T, None, ids, val, 1, 0.0, 1.0, C)
+    check("row_loss", row, ref, tol)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("z,T", [(0.0, 1.0), (3.75, 0.7), (-200.0, 3.0)])
+@pytest.mark.parametrize("C,k", [(8, 4), (3, 3), (31, 31), (47, 8), (47, 47), (100, 33), (200, 128), (200, 200), (256, 256), (700, 7), (700, 200), (5000, 11),
+                                 (10_007, 32), (30_000, 255), (60_001, 64), (150_000, 3)])
+def test_equal_logits_without_a_remainder(C, k, z, T):
+    """Equal logits on both sides: every exponential is 1 and every sum a whole number, so the divergence is ln(C / k) but for the roundings of
+    q = 1/k, which count with it, and the result's own; 0 where every class is listed."""
+    for n in (1, 300 if C <= 5000 else 60):
+        Z = np.full((n, C), z)
+        ids = np.tile(np.random.default_rng(C + k).permutation(C)[:k].astype(np.int32), (n, 1))
+        val = np.full((n, k), -1.5, np.float32)
+        ref = np.full(n, np.log(C / k))
+        for dtype in ("f32", "bf16"):
+            loss, row, dZ = run_distill(device(Z, dtype, C), C, dtype, "f32", T, None, ids, val, 0, 0.0, 1.0, C)
+            check("row_loss", row, ref, 3 * EPS * ref + 1e-13)
+            check("loss", loss, ref[0], 4 * EPS * ref[0] + 1e-13)
