@@ -525,8 +525,8 @@ int capgnn_logprobs_bwd(int64_t n, int C, const void *Z, int64_t ldz, int z_dtyp
  *   rest = 0: q_a = exp(v_a / temperature) / sum_b exp(v_b / temperature), v = teacher_val[i,:], logits or log-probabilities alike:
  *             the teacher's mass is taken to lie on its k classes.
  *             row_loss[i] = sum_a q_a (ln q_a - ln p_i[t_a])
- *   rest = 1: v are log-probabilities at this temperature, q_a = exp(v_a), and what is left, r = 1 - sum_a q_a (less than 2^-20 is
- *             rounding and counts as 0), is one more outcome, "none of the k classes", which the row gives P = sum of its other p:
+ *   rest = 1: v are log-probabilities at this temperature, q_a = exp(v_a), and what is left, r = 1 - sum_a q_a (less than 2^-20, or
+ *             than 2^-13 in a row whose other classes are all barred or none, is rounding and counts as 0), is one more outcome, "none of the k classes", which the row gives P = sum of its other p:
  *             row_loss[i] = sum_a q_a (ln q_a - ln p_i[t_a]) + r (ln r - ln P).
  * loss = weight / norm * sum over masked rows of row_loss; norm = loss_norm, or the number of masked rows (at least 1) when
  * loss_norm <= 0.  (The usual weight is temperature^2.)  dZ = gradient of that loss (0 in masked-out rows); added to what dZ holds when

@@ -421,7 +421,8 @@ def distill(Z, t_ids, t_val, rest: bool = False, temperature: float = 1.0, mask=
         listed = np.zeros(C, bool)
         listed[[c for c, _ in entries]] = True
         r = 1.0 - w.sum() if rest else 0.0
-        rs[i] = r = 0.0 if r < 2.0 ** -20 else r
+        others = not np.isneginf(Z[i, ~listed]).all()           # (some class that is not listed is allowed)
+        rs[i] = r = 0.0 if r < (2.0 ** -20 if others else 2.0 ** -13) else r
         Ps[i] = P = p[i, ~listed].sum()
         with np.errstate(divide="ignore", invalid="ignore"):
             row[i] = np.where(q[i] == 0.0, 0.0, q[i] * (np.log(q[i]) - lp[i])).sum() + (r * (np.log(r) - np.log(P)) if r > 0.0 else 0.0)

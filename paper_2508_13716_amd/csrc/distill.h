@@ -31,6 +31,9 @@ __device__ __forceinline__ float distill_norm(const DistillArgs &a) {
 }
 
 constexpr float REST_LEAST = 9.5367431640625e-7f;       // 2^-20
+// Next to no other class a remainder makes the divergence infinite, so it has to be one: z / T and ln sum exp(z / T) as floats, up to some 500 each,
+// leave the sum of q off by 2^-14.
+constexpr float REST_LEAST_ALONE = 1.220703125e-4f;     // 2^-13
 
 // Exponential and logarithm in doubles, of a few numbers a row, to some 1e-14 (what they give is stored as a float): the series of exp on
 // |r| <= ln 2 / 2 and of 2 atanh((m - 1) / (m + 1)) on 1/sqrt 2 <= m <= sqrt 2, their coefficients read where they are used.  (As constants of
@@ -346,8 +349,14 @@ struct RestSums {
     }
 };
 
+// what a teacher leaves counts as, next to others of sum s (0: none, or all barred)
+__device__ __forceinline__ double rest_left(double r, float s) { return s == 0.f && r < REST_LEAST_ALONE ? 0.0 : r; }
+
 // r (ln r - ln P), from the logarithm of r S / s
-__device__ __forceinline__ double rest_others(float s, double r, double ln, double far) { return r > 0.0 ? s == 0.f ? INFINITY : r * (ln - far) : 0.0; }
+__device__ __forceinline__ double rest_others(float s, double r, double ln, double far) {
+    if (s == 0.f) return rest_left(r, s) > 0.0 ? INFINITY : 0.0;
+    return r > 0.0 ? r * (ln - far) : 0.0;
+}
 
 // The divergence of one row, sum q (ln q - ln p) over the listed classes, ln p = (z - m0) / T - ln S, and with REST r (ln r - ln P): in the first
 // wave (every lane); s is the row's sum, or (REST) that of the others, S over all.  It is the small difference of its terms where the student is
@@ -475,7 +484,8 @@ __global__ __launch_bounds__(THREADS) __attribute__((amdgpu_waves_per_eu(4))) vo
             if (a.row_loss && threadIdx.x == 0) a.row_loss[row] = static_cast<float>(kl);
         }
         if (dz) {
-            const float inv_s = 1.f / S, mass = t.mass * scale, away = REST ? rest.factor(s, t.r, t.mass, scale) : mass * inv_s;
+            const float inv_s = 1.f / S, mass = (REST ? t.mass - static_cast<float>(t.r - rest_left(t.r, s)) : t.mass) * scale;
+            const float away = REST ? rest.factor(s, t.r, t.mass, scale) : mass * inv_s;
             if (a.accumulate) {         // what the listed classes hold, before anything is written
                 if (first_wave)
                     for (int i = threadIdx.x; i < a.k; i += 64)
@@ -674,7 +684,7 @@ __global__ __launch_bounds__(64 * NARROW_WAVES) __attribute__((amdgpu_waves_per_
         if constexpr (REST) {
             double r = 1.0 - Q;
             if (r < REST_LEAST) r = 0.0;
-            mass = static_cast<float>(Q + r);
+            mass = static_cast<float>(Q + rest_left(r, others));
             const RestSums rest(m, others, top, listed, a.t);
             m0 = rest.m0;
             S = static_cast<float>(rest.S);

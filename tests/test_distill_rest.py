@@ -107,3 +107,50 @@ def test_equal_logits_without_a_remainder(C, k, z, T):
             loss, row, dZ = run_distill(device(Z, dtype, C), C, dtype, "f32", T, None, ids, val, 0, 0.0, 1.0, C)
             check("row_loss", row, ref, 3 * EPS * ref + 1e-13)
             check("loss", loss, ref[0], 4 * EPS * ref[0] + 1e-13)
+
+
+def listed_everywhere(C, k, scale, seed):
+    """rows whose teacher lists every allowed class (some of the student's others are barred), log-probabilities formed in float as z / T - ln sum"""
+    n, T = 40, 0.5
+    rng = np.random.default_rng(seed)
+    Z = scale * rng.standard_normal((n, C))
+    ids = np.stack([rng.permutation(C)[:k] for _ in range(n)]).astype(np.int32)
+    out = np.full((n, C), -np.inf)
+    np.put_along_axis(out, ids.astype(np.int64), np.take_along_axis(Z, ids.astype(np.int64), 1), 1)
+    Z = to_dtype(out, "f32")
+    t = (np.take_along_axis(Z, ids.astype(np.int64), 1) + 0.1 * scale * rng.standard_normal((n, k))).astype(np.float32) / np.float32(T)
+    top = t.max(1, keepdims=True)
+    lse = np.log(np.exp(t - top).sum(1, keepdims=True, dtype=np.float32)) + top
+    val = t - lse
+    assert val.dtype == np.float32
+    return Z, ids, val, T, 1.0 - np.exp(val.astype(np.float64)).sum(1)
+
+
+LISTED_EVERYWHERE = [(8, 8), (47, 47), (100, 100), (200, 200), (47, 20), (700, 150), (9001, 64), (40_003, 100), (131_077, 30)]
+
+
+def test_oracle_a_remainder_of_roundings_counts_as_none_where_there_is_no_other_class():
+    Z, ids, val, T, r = listed_everywhere(8, 8, 100.0, 8)
+    assert ((r >= 2.0 ** -20) & (r < 2.0 ** -13)).any()
+    loss, row, dZ, ex = orc.distill(Z, ids, val, True, T)
+    assert np.isfinite(row).all() and (ex["r"] == 0.0).all()
+    val[:, 0] -= 0.5                                    # a teacher that does leave something: there the student has nothing to give
+    loss, row, dZ, ex = orc.distill(Z, ids, val, True, T)
+    big = 1.0 - np.exp(val.astype(np.float64)).sum(1) >= 2.0 ** -13
+    assert big.any() and np.isposinf(row[big]).all() and np.isfinite(row[~big]).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("scale", [3.0, 100.0, 300.0])
+@pytest.mark.parametrize("C,k", LISTED_EVERYWHERE)
+def test_a_remainder_of_roundings_counts_as_none_where_there_is_no_other_class(C, k, scale):
+    Z, ids, val, T, r = listed_everywhere(C, k, scale, C + k)
+    assert r.max() < 2.0 ** -13
+    with np.errstate(divide="ignore", invalid="ignore"):
+        ref_loss, ref_row, dref, ex = orc.distill(Z, ids, val, True, T)
+        row_tol, dz_tol = distill_tol(Z, ex, ref_row, dref, T, C, k, 1.0, "f32")
+    assert np.isfinite(ref_row).all()
+    for rows in (slice(0, 1), slice(0, 40)):
+        loss, row, dZ = run_distill(device(Z[rows], "f32", C), C, "f32", "f32", T, None, ids[rows], val[rows], 1, 40.0, 1.0, C)
+        check("row_loss", row, ref_row[rows], row_tol[rows])
+        check("dZ", dZ, dref[rows], dz_tol[rows])
