@@ -184,7 +184,11 @@ def _p(x):
     try:
         return x.data_ptr()      # torch.Tensor
     except AttributeError:
-        return x.ctypes.data if isinstance(x, np.ndarray) else x
+        if isinstance(x, np.ndarray):
+            return x.ctypes.data
+        if isinstance(x, int):
+            return x
+        raise                    # (a str or bytes would reach the kernels as a host address)
 
 
 def _stream(s):
