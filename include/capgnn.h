@@ -576,7 +576,8 @@ typedef struct {
  *     those of the loss as loss, other_ms holds passes over a gradient alone and the update.  An epoch without times may
  *     copy the halo rows of all layers in one launch at its start, and leave those sums and the update to one at its end;
  *     its results are the same bits.
- *   ws: capgnn_epoch_workspace_bytes() (at most 64 MiB of it for parts of weight gradients kept to the epoch's end);
+ *   ws: capgnn_epoch_workspace_bytes() (at most 64 MiB of it for parts of weight gradients kept to the epoch's end; the last
+ *     capgnn_distill_workspace_bytes() of the last layer's classes, rounded up to 256, are capgnn_epoch_distill's and may be missing elsewhere);
  *     side_stream may be NULL (then everything runs on `stream`).
  * Errors: EINVAL, ENOMEM (workspace too small), EUNSUPPORTED, EHIP. */
 size_t capgnn_epoch_workspace_bytes(const capgnn_graph *g, const capgnn_cache *c,

@@ -377,7 +377,7 @@ struct EpochPlan {
     std::vector<int64_t> ldx;          // leading dimension of layer l's input
     std::vector<size_t> x_off, saved_off, later_off, later_bytes;     // later: parts of weight gradients kept to the epoch's end
     size_t logits_off = 0, dz32_off = 0, grad_off[2] = {0, 0}, layer_ws_off = 0, layer_ws_bytes = 0, loss_ws_off = 0,
-           loss_val_off = 0, staging_off = 0, total = 0;
+           loss_val_off = 0, staging_off = 0, total = 0, distill_off = 0, total_distill = 0;
     int64_t ld_grad = 0, ldz = 0;
 };
 
@@ -409,7 +409,7 @@ static int plan_epoch(const capgnn_graph *g, const capgnn_cache *c, const capgnn
     p->grad_off[1] = take(static_cast<size_t>(g->n_loc) * max_w * sizeof(float));
     p->layer_ws_bytes = lws;
     p->layer_ws_off = take(lws);
-    p->loss_ws_off = take(std::max(loss_epoch_ws_bytes(g->n_loc, layers[L - 1].f_out), capgnn_distill_workspace_bytes(g->n_loc, layers[L - 1].f_out)));
+    p->loss_ws_off = take(loss_epoch_ws_bytes(g->n_loc, layers[L - 1].f_out));
     p->loss_val_off = take(256);
     // few bytes of parts: their sums wait for the epoch's last launch, so each layer keeps its own
     p->later_off.assign(L, 0); p->later_bytes.assign(L, 0);
@@ -432,6 +432,9 @@ static int plan_epoch(const capgnn_graph *g, const capgnn_cache *c, const capgnn
         p->staging_off = take(hb);
     }
     p->total = off;
+    // behind everything else: an epoch on labels needs none of it, and has its buffers in the same places
+    p->distill_off = take(capgnn_distill_workspace_bytes(g->n_loc, layers[L - 1].f_out));
+    p->total_distill = off;
     return CAPGNN_OK;
 }
 
@@ -504,7 +507,7 @@ extern "C" size_t capgnn_epoch_workspace_bytes(const capgnn_graph *g, const capg
     EpochPlan p;
     // ld0 does not enter the plan's sizes (layer 0 reads the caller's buffer)
     plan_epoch(g, c, layers, L, layers[0].f_in, &p);
-    return p.total;
+    return p.total_distill;
 }
 
 extern "C" int capgnn_epoch_activation(const capgnn_graph *g, const capgnn_cache *c, const capgnn_layer *layers, int L,
@@ -583,7 +586,8 @@ static int epoch_impl(const capgnn_graph *g, capgnn_cache *c, const capgnn_layer
     if (lr != 0.f && dt != CAPGNN_F32) CG_FAIL(CAPGNN_EUNSUPPORTED, "epoch: the in-place SGD step needs float weights");
     EpochPlan p;
     plan_epoch(g, c, layers, L, ld0, &p);
-    if (!ws || ws_bytes < p.total) CG_FAIL(CAPGNN_ENOMEM, "epoch: workspace of %zu bytes needed, %zu given", p.total, ws_bytes);
+    const size_t need = teacher ? p.total_distill : p.total;
+    if (!ws || ws_bytes < need) CG_FAIL(CAPGNN_ENOMEM, "epoch: workspace of %zu bytes needed, %zu given", need, ws_bytes);
     if (reinterpret_cast<uintptr_t>(ws) & 255u) CG_FAIL(CAPGNN_EINVAL, "epoch: workspace must be 256-byte aligned");
     hipStream_t st = static_cast<hipStream_t>(stream);
     hipStream_t side = side_stream ? static_cast<hipStream_t>(side_stream) : st;
@@ -716,7 +720,7 @@ static int epoch_impl(const capgnn_graph *g, capgnn_cache *c, const capgnn_layer
         if (teacher) {          // the layer's backward pass masks, sums and scales the gradient itself
             CG_TRY(capgnn_distill(g->n_loc, C, Z, ldz, CAPGNN_F32, teacher->ids, teacher->val, teacher->ld, teacher->k, teacher->rest,
                                   teacher->temperature, mask, loss_norm, teacher->weight, loss_dev, nullptr, dz, lddz, dzt, 0,
-                                  w + p.loss_ws_off, capgnn_distill_workspace_bytes(g->n_loc, C), st));
+                                  w + p.distill_off, p.total_distill - p.distill_off, st));
             if (logits && g->n_loc > 0)
                 CG_HIP(hipMemcpy2DAsync(logits, C * sizeof(float), Z, ldz * sizeof(float), C * sizeof(float), g->n_loc, hipMemcpyDeviceToDevice, st));
         } else {

@@ -118,3 +118,30 @@ def test_a_teachers_epoch_then_its_students(orc):
     assert O.normwise(got["db"][-1], dref.sum(0)) <= 1e-4
     teacher_dp.close()
     student.close()
+
+
+@pytest.mark.gpu
+def test_an_epoch_on_labels_needs_none_of_the_distillations_workspace(orc):
+    import torch
+    from paper_2508_13716_amd import harness as H
+    prob = H.make_problem(config("gcn", "f32", [16, 8], 8))
+    dp = H.DeviceProblem(prob)
+    n, C = prob.part.n_loc, 8
+    loss, _ = dp.run_epoch()
+    before = dp.results()
+    full = dp.ws_bytes
+    dp.ws_bytes = full - (B.distill_workspace_bytes(n, C) + 255) // 256 * 256
+    dp.ws[dp.ws_bytes:] = 0xA5
+    torch.cuda.synchronize()
+    short, _ = dp.run_epoch()
+    after = dp.results()
+    assert short == loss and all(np.array_equal(a, b) for a, b in zip(before["dW"], after["dW"]))
+    assert bool((dp.ws[dp.ws_bytes:] == 0xA5).all())
+    ids, val = torch.zeros((n, 2), dtype=torch.int32, device="cuda"), torch.zeros((n, 2), device="cuda")
+    teacher = B.make_teacher(ids, val, 2, 2, 0, 1.0, 1.0)
+    with pytest.raises(B.CapgnnError) as e:
+        dp.run_epoch(teacher=teacher)
+    assert e.value.code == B.ENOMEM
+    dp.ws_bytes = full
+    dp.run_epoch(teacher=teacher)
+    dp.close()
