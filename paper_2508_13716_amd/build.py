@@ -28,7 +28,7 @@ def build(force: bool = True, verbose: bool = False) -> str:
     """Compile every translation unit and link the shared library.  Returns its path."""
     os.makedirs(OBJ, exist_ok=True)
     hipcc = _hipcc()
-    headers = [os.path.join(CSRC, h) for h in ("common.h", "softrow.h", "distill.h")] + [os.path.join(HERE, "..", "include", "capgnn.h")]
+    headers = [os.path.join(CSRC, h) for h in ("common.h", "grid.h", "softrow.h", "distill.h")] + [os.path.join(HERE, "..", "include", "capgnn.h")]
     newest_h = max(os.path.getmtime(h) for h in headers)
 
     def one(src: str) -> str:

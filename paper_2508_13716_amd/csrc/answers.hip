@@ -1,4 +1,5 @@
 // What a classifier answers with: log-probabilities of given classes, entropy, the most likely classes; and their gradient.
+#include "grid.h"
 #include "softrow.h"
 
 #include <algorithm>
@@ -887,8 +888,7 @@ extern "C" int capgnn_logprobs(int64_t n, int C, const void *Z, int64_t ldz, int
     // fp32 82 and 36; but 600 x 10007 fp32 15 and 19, and from 33000 classes on no difference; k = 64: 8000 x 5000 fp32 95 and 72, 2500 x
     // 16384 bf16 41 and 70).
     const bool wave = w.chunk <= 64 * ANSWER_VECTORS * (bf16 ? 8 : 4) || (n >= 2048 && C <= (k > 32 ? ANSWER_WAVE_C / 2 : ANSWER_WAVE_C));
-    const unsigned grid = static_cast<unsigned>(std::min<int64_t>(n * w.parts, 1 << 24));
-    auto go = [&](auto kernel, int threads) { hipLaunchKernelGGL(kernel, dim3(grid), dim3(threads), 0, st, a, w); };
+    auto go = [&](auto kernel, int threads) { hipLaunchKernelGGL(kernel, dim3(stride_grid(n * w.parts, threads)), dim3(threads), 0, st, a, w); };
     if (bf16) {
         if (wave) entropy ? go(answers_rows_kernel<true, 64, true>, 64) : go(answers_rows_kernel<true, 64, false>, 64);
         else entropy ? go(answers_rows_kernel<true, 256, true>, 256) : go(answers_rows_kernel<true, 256, false>, 256);
@@ -945,7 +945,7 @@ extern "C" int capgnn_logprobs_bwd(int64_t n, int C, const void *Z, int64_t ldz,
         // f32 87 / 116, 2000 bf16 84 / 114.
         const int V = zb ? 8 : 4, threads = C <= 64 * GRAD_VECTORS * V ? 64 : 256;
         const int chunks = (C + threads * GRAD_VECTORS * V - 1) / (threads * GRAD_VECTORS * V);
-        const unsigned grid = static_cast<unsigned>(std::min<int64_t>(n * chunks, 1 << 24));
+        const unsigned grid = stride_grid(n * chunks, threads);
         types([&](auto z, auto d, auto e) {
             if (threads == 64) hipLaunchKernelGGL((answers_grad_rows_kernel<z.value, d.value, 64, e.value>), dim3(grid), dim3(64), 0, st, a, chunks);
             else hipLaunchKernelGGL((answers_grad_rows_kernel<z.value, d.value, 256, e.value>), dim3(grid), dim3(256), 0, st, a, chunks);
