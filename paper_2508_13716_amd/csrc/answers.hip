@@ -419,6 +419,8 @@ __global__ __launch_bounds__(THREADS) __attribute__((amdgpu_waves_per_eu(4))) vo
 // logits among the k largest, or with NaN, are gone over once more by one lane, class by class.  The places of the wave's rows are
 // written out together.  612000 x 47, k = 5: 53 us, 2.8 TB/s, bound by instruction issue and LDS latency in about equal parts; without top
 // classes 28 us, 4.1 TB/s.  (Ranking the classes found against one another, out of LDS: 131 us.)
+// 100000 rows, this kernel with k = 8 against a wave a row with 9, us: 20 f32 12 / 139, 47 f32 15 / 149, bf16 22 / 178, 100 f32 25 / 218, 256 f32
+// 44 / 582, bf16 93 / 617.
 constexpr int NARROW_TOP = 8;
 template <bool BF16, bool ENT, bool TOP>
 __global__ __launch_bounds__(64 * NARROW_WAVES) __attribute__((amdgpu_waves_per_eu(4))) void answers_narrow_kernel(AnswerArgs a, NarrowShape s) {

@@ -528,7 +528,11 @@ __global__ __launch_bounds__(THREADS) __attribute__((amdgpu_waves_per_eu(4))) vo
 // mentions of its class.  rest: the listed classes' logits are taken out of the row before it is summed.
 // 612000 x 47, k = 8: 110 us, 2 TB/s, bound by instruction issue (53 us of it) and LDS latency.  (Entries read where they are used, by one lane
 // a row: 278 us; the teacher's probabilities by class in a second set of rows, which leaves LDS for ten waves per compute unit: 170 us.)
+// Every entry is compared with all of its row's, so long lists go to a wave a row.  100000 rows, few-class kernel against a wave a row, us: 30 f32
+// k = 16 87 / 138 (k = 17 by a wave 143), 64 f32 k = 24 90 / 144, 100 f32 k = 32 113 / 153, k = 40 196 / 162, k = 64 448 / 190, 256 f32 k = 40 168 /
+// 169, k = 64 298 / 194; with rest 100 f32 k = 40 217 / 222, 256 f32 k = 48 217 / 260, k = 64 326 / 277; bf16 256 k = 40 142 / 175, k = 64 274 / 213.
 constexpr int NARROW_ENTRIES = 16;      // of a lane
+constexpr int NARROW_LIST = 40;         // of a row
 // (an odd number of words between rows: their lanes hit different banks)
 static inline size_t distill_narrow_lds(const NarrowShape &s, int k) { return s.lds_wave + static_cast<size_t>(s.rows) * (k | 1) * 3 * sizeof(float); }
 
@@ -753,7 +757,7 @@ template <bool BF16, bool DBF16, bool REST>
 void launch_distill(const DistillArgs &a, DistillParts w, int *groups, hipStream_t st) {
     constexpr int V = Raw<BF16>::V;
     const NarrowShape s = narrow_shape(a.C < NARROW_C ? a.C : NARROW_C, BF16 ? CAPGNN_BF16 : CAPGNN_F32);
-    if (a.C <= NARROW_C && a.k <= NARROW_ENTRIES << s.lg) {
+    if (a.C <= NARROW_C && a.k <= NARROW_LIST && a.k <= NARROW_ENTRIES << s.lg) {
         const size_t lds = NARROW_WAVES * distill_narrow_lds(s, a.k);
         *groups = static_cast<int>(narrow_grid(s, a.n, lds));
         hipLaunchKernelGGL((distill_narrow_kernel<BF16, DBF16, REST>), dim3(*groups), dim3(64 * NARROW_WAVES), lds, st, a, s);

@@ -196,8 +196,9 @@ __device__ __forceinline__ int uniform_anew(int x) {
 // 612000 rows were bound by them, not by memory).  The next rows' loads are under way while a wave works on its own.  A row starts
 // G * odd words after the one before it: lanes that read the same class of their rows at once hit different banks.  A lane reads its
 // classes NARROW_BATCH at a time; what is behind a row's end holds -inf (narrow_ends).
-// Up to NARROW_C classes it is the faster one throughout, against a wave a row, us: answers of 100000 rows of 100 f32 26 / 234, 200 f32
-// 50 / 494, 256 bf16 88 / 648; their gradient, 100 f32 22 / 169, 256 bf16 39 / 157; distillation, 100 f32 42 / 125, 200 f32 62 / 122.
+// Up to NARROW_C classes it is the faster one throughout, against a wave a row, us: answers of 100000 rows with k = 8, 100 f32 25 / 218, 256 f32
+// 44 / 581, bf16 93 / 615; their gradient, 256 f32 54 / 72, bf16 37 / 53; distillation with k = 16, 100 f32 63 / 135, 256 f32 89 / 139, bf16
+// 66 / 146.  By a wave beyond: 257 classes, answers 134 f32, 139 bf16, gradient 89 and 57, distillation 158 and 150.
 constexpr int NARROW_C = 256;
 constexpr int NARROW_G = NARROW_C / 32;     // lanes of a row at most
 constexpr int NARROW_BATCH = 8;
