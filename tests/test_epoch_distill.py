@@ -145,3 +145,30 @@ def test_an_epoch_on_labels_needs_none_of_the_distillations_workspace(orc):
     dp.ws_bytes = full
     dp.run_epoch(teacher=teacher)
     dp.close()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("rest", [0, 1])
+def test_epoch_distill_with_every_way_of_the_host_tier(orc, rest):
+    """host-tier rows staged, prefetched by the epoch before, or read in place, a stream or two, label epochs in between: the same bits"""
+    import torch
+    from paper_2508_13716_amd import harness as H
+    prob = H.make_problem(config("sage", "f32", [40, 32, 12], 9), mask_frac=0.5)
+    ids, val = teacher_for(prob, 4, 2.0, rest, 3)
+    idd, vd = torch.from_numpy(ids).cuda(), torch.from_numpy(val).cuda()
+    teacher = B.make_teacher(idd, vd, 4, 4, rest, 2.0, 4.0)
+    seen = {}
+    for mode in (B.MISS_STAGED, B.MISS_PIPELINED, B.MISS_ZEROCOPY):
+        for side in (True, False):
+            if mode == B.MISS_PIPELINED and not side:
+                continue
+            dp = H.DeviceProblem(prob, miss_mode=mode, use_side_stream=side)
+            for kind in ("teacher", "labels", "teacher", "teacher", "labels"):
+                loss, _ = dp.run_epoch(teacher=teacher if kind == "teacher" else None)
+                got = dp.results()
+                loss0, first = seen.setdefault(kind, (loss, got))
+                assert loss == loss0, (mode, side, kind)
+                for key in ("dW", "dW_self", "db"):
+                    assert all(a is None or np.array_equal(a, b) for a, b in zip(got[key], first[key])), (mode, side, kind, key)
+                assert np.array_equal(got["logits"], first["logits"])
+            dp.close()
