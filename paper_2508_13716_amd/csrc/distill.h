@@ -36,18 +36,24 @@ constexpr float REST_LEAST = 9.5367431640625e-7f;       // 2^-20
 constexpr float REST_LEAST_ALONE = 1.220703125e-4f;     // 2^-13
 
 // Exponential and logarithm in doubles, of a few numbers a row, to some 1e-14 (what they give is stored as a float): the series of exp on
-// |r| <= ln 2 / 2 and of 2 atanh((m - 1) / (m + 1)) on 1/sqrt 2 <= m <= sqrt 2, their coefficients read where they are used.  (As constants of
-// the program they are kept in registers across the loop over the rows, next to the logits: 16 to 53 of them in scratch memory.)
-static __constant__ double exp_terms[12] = {1.0 / 39916800, 1.0 / 3628800, 1.0 / 362880, 1.0 / 40320, 1.0 / 5040, 1.0 / 720, 1.0 / 120, 1.0 / 24, 1.0 / 6,
-                                            0.5, 1.4426950408889634074, 0.69314718055994530942};
-static __constant__ double log_terms[10] = {1.0 / 17, 1.0 / 15, 1.0 / 13, 1.0 / 11, 1.0 / 9, 1.0 / 7, 1.0 / 5, 1.0 / 3, 1.0, 0.69314718055994530942};
-__device__ __forceinline__ const double *terms_anew(const double *p) {
+// |r| <= ln 2 / 2 and of 2 atanh((m - 1) / (m + 1)) on 1/sqrt 2 <= m <= sqrt 2.  READ: their coefficients are read where they are used.  (As constants
+// of the program they are kept in registers across the loop over the rows, next to the logits, up to 53 of them in scratch memory.  Read and
+// held, us: workgroups of 512 threads, 8192 x 64000 bf16 410 and 444, 2048 x 131072 fp32 with rest 582 and 622; of fewer, 2999 x 10007 fp32
+// with rest 72.4 and 71.3, 20000 x 1000 bf16 40.5 and 39.1, with rest 52.5 and 47.8; few classes, 612000 x 47 118.9 and 116.7, with rest 136 and 156.)
+struct Terms { double c[12]; };
+constexpr Terms EXP_TERMS = {{1.0 / 39916800, 1.0 / 3628800, 1.0 / 362880, 1.0 / 40320, 1.0 / 5040, 1.0 / 720, 1.0 / 120, 1.0 / 24, 1.0 / 6, 0.5,
+                              1.4426950408889634074, 0.69314718055994530942}};
+constexpr Terms LOG_TERMS = {{1.0 / 17, 1.0 / 15, 1.0 / 13, 1.0 / 11, 1.0 / 9, 1.0 / 7, 1.0 / 5, 1.0 / 3, 1.0, 0.69314718055994530942}};
+static __constant__ Terms exp_terms = EXP_TERMS, log_terms = LOG_TERMS;
+__device__ __forceinline__ const double *terms_anew(const Terms &t) {
+    const double *p = t.c;
     asm volatile("" : "+s"(p));
     return p;
 }
 // x from -inf (0) to what a double holds; NaN stays
-__device__ __forceinline__ double exp_wide(double x) {
-    const double *c = terms_anew(exp_terms);
+template <bool READ> __device__ __forceinline__ double exp_wide(double x) {
+    constexpr Terms held = EXP_TERMS;
+    const double *c = READ ? terms_anew(exp_terms) : held.c;
     x = x < -800.0 ? -800.0 : x > 800.0 ? 800.0 : x;
     const double n = rint(x * c[10]), r = fma(-n, c[11], x);
     double e = c[0];
@@ -62,8 +68,9 @@ __device__ __forceinline__ double inverse(double x) {
     return fma(y, fma(-x, y, 1.0), y);
 }
 // x > 0 and finite; NaN stays
-__device__ __forceinline__ double log_wide(double x) {
-    const double *c = terms_anew(log_terms);
+template <bool READ> __device__ __forceinline__ double log_wide(double x) {
+    constexpr Terms held = LOG_TERMS;
+    const double *c = READ ? terms_anew(log_terms) : held.c;
     int n;
     double m = frexp(x, &n);
     if (m < 0.70710678118654752) { m += m; --n; }
@@ -125,7 +132,7 @@ template <bool BF16, int THREADS, int NV> struct Seen {
 
 // What the teacher leaves (rest) is the small difference of numbers near 1: its exponentials and their sum are doubles.  listed: where another
 // launch has left the logits of the entries' classes, or null.
-template <bool BF16>
+template <bool BF16, bool READ>
 __device__ __forceinline__ void read_teacher(const DistillArgs &a, int64_t row, const char *z, const float *listed, Teacher &t) {
     const int lane = threadIdx.x;
     float top = -INFINITY, top_z = -INFINITY, v[Teacher::OWN], z_of[Teacher::OWN];
@@ -158,9 +165,9 @@ __device__ __forceinline__ void read_teacher(const DistillArgs &a, int64_t row, 
 #pragma unroll
     for (int o = 0; o < Teacher::OWN; ++o) {
         if (o * 64 >= a.k) break;
-        w[o] = a.rest ? exp_wide(v[o]) : static_cast<double>(exp_difference(v[o], top, a.t));      // (none: 0)
+        w[o] = a.rest ? exp_wide<READ>(v[o]) : static_cast<double>(exp_difference(v[o], top, a.t));      // (none: 0)
         Q += w[o];
-        if (a.rest) listed_sum += exp_wide(scaled(z_of[o], ref_z, a.t));
+        if (a.rest) listed_sum += exp_wide<READ>(scaled(z_of[o], ref_z, a.t));
     }
     Q = wave_all(Q, OpSum());
     const double one = a.rest ? 1.0 : 1.0 / Q;
@@ -193,7 +200,7 @@ __device__ __forceinline__ void read_teacher(const DistillArgs &a, int64_t row, 
         if (i < a.k) {
             t.q[i] = sum;
             t.c[i] = c >= 0 && before == 0 ? c : -1;
-            if (a.rest && c >= 0 && before > 0) listed_sum -= exp_wide(scaled(t.z[i], ref_z, a.t));        // (the very number that was added)
+            if (a.rest && c >= 0 && before > 0) listed_sum -= exp_wide<READ>(scaled(t.z[i], ref_z, a.t));        // (the very number that was added)
         }
     }
     double r = a.rest ? 1.0 - Q : 0.0;
@@ -334,11 +341,11 @@ __device__ __forceinline__ void no_gradient(const DistillArgs &a, char *dz, int 
 
 // What the row gives to the classes that are not listed: P = exp((m - m0) / T) s / S, from their own maximum and sum (m, s), next to the listed
 // classes' (top, sum); m0: the larger maximum.  P may leave float's (and double's) range; its logarithm and the others' shares of it do not.
-struct RestSums {
+template <bool READ> struct RestSums {
     double S, own;          // over all classes, from m0; 0 for an empty row; the others' part of it
     float m0;
     __device__ __forceinline__ RestSums(float m, float s, float top, double sum, const TempScale &t) {
-        const double e = m == top ? 1.0 : exp_wide(-fabs(scaled(m, top, t)));
+        const double e = m == top ? 1.0 : exp_wide<READ>(-fabs(scaled(m, top, t)));
         m0 = safe_max(max_of(m, top));
         own = m < top ? s * e : s;
         S = own + (m < top ? sum : sum * e);
@@ -362,17 +369,17 @@ __device__ __forceinline__ double rest_others(float s, double r, double ln, doub
 // wave (every lane); s is the row's sum, or (REST) that of the others, S over all.  It is the small difference of its terms where the student is
 // close to the teacher.  So they are doubles, ln q comes from the teacher's value (from q only where a class is listed again), and q's
 // rounding counts with ln q - ln p.  With REST the others' sum counts with P - r; without, the roundings of S stay, some 1e-7.
-template <bool REST>
+template <bool REST, bool READ>
 __device__ __forceinline__ double divergence(const DistillArgs &a, const Teacher &t, float m, float m0, float s, double S) {
     // both logarithms at once, one in the even lanes, one in the odd ones: of S and r S / s, or of S / Z with Z the sum of the teacher's exponentials
-    const double ln = log_wide(!REST ? s * inverse(t.sum) : threadIdx.x & 1 ? t.r * S * inverse(s) : S), ln_S = REST ? __shfl(ln, 0) : ln;
+    const double ln = log_wide<READ>(!REST ? s * inverse(t.sum) : threadIdx.x & 1 ? t.r * S * inverse(s) : S), ln_S = REST ? __shfl(ln, 0) : ln;
     double kl = 0.0;
 #pragma unroll 1
     for (int i = threadIdx.x; i < a.k; i += 64) {
         const float q = t.q[i];
         if (t.c[i] < 0 || q == 0.f) continue;
         double ln_q = REST ? static_cast<double>(t.v[i]) : (static_cast<double>(t.v[i]) - t.top) * teacher_scale(a.t);     // (without REST: and ln Z)
-        if (q != t.w[i]) ln_q = log_wide(REST ? q : q * t.sum);
+        if (q != t.w[i]) ln_q = log_wide<READ>(REST ? q : q * t.sum);
         kl += q * (ln_q + ln_S - scaled(t.z[i], m0, a.t));
     }
     if (REST && threadIdx.x == 1) kl += rest_others(s, t.r, ln, scaled(m, m0, a.t));
@@ -404,6 +411,7 @@ template <bool BF16, bool DBF16, int THREADS, int NV, bool REST, DistillStage ST
 __global__ __launch_bounds__(THREADS) __attribute__((amdgpu_waves_per_eu(4))) void distill_rows_kernel(DistillArgs a, DistillParts w) {
     typedef Raw<BF16> R;
     constexpr int TILE = THREADS * NV * R::V;
+    constexpr bool READ = THREADS == 512;
     constexpr bool PARTS = STAGE == PART_SUMS || STAGE == PART_GRADIENT;
     extern __shared__ __align__(16) uint32_t seen_bits[];
     __shared__ Teacher t;
@@ -435,7 +443,7 @@ __global__ __launch_bounds__(THREADS) __attribute__((amdgpu_waves_per_eu(4))) vo
         }
         if (first_wave) {
             float *left = STAGE == PART_SUMS || STAGE == PART_GRADIENT ? w.listed + row * CAPGNN_GIVEN_MAX : nullptr;
-            if (STAGE != PART_SUMS || REST || part == 0) read_teacher<BF16>(a, row, z, STAGE == PART_GRADIENT ? left : nullptr, t);
+            if (STAGE != PART_SUMS || REST || part == 0) read_teacher<BF16, READ>(a, row, z, STAGE == PART_GRADIENT ? left : nullptr, t);
             if constexpr (STAGE == PART_SUMS)
                 if (part == 0)
                     for (int i = threadIdx.x; i < a.k; i += 64) left[i] = t.z[i];
@@ -470,7 +478,7 @@ __global__ __launch_bounds__(THREADS) __attribute__((amdgpu_waves_per_eu(4))) vo
         }
         __syncthreads();
         const float ref = safe_max(m);          // REST: of the others
-        const RestSums rest(m, s, REST ? t.top : m, REST ? t.sum : 0.0, a.t);
+        const RestSums<READ> rest(m, s, REST ? t.top : m, REST ? t.sum : 0.0, a.t);
         const float m0 = REST ? rest.m0 : ref, S = REST ? static_cast<float>(rest.S) : s;
         if (t.entries == 0 || S == 0.f) {
             if (a.row_loss && part == 0 && threadIdx.x == 0) a.row_loss[row] = 0.f;
@@ -479,7 +487,7 @@ __global__ __launch_bounds__(THREADS) __attribute__((amdgpu_waves_per_eu(4))) vo
             continue;
         }
         if (first_wave && part == 0) {
-            const double kl = divergence<REST>(a, t, m, m0, s, rest.S);
+            const double kl = divergence<REST, READ>(a, t, m, m0, s, rest.S);
             loss += kl;
             if (a.row_loss && threadIdx.x == 0) a.row_loss[row] = static_cast<float>(kl);
         }
@@ -538,6 +546,7 @@ static inline size_t distill_narrow_lds(const NarrowShape &s, int k) { return s.
 
 template <bool BF16, bool DBF16, bool REST>
 __global__ __launch_bounds__(64 * NARROW_WAVES) __attribute__((amdgpu_waves_per_eu(4))) void distill_narrow_kernel(DistillArgs a, NarrowShape s) {
+    constexpr bool READ = REST;
     extern __shared__ __align__(16) uint32_t seen_bits[];
     __shared__ double red[NARROW_WAVES];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), k = a.k, kp = k | 1, all_items = s.rows * k;
@@ -645,11 +654,11 @@ __global__ __launch_bounds__(64 * NARROW_WAVES) __attribute__((amdgpu_waves_per_
             }
             q[i] = first ? p : -1.f;
             if (c >= 0 && p != w[i]) {              // a class listed again: q ln q of the sum for that of its parts (a part that is the sum stays)
-                if (w[i] != 0.f) kl -= w[i] * log_wide(w[i]);
+                if (w[i] != 0.f) kl -= w[i] * log_wide<READ>(w[i]);
                 if (first) {
                     bool there = false;
                     for (int b = 0; b < k; ++b) there = there || (id[b] == c && w[b] == p);
-                    if (!there) kl += p * log_wide(p);
+                    if (!there) kl += p * log_wide<READ>(p);
                 }
             }
         }
@@ -689,15 +698,15 @@ __global__ __launch_bounds__(64 * NARROW_WAVES) __attribute__((amdgpu_waves_per_
             double r = 1.0 - Q;
             if (r < REST_LEAST) r = 0.0;
             mass = static_cast<float>(Q + rest_left(r, others));
-            const RestSums rest(m, others, top, listed, a.t);
+            const RestSums<READ> rest(m, others, top, listed, a.t);
             m0 = rest.m0;
             S = static_cast<float>(rest.S);
             away = rest.factor(others, r, mass, scale);
             mass *= scale;
-            ln_S = log_wide(rest.S);
-            tail = rest_others(others, r, log_wide(r * rest.S * inverse(others)), scaled(m, m0, a.t));
+            ln_S = log_wide<READ>(rest.S);
+            tail = rest_others(others, r, log_wide<READ>(r * rest.S * inverse(others)), scaled(m, m0, a.t));
         } else {
-            ln_S = log_wide(S * inverse(Q));
+            ln_S = log_wide<READ>(S * inverse(Q));
             mass = (1.f + 0.f * one) * scale;         // (a NaN among the teacher's values reaches every class)
         }
         const bool live = on && entries > 0 && S != 0.f;
