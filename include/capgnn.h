@@ -484,7 +484,8 @@ int capgnn_sigmoid_bce(int64_t n, int C, const float *Z, int64_t ldz, const uint
  * What a classifier answers with, and what it learns from another one's answers.  Rows of logits Z: device [n x ldz] of
  * z_dtype (C classes; rows need no alignment beyond their elements'), divided by `temperature` (2^-64 to 2^64) before the softmax.
  * p_i = softmax(Z_i / temperature).  A logit of -infinity bars its class: p = 0, nothing is added to the entropy, and its gradient is 0,
- * but for the term of its own that a class given below, or listed by a teacher, has in the formulas.  A row whose classes are all barred is empty.  A NaN or +infinity makes the row's numbers NaN, no other row's.
+ * but for the term of its own that a class given below, or listed by a teacher, has in the formulas.  A row whose classes are all
+ * barred is empty.  A NaN or +infinity makes the row's numbers NaN, no other row's.
  * mask: device uint8[n] or NULL: rows with 0 are left out, whatever they hold.  dZ may be Z itself if type and pitch are the same too (each
  * logit is then replaced by its gradient); else they must not overlap.  No result depends on the order of atomic operations.
  * Asynchronous on `stream`, which belongs to the current device; nothing is allocated, so calls can be recorded into HIP graphs

@@ -403,10 +403,11 @@ enum DistillStage : int {
 
 // One workgroup per row (or part): the first wave reads the teacher while all of them have the row's logits on their way; maximum and sums from
 // registers, one meeting, then the gradient from the same registers; the listed classes' own terms follow behind a barrier.  Bound by
-// HBM: 8192 x 64000 bf16 415 us (5.05 TB/s read and written).  Rows longer than the registers hold come out of the Infinity Cache a second
-// time, all but the last tile: 2048 x 131072 fp32 573 us for 2.1 GB (a second pass over everything: 650).  Rows of some ten thousand
+// HBM: 8192 x 64000 bf16 406 us (5.2 TB/s read and written).  Rows longer than the registers hold come out of the Infinity Cache a second
+// time, all but the last tile: 2048 x 131072 fp32 580 us for 2.1 GB (a second pass over everything: 650).  Rows of some ten thousand
 // classes are held up by the teacher's chain of dependent reads, four workgroups a compute unit: 2999 x 10007 fp32, k = 32, rest, 70 us.
-// At most 128 registers, for sixteen waves per compute unit: without that bound the compiler takes twice as many and has half the waves.
+// At most 128 registers, for sixteen waves per compute unit: without that bound the compiler takes twice as many and has half the waves.  With
+// 12 and 16 vectors a thread up to 21 registers go to scratch memory (80 bytes a thread).
 template <bool BF16, bool DBF16, int THREADS, int NV, bool REST, DistillStage STAGE>
 __global__ __launch_bounds__(THREADS) __attribute__((amdgpu_waves_per_eu(4))) void distill_rows_kernel(DistillArgs a, DistillParts w) {
     typedef Raw<BF16> R;
@@ -533,8 +534,9 @@ __global__ __launch_bounds__(THREADS) __attribute__((amdgpu_waves_per_eu(4))) vo
 
 // ------------------------------------------------------------------ few classes
 // As answers_grad_narrow_kernel, the teacher's entries beside the rows in LDS, shared by the lanes of a row; each entry looks for other
-// mentions of its class.  rest: the listed classes' logits are taken out of the row before it is summed.
-// 612000 x 47, k = 8: 110 us, 2 TB/s, bound by instruction issue (53 us of it) and LDS latency.  (Entries read where they are used, by one lane
+// mentions of its class.  rest: the listed classes' logits are taken out of the row before its maximum.
+// 612000 x 47, k = 8: 109 us, 2 TB/s, bound by instruction issue (59 us of it) and LDS latency; with rest, which has 16 registers in scratch memory,
+// 127.  (Entries read where they are used, by one lane
 // a row: 278 us; the teacher's probabilities by class in a second set of rows, which leaves LDS for ten waves per compute unit: 170 us.)
 // Every entry is compared with all of its row's, so long lists go to a wave a row.  100000 rows, few-class kernel against a wave a row, us: 30 f32
 // k = 16 87 / 138 (k = 17 by a wave 143), 64 f32 k = 24 90 / 144, 100 f32 k = 32 113 / 153, k = 40 196 / 162, k = 64 448 / 190, 256 f32 k = 40 168 /
