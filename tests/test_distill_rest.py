@@ -154,3 +154,23 @@ def test_a_remainder_of_roundings_counts_as_none_where_there_is_no_other_class(C
         loss, row, dZ = run_distill(device(Z[rows], "f32", C), C, "f32", "f32", T, None, ids[rows], val[rows], 1, 40.0, 1.0, C)
         check("row_loss", row, ref_row[rows], row_tol[rows])
         check("dZ", dZ, dref[rows], dz_tol[rows])
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("rest", [0, 1])
+@pytest.mark.parametrize("C,k", [(1, 1), (1, 41), (1, 256), (2, 41), (5, 64), (7, 40), (7, 41), (9, 200), (250, 40), (250, 41)])
+def test_lists_longer_than_rows_of_a_few_classes(C, k, rest):
+    """rows shorter than 16 bytes next to lists of which most entries repeat a class or are none, on both sides of the longest list of few classes"""
+    n = 70
+    for dtype in ("f32", "bf16"):
+        rng = np.random.default_rng(1000 * C + k + rest)
+        Z = to_dtype(2 * rng.standard_normal((n, C)), dtype)
+        ids = rng.integers(-1, C + 1, (n, k)).astype(np.int32)
+        val = (np.log(0.9 / k) + 0.1 * rng.standard_normal((n, k)) - 0.2).astype(np.float32)
+        with np.errstate(divide="ignore", invalid="ignore"):
+            ref_loss, ref_row, dref, ex = orc.distill(Z, ids, val, bool(rest), 1.5)
+            row_tol, dz_tol = distill_tol(Z, ex, ref_row, dref, 1.5, C, k, 1.0, dtype)
+        loss, row, dZ = run_distill(device(Z, dtype, C + 1), C, dtype, dtype, 1.5, None, ids, val, rest, 0.0, 1.0, C + 2)
+        check("row_loss", row, ref_row, row_tol)
+        check("dZ", dZ[:, :C], dref, dz_tol)
+        assert (dZ[:, C:] == 9.0).all()
