@@ -535,8 +535,8 @@ __global__ __launch_bounds__(THREADS) __attribute__((amdgpu_waves_per_eu(4))) vo
 // ------------------------------------------------------------------ few classes
 // As answers_grad_narrow_kernel, the teacher's entries beside the rows in LDS, shared by the lanes of a row; each entry looks for other
 // mentions of its class.  rest: the listed classes' logits are taken out of the row before its maximum.
-// 612000 x 47, k = 8: 109 us, 2 TB/s, bound by instruction issue (59 us of it) and LDS latency; with rest, which has 16 registers in scratch memory,
-// 127.  (Entries read where they are used, by one lane
+// 612000 x 47, k = 8: 109 us, 2 TB/s, bound by instruction issue (59 us of it) and LDS latency (with rest, and
+// 16 registers in scratch memory, the call takes 135 us against 116).  (Entries read where they are used, by one lane
 // a row: 278 us; the teacher's probabilities by class in a second set of rows, which leaves LDS for ten waves per compute unit: 170 us.)
 // Every entry is compared with all of its row's, so long lists go to a wave a row.  100000 rows, few-class kernel against a wave a row, us: 30 f32
 // k = 16 87 / 138 (k = 17 by a wave 143), 64 f32 k = 24 90 / 144, 100 f32 k = 32 113 / 153, k = 40 196 / 162, k = 64 448 / 190, 256 f32 k = 40 168 /
