@@ -45,12 +45,15 @@ extern "C" {
 
 #define CAPGNN_F32   0
 #define CAPGNN_BF16  1
+#define CAPGNN_E4M3  2   /* 8 bits: sign, 4 of exponent, 3 of mantissa, largest 448, no infinity; only where an entry point names it */
 
 #define CAPGNN_GCN        0
 #define CAPGNN_SAGE_MEAN  1
 
 #define CAPGNN_ACT_NONE 0
 #define CAPGNN_ACT_RELU 1
+#define CAPGNN_ACT_GELU 2   /* u Phi(u), Phi the normal distribution's; capgnn_linear and its backward pass only */
+#define CAPGNN_ACT_SILU 3   /* u / (1 + exp(-u)); likewise                                                      */
 
 #define CAPGNN_ORDER_AUTO   0   /* library picks the cheaper association of A_hat X W          */
 #define CAPGNN_AGG_FIRST    1   /* (A_hat X) W : SpMM at f_in, GEMM over local rows            */
@@ -544,6 +547,99 @@ int capgnn_distill(int64_t n, int C, const void *Z, int64_t ldz, int z_dtype, co
                    int64_t ldt, int k, int rest, float temperature, const uint8_t *mask, double loss_norm, float weight,
                    float *loss_dev, float *row_loss, void *dZ, int64_t lddz, int dz_dtype, int accumulate, void *ws,
                    size_t ws_bytes, void *stream);
+
+/* ------------------------------------------------------------------------------------------
+ * What a residual vertex model is built and trained with beside its aggregation: learnt input rows, the root-mean-square norm, products
+ * with an epilogue, the clipped update.  (None of it is the paper's.)
+ * Rows need no alignment beyond their elements'.  No result depends on the order of atomic operations, and padding columns are neither
+ * used nor written.  Outputs may overlap inputs only where it says so.  Asynchronous on `stream`, which belongs to the current device;
+ * nothing is allocated (but by capgnn_tensors_create), so calls can be recorded into HIP graphs (calls that may overlap in time need a
+ * workspace each).  Workspaces: the *_workspace_bytes() of the same sizes, 256-byte aligned; NULL where that is 0.
+ * ---------------------------------------------------------------------------------------- */
+
+/* Rows of a learnt table: out[i, 0:F] = scale * table[ids[i], 0:F], i < n; rounded once.  ids: device int64[n], any order, the same any number
+ * of times; an id outside [0, V) gives a row of zeros.  table: device [V x ldt] of `dtype`; out: device [n x ldo] of out_dtype (CAPGNN_F32
+ * or CAPGNN_BF16 each).  V < 2^31, F <= 2^22.  Errors: EINVAL, EUNSUPPORTED (wider rows), EHIP. */
+int capgnn_embed(int64_t n, const int64_t *ids, int64_t V, int F, const void *table, int64_t ldt, int dtype, float scale, void *out,
+                 int64_t ldo, int out_dtype, void *stream);
+
+/* Its gradient: dtable[v, 0:F] = scale * sum over i with ids[i] = v of dY[i, 0:F] (0 for rows that no id names); with accumulate != 0 that is
+ * added to what dtable holds, and rows that no id names are not touched.  dY: device [n x lddy] of dy_dtype; dtable: device float
+ * [V x lddt].  ids outside [0, V) add to nothing.  The sums are formed in float, in an order that the sizes, dy_dtype and
+ * the ids alone decide.  n, V < 2^31, F <= 2^22.  Errors: EINVAL, EUNSUPPORTED (wider rows), ENOMEM (workspace too small), EHIP. */
+size_t capgnn_embed_bwd_workspace_bytes(int64_t n, int64_t V, int F);
+int capgnn_embed_bwd(int64_t n, const int64_t *ids, int64_t V, int F, const void *dY, int64_t lddy, int dy_dtype, float scale,
+                     float *dtable, int64_t lddt, int accumulate, void *ws, size_t ws_bytes, void *stream);
+
+#define CAPGNN_NORM_MAX 32768   /* widest row of the norm and of capgnn_quantize_rows */
+
+/* Root-mean-square norm with the residual's addition, row by row:
+ *   h = X[i,:] + R[i,:] (R NULL: h = X[i,:]);  rstd[i] = (mean h^2 + eps)^-1/2;  y = h * rstd[i] * w
+ * X, R, H: device [n x ldx / ldr / ldh] of `dtype` (CAPGNN_F32 or CAPGNN_BF16); H receives h, or is NULL; it may be X or R (same pitch).
+ * w: device float[F] or NULL (= 1).  rstd: device float[n] (what the backward pass reads) or NULL.  Y: device [n x ldy] of y_dtype, may be
+ * X or R if type and pitch are the same too (and H is not); y comes from the unrounded h.  Everything is formed in float.
+ * y_dtype CAPGNN_F32 or CAPGNN_BF16: Y = y, y_scale NULL.  CAPGNN_E4M3: y_scale (device float[n]) = max(max_j |y_j|, 2^-100) / 448 and
+ * Y = y / y_scale[i] rounded to nearest even (bytes); a row that holds NaN has a scale of NaN.
+ * eps >= 0, finite (with eps = 0 a row of zeros is 0 * infinity = NaN).  F <= CAPGNN_NORM_MAX.  Errors: EINVAL, EUNSUPPORTED (wider rows), EHIP. */
+int capgnn_rmsnorm(int64_t n, int F, const void *X, int64_t ldx, const void *R, int64_t ldr, void *H, int64_t ldh, int dtype, const float *w,
+                   float eps, void *Y, int64_t ldy, int y_dtype, float *y_scale, float *rstd, void *stream);
+
+/* Its gradient, from h as the forward pass left it (X itself where there was no R) and rstd:
+ *   g = dY[i,:] * w;  dX[i,:] = rstd g - h rstd^3 mean(g h) + dH[i,:];  dw = sum_i dY[i,:] h rstd[i]
+ * dX is the gradient of X and of R alike.  dY: device [n x lddy] of dy_dtype; H, dH (the gradient that reaches h on the residual's way, or
+ * NULL), dX: of `dtype`; dX may be dY, dH or H if type and pitch are the same.  dw: device float[F] or NULL.  A backward pass through an
+ * 8-bit Y takes the gradient of the values that it stands for. */
+size_t capgnn_rmsnorm_bwd_workspace_bytes(int64_t n, int F);
+int capgnn_rmsnorm_bwd(int64_t n, int F, const void *dY, int64_t lddy, int dy_dtype, const void *H, int64_t ldh, int dtype, const float *w,
+                       const float *rstd, const void *dH, int64_t lddh, void *dX, int64_t lddx, float *dw, void *ws, size_t ws_bytes,
+                       void *stream);
+
+/* Rows in 8 bits without the norm (weights for capgnn_linear): q_scale[i] = max(max_j |X_ij|, 2^-100) / 448, Q[i,:] = X[i,:] / q_scale[i]. */
+int capgnn_quantize_rows(int64_t n, int F, const void *X, int64_t ldx, int dtype, void *Q, int64_t ldq, float *q_scale, void *stream);
+
+/* Product with an epilogue:  U = (a_scale[i] w_scale[j] sum_k A[i,k] W[j,k]) + bias[j];  Y = act(U) + R.
+ * A: device [M x lda], W: device [N x ldw] (a row of weights per output, so that both run along K), both of `dtype`: CAPGNN_F32, CAPGNN_BF16,
+ * or CAPGNN_E4M3 with a_scale (device float[M]) and w_scale (device float[N]), NULL = 1 (NULL for the other types).  Sums in float;
+ * with 8-bit operands and a bf16 result the matrix instruction adds eight neighbouring products with a common exponent first, dropping what
+ * lies below 2^-13 of the largest (some 1e-5 of a sum's size; with a float result nothing is dropped).
+ * bias: device float[N] or NULL.  act: CAPGNN_ACT_*.  R: device [M x ldr] or NULL; U: device [M x ldu] or NULL (kept for the backward
+ * pass); Y: device [M x ldy]; all of out_dtype (CAPGNN_F32 or CAPGNN_BF16), each rounded once.  Y may be R (same pitch).
+ * K = 0: the sums are 0.  M, N, K < 2^31, a row of A or W shorter than 2^31 bytes.
+ * Errors: EINVAL, ENOMEM (workspace too small), EHIP. */
+size_t capgnn_linear_workspace_bytes(int64_t M, int64_t N, int64_t K, int dtype);
+int capgnn_linear(int64_t M, int64_t N, int64_t K, const void *A, int64_t lda, const float *a_scale, const void *W, int64_t ldw,
+                  const float *w_scale, int dtype, const float *bias, int act, const void *R, int64_t ldr, void *U, int64_t ldu, void *Y,
+                  int64_t ldy, int out_dtype, void *ws, size_t ws_bytes, void *stream);
+
+/* The epilogue's gradient: dU = dY * act'(U), dbias[j] = sum_i dU[i,j] (of the unrounded dU, in a fixed order).  (R's gradient is dY.  What
+ * is left are capgnn_gemm's products of dU: dA = dU W, capgnn_gemm(0, 0, M, K, N, dU, W); dW = dU^T A, capgnn_gemm(1, 0, N, K, M, dU, A).)
+ * dY, U, dU: device [M x lddy / ldu / lddu] of `dtype` (CAPGNN_F32 or CAPGNN_BF16); U may be NULL for CAPGNN_ACT_NONE; dU may be dY or U
+ * (same pitch), or NULL; dbias: device float[N] or NULL.  The slope of ReLU at 0 is 0. */
+size_t capgnn_linear_act_bwd_workspace_bytes(int64_t M, int64_t N);
+int capgnn_linear_act_bwd(int64_t M, int64_t N, const void *dY, int64_t lddy, const void *U, int64_t ldu, int dtype, int act, void *dU,
+                          int64_t lddu, float *dbias, void *ws, size_t ws_bytes, void *stream);
+
+/* Gradients of many tensors, and the tensors they belong to, as one list.  grads, params: host arrays of `count` device addresses, copied
+ * (params NULL: a list of gradients alone); counts: host int64[count], elements of each (0 allowed); grad_dtype, param_dtype: host
+ * int32[count], CAPGNN_F32 or CAPGNN_BF16 each.  Tensors are dense and aligned to their elements; no tensor that is written may overlap
+ * another of the list (EINVAL: two gradients, two params, or a param and a gradient that share memory).  The list holds addresses: the
+ * tensors stay allocated while it is used.  Synchronises `stream`.  Errors: EINVAL, ENOMEM, EHIP. */
+typedef struct capgnn_tensors capgnn_tensors;
+int capgnn_tensors_create(capgnn_tensors **t, int count, void *const *grads, const int32_t *grad_dtype, void *const *params,
+                          const int32_t *param_dtype, const int64_t *counts, void *stream);
+int capgnn_tensors_destroy(capgnn_tensors *t);
+
+/* norm = (sum of g^2 over all elements of all gradients)^1/2, summed in double, in a fixed order.  norm_dev: device float[1].
+ *   capgnn_grad_norm:    writes the norm.
+ *   capgnn_grad_clip:    and multiplies every gradient by c = min(1, max_norm / norm).
+ *   capgnn_clipped_step: and updates param <- param - lr * c * g (in float, rounded once to the param's type); the gradients stay.
+ * max_norm >= 0 (infinity: c = 1).  A norm that is not finite (a gradient holds infinity or NaN) changes no gradient and no param.  No handle
+ * state changes: calls on one list may be recorded, and may overlap if they write different memory and have workspaces of their own.
+ * Errors: EINVAL (no params in the list), ENOMEM (workspace too small), EHIP. */
+size_t capgnn_grad_workspace_bytes(const capgnn_tensors *t);
+int capgnn_grad_norm(const capgnn_tensors *t, float *norm_dev, void *ws, size_t ws_bytes, void *stream);
+int capgnn_grad_clip(const capgnn_tensors *t, float max_norm, float *norm_dev, void *ws, size_t ws_bytes, void *stream);
+int capgnn_clipped_step(const capgnn_tensors *t, float lr, float max_norm, float *norm_dev, void *ws, size_t ws_bytes, void *stream);
 
 #define CAPGNN_MAX_RECORDS 96
 #define CAPGNN_K_GATHER_HIT   1

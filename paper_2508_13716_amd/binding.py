@@ -16,9 +16,9 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 SO_PATH = os.path.join(_HERE, "libcapgnn.so")
 
 OK, EINVAL, ENOMEM, EHIP, ENOTFOUND, EUNSUPPORTED = 0, -1, -2, -3, -4, -5
-F32, BF16 = 0, 1
+F32, BF16, E4M3 = 0, 1, 2
 GCN, SAGE_MEAN = 0, 1
-ACT_NONE, ACT_RELU = 0, 1
+ACT_NONE, ACT_RELU, ACT_GELU, ACT_SILU = 0, 1, 2, 3
 ORDER_AUTO, AGG_FIRST, XFORM_FIRST = 0, 1, 2
 MAP_DIRECT, MAP_HASH = 0, 1
 NORM_SYM, NORM_MEAN = 0, 1
@@ -136,6 +136,24 @@ SIGNATURES = {
     "capgnn_distill_workspace_bytes": (_sz, [_i64, _i32]),
     "capgnn_distill": (_i32, [_i64, _i32, _vp, _i64, _i32, _vp, _vp, _i64, _i32, _i32, C.c_float, _vp, C.c_double, C.c_float, _vp, _vp,
                               _vp, _i64, _i32, _i32, _vp, _sz, _vp]),
+    "capgnn_embed": (_i32, [_i64, _vp, _i64, _i32, _vp, _i64, _i32, C.c_float, _vp, _i64, _i32, _vp]),
+    "capgnn_embed_bwd_workspace_bytes": (_sz, [_i64, _i64, _i32]),
+    "capgnn_embed_bwd": (_i32, [_i64, _vp, _i64, _i32, _vp, _i64, _i32, C.c_float, _vp, _i64, _i32, _vp, _sz, _vp]),
+    "capgnn_rmsnorm": (_i32, [_i64, _i32, _vp, _i64, _vp, _i64, _vp, _i64, _i32, _vp, C.c_float, _vp, _i64, _i32, _vp, _vp, _vp]),
+    "capgnn_rmsnorm_bwd_workspace_bytes": (_sz, [_i64, _i32]),
+    "capgnn_rmsnorm_bwd": (_i32, [_i64, _i32, _vp, _i64, _i32, _vp, _i64, _i32, _vp, _vp, _vp, _i64, _vp, _i64, _vp, _vp, _sz, _vp]),
+    "capgnn_quantize_rows": (_i32, [_i64, _i32, _vp, _i64, _i32, _vp, _i64, _vp, _vp]),
+    "capgnn_linear_workspace_bytes": (_sz, [_i64, _i64, _i64, _i32]),
+    "capgnn_linear": (_i32, [_i64, _i64, _i64, _vp, _i64, _vp, _vp, _i64, _vp, _i32, _vp, _i32, _vp, _i64, _vp, _i64, _vp, _i64, _i32,
+                             _vp, _sz, _vp]),
+    "capgnn_linear_act_bwd_workspace_bytes": (_sz, [_i64, _i64]),
+    "capgnn_linear_act_bwd": (_i32, [_i64, _i64, _vp, _i64, _vp, _i64, _i32, _i32, _vp, _i64, _vp, _vp, _sz, _vp]),
+    "capgnn_tensors_create": (_i32, [C.POINTER(_vp), _i32, _vp, _vp, _vp, _vp, _vp, _vp]),
+    "capgnn_tensors_destroy": (_i32, [_vp]),
+    "capgnn_grad_workspace_bytes": (_sz, [_vp]),
+    "capgnn_grad_norm": (_i32, [_vp, _vp, _vp, _sz, _vp]),
+    "capgnn_grad_clip": (_i32, [_vp, C.c_float, _vp, _vp, _sz, _vp]),
+    "capgnn_clipped_step": (_i32, [_vp, C.c_float, C.c_float, _vp, _vp, _sz, _vp]),
     "capgnn_epoch_multilabel": (_i32, [_vp, _vp, C.POINTER(Layer), _i32, _vp, _i64, _vp, _i64, _vp, C.c_double, _vp,
                                        C.POINTER(_vp), C.POINTER(_vp), C.POINTER(_vp), C.c_float, C.POINTER(C.c_float),
                                        C.POINTER(EpochTimes), _vp, _sz, _vp, _vp]),
@@ -564,6 +582,121 @@ def distill(n: int, n_classes: int, Z, ldz: int, z_dtype: int, teacher_ids, teac
 def make_teacher(ids, val, ld: int, k: int, rest: int, temperature: float, weight: float) -> Teacher:
     """What a student's epoch learns from: the teacher's k classes of every local vertex (keep the tensors alive)."""
     return Teacher(_p(ids), _p(val), ld, k, rest, temperature, weight)
+
+
+# --------------------------------------------------------------------------- learnt rows, norm, products with an epilogue, clipped update
+def embed(n: int, ids, V: int, F: int, table, ldt: int, dtype: int, scale: float, out, ldo: int, out_dtype: int, stream=None):
+    """out[i] = scale * table[ids[i]] (ids: int64 on the device; one outside the table gives zeros)."""
+    _check(lib().capgnn_embed(n, _p(ids), V, F, _p(table), ldt, dtype, scale, _p(out), ldo, out_dtype, _stream(stream)))
+
+
+def embed_bwd_workspace_bytes(n: int, V: int, F: int) -> int:
+    return int(lib().capgnn_embed_bwd_workspace_bytes(n, V, F))
+
+
+def embed_bwd(n: int, ids, V: int, F: int, dY, lddy: int, dy_dtype: int, scale: float, dtable, lddt: int, accumulate: int, ws,
+              ws_bytes: int, stream=None):
+    """dtable[v] (+)= scale * the sum of dY's rows whose id is v."""
+    _check(lib().capgnn_embed_bwd(n, _p(ids), V, F, _p(dY), lddy, dy_dtype, scale, _p(dtable), lddt, accumulate, _p(ws), ws_bytes,
+                                  _stream(stream)))
+
+
+NORM_MAX = 32768
+
+
+def rmsnorm(n: int, F: int, X, ldx: int, R, ldr: int, H, ldh: int, dtype: int, w, eps: float, Y, ldy: int, y_dtype: int, y_scale=None,
+            rstd=None, stream=None):
+    """h = X + R, Y = h / rms(h) * w; 8-bit rows with a scale each for y_dtype = E4M3."""
+    _check(lib().capgnn_rmsnorm(n, F, _p(X), ldx, _p(R), ldr, _p(H), ldh, dtype, _p(w), eps, _p(Y), ldy, y_dtype, _p(y_scale), _p(rstd),
+                                _stream(stream)))
+
+
+def rmsnorm_bwd_workspace_bytes(n: int, F: int) -> int:
+    return int(lib().capgnn_rmsnorm_bwd_workspace_bytes(n, F))
+
+
+def rmsnorm_bwd(n: int, F: int, dY, lddy: int, dy_dtype: int, H, ldh: int, dtype: int, w, rstd, dH, lddh: int, dX, lddx: int, dw, ws,
+                ws_bytes: int, stream=None):
+    _check(lib().capgnn_rmsnorm_bwd(n, F, _p(dY), lddy, dy_dtype, _p(H), ldh, dtype, _p(w), _p(rstd), _p(dH), lddh, _p(dX), lddx, _p(dw),
+                                    _p(ws), ws_bytes, _stream(stream)))
+
+
+def quantize_rows(n: int, F: int, X, ldx: int, dtype: int, Q, ldq: int, q_scale, stream=None):
+    """Rows in 8 bits (E4M3) with a scale each."""
+    _check(lib().capgnn_quantize_rows(n, F, _p(X), ldx, dtype, _p(Q), ldq, _p(q_scale), _stream(stream)))
+
+
+def linear_workspace_bytes(M: int, N: int, K: int, dtype: int) -> int:
+    return int(lib().capgnn_linear_workspace_bytes(M, N, K, dtype))
+
+
+def linear(M: int, N: int, K: int, A, lda: int, a_scale, W, ldw: int, w_scale, dtype: int, bias, act: int, R, ldr: int, U, ldu: int, Y,
+           ldy: int, out_dtype: int, ws, ws_bytes: int, stream=None):
+    """Y = act(A W^T + bias) + R, one row of W per output; U (or None) keeps the values before the activation."""
+    _check(lib().capgnn_linear(M, N, K, _p(A), lda, _p(a_scale), _p(W), ldw, _p(w_scale), dtype, _p(bias), act, _p(R), ldr, _p(U), ldu,
+                               _p(Y), ldy, out_dtype, _p(ws), ws_bytes, _stream(stream)))
+
+
+def linear_act_bwd_workspace_bytes(M: int, N: int) -> int:
+    return int(lib().capgnn_linear_act_bwd_workspace_bytes(M, N))
+
+
+def linear_act_bwd(M: int, N: int, dY, lddy: int, U, ldu: int, dtype: int, act: int, dU, lddu: int, dbias, ws, ws_bytes: int, stream=None):
+    """dU = dY * act'(U) and its column sums (the products that follow are gemm's)."""
+    _check(lib().capgnn_linear_act_bwd(M, N, _p(dY), lddy, _p(U), ldu, dtype, act, _p(dU), lddu, _p(dbias), _p(ws), ws_bytes,
+                                       _stream(stream)))
+
+
+class TensorList:
+    """capgnn_tensors_create on dense tensors (float32 or bfloat16): gradients, and what they belong to (None: gradients alone).  Keeps
+    references to the tensors: the list holds their addresses."""
+
+    def __init__(self, grads: Sequence, params: Optional[Sequence] = None, stream=None):
+        n = len(grads)
+        if params is not None and [p.numel() for p in params] != [g.numel() for g in grads]:
+            raise ValueError("gradients and parameters of different sizes")
+        both = [*grads, *(params or [])]
+        kinds = {"torch.float32": F32, "torch.bfloat16": BF16}
+        if any(str(t.dtype) not in kinds or not t.is_contiguous() for t in both):
+            raise ValueError("dense float32 or bfloat16 tensors are expected")
+        arrays = lambda ts: ((C.c_void_p * n)(*[t.data_ptr() or None for t in ts]), (C.c_int32 * n)(*[kinds[str(t.dtype)] for t in ts]))
+        pg, tg = arrays(grads)
+        pp, tp = arrays(params) if params is not None else (None, None)
+        self._keep = both
+        self.h = C.c_void_p()
+        _check(lib().capgnn_tensors_create(C.byref(self.h), n, pg, tg, pp, tp, (C.c_int64 * n)(*[g.numel() for g in grads]),
+                                           _stream(stream)))
+
+    def close(self):
+        if self.h:
+            lib().capgnn_tensors_destroy(self.h)
+            self.h = None
+            self._keep = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+def grad_workspace_bytes(t: TensorList) -> int:
+    return int(lib().capgnn_grad_workspace_bytes(t.h))
+
+
+def grad_norm(t: TensorList, norm, ws, ws_bytes: int, stream=None):
+    """The global norm of the list's gradients, to a device float."""
+    _check(lib().capgnn_grad_norm(t.h, _p(norm), _p(ws), ws_bytes, _stream(stream)))
+
+
+def grad_clip(t: TensorList, max_norm: float, norm, ws, ws_bytes: int, stream=None):
+    """... and the gradients brought to a norm of max_norm at most."""
+    _check(lib().capgnn_grad_clip(t.h, max_norm, _p(norm), _p(ws), ws_bytes, _stream(stream)))
+
+
+def clipped_step(t: TensorList, lr: float, max_norm: float, norm, ws, ws_bytes: int, stream=None):
+    """... and the parameters updated with the clipped gradients, which stay as they are."""
+    _check(lib().capgnn_clipped_step(t.h, lr, max_norm, _p(norm), _p(ws), ws_bytes, _stream(stream)))
 
 
 def gin_operator(n_loc: int, n_halo: int, rowptr, col, eps: float):

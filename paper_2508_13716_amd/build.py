@@ -11,7 +11,7 @@ CSRC = os.path.join(HERE, "csrc")
 OBJ = os.path.join(HERE, "_build")
 SO = os.path.join(HERE, "libcapgnn.so")
 SOURCES = ["graph.hip", "spmm.hip", "gemm.hip", "cache.hip", "ops.hip", "layer.hip", "policy.hip", "reorder.hip", "rapa.hip",
-           "answers.hip", "distill.hip", "distill_rest.hip"]
+           "answers.hip", "distill.hip", "distill_rest.hip", "embed.hip", "norm.hip", "linear.hip", "clip.hip"]
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-fno-gpu-rdc",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
          "-Wall", "-Wno-unused-function", "-Wno-unknown-warning-option"]
@@ -28,7 +28,7 @@ def build(force: bool = True, verbose: bool = False) -> str:
     """Compile every translation unit and link the shared library.  Returns its path."""
     os.makedirs(OBJ, exist_ok=True)
     hipcc = _hipcc()
-    headers = [os.path.join(CSRC, h) for h in ("common.h", "grid.h", "softrow.h", "distill.h")] + [os.path.join(HERE, "..", "include", "capgnn.h")]
+    headers = [os.path.join(CSRC, h) for h in ("common.h", "grid.h", "softrow.h", "distill.h", "rows.h")] + [os.path.join(HERE, "..", "include", "capgnn.h")]
     newest_h = max(os.path.getmtime(h) for h in headers)
 
     def one(src: str) -> str:

@@ -1,0 +1,283 @@
+"""capgnn_linear and capgnn_linear_act_bwd against float64, and what they refuse.
+
+Tolerances: a sum of K products in float, in any order, is off by at most K + 8 roundings of the terms' magnitudes (products of bf16 and
+e4m3 numbers are exact in float, those of float add one); scales and bias one each.  An activation passes that on with a slope of at
+most 1.13 and is itself off by at most 8 EPS |u|; the residual's sum is one more.  A slope is off by at most 16 EPS (1 + |u|).
+
+8-bit operands of a bf16 result take the 8-bit matrix instruction.  It adds the products of eight neighbouring k with a common exponent, that
+of the largest, and drops what of the others lies below 2^-13 of that power of two: each of them loses less than 2^-13 of the largest
+product, the largest itself (at most 6 bits behind the point) nothing, so a group loses less than 7 * 2^-13 of its largest product."""
+import numpy as np
+import pytest
+
+from paper_2508_13716_amd import binding as B
+from tests.row_ops import CODE, EPS, FAKE, HALF, Mat, close, held, new, p, refuse, replayed, vec, ws_of
+
+ACTS = {"none": B.ACT_NONE, "relu": B.ACT_RELU, "gelu": B.ACT_GELU, "silu": B.ACT_SILU}
+
+
+# ----------------------------------------------------------------------------- refusals
+def fwd_args(**kw):
+    a = dict(M=4, N=8, K=16, A=FAKE, lda=16, a_scale=None, W=2 * FAKE, ldw=16, w_scale=None, dtype=B.F32, bias=FAKE, act=B.ACT_NONE, R=3 * FAKE, ldr=8,
+             U=4 * FAKE, ldu=8, Y=5 * FAKE, ldy=8, out_dtype=B.F32, ws=FAKE, ws_bytes=1 << 40)
+    a.update(kw)
+    return a
+
+
+@pytest.mark.parametrize("bad", [
+    dict(M=-1), dict(N=-1), dict(K=-1), dict(M=1 << 31), dict(N=1 << 31), dict(K=1 << 31, lda=1 << 31, ldw=1 << 31), dict(dtype=3), dict(dtype=-1),
+    dict(out_dtype=2), dict(act=4), dict(act=-1), dict(A=None), dict(W=None), dict(Y=None), dict(lda=15), dict(ldw=15), dict(ldr=7), dict(ldu=7), dict(ldy=7),
+    dict(a_scale=FAKE), dict(w_scale=FAKE), dict(a_scale=FAKE, dtype=B.BF16), dict(A=FAKE + 2), dict(W=FAKE + 1, dtype=B.BF16), dict(R=FAKE + 2), dict(U=FAKE + 2),
+    dict(Y=FAKE + 1, out_dtype=B.BF16), dict(bias=FAKE + 2), dict(w_scale=FAKE + 2, dtype=B.E4M3), dict(Y=4 * FAKE), dict(U=3 * FAKE), dict(Y=3 * FAKE, ldy=9),
+    dict(Y=FAKE), dict(Y=2 * FAKE), dict(U=FAKE), dict(K=1 << 30, lda=1 << 30, ldw=1 << 30)])
+def test_linear_refuses(bad):
+    refuse(B.EINVAL, B.linear, **fwd_args(**bad))
+
+
+def test_linear_workspace():
+    for M, N, K, t in ((1, 16, 65_536, B.BF16), (100, 100, 16_384, B.F32), (40, 8, 40_000, B.E4M3)):
+        need = B.linear_workspace_bytes(M, N, K, t)
+        if need:
+            a = fwd_args(M=M, N=N, K=K, lda=K, ldw=K, ldr=N, ldu=N, ldy=N, dtype=t)
+            refuse(B.ENOMEM, B.linear, **dict(a, ws_bytes=need - 1))
+            refuse(B.ENOMEM, B.linear, **dict(a, ws=None))
+            refuse(B.EINVAL, B.linear, **dict(a, ws=FAKE + 16))
+    assert B.linear_workspace_bytes(0, 5, 5, B.F32) == 0
+
+
+def bwd_args(**kw):
+    a = dict(M=4, N=8, dY=FAKE, lddy=8, U=2 * FAKE, ldu=8, dtype=B.F32, act=B.ACT_GELU, dU=3 * FAKE, lddu=8, dbias=FAKE, ws=FAKE, ws_bytes=1 << 30)
+    a.update(kw)
+    return a
+
+
+@pytest.mark.parametrize("bad", [dict(M=-1), dict(N=-1), dict(dtype=2), dict(act=4), dict(dY=None), dict(U=None), dict(lddy=7), dict(ldu=7), dict(lddu=7),
+                                 dict(dY=FAKE + 2), dict(U=FAKE + 2), dict(dU=FAKE + 1, dtype=B.BF16), dict(dbias=FAKE + 2), dict(dU=FAKE, lddu=9),
+                                 dict(dU=2 * FAKE, lddu=9), dict(ws=FAKE + 16)])
+def test_linear_act_bwd_refuses(bad):
+    refuse(B.EINVAL, B.linear_act_bwd, **bwd_args(**bad))
+
+
+def test_little_workspace_and_no_work():
+    refuse(B.ENOMEM, B.linear_act_bwd, **bwd_args(ws_bytes=B.linear_act_bwd_workspace_bytes(4, 8) - 1))
+    refuse(B.ENOMEM, B.linear_act_bwd, **bwd_args(ws=None))
+    B.linear(**fwd_args(M=0, A=None, Y=None))
+    B.linear(**fwd_args(N=0, W=None, Y=None))
+    B.linear_act_bwd(**bwd_args(M=0, dY=None, U=None, dU=None, dbias=None, ws=None, ws_bytes=0))
+    B.linear_act_bwd(**bwd_args(N=0))
+
+
+# ----------------------------------------------------------------------------- the formulas in 64 bits
+def erf(x):
+    import torch
+    return torch.special.erf(torch.from_numpy(np.asarray(x, np.float64))).numpy()
+
+
+def act(kind, u):
+    with np.errstate(over="ignore", invalid="ignore"):
+        return {"none": lambda: u, "relu": lambda: np.where(u > 0, u, 0.0), "gelu": lambda: 0.5 * u * (1 + erf(u / np.sqrt(2))),
+                "silu": lambda: u / (1 + np.exp(-u))}[kind]()
+
+
+def slope(kind, u):
+    with np.errstate(over="ignore", invalid="ignore"):
+        s = 1 / (1 + np.exp(-u))
+        return {"none": lambda: np.ones_like(u), "relu": lambda: (u > 0) * 1.0,
+                "gelu": lambda: 0.5 * (1 + erf(u / np.sqrt(2))) + u * np.exp(-0.5 * u * u) / np.sqrt(2 * np.pi), "silu": lambda: s * (1 + u * (1 - s))}[kind]()
+
+
+def check(M, N, K, t, to, kind, bias=True, residual=False, save=False, pad=0, in_place=False, seed=0, spread=1.0):
+    import torch
+    rng = np.random.default_rng(M + 3 * N + 7 * K + seed)
+    a, w = held(rng.standard_normal((M, K)), t), held(rng.standard_normal((N, K)) * (spread / np.sqrt(max(K, 1))), t)
+    sa, sw = (held(np.exp(rng.standard_normal((1, M))), "f32"), held(np.exp(rng.standard_normal((1, N))), "f32")) if t == "e4m3" else (None, None)
+    if t == "e4m3":
+        w = held(rng.standard_normal((N, K)), t)
+        sw = held(sw / np.sqrt(max(K, 1)), "f32")
+    b = held(rng.standard_normal((1, N)), "f32") if bias else None
+    r = held(rng.standard_normal((M, N)), to) if residual else None
+    ldk, ldn = K + pad, N + pad
+    A, W, bd, sad, swd = Mat(a, t, ldk, pad % 2), Mat(w, t, ldk, pad % 3), vec(b), vec(sa), vec(sw)
+    R = Mat(r, to, ldn, pad % 2) if residual else None
+    U = new(M, N, to, ldn, pad % 3) if save else None
+    Y = R if in_place else new(M, N, to, ldn, pad % 5)
+    size = B.linear_workspace_bytes(M, N, K, CODE[t])
+    ws, size = ws_of(size)
+    args = (M, N, K, A.p, ldk, p(sad), W.p, ldk, p(swd), CODE[t], p(bd), ACTS[kind], p(R), ldn, p(U), ldn, Y.p, ldn, CODE[to], ws, size)
+    B.linear(*args)
+    torch.cuda.synchronize()
+    sums, mass = a @ w.T, np.abs(a) @ np.abs(w).T
+    dropped = np.zeros((M, N))
+    if t == "e4m3" and to == "bf16":
+        for k in range(0, K, 8):
+            largest = np.zeros((M, N))
+            for q in range(k, min(k + 8, K)):
+                largest = np.maximum(largest, np.outer(np.abs(a[:, q]), np.abs(w[:, q])))
+            dropped += 7 * 2.0 ** -13 * largest
+    if sa is not None:
+        both = sa.T @ sw
+        sums, mass, dropped = sums * both, mass * both, dropped * both
+    u = sums + (b if bias else 0.0)
+    u_err = mass * (K + 12) * EPS + dropped + 2 * EPS * np.abs(u) + 1e-36
+    if save:
+        close(U.get(), u, u_err * 1.001 + np.abs(u) * HALF[to] * 1.001, "U")
+    y = act(kind, u) + (r if residual else 0.0)
+    err = 1.13 * u_err + 8 * EPS * np.abs(u) + 2 * EPS * np.abs(y)
+    close(Y.get(), y, err * 1.001 + np.abs(y) * HALF[to] * 1.001, "Y")
+    if not in_place:                                 # the same every time
+        first = Y.raw()
+        B.linear(*args)
+        torch.cuda.synchronize()
+        assert torch.equal(first, Y.raw())
+    A.get(), W.get()
+
+
+SIZES = [(1, 1, 1), (1, 47, 602), (3, 5, 7), (2, 64, 128), (7, 1, 33), (15, 17, 65), (16, 16, 64), (17, 33, 129), (33, 65, 31), (64, 64, 64), (65, 129, 257),
+         (128, 256, 96), (130, 100, 1000), (1, 1030, 512), (5, 300, 2050), (257, 1, 40), (200, 3, 5000), (16, 300, 8200), (100, 90, 12_000), (300, 520, 64)]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("M,N,K", SIZES)
+@pytest.mark.parametrize("t,to", [("f32", "f32"), ("bf16", "bf16"), ("e4m3", "bf16"), ("bf16", "f32"), ("e4m3", "f32"), ("f32", "bf16")])
+@pytest.mark.parametrize("kind,residual,save,pad", [("none", False, False, 0), ("gelu", True, True, 5), ("silu", True, False, 16)])
+def test_linear(M, N, K, t, to, kind, residual, save, pad):
+    check(M, N, K, t, to, kind, residual=residual, save=save, pad=pad)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("t", ["f32", "bf16", "e4m3"])
+@pytest.mark.parametrize("M,N,K", [(1, 70, 300), (40, 50, 300), (300, 260, 300)])
+def test_variants(M, N, K, t):
+    for k, (kind, bias, residual, save, pad) in enumerate([("relu", False, False, True, 0), ("relu", True, True, False, 3), ("none", False, True, False, 8),
+                                                            ("gelu", False, False, False, 1), ("silu", True, False, True, 7)]):
+        check(M, N, K, t, "bf16" if k % 2 else "f32", kind, bias, residual, save, pad, seed=k)
+    check(M, N, K, t, "f32", "gelu", residual=True, in_place=True, save=True)
+    check(M, N, K, t, "bf16", "silu", residual=True, in_place=True, pad=3)
+    check(M, N, K, t, "f32", "silu", spread=40.0)    # far out on both sides of the activations
+    check(M, N, K, t, "f32", "gelu", spread=40.0)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("M,N,K,t", [(1000, 1100, 700, "bf16"), (513, 2049, 384, "e4m3"), (700, 600, 513, "f32"), (2100, 515, 2048, "bf16"), (1030, 1030, 1024, "e4m3"),
+                                     (1500, 47, 256, "f32"), (2600, 2600, 128, "bf16"), (2570, 2590, 256, "f32")])
+def test_large_tiles(M, N, K, t):
+    check(M, N, K, t, "f32", "none")
+    check(M, N, K, t, "bf16", "gelu", residual=True, save=True, pad=8)
+    check(M, N, K, t, "bf16", "silu", residual=True, pad=3)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("M", [1, 20, 200])
+def test_no_reduction(M):
+    """K = 0: the epilogue of zeros"""
+    import torch
+    N = 70
+    rng = np.random.default_rng(1)
+    b, r = held(rng.standard_normal((1, N)), "f32"), held(rng.standard_normal((M, N)), "f32")
+    for t in ("f32", "bf16", "e4m3"):
+        Y, R, bd = new(M, N, "f32"), Mat(r, "f32"), vec(b)
+        B.linear(M, N, 0, None, 0, None, None, 0, None, CODE[t], bd.p, B.ACT_RELU, R.p, N, None, 0, Y.p, N, B.F32, *ws_of(B.linear_workspace_bytes(M, N, 0, CODE[t])))
+        torch.cuda.synchronize()
+        assert np.array_equal(Y.get(), held(np.maximum(b, 0) + r, "f32"))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("M,N,K", [(2, 40, 100), (30, 50, 130), (300, 400, 200)])
+@pytest.mark.parametrize("t", ["f32", "bf16", "e4m3"])
+def test_what_is_not_finite_stays_in_its_row_and_column(M, N, K, t):
+    import torch
+    a, w = np.ones((M, K)), np.ones((N, K))
+    a[M - 1, K - 1] = np.nan
+    w[N - 1, 0] = np.nan
+    for pad in (0, 5):                               # (the padding holds NaN, too)
+        A, W, Y = Mat(a, t, K + pad), Mat(w, t, K + pad), new(M, N, "f32")
+        B.linear(M, N, K, A.p, K + pad, None, W.p, K + pad, None, CODE[t], None, B.ACT_NONE, None, 0, None, 0, Y.p, N, B.F32,
+                 *ws_of(B.linear_workspace_bytes(M, N, K, CODE[t])))
+        torch.cuda.synchronize()
+        y = Y.get()
+        assert np.isnan(y[M - 1]).all() and np.isnan(y[:, N - 1]).all() and (y[:M - 1, :N - 1] == K).all()
+
+
+@pytest.mark.gpu
+def test_operands_beyond_32_bit_offsets():
+    import torch
+    M, K = 4_200_000, 1030                           # A has more than 2^32 elements
+    A = torch.zeros((M, K), dtype=torch.bfloat16, device="cuda")
+    A[-1] = 2.0
+    A[0] = 1.0
+    W = torch.ones((3, K), dtype=torch.bfloat16, device="cuda")
+    Y = torch.empty((M, 3), device="cuda")
+    ws, size = ws_of(B.linear_workspace_bytes(M, 3, K, B.BF16))
+    B.linear(M, 3, K, A, K, None, W, K, None, B.BF16, None, B.ACT_NONE, None, 0, None, 0, Y, 3, B.F32, ws, size)
+    torch.cuda.synchronize()
+    assert Y[0].tolist() == [1030.0] * 3 and Y[-1].tolist() == [2060.0] * 3 and int(torch.count_nonzero(Y)) == 6
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("M,N,K,t", [(1, 100, 4000, "bf16"), (90, 80, 9000, "f32"), (600, 700, 256, "e4m3"), (1200, 1100, 128, "bf16")])
+def test_recorded_and_replayed(M, N, K, t):
+    rng = np.random.default_rng(3)
+    A, W, R, U, Y, bias = Mat(rng.standard_normal((M, K)), t), Mat(rng.standard_normal((N, K)), t), Mat(rng.standard_normal((M, N)), "bf16"), new(M, N, "bf16"), new(M, N, "bf16"), vec(rng.standard_normal(N))
+    dU, db = new(M, N, "bf16"), new(1, N, "f32")
+    ws, size = ws_of(max(B.linear_workspace_bytes(M, N, K, CODE[t]), B.linear_act_bwd_workspace_bytes(M, N)))
+
+    def run(st):
+        B.linear(M, N, K, A.p, K, None, W.p, K, None, CODE[t], bias.p, B.ACT_GELU, R.p, N, U.p, N, Y.p, N, B.BF16, ws, size, stream=st)
+        B.linear_act_bwd(M, N, Y.p, N, U.p, N, B.BF16, B.ACT_GELU, dU.p, N, db.p, ws, size, stream=st)
+    replayed(run, lambda: [Y.raw(), U.raw(), dU.raw(), db.raw()])
+
+
+# ----------------------------------------------------------------------------- the epilogue's gradient
+@pytest.mark.gpu
+@pytest.mark.parametrize("M,N", [(1, 1), (3, 5), (17, 8), (70, 100), (33, 1009), (5, 4096), (1500, 47), (4001, 260)])
+@pytest.mark.parametrize("t", ["f32", "bf16"])
+@pytest.mark.parametrize("kind", ["none", "relu", "gelu", "silu"])
+def test_epilogue_gradient(M, N, t, kind):
+    import torch
+    rng = np.random.default_rng(M + N)
+    dy, u = held(rng.standard_normal((M, N)), t), held(rng.standard_normal((M, N)) * 3, t)
+    u[0, 0] = 0.0
+    want = dy * slope(kind, u)
+    err = 16 * EPS * (1 + np.abs(u)) * np.abs(dy)
+    for way, pad in (("own", 0), ("dY", 3), ("U", 5), ("none", 1)):
+        dY, U = Mat(dy, t, N + pad, pad % 2), Mat(u, t, N + pad, pad % 2)
+        dU = {"own": new(M, N, t, N + pad), "dY": dY, "U": U, "none": None}[way]
+        if way == "U" and kind == "none":
+            continue
+        db = new(1, N, "f32")
+        ws, size = ws_of(B.linear_act_bwd_workspace_bytes(M, N))
+        B.linear_act_bwd(M, N, dY.p, N + pad, U.p, N + pad, CODE[t], ACTS[kind], p(dU), N + pad, db.p, ws, size)
+        torch.cuda.synchronize()
+        if dU is not None:
+            close(dU.get(), want, err + np.abs(want) * HALF[t] * 1.001, way)
+        close(db.get()[0], want.sum(0), (np.abs(want).sum(0) * (M + 8) * EPS + err.sum(0)) * 1.001, "dbias")
+    if kind == "none":
+        dU = new(M, N, t)
+        B.linear_act_bwd(M, N, Mat(dy, t).p, N, None, 0, CODE[t], B.ACT_NONE, dU.p, N, None, None, 0)
+        torch.cuda.synchronize()
+        assert np.array_equal(dU.get(), dy)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("kind", ["gelu", "silu"])
+def test_gradients_of_a_layer_are_those_of_differences(kind):
+    """dA, dW, db, dR of Y = act(A W^T + b) + R by the epilogue's gradient and capgnn_gemm's products"""
+    import torch
+    M, N, K, step = 9, 14, 21, 1e-5
+    rng = np.random.default_rng(8)
+    a, w, b, up = (held(rng.standard_normal(s), "f32") for s in ((M, K), (N, K), (1, N), (M, N)))
+    w = held(w / np.sqrt(K), "f32")
+    loss = lambda a, w, b: float((act(kind, a @ w.T + b) * up).sum())
+    A, W, bd, U, Y, dY = Mat(a, "f32"), Mat(w, "f32"), vec(b), new(M, N, "f32"), new(M, N, "f32"), Mat(up, "f32")
+    ws, size = ws_of(max(B.linear_workspace_bytes(M, N, K, B.F32), B.linear_act_bwd_workspace_bytes(M, N), B.gemm_workspace_bytes(1, N, K, M), B.gemm_workspace_bytes(0, M, K, N)))
+    B.linear(M, N, K, A.p, K, None, W.p, K, None, B.F32, bd.p, ACTS[kind], None, 0, U.p, N, Y.p, N, B.F32, ws, size)
+    dU, db, dA, dW = new(M, N, "f32"), new(1, N, "f32"), new(M, K, "f32"), new(N, K, "f32")
+    B.linear_act_bwd(M, N, dY.p, N, U.p, N, B.F32, ACTS[kind], dU.p, N, db.p, ws, size)
+    B.gemm(0, 0, M, K, N, dU.p, N, W.p, K, dA.p, K, B.F32, 1, 0, None, 0, None, 0, ws=ws, ws_bytes=size)
+    B.gemm(1, 0, N, K, M, dU.p, N, A.p, K, dW.p, K, B.F32, 1, 0, None, 0, None, 0, ws=ws, ws_bytes=size)
+    torch.cuda.synchronize()
+    for _ in range(6):
+        x, y, z = rng.standard_normal((M, K)), rng.standard_normal((N, K)), rng.standard_normal((1, N))
+        want = (loss(a + step * x, w + step * y, b + step * z) - loss(a - step * x, w - step * y, b - step * z)) / (2 * step)
+        terms = [dA.get() * x, dW.get() * y, db.get() * z]
+        assert abs(sum(float(q.sum()) for q in terms) - want) <= 1e-5 * sum(float(np.abs(q).sum()) for q in terms)
