@@ -10,6 +10,8 @@
 #include "grid.h"
 
 #include <algorithm>
+#include <type_traits>
+#include <utility>
 
 namespace capgnn {
 
@@ -30,55 +32,93 @@ struct LinearArgs {
 };
 
 // ------------------------------------------------------------------ activations
-__device__ __forceinline__ float act_of(int act, float u) {
-    if (act == CAPGNN_ACT_RELU) return u > 0.f ? u : 0.f;
-    if (act == CAPGNN_ACT_GELU) return 0.5f * u * (1.f + erff(u * 0.70710678118654752f));
-    if (act == CAPGNN_ACT_SILU) return u / (1.f + expf(-u));
-    return u;
+// exp(-x) and 1 / x by the hardware's instructions, one unit in the last place each: what the formulas lose by that is a few EPS |u|.
+__device__ __forceinline__ float exp_minus(float x) { return __builtin_amdgcn_exp2f(x * -1.4426950408889634f); }
+__device__ __forceinline__ float logistic(float u) { return __builtin_amdgcn_rcpf(1.f + exp_minus(u)); }
+
+// Phi(u), the normal distribution, and exp(-u^2 / 2): 1 - Phi(|u|) = t (a1 + t (a2 + ...)) exp(-u^2 / 2) / 2 with t = 1 / (1 + p |u| / 2^1/2),
+// Abramowitz and Stegun, Handbook of Mathematical Functions, 7.1.26: erf to 1.5e-7, Phi to 0.75e-7.  (erff takes two branches
+// of polynomials, several times the operations.)
+__device__ __forceinline__ float normal(float u, float *bell) {
+    const float t = __builtin_amdgcn_rcpf(fmaf(0.3275911f * 0.70710678118654752f, fabsf(u), 1.f));
+    const float e = exp_minus(0.5f * u * u);
+    *bell = e;
+    const float p = fmaf(fmaf(fmaf(fmaf(0.5f * 1.061405429f, t, 0.5f * -1.453152027f), t, 0.5f * 1.421413741f), t, 0.5f * -0.284496736f), t, 0.5f * 0.254829592f);
+    const float tail = p * t * e;
+    return u < 0.f ? tail : 1.f - tail;
 }
-__device__ __forceinline__ float act_slope(int act, float u) {
-    if (act == CAPGNN_ACT_RELU) return u > 0.f ? 1.f : 0.f;
-    if (act == CAPGNN_ACT_GELU) return 0.5f * (1.f + erff(u * 0.70710678118654752f)) + u * expf(-0.5f * u * u) * 0.39894228040143268f;
-    if (act == CAPGNN_ACT_SILU) {
-        const float s = 1.f / (1.f + expf(-u));
-        return s * (1.f + u * (1.f - s));
-    }
-    return 1.f;
+template <int ACT> __device__ __forceinline__ float act_of(float u) {
+    float bell;
+    if constexpr (ACT == CAPGNN_ACT_RELU) return u > 0.f ? u : 0.f;
+    else if constexpr (ACT == CAPGNN_ACT_GELU) return u * normal(u, &bell);
+    else if constexpr (ACT == CAPGNN_ACT_SILU) return u * logistic(u);
+    else return u;
+}
+template <int ACT> __device__ __forceinline__ float act_slope(float u) {
+    if constexpr (ACT == CAPGNN_ACT_RELU) return u > 0.f ? 1.f : 0.f;
+    else if constexpr (ACT == CAPGNN_ACT_GELU) {
+        float bell;
+        const float phi = normal(u, &bell);
+        return fmaf(u * 0.39894228040143268f, bell, phi);
+    } else if constexpr (ACT == CAPGNN_ACT_SILU) {
+        const float s = logistic(u);
+        return s * fmaf(u, 1.f - s, 1.f);
+    } else return 1.f;
+}
+// f(ACT) with the activation as a compile-time number
+template <class F> __host__ __device__ __forceinline__ void with_act(int act, F f) {
+    if (act == CAPGNN_ACT_GELU) f(std::integral_constant<int, CAPGNN_ACT_GELU>());
+    else if (act == CAPGNN_ACT_SILU) f(std::integral_constant<int, CAPGNN_ACT_SILU>());
+    else if (act == CAPGNN_ACT_RELU) f(std::integral_constant<int, CAPGNN_ACT_RELU>());
+    else f(std::integral_constant<int, CAPGNN_ACT_NONE>());
+}
+template <int V> __device__ __forceinline__ void act_all(int act, float (&v)[V]) {
+    with_act(act, [&](auto k) {
+#pragma unroll
+        for (int e = 0; e < V; ++e) v[e] = act_of<k.value>(v[e]);
+    });
+}
+
+// V elements of which the first `count` are inside the matrix
+template <int V> __device__ __forceinline__ void ld_some(bool bf16, const char *p, int count, float (&v)[V]) {
+    if (count == V) return ld_row_of<V>(bf16, p, 0, v);
+#pragma unroll
+    for (int e = 0; e < V; ++e) v[e] = e < count ? bf16 ? ld_logit<true>(p, e) : ld_logit<false>(p, e) : 0.f;
+}
+template <int V> __device__ __forceinline__ void st_some(bool bf16, char *p, int count, const float (&v)[V]) {
+    if (count == V) return st_row_of<V>(bf16, p, 0, v);
+#pragma unroll
+    for (int e = 0; e < V; ++e)
+        if (e < count) bf16 ? st_grad<true>(p, e, v[e]) : st_grad<false>(p, e, v[e]);
 }
 
 // V neighbouring sums of row i from column j on, the first `count` of them inside the matrix: the whole epilogue
 template <int V> __device__ __forceinline__ void finish(const LinearArgs &g, int64_t i, int64_t j, int count, float (&v)[V]) {
     const int es = g.out_bf16 ? 2 : 4;
-    const float sa = g.a_scale ? g.a_scale[i] : 1.f;
+    if (g.a_scale) {
+        const float s = g.a_scale[i];
 #pragma unroll
-    for (int e = 0; e < V; ++e)
-        if (e < count) {
-            if (g.a_scale || g.w_scale) v[e] *= g.w_scale ? sa * g.w_scale[j + e] : sa;
-            if (g.bias) v[e] += g.bias[j + e];
-        }
-    char *y = g.Y + i * g.ldy + j * es, *u = g.U + i * g.ldu + j * es;
-    const char *r = g.R + i * g.ldr + j * es;
-    if (count == V) {
-        if (g.U) st_row_of<V>(g.out_bf16, u, 0, v);
-#pragma unroll
-        for (int e = 0; e < V; ++e) v[e] = act_of(g.act, v[e]);
-        if (g.R) {
-            float x[V];
-            ld_row_of<V>(g.out_bf16, r, 0, x);
-#pragma unroll
-            for (int e = 0; e < V; ++e) v[e] += x[e];
-        }
-        st_row_of<V>(g.out_bf16, y, 0, v);
-    } else {
-#pragma unroll
-        for (int e = 0; e < V; ++e)
-            if (e < count) {
-                if (g.U) g.out_bf16 ? st_grad<true>(u, e, v[e]) : st_grad<false>(u, e, v[e]);
-                v[e] = act_of(g.act, v[e]);
-                if (g.R) v[e] += g.out_bf16 ? ld_logit<true>(r, e) : ld_logit<false>(r, e);
-                g.out_bf16 ? st_grad<true>(y, e, v[e]) : st_grad<false>(y, e, v[e]);
-            }
+        for (int e = 0; e < V; ++e) v[e] *= s;
     }
+    float x[V];
+    if (g.w_scale) {
+        ld_some<V>(false, reinterpret_cast<const char *>(g.w_scale + j), count, x);
+#pragma unroll
+        for (int e = 0; e < V; ++e) v[e] *= x[e];
+    }
+    if (g.bias) {
+        ld_some<V>(false, reinterpret_cast<const char *>(g.bias + j), count, x);
+#pragma unroll
+        for (int e = 0; e < V; ++e) v[e] += x[e];
+    }
+    if (g.U) st_some<V>(g.out_bf16, g.U + i * g.ldu + j * es, count, v);
+    act_all<V>(g.act, v);
+    if (g.R) {
+        ld_some<V>(g.out_bf16, g.R + i * g.ldr + j * es, count, x);
+#pragma unroll
+        for (int e = 0; e < V; ++e) v[e] += x[e];
+    }
+    st_some<V>(g.out_bf16, g.Y + i * g.ldy + j * es, count, v);
 }
 
 // ------------------------------------------------------------------ the matrix instructions, on 16-byte units
@@ -100,57 +140,6 @@ __device__ __forceinline__ half8 widen8(raw16 u, int e) {
     return half8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
 }
 
-// the products of a tile's 128 bytes of k; a and b: the lane's rows in LDS (row % 32 is the lane's)
-template <int DT, int TM, int TN>
-__device__ __forceinline__ void multiply(const raw16 *As, const raw16 *Bs, int row_a, int row_b, int half, acc16 (&acc)[TM][TN]) {
-    if constexpr (DT == CAPGNN_E4M3) {
-#pragma unroll
-        for (int s = 0; s < 2; ++s) {
-            int8v a[TM], b[TN];
-#pragma unroll
-            for (int i = 0; i < TM; ++i) {
-                const raw16 lo = As[unit_at(row_a + i * 32, 4 * s + 2 * half)], hi = As[unit_at(row_a + i * 32, 4 * s + 2 * half + 1)];
-                a[i] = int8v{int(lo[0]), int(lo[1]), int(lo[2]), int(lo[3]), int(hi[0]), int(hi[1]), int(hi[2]), int(hi[3])};
-            }
-#pragma unroll
-            for (int i = 0; i < TN; ++i) {
-                const raw16 lo = Bs[unit_at(row_b + i * 32, 4 * s + 2 * half)], hi = Bs[unit_at(row_b + i * 32, 4 * s + 2 * half + 1)];
-                b[i] = int8v{int(lo[0]), int(lo[1]), int(lo[2]), int(lo[3]), int(hi[0]), int(hi[1]), int(hi[2]), int(hi[3])};
-            }
-#pragma unroll
-            for (int i = 0; i < TM; ++i)
-#pragma unroll
-                for (int j = 0; j < TN; ++j)
-                    acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a[i], b[j], acc[i][j], 0, 0, 0, 0x7f7f7f7f, 0, 0x7f7f7f7f);
-        }
-    } else {
-#pragma unroll
-        for (int s = 0; s < 4; ++s) {
-            raw16 a[TM], b[TN];
-#pragma unroll
-            for (int i = 0; i < TM; ++i) a[i] = As[unit_at(row_a + i * 32, 2 * s + half)];
-#pragma unroll
-            for (int i = 0; i < TN; ++i) b[i] = Bs[unit_at(row_b + i * 32, 2 * s + half)];
-#pragma unroll
-            for (int i = 0; i < TM; ++i)
-#pragma unroll
-                for (int j = 0; j < TN; ++j) {
-                    if constexpr (DT == CAPGNN_BF16) {
-                        acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(half8, a[i]), __builtin_bit_cast(half8, b[j]), acc[i][j], 0, 0, 0);
-                    } else if constexpr (DT == E4M3_FINE) {
-#pragma unroll
-                        for (int e = 0; e < 2; ++e)
-                            acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(widen8(a[i], e), widen8(b[j], e), acc[i][j], 0, 0, 0);
-                    } else {
-#pragma unroll
-                        for (int e = 0; e < 4; ++e)
-                            acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(a[i][e]), __uint_as_float(b[j][e]), acc[i][j], 0, 0, 0);
-                    }
-                }
-        }
-    }
-}
-
 // 16 bytes of a row from element k on; elements from `end` on are zero and not read
 template <int DT> __device__ __forceinline__ raw16 load_unit(const char *row, int64_t k, int64_t end) {
     constexpr int E = 16 / BYTES<DT>;
@@ -167,13 +156,137 @@ template <int DT> __device__ __forceinline__ raw16 load_unit(const char *row, in
     return r;
 }
 
+// a step's products are formed a slice of k at a time, one instruction's (of fp32: four) for each pair of tiles
+template <int DT> constexpr int SLICES = DT == CAPGNN_E4M3 ? 2 : 4;
+
+template <int DT, int T> struct Slice {                                 // a lane's operands of T tiles' rows
+    static constexpr int U = DT == CAPGNN_E4M3 ? 2 : 1;
+    raw16 u[T][U];
+    __device__ __forceinline__ void read(const raw16 *tile, int row, int half, int s) {
+#pragma unroll
+        for (int i = 0; i < T; ++i)
+#pragma unroll
+            for (int q = 0; q < U; ++q) u[i][q] = tile[unit_at(row + i * 32, (2 * s + half) * U + q)];
+    }
+};
+__device__ __forceinline__ int8v join_units(raw16 lo, raw16 hi) {
+    return int8v{int(lo[0]), int(lo[1]), int(lo[2]), int(lo[3]), int(hi[0]), int(hi[1]), int(hi[2]), int(hi[3])};
+}
+template <int DT, int TM, int TN>
+__device__ __forceinline__ void multiply_slice(const Slice<DT, TM> &a, const Slice<DT, TN> &b, acc16 (&acc)[TM][TN]) {
+#pragma unroll
+    for (int i = 0; i < TM; ++i)
+#pragma unroll
+        for (int j = 0; j < TN; ++j) {
+            if constexpr (DT == CAPGNN_E4M3) {
+                acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(join_units(a.u[i][0], a.u[i][1]), join_units(b.u[j][0], b.u[j][1]), acc[i][j], 0, 0, 0,
+                                                                            0x7f7f7f7f, 0, 0x7f7f7f7f);
+            } else if constexpr (DT == CAPGNN_BF16) {
+                acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(half8, a.u[i][0]), __builtin_bit_cast(half8, b.u[j][0]), acc[i][j], 0, 0, 0);
+            } else if constexpr (DT == E4M3_FINE) {
+#pragma unroll
+                for (int e = 0; e < 2; ++e)
+                    acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(widen8(a.u[i][0], e), widen8(b.u[j][0], e), acc[i][j], 0, 0, 0);
+            } else {
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(a.u[i][0][e]), __uint_as_float(b.u[j][0][e]), acc[i][j], 0, 0, 0);
+            }
+        }
+}
+
 // ------------------------------------------------------------------ tiles
+// Where a wave's results leave through: 32 rows at a time, so that memory is read and written along the rows
+template <int TN> constexpr int STAGE_PITCH = TN * 32 + 8;              // floats: four rows further lie in the other half of the banks
+template <int WAVES, int TN> constexpr int STAGE_BYTES = WAVES * 32 * STAGE_PITCH<TN> * 4;
+
+template <int... I, class F> __device__ __forceinline__ void repeat(std::integer_sequence<int, I...>, F f) { (f(std::integral_constant<int, I>()), ...); }
+
+// 8 neighbouring results as they lie in memory
+template <bool OB> struct RawOut {
+    raw16 r[OB ? 1 : 2];
+    __device__ __forceinline__ void load(const char *p) {
+        if constexpr (OB) r[0] = *reinterpret_cast<const raw16_by2 *>(p);
+        else {
+            r[0] = *reinterpret_cast<const raw16_by4 *>(p);
+            r[1] = *reinterpret_cast<const raw16_by4 *>(p + 16);
+        }
+    }
+    __device__ __forceinline__ float get(int e) const { return OB ? Raw<true>::get(r[0], e) : __uint_as_float(r[OB ? 0 : e / 4][e % 4]); }
+};
+
+// OB: results in bf16.  A lane keeps its 8 columns, so their bias and scales are read once; the residual's rows are all asked for before the
+// results of the 32 rows are on their way through LDS.
+template <bool OB, int WR, int WC, int TM, int TN>
+__device__ __forceinline__ void store_tile(const LinearArgs &g, raw16 *lds, int64_t m0, int64_t n0, const acc16 (&acc)[TM][TN]) {
+    constexpr int PITCH = STAGE_PITCH<TN>, LANES = TN * 4, ROWS = 64 / LANES, PASSES = 32 / ROWS, ES = OB ? 2 : 4;
+    const int wave = threadIdx.x / 64, lane = threadIdx.x & 63, half = lane / 32;
+    float *stage = reinterpret_cast<float *>(lds) + wave * 32 * PITCH;
+    const float *mine = stage + lane / LANES * PITCH + lane % LANES * 8;
+    const int64_t col = n0 + lane % LANES * 8;
+    const int count = static_cast<int>(max(min(g.N - col, int64_t(8)), int64_t(0)));
+    float bias[8], scale[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        bias[e] = 0.f;
+        scale[e] = 1.f;
+    }
+    if (count) {
+        if (g.bias) ld_some<8>(false, reinterpret_cast<const char *>(g.bias + col), count, bias);
+        if (g.w_scale) ld_some<8>(false, reinterpret_cast<const char *>(g.w_scale + col), count, scale);
+    }
+    // (one copy of the code per 32 rows, whatever its size: a loop over accumulators that is not unrolled would put them into memory)
+    repeat(std::make_integer_sequence<int, TM>(), [&](auto at) __attribute__((always_inline)) {
+        constexpr int i = at.value;
+        const int64_t first = m0 + i * 32 + lane / LANES;               // the lane's rows: first + p * ROWS
+        RawOut<OB> r[PASSES];
+        if (g.R && count == 8) {
+#pragma unroll
+            for (int p = 0; p < PASSES; ++p) r[p].load(g.R + min(first + p * ROWS, g.M - 1) * g.ldr + col * ES);
+        }
+#pragma unroll
+        for (int j = 0; j < TN; ++j)
+#pragma unroll
+            for (int k = 0; k < 16; ++k) stage[(8 * (k / 4) + 4 * half + k % 4) * PITCH + j * 32 + lane % 32] = acc[i][j][k];
+        __builtin_amdgcn_wave_barrier();
+        if (count == 8) {
+            with_act(g.act, [&](auto act) {
+#pragma unroll
+                for (int p = 0; p < PASSES; ++p) {
+                    const int64_t row = first + p * ROWS;
+                    if (row >= g.M) continue;
+                    float v[8];
+                    ld_row<false, 8>(reinterpret_cast<const char *>(mine + p * ROWS * PITCH), 0, v);
+                    const float s = g.a_scale ? g.a_scale[row] : 1.f;
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) v[e] = fmaf(v[e], s * scale[e], bias[e]);
+                    if (g.U) st_row<OB, 8>(g.U + row * g.ldu + col * ES, 0, v);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        v[e] = act_of<act.value>(v[e]);
+                        if (g.R) v[e] += r[p].get(e);
+                    }
+                    st_row<OB, 8>(g.Y + row * g.ldy + col * ES, 0, v);
+                }
+            });
+        } else if (count) {
+#pragma unroll 1
+            for (int p = 0; p < PASSES; ++p) {
+                if (first + p * ROWS >= g.M) break;
+                float v[8];
+                ld_row<false, 8>(reinterpret_cast<const char *>(mine + p * ROWS * PITCH), 0, v);
+                finish<8>(g, first + p * ROWS, col, count, v);
+            }
+        }
+        __builtin_amdgcn_wave_barrier();
+    });
+}
+
 // WR x WC waves with TM x TN accumulators of 32 x 32 each: a tile of WR TM 32 rows of A by WC TN 32 rows of W.
-template <int DT, int WR, int WC, int TM, int TN> __global__ __launch_bounds__(WR *WC * 64) void linear_tile_kernel(LinearArgs g) {
+template <int DT, bool OB, int WR, int WC, int TM, int TN> __global__ __launch_bounds__(WR *WC * 64) void linear_tile_kernel(LinearArgs g) {
     constexpr int T = WR * WC * 64, BM = WR * TM * 32, BN = WC * TN * 32, STEP = 128 / BYTES<DT>;
     constexpr int PA = BM * UNITS / T, PB = BN * UNITS / T;             // units that a thread loads
-    constexpr int PITCH = TN * 32 + 8;                                  // floats: four rows further lie in the other half of the banks
-    constexpr int STAGE = WR * WC * 32 * PITCH * 4, TILES = (BM + BN) * UNITS * 16;
+    constexpr int STAGE = STAGE_BYTES<WR * WC, TN>, TILES = (BM + BN) * UNITS * 16;
     __shared__ raw16 lds[(STAGE > TILES ? STAGE : TILES) / 16];
     raw16 *As = lds, *Bs = lds + BM * UNITS;
     const int wave = threadIdx.x / 64, lane = threadIdx.x & 63, half = lane / 32;
@@ -202,29 +315,97 @@ template <int DT, int WR, int WC, int TM, int TN> __global__ __launch_bounds__(W
         for (int p = 0; p < PB; ++p) Bs[unit_at((p * T + threadIdx.x) / UNITS, threadIdx.x % UNITS)] = rb[p];
         __syncthreads();
         if (k + STEP < g.K) fetch(k + STEP);
-        multiply<DT, TM, TN>(As, Bs, wm + lane % 32, wn + lane % 32, half, acc);
+#pragma unroll
+        for (int s = 0; s < SLICES<DT>; ++s) {
+            Slice<DT, TM> a;
+            Slice<DT, TN> b;
+            a.read(As, wm + lane % 32, half, s);
+            b.read(Bs, wn + lane % 32, half, s);
+            multiply_slice<DT, TM, TN>(a, b, acc);
+        }
     }
     __syncthreads();
-    // 32 rows of a wave's results at a time through LDS, so that memory is read and written along the rows
-    float *stage = reinterpret_cast<float *>(lds) + wave * 32 * PITCH;
+    store_tile<OB, WR, WC, TM, TN>(g, lds, m0 + wm, n0 + wn, acc);
+}
+
+// The same for aligned operands (16 bytes) that need no check but at the last step: loads go straight to LDS, one step ahead, and the operands
+// of a slice (half or a quarter of a step) are read while the one before is multiplied, across the barrier too: behind the last slice's
+// reads the other buffer's loads are waited for, this one's are free to start, and the next step's first slice is read.
+// Tile of a workgroup.  Workgroups go round the L2 domains one by one: each domain gets a stretch of tiles, in bands of 8 rows of tiles, so that
+// what runs on it at a time shares rows of both operands.
+__device__ __forceinline__ void tile_of(unsigned tiles_m, unsigned tiles_n, unsigned *m, unsigned *n) {
+    const unsigned all = tiles_m * tiles_n, d = blockIdx.x % NUM_XCD, k = blockIdx.x / NUM_XCD;
+    const unsigned t = all / NUM_XCD * d + min(d, all % NUM_XCD) + k;
+    const unsigned band = t / (8 * tiles_n), first = band * 8, rows = min(8u, tiles_m - first), in = t - band * 8 * tiles_n;
+    *m = first + in % rows;
+    *n = in / rows;
+}
+
+template <int DT, bool OB, int WR, int WC, int TM, int TN> __global__ __launch_bounds__(WR *WC * 64) void linear_direct_kernel(LinearArgs g) {
+    constexpr int T = WR * WC * 64, BM = WR * TM * 32, BN = WC * TN * 32, STEP = 128 / BYTES<DT>, S = SLICES<DT>;
+    constexpr int PA = BM * UNITS / T, PB = BN * UNITS / T, TILE = (BM + BN) * UNITS;
+    static_assert(STAGE_BYTES<WR * WC, TN> <= 2 * TILE * 16, "results leave through the tiles' memory");
+    __shared__ raw16 lds[2 * TILE];
+    const int wave = threadIdx.x / 64, lane = threadIdx.x & 63, half = lane / 32;
+    const int wm = wave / WC * TM * 32, wn = wave % WC * TN * 32;
+    unsigned tm, tn;
+    tile_of(static_cast<unsigned>((g.M + BM - 1) / BM), static_cast<unsigned>((g.N + BN - 1) / BN), &tm, &tn);
+    const int64_t m0 = int64_t(tm) * BM, n0 = int64_t(tn) * BN;
+    const int rows_a = static_cast<int>(min(g.M - m0, int64_t(BM))), rows_b = static_cast<int>(min(g.N - n0, int64_t(BN)));
+    const uint32_t lda = static_cast<uint32_t>(g.lda), ldw = static_cast<uint32_t>(g.ldw);
+    const uint32_t width = static_cast<uint32_t>(g.K * BYTES<DT>);
+    const char *A = g.A + m0 * g.lda, *W = g.W + n0 * g.ldw;
+    // rows behind the last one are out of the buffer's bounds, and zero
+    auto sa = __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(A), 0, (rows_a - 1) * lda + width, 0x00027000);
+    auto sb = __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(W), 0, (rows_b - 1) * ldw + width, 0x00027000);
+    // a wave's load fills 8 rows of LDS in order: lane l has place l % 8 of row l / 8, which holds unit (l % 8) ^ (row % 8)
+    const uint32_t row = threadIdx.x / UNITS, unit = (threadIdx.x % UNITS) ^ (row & 7);
+    const uint32_t oa = row * lda + unit * 16, ob = row * ldw + unit * 16;
+    const int steps = static_cast<int>(g.K / STEP), all = steps + (g.K % STEP ? 1 : 0);
+    auto fill = [&](int t) __attribute__((always_inline)) {
+        raw16 *As = lds + (t & 1) * TILE, *Bs = As + BM * UNITS;
+        if (t < steps) {
 #pragma unroll
-    for (int i = 0; i < TM; ++i) {
+            for (int p = 0; p < PA; ++p)
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(sa, As + p * T + wave * 64, 16, oa, t * 128 + p * (T / UNITS) * lda, 0, 0);
 #pragma unroll
-        for (int j = 0; j < TN; ++j)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) stage[(8 * (r / 4) + 4 * half + r % 4) * PITCH + j * 32 + lane % 32] = acc[i][j][r];
-        __builtin_amdgcn_wave_barrier();
-        constexpr int LANES = TN * 4;                                   // of a row, 8 columns each
-#pragma unroll
-        for (int r = lane / LANES; r < 32; r += 64 / LANES) {
-            const int64_t row = m0 + wm + i * 32 + r, col = n0 + wn + lane % LANES * 8;
-            float v[8];
-            ld_row<false, 8>(reinterpret_cast<const char *>(stage + r * PITCH + lane % LANES * 8), 0, v);
-            const int count = static_cast<int>(min(g.N - col, int64_t(8)));
-            if (row < g.M && count > 0) finish<8>(g, row, col, count, v);
+            for (int p = 0; p < PB; ++p)
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(sb, Bs + p * T + wave * 64, 16, ob, t * 128 + p * (T / UNITS) * ldw, 0, 0);
+        } else {                // what is left of the reduction, element by element at its end
+            const int64_t k = int64_t(steps) * STEP + threadIdx.x % UNITS * (16 / BYTES<DT>);
+#pragma unroll 1
+            for (int r = row; r < BM + BN; r += T / UNITS)
+                As[unit_at(r, threadIdx.x % UNITS)] = r < BM ? load_unit<DT>(A + int64_t(min(r, rows_a - 1)) * g.lda, k, g.K)
+                                                            : load_unit<DT>(W + int64_t(min(r - BM, rows_b - 1)) * g.ldw, k, g.K);
         }
-        __builtin_amdgcn_wave_barrier();
+    };
+    acc16 acc[TM][TN] = {};
+    Slice<DT, TM> a[2];
+    Slice<DT, TN> b[2];
+    auto read = [&](int k, int t, int s) {
+        const raw16 *As = lds + (t & 1) * TILE;
+        a[k].read(As, wm + lane % 32, half, s);
+        b[k].read(As + BM * UNITS, wn + lane % 32, half, s);
+    };
+#pragma unroll 1
+    for (int t = 0; t < min(all, 2); ++t) fill(t);
+    __syncthreads();
+    read(0, 0, 0);
+    for (int t = 0; t < all; ++t) {
+#pragma unroll
+        for (int s = 0; s + 1 < S; ++s) {
+            read((s + 1) & 1, t, s + 1);
+            multiply_slice<DT, TM, TN>(a[s & 1], b[s & 1], acc);
+        }
+        if (t + 1 < all) {
+            __syncthreads();
+            if (t + 2 < all) fill(t + 2);
+            read(0, t + 1, 0);
+        }
+        multiply_slice<DT, TM, TN>(a[1], b[1], acc);
     }
+    __syncthreads();
+    store_tile<OB, WR, WC, TM, TN>(g, lds, m0 + wm, n0 + wn, acc);
 }
 
 // ------------------------------------------------------------------ the epilogue's gradient
@@ -233,14 +414,13 @@ struct ActGradArgs {
     const char *dY, *U;
     char *dU;
     int64_t lddy, ldu, lddu;    // in bytes
-    int act, bf16;
     float *part;                // [parts][N], or null
     int64_t rows;               // of a part
 };
 
 // A workgroup: 64 columns' vectors by 4 rows at a time, `rows` rows in all.  What is left at a row's end is taken element by element: dU may be
 // dY or U, and nothing else may be read where it is written.
-template <bool BF16> __global__ __launch_bounds__(256) void act_grad_kernel(ActGradArgs a) {
+template <bool BF16, int ACT> __global__ __launch_bounds__(256) void act_grad_kernel(ActGradArgs a) {
     constexpr int V = ROW_V<BF16>, ES = BF16 ? 2 : 4;
     __shared__ float s[4][64 * V];
     const int lane = threadIdx.x & 63, q = threadIdx.x / 64;
@@ -254,10 +434,10 @@ template <bool BF16> __global__ __launch_bounds__(256) void act_grad_kernel(ActG
         for (int64_t i = blockIdx.y * a.rows + q; i < end; i += 4) {
             float d[V], u[V];
             ld_row<BF16, V>(a.dY + i * a.lddy + j * ES, 0, d);
-            if (a.act != CAPGNN_ACT_NONE) {
+            if constexpr (ACT != CAPGNN_ACT_NONE) {
                 ld_row<BF16, V>(a.U + i * a.ldu + j * ES, 0, u);
 #pragma unroll
-                for (int e = 0; e < V; ++e) d[e] *= act_slope(a.act, u[e]);
+                for (int e = 0; e < V; ++e) d[e] *= act_slope<ACT>(u[e]);
             }
 #pragma unroll
             for (int e = 0; e < V; ++e) sum[e] += d[e];
@@ -269,7 +449,7 @@ template <bool BF16> __global__ __launch_bounds__(256) void act_grad_kernel(ActG
             for (int e = 0; e < V; ++e)
                 if (e < count) {
                     float d = ld_logit<BF16>(a.dY + i * a.lddy + j * ES, e);
-                    if (a.act != CAPGNN_ACT_NONE) d *= act_slope(a.act, ld_logit<BF16>(a.U + i * a.ldu + j * ES, e));
+                    if constexpr (ACT != CAPGNN_ACT_NONE) d *= act_slope<ACT>(ld_logit<BF16>(a.U + i * a.ldu + j * ES, e));
                     sum[e] += d;
                     if (a.dU) st_grad<BF16>(a.dU + i * a.lddu + j * ES, e, d);
                 }
@@ -301,6 +481,16 @@ using namespace capgnn;
 
 static bool bad_act(int act) { return act < CAPGNN_ACT_NONE || act > CAPGNN_ACT_SILU; }
 
+// f(operands, results in bf16) as compile-time numbers
+template <class F> static void with_types(int dtype, int out_dtype, F f) {
+    using Y = std::true_type;
+    using N = std::false_type;
+    const bool o = out_dtype == CAPGNN_BF16;
+    if (dtype == CAPGNN_F32) o ? f(std::integral_constant<int, CAPGNN_F32>(), Y()) : f(std::integral_constant<int, CAPGNN_F32>(), N());
+    else if (dtype == CAPGNN_BF16) o ? f(std::integral_constant<int, CAPGNN_BF16>(), Y()) : f(std::integral_constant<int, CAPGNN_BF16>(), N());
+    else o ? f(std::integral_constant<int, CAPGNN_E4M3>(), Y()) : f(std::integral_constant<int, E4M3_FINE>(), N());
+}
+
 extern "C" size_t capgnn_linear_workspace_bytes(int64_t, int64_t, int64_t, int) { return 0; }
 
 extern "C" int capgnn_linear(int64_t M, int64_t N, int64_t K, const void *A, int64_t lda, const float *a_scale, const void *W, int64_t ldw,
@@ -328,11 +518,20 @@ extern "C" int capgnn_linear(int64_t M, int64_t N, int64_t K, const void *A, int
     hipStream_t st = static_cast<hipStream_t>(stream);
     (void)ws;
     (void)ws_bytes;
+    const bool aligned = K > 0 && ((reinterpret_cast<uintptr_t>(A) | reinterpret_cast<uintptr_t>(W) | uintptr_t(g.lda) | uintptr_t(g.ldw)) & 15u) == 0 &&
+                         g.lda < most / 256 && g.ldw < most / 256;
+    if (aligned && M * N >= 256 * 256 * 128) {
+        const unsigned tiles = static_cast<unsigned>((M + 255) / 256 * ((N + 255) / 256));
+        with_types(dtype, out_dtype, [&](auto d, auto o) {
+            hipLaunchKernelGGL((linear_direct_kernel<d.value, o.value, 2, 2, 4, 4>), dim3(tiles), dim3(256), 0, st, g);
+        });
+        CG_HIP(hipGetLastError());
+        return CAPGNN_OK;
+    }
     const dim3 grid(static_cast<unsigned>((M + 63) / 64), static_cast<unsigned>((N + 63) / 64));
-    if (dtype == CAPGNN_F32) hipLaunchKernelGGL((linear_tile_kernel<CAPGNN_F32, 2, 2, 1, 1>), grid, dim3(256), 0, st, g);
-    else if (dtype == CAPGNN_BF16) hipLaunchKernelGGL((linear_tile_kernel<CAPGNN_BF16, 2, 2, 1, 1>), grid, dim3(256), 0, st, g);
-    else if (out_dtype == CAPGNN_F32) hipLaunchKernelGGL((linear_tile_kernel<E4M3_FINE, 2, 2, 1, 1>), grid, dim3(256), 0, st, g);
-    else hipLaunchKernelGGL((linear_tile_kernel<CAPGNN_E4M3, 2, 2, 1, 1>), grid, dim3(256), 0, st, g);
+    with_types(dtype, out_dtype, [&](auto d, auto o) {
+        hipLaunchKernelGGL((linear_tile_kernel<d.value, o.value, 2, 2, 1, 1>), grid, dim3(256), 0, st, g);
+    });
     CG_HIP(hipGetLastError());
     return CAPGNN_OK;
 }
@@ -367,10 +566,12 @@ extern "C" int capgnn_linear_act_bwd(int64_t M, int64_t N, const void *dY, int64
     int64_t rows;
     const int parts = act_parts(M, N, &rows);
     const ActGradArgs a{M, N, static_cast<const char *>(dY), static_cast<const char *>(U), static_cast<char *>(dU), lddy * es, ldu * es,
-                        lddu * es, act, bf16, dbias ? static_cast<float *>(ws) : nullptr, rows};
+                        lddu * es, dbias ? static_cast<float *>(ws) : nullptr, rows};
     const dim3 grid(static_cast<unsigned>((N + 64 * V - 1) / (64 * V)), parts);
-    if (bf16) hipLaunchKernelGGL(act_grad_kernel<true>, grid, dim3(256), 0, st, a);
-    else hipLaunchKernelGGL(act_grad_kernel<false>, grid, dim3(256), 0, st, a);
+    with_act(act, [&](auto k) {
+        if (bf16) hipLaunchKernelGGL((act_grad_kernel<true, k.value>), grid, dim3(256), 0, st, a);
+        else hipLaunchKernelGGL((act_grad_kernel<false, k.value>), grid, dim3(256), 0, st, a);
+    });
     CG_HIP(hipGetLastError());
     return dbias ? launch_column_join(a.part, parts, N, dbias, st) : CAPGNN_OK;
 }
