@@ -331,6 +331,24 @@ template <int DT, bool OB, int WR, int WC, int TM, int TN> __global__ __launch_b
 // The same for aligned operands (16 bytes) that need no check but at the last step: loads go straight to LDS, one step ahead, and the operands
 // of a slice (half or a quarter of a step) are read while the one before is multiplied, across the barrier too: behind the last slice's
 // reads the other buffer's loads are waited for, this one's are free to start, and the next step's first slice is read.
+// The order of a slice: reads of the next one's operands, then loads to LDS, between its matrix instructions.  (Asked for all at once they
+// keep the only wave of a SIMD from issuing matrix instructions for a fifth of a step.)
+template <int MFMAS, int READS, int LOADS> __device__ __forceinline__ void interleave() {
+    constexpr int GROUPS = 8, SHARE = LOADS ? MFMAS / 2 : MFMAS;
+#pragma unroll
+    for (int i = 0; i < GROUPS; ++i) {
+        __builtin_amdgcn_sched_group_barrier(0x008, SHARE / GROUPS, 0);         // matrix instructions
+        __builtin_amdgcn_sched_group_barrier(0x100, READS / GROUPS, 0);         // reads of LDS
+    }
+    if constexpr (LOADS > 0) {
+#pragma unroll
+        for (int i = 0; i < GROUPS; ++i) {
+            __builtin_amdgcn_sched_group_barrier(0x008, SHARE / GROUPS, 0);
+            __builtin_amdgcn_sched_group_barrier(0x020, LOADS / GROUPS, 0);     // loads
+        }
+    }
+}
+
 // Tile of a workgroup.  Workgroups go round the L2 domains one by one: each domain gets a stretch of tiles, in bands of 8 rows of tiles, so that
 // what runs on it at a time shares rows of both operands.
 __device__ __forceinline__ void tile_of(unsigned tiles_m, unsigned tiles_n, unsigned *m, unsigned *n) {
@@ -355,31 +373,34 @@ template <int DT, bool OB, int WR, int WC, int TM, int TN> __global__ __launch_b
     const uint32_t lda = static_cast<uint32_t>(g.lda), ldw = static_cast<uint32_t>(g.ldw);
     const uint32_t width = static_cast<uint32_t>(g.K * BYTES<DT>);
     const char *A = g.A + m0 * g.lda, *W = g.W + n0 * g.ldw;
-    // rows behind the last one are out of the buffer's bounds, and zero
     auto sa = __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(A), 0, (rows_a - 1) * lda + width, 0x00027000);
     auto sb = __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(W), 0, (rows_b - 1) * ldw + width, 0x00027000);
-    // a wave's load fills 8 rows of LDS in order: lane l has place l % 8 of row l / 8, which holds unit (l % 8) ^ (row % 8)
+    // A wave's load fills 8 rows of LDS in order: lane l has place l % 8 of row l / 8, which holds unit (l % 8) ^ (row % 8).  Rows behind the last
+    // one are the last one again: their results are not stored, and nothing depends on the buffer's bounds.
     const uint32_t row = threadIdx.x / UNITS, unit = (threadIdx.x % UNITS) ^ (row & 7);
-    const uint32_t oa = row * lda + unit * 16, ob = row * ldw + unit * 16;
+    uint32_t oa[PA], ob[PB];
+#pragma unroll
+    for (int p = 0; p < PA; ++p) oa[p] = min(row + p * (T / UNITS), rows_a - 1u) * lda + unit * 16;
+#pragma unroll
+    for (int p = 0; p < PB; ++p) ob[p] = min(row + p * (T / UNITS), rows_b - 1u) * ldw + unit * 16;
     const int steps = static_cast<int>(g.K / STEP), all = steps + (g.K % STEP ? 1 : 0);
     auto fill = [&](int t) __attribute__((always_inline)) {
         raw16 *As = lds + (t & 1) * TILE, *Bs = As + BM * UNITS;
-        if (t < steps) {
 #pragma unroll
-            for (int p = 0; p < PA; ++p)
-                __builtin_amdgcn_raw_ptr_buffer_load_lds(sa, As + p * T + wave * 64, 16, oa, t * 128 + p * (T / UNITS) * lda, 0, 0);
+        for (int p = 0; p < PA; ++p) __builtin_amdgcn_raw_ptr_buffer_load_lds(sa, As + p * T + wave * 64, 16, static_cast<int>(oa[p]), t * 128, 0, 0);
 #pragma unroll
-            for (int p = 0; p < PB; ++p)
-                __builtin_amdgcn_raw_ptr_buffer_load_lds(sb, Bs + p * T + wave * 64, 16, ob, t * 128 + p * (T / UNITS) * ldw, 0, 0);
-        } else {                // what is left of the reduction, element by element at its end
-            const int64_t k = int64_t(steps) * STEP + threadIdx.x % UNITS * (16 / BYTES<DT>);
+        for (int p = 0; p < PB; ++p) __builtin_amdgcn_raw_ptr_buffer_load_lds(sb, Bs + p * T + wave * 64, 16, static_cast<int>(ob[p]), t * 128, 0, 0);
+    };
+    auto fill_end = [&]() __attribute__((always_inline)) {              // what is left of the reduction, element by element at its end
+        raw16 *As = lds + (steps & 1) * TILE;
+        const int64_t k = int64_t(steps) * STEP + threadIdx.x % UNITS * (16 / BYTES<DT>);
 #pragma unroll 1
-            for (int r = row; r < BM + BN; r += T / UNITS)
-                As[unit_at(r, threadIdx.x % UNITS)] = r < BM ? load_unit<DT>(A + int64_t(min(r, rows_a - 1)) * g.lda, k, g.K)
-                                                            : load_unit<DT>(W + int64_t(min(r - BM, rows_b - 1)) * g.ldw, k, g.K);
-        }
+        for (int r = row; r < BM + BN; r += T / UNITS)
+            As[unit_at(r, threadIdx.x % UNITS)] = r < BM ? load_unit<DT>(A + int64_t(min(r, rows_a - 1)) * g.lda, k, g.K)
+                                                        : load_unit<DT>(W + int64_t(min(r - BM, rows_b - 1)) * g.ldw, k, g.K);
     };
     acc16 acc[TM][TN] = {};
+    constexpr int MFMAS = TM * TN * (DT == CAPGNN_F32 ? 4 : DT == E4M3_FINE ? 2 : 1), READS = (TM + TN) * Slice<DT, TM>::U;
     Slice<DT, TM> a[2];
     Slice<DT, TN> b[2];
     auto read = [&](int k, int t, int s) {
@@ -387,19 +408,37 @@ template <int DT, bool OB, int WR, int WC, int TM, int TN> __global__ __launch_b
         a[k].read(As, wm + lane % 32, half, s);
         b[k].read(As + BM * UNITS, wn + lane % 32, half, s);
     };
-#pragma unroll 1
-    for (int t = 0; t < min(all, 2); ++t) fill(t);
-    __syncthreads();
-    read(0, 0, 0);
-    for (int t = 0; t < all; ++t) {
+    auto arrived = [&]() __attribute__((always_inline)) {               // everyone's loads to LDS are there, and everyone has read what he asked for
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        __syncthreads();
+    };
+    auto most = [&](int t) __attribute__((always_inline)) {             // the slices of step t but the last
 #pragma unroll
         for (int s = 0; s + 1 < S; ++s) {
             read((s + 1) & 1, t, s + 1);
             multiply_slice<DT, TM, TN>(a[s & 1], b[s & 1], acc);
+            interleave<MFMAS, READS, 0>();
         }
+    };
+#pragma unroll 1
+    for (int t = 0; t < min(steps, 2); ++t) fill(t);
+    if (steps < 2 && steps < all) fill_end();
+    arrived();
+    read(0, 0, 0);
+    int t = 0;
+    for (; t + 2 < steps; ++t) {
+        most(t);
+        arrived();
+        read(0, t + 1, 0);
+        fill(t + 2);
+        multiply_slice<DT, TM, TN>(a[1], b[1], acc);
+        interleave<MFMAS, READS, PA + PB>();
+    }
+    for (; t < all; ++t) {
+        most(t);
         if (t + 1 < all) {
-            __syncthreads();
-            if (t + 2 < all) fill(t + 2);
+            arrived();
+            if (t + 2 == steps && steps < all) fill_end();
             read(0, t + 1, 0);
         }
         multiply_slice<DT, TM, TN>(a[1], b[1], acc);
