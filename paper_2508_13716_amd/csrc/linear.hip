@@ -1,8 +1,8 @@
 // Products with an epilogue, Y = act(A W^T + bias) + R, and the epilogue's gradient.
 //
 // Both operands run along the reduction index, so a tile of either is the same thing whatever its type: rows of 128 bytes, 32 fp32,
-// 64 bf16 or 128 e4m3 numbers of k.  LDS holds such tiles in units of 16 bytes, unit u of row r at place u ^ (r % 8): eight rows' units of
-// the same k lie in different banks.  The matrix instructions take 32 x 32 results; which k a lane's bytes are does not matter as long as
+// 64 bf16 or 128 e4m3 numbers of k.  LDS holds such tiles in units of 16 bytes, unit u of row r at place u ^ (r / 2 % 8): the units of the
+// same k of sixteen rows lie in different banks (of eight rows only, u ^ (r % 8): 8192^3 bf16 4 % slower).  The matrix instructions take 32 x 32 results; which k a lane's bytes are does not matter as long as
 // both operands agree, so a lane of the lower and one of the upper half take alternate units of their row.
 //
 // D layout of the 32 x 32 instructions: register r of lane l holds row 8 (r / 4) + 4 (l / 32) + r % 4, column l % 32.
@@ -29,7 +29,21 @@ struct LinearArgs {
     char *U, *Y;
     int64_t ldr, ldu, ldy;      // in bytes
     int out_bf16;
+    float *part;                // sums of parts of the reduction, [parts][M][part_ld], or null
+    int64_t part_ld;
+    int64_t part_k;             // of a part: whole steps
 };
+
+// A's and W's part of the reduction that is workgroup row blockIdx.y's
+struct Stretch {
+    const char *A, *W;
+    int64_t K;
+};
+template <int ES> __device__ __forceinline__ Stretch stretch_of(const LinearArgs &g) {
+    if (!g.part) return {g.A, g.W, g.K};
+    const int64_t k0 = g.part_k * blockIdx.y;
+    return {g.A + k0 * ES, g.W + k0 * ES, min(g.part_k, g.K - k0)};
+}
 
 // ------------------------------------------------------------------ activations
 // exp(-x) and 1 / x by the hardware's instructions, one unit in the last place each: what the formulas lose by that is a few EPS |u|.
@@ -131,7 +145,7 @@ constexpr int UNITS = 8;                // units of a tile's row
 constexpr int E4M3_FINE = 3;
 template <int DT> constexpr int BYTES = DT == CAPGNN_F32 ? 4 : DT == CAPGNN_BF16 ? 2 : 1;
 
-__device__ __forceinline__ int unit_at(int row, int unit) { return row * UNITS + (unit ^ (row & 7)); }
+__device__ __forceinline__ int unit_at(int row, int unit) { return row * UNITS + (unit ^ (row >> 1 & 7)); }
 
 // half e (eight numbers) of a unit of e4m3, as bf16
 __device__ __forceinline__ half8 widen8(raw16 u, int e) {
@@ -225,6 +239,27 @@ __device__ __forceinline__ void store_tile(const LinearArgs &g, raw16 *lds, int6
     const float *mine = stage + lane / LANES * PITCH + lane % LANES * 8;
     const int64_t col = n0 + lane % LANES * 8;
     const int count = static_cast<int>(max(min(g.N - col, int64_t(8)), int64_t(0)));
+    if (g.part) {
+        repeat(std::make_integer_sequence<int, TM>(), [&](auto at) __attribute__((always_inline)) {
+            constexpr int i = at.value;
+#pragma unroll
+            for (int j = 0; j < TN; ++j)
+#pragma unroll
+                for (int k = 0; k < 16; ++k) stage[(8 * (k / 4) + 4 * half + k % 4) * PITCH + j * 32 + lane % 32] = acc[i][j][k];
+            __builtin_amdgcn_wave_barrier();
+#pragma unroll
+            for (int p = 0; p < PASSES; ++p) {
+                const int64_t row = m0 + i * 32 + lane / LANES + p * ROWS;
+                if (row < g.M && count) {               // (rows of parts are whole vectors of 8)
+                    float v[8];
+                    ld_row<false, 8>(reinterpret_cast<const char *>(mine + p * ROWS * PITCH), 0, v);
+                    st_row<false, 8>(reinterpret_cast<char *>(g.part + (blockIdx.y * g.M + row) * g.part_ld + col), 0, v);
+                }
+            }
+            __builtin_amdgcn_wave_barrier();
+        });
+        return;
+    }
     float bias[8], scale[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
@@ -282,6 +317,16 @@ __device__ __forceinline__ void store_tile(const LinearArgs &g, raw16 *lds, int6
     });
 }
 
+// Tile of a workgroup.  Workgroups go round the L2 domains one by one: each domain gets a stretch of tiles, in bands of 8 rows of tiles, so that
+// what runs on it at a time shares rows of both operands.
+__device__ __forceinline__ void tile_of(unsigned tiles_m, unsigned tiles_n, unsigned *m, unsigned *n) {
+    const unsigned all = tiles_m * tiles_n, d = blockIdx.x % NUM_XCD, k = blockIdx.x / NUM_XCD;
+    const unsigned t = all / NUM_XCD * d + min(d, all % NUM_XCD) + k;
+    const unsigned band = t / (8 * tiles_n), first = band * 8, rows = min(8u, tiles_m - first), in = t - band * 8 * tiles_n;
+    *m = first + in % rows;
+    *n = in / rows;
+}
+
 // WR x WC waves with TM x TN accumulators of 32 x 32 each: a tile of WR TM 32 rows of A by WC TN 32 rows of W.
 template <int DT, bool OB, int WR, int WC, int TM, int TN> __global__ __launch_bounds__(WR *WC * 64) void linear_tile_kernel(LinearArgs g) {
     constexpr int T = WR * WC * 64, BM = WR * TM * 32, BN = WC * TN * 32, STEP = 128 / BYTES<DT>;
@@ -291,30 +336,33 @@ template <int DT, bool OB, int WR, int WC, int TM, int TN> __global__ __launch_b
     raw16 *As = lds, *Bs = lds + BM * UNITS;
     const int wave = threadIdx.x / 64, lane = threadIdx.x & 63, half = lane / 32;
     const int wm = wave / WC * TM * 32, wn = wave % WC * TN * 32;
-    const int64_t m0 = int64_t(blockIdx.x) * BM, n0 = int64_t(blockIdx.y) * BN;
+    unsigned tm, tn;
+    tile_of(static_cast<unsigned>((g.M + BM - 1) / BM), static_cast<unsigned>((g.N + BN - 1) / BN), &tm, &tn);
+    const int64_t m0 = int64_t(tm) * BM, n0 = int64_t(tn) * BN;
+    const Stretch x = stretch_of<BYTES<DT>>(g);
     acc16 acc[TM][TN] = {};
     raw16 ra[PA], rb[PB];
     auto fetch = [&](int64_t k) {
 #pragma unroll
         for (int p = 0; p < PA; ++p) {
             const int u = p * T + threadIdx.x;
-            ra[p] = load_unit<DT>(g.A + min(m0 + u / UNITS, g.M - 1) * g.lda, k + u % UNITS * (16 / BYTES<DT>), g.K);
+            ra[p] = load_unit<DT>(x.A + min(m0 + u / UNITS, g.M - 1) * g.lda, k + u % UNITS * (16 / BYTES<DT>), x.K);
         }
 #pragma unroll
         for (int p = 0; p < PB; ++p) {
             const int u = p * T + threadIdx.x;
-            rb[p] = load_unit<DT>(g.W + min(n0 + u / UNITS, g.N - 1) * g.ldw, k + u % UNITS * (16 / BYTES<DT>), g.K);
+            rb[p] = load_unit<DT>(x.W + min(n0 + u / UNITS, g.N - 1) * g.ldw, k + u % UNITS * (16 / BYTES<DT>), x.K);
         }
     };
-    if (g.K > 0) fetch(0);
-    for (int64_t k = 0; k < g.K; k += STEP) {
+    if (x.K > 0) fetch(0);
+    for (int64_t k = 0; k < x.K; k += STEP) {
         __syncthreads();
 #pragma unroll
         for (int p = 0; p < PA; ++p) As[unit_at((p * T + threadIdx.x) / UNITS, threadIdx.x % UNITS)] = ra[p];
 #pragma unroll
         for (int p = 0; p < PB; ++p) Bs[unit_at((p * T + threadIdx.x) / UNITS, threadIdx.x % UNITS)] = rb[p];
         __syncthreads();
-        if (k + STEP < g.K) fetch(k + STEP);
+        if (k + STEP < x.K) fetch(k + STEP);
 #pragma unroll
         for (int s = 0; s < SLICES<DT>; ++s) {
             Slice<DT, TM> a;
@@ -334,29 +382,20 @@ template <int DT, bool OB, int WR, int WC, int TM, int TN> __global__ __launch_b
 // The order of a slice: reads of the next one's operands, then loads to LDS, between its matrix instructions.  (Asked for all at once they
 // keep the only wave of a SIMD from issuing matrix instructions for a fifth of a step.)
 template <int MFMAS, int READS, int LOADS> __device__ __forceinline__ void interleave() {
-    constexpr int GROUPS = 8, SHARE = LOADS ? MFMAS / 2 : MFMAS;
-#pragma unroll
-    for (int i = 0; i < GROUPS; ++i) {
-        __builtin_amdgcn_sched_group_barrier(0x008, SHARE / GROUPS, 0);         // matrix instructions
-        __builtin_amdgcn_sched_group_barrier(0x100, READS / GROUPS, 0);         // reads of LDS
-    }
-    if constexpr (LOADS > 0) {
-#pragma unroll
-        for (int i = 0; i < GROUPS; ++i) {
-            __builtin_amdgcn_sched_group_barrier(0x008, SHARE / GROUPS, 0);
-            __builtin_amdgcn_sched_group_barrier(0x020, LOADS / GROUPS, 0);     // loads
+    constexpr int BATCH = MFMAS > 32 ? MFMAS / 32 : 1, N = MFMAS / BATCH, HALF = LOADS ? N / 2 : N;     // loads follow the reads (the compiler
+#pragma unroll                                                                                          // takes them for writes of what is read)
+    for (int i = 0; i < N; ++i) {
+        __builtin_amdgcn_sched_group_barrier(0x008, BATCH, 0);                  // matrix instructions
+        constexpr auto due = [](int k, int n, int of) { return (k + 1) * n / of - k * n / of; };
+        if (i < HALF) {
+            if (due(i, READS, HALF) == 1) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);            // reads of LDS
+            if (due(i, READS, HALF) == 2) __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+            if (due(i, READS, HALF) == 3) __builtin_amdgcn_sched_group_barrier(0x100, 3, 0);
+        } else {
+            if (due(i - HALF, LOADS, N - HALF) == 1) __builtin_amdgcn_sched_group_barrier(0x020, 1, 0); // loads
+            if (due(i - HALF, LOADS, N - HALF) == 2) __builtin_amdgcn_sched_group_barrier(0x020, 2, 0);
         }
     }
-}
-
-// Tile of a workgroup.  Workgroups go round the L2 domains one by one: each domain gets a stretch of tiles, in bands of 8 rows of tiles, so that
-// what runs on it at a time shares rows of both operands.
-__device__ __forceinline__ void tile_of(unsigned tiles_m, unsigned tiles_n, unsigned *m, unsigned *n) {
-    const unsigned all = tiles_m * tiles_n, d = blockIdx.x % NUM_XCD, k = blockIdx.x / NUM_XCD;
-    const unsigned t = all / NUM_XCD * d + min(d, all % NUM_XCD) + k;
-    const unsigned band = t / (8 * tiles_n), first = band * 8, rows = min(8u, tiles_m - first), in = t - band * 8 * tiles_n;
-    *m = first + in % rows;
-    *n = in / rows;
 }
 
 template <int DT, bool OB, int WR, int WC, int TM, int TN> __global__ __launch_bounds__(WR *WC * 64) void linear_direct_kernel(LinearArgs g) {
@@ -371,19 +410,20 @@ template <int DT, bool OB, int WR, int WC, int TM, int TN> __global__ __launch_b
     const int64_t m0 = int64_t(tm) * BM, n0 = int64_t(tn) * BN;
     const int rows_a = static_cast<int>(min(g.M - m0, int64_t(BM))), rows_b = static_cast<int>(min(g.N - n0, int64_t(BN)));
     const uint32_t lda = static_cast<uint32_t>(g.lda), ldw = static_cast<uint32_t>(g.ldw);
-    const uint32_t width = static_cast<uint32_t>(g.K * BYTES<DT>);
-    const char *A = g.A + m0 * g.lda, *W = g.W + n0 * g.ldw;
+    const Stretch x = stretch_of<BYTES<DT>>(g);
+    const uint32_t width = static_cast<uint32_t>(x.K * BYTES<DT>);
+    const char *A = x.A + m0 * g.lda, *W = x.W + n0 * g.ldw;
     auto sa = __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(A), 0, (rows_a - 1) * lda + width, 0x00027000);
     auto sb = __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(W), 0, (rows_b - 1) * ldw + width, 0x00027000);
-    // A wave's load fills 8 rows of LDS in order: lane l has place l % 8 of row l / 8, which holds unit (l % 8) ^ (row % 8).  Rows behind the last
+    // A wave's load fills 8 rows of LDS in order: lane l has place l % 8 of row l / 8, which holds unit (l % 8) ^ (row / 2 % 8).  Rows behind the last
     // one are the last one again: their results are not stored, and nothing depends on the buffer's bounds.
-    const uint32_t row = threadIdx.x / UNITS, unit = (threadIdx.x % UNITS) ^ (row & 7);
+    const uint32_t row = threadIdx.x / UNITS, unit = (threadIdx.x % UNITS) ^ (row >> 1 & 7);
     uint32_t oa[PA], ob[PB];
 #pragma unroll
     for (int p = 0; p < PA; ++p) oa[p] = min(row + p * (T / UNITS), rows_a - 1u) * lda + unit * 16;
 #pragma unroll
     for (int p = 0; p < PB; ++p) ob[p] = min(row + p * (T / UNITS), rows_b - 1u) * ldw + unit * 16;
-    const int steps = static_cast<int>(g.K / STEP), all = steps + (g.K % STEP ? 1 : 0);
+    const int steps = static_cast<int>(x.K / STEP), all = steps + (x.K % STEP ? 1 : 0);
     auto fill = [&](int t) __attribute__((always_inline)) {
         raw16 *As = lds + (t & 1) * TILE, *Bs = As + BM * UNITS;
 #pragma unroll
@@ -396,8 +436,8 @@ template <int DT, bool OB, int WR, int WC, int TM, int TN> __global__ __launch_b
         const int64_t k = int64_t(steps) * STEP + threadIdx.x % UNITS * (16 / BYTES<DT>);
 #pragma unroll 1
         for (int r = row; r < BM + BN; r += T / UNITS)
-            As[unit_at(r, threadIdx.x % UNITS)] = r < BM ? load_unit<DT>(A + int64_t(min(r, rows_a - 1)) * g.lda, k, g.K)
-                                                        : load_unit<DT>(W + int64_t(min(r - BM, rows_b - 1)) * g.ldw, k, g.K);
+            As[unit_at(r, threadIdx.x % UNITS)] = r < BM ? load_unit<DT>(A + int64_t(min(r, rows_a - 1)) * g.lda, k, x.K)
+                                                        : load_unit<DT>(W + int64_t(min(r - BM, rows_b - 1)) * g.ldw, k, x.K);
     };
     acc16 acc[TM][TN] = {};
     constexpr int MFMAS = TM * TN * (DT == CAPGNN_F32 ? 4 : DT == E4M3_FINE ? 2 : 1), READS = (TM + TN) * Slice<DT, TM>::U;
@@ -445,6 +485,98 @@ template <int DT, bool OB, int WR, int WC, int TM, int TN> __global__ __launch_b
     }
     __syncthreads();
     store_tile<OB, WR, WC, TM, TN>(g, lds, m0 + wm, n0 + wn, acc);
+}
+
+// The parts' sums, in order, and the epilogue: a thread 8 columns of a row
+__global__ __launch_bounds__(256) void linear_join_kernel(LinearArgs g, int parts) {
+    const int64_t across = g.part_ld / 8, at = int64_t(blockIdx.x) * 256 + threadIdx.x, row = at / across, col = at % across * 8;
+    if (row >= g.M) return;
+    float sum[8];
+    ld_row<false, 8>(reinterpret_cast<const char *>(g.part + row * g.part_ld + col), 0, sum);
+#pragma unroll 4
+    for (int p = 1; p < parts; ++p) {
+        float v[8];
+        ld_row<false, 8>(reinterpret_cast<const char *>(g.part + (p * g.M + row) * g.part_ld + col), 0, v);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) sum[e] += v[e];
+    }
+    const int count = static_cast<int>(min(g.N - col, int64_t(8)));
+    if (count > 0) finish<8>(g, row, col, count, sum);
+}
+
+// ------------------------------------------------------------------ a few rows of A
+// The weights' bytes bound these: every row of W is read once, straight into the registers of the matrix instruction (16 x 16 results: lane l has
+// row l % 16 of W, and of A, and every fourth 16-byte unit of it, from l / 16 on), by a workgroup per 16 rows, whose waves take lines of
+// 128 bytes in turn.  Their sums meet in LDS, in wave order.  A stays in the caches.  8-bit operands are widened to bf16 whatever the result.
+// D layout of the 16 x 16 instructions: register r of lane l holds row 4 (l / 16) + r, column l % 16: 4 neighbouring columns of a row of Y, with W
+// as the first operand.
+typedef float acc4 __attribute__((ext_vector_type(4)));
+template <int DT> __device__ __forceinline__ acc4 multiply16(raw16 w, raw16 a, acc4 acc) {
+    if constexpr (DT == CAPGNN_F32) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(w[e]), __uint_as_float(a[e]), acc, 0, 0, 0);
+        return acc;
+    } else if constexpr (DT == CAPGNN_BF16) {
+        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(half8, w), __builtin_bit_cast(half8, a), acc, 0, 0, 0);
+    } else {
+        acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen8(w, 0), widen8(a, 0), acc, 0, 0, 0);
+        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen8(w, 1), widen8(a, 1), acc, 0, 0, 0);
+    }
+}
+
+constexpr int FEW_WAVES = 16, FEW_AHEAD = 4;        // waves of a workgroup, at most; units of a row on their way at a time, per lane
+
+// TM: groups of 16 rows of A
+template <int DT, int TM> __global__ __launch_bounds__(FEW_WAVES * 64) void linear_few_kernel(LinearArgs g) {
+    constexpr int E = 16 / BYTES<DT>;
+    __shared__ acc4 sums[FEW_WAVES][TM][64];
+    const int wave = threadIdx.x / 64, waves = blockDim.x / 64, lane = threadIdx.x & 63;
+    const int64_t n0 = int64_t(blockIdx.x) * 16;
+    const Stretch x = stretch_of<BYTES<DT>>(g);
+    const char *w = x.W + min(n0 + lane % 16, g.N - 1) * g.ldw, *a[TM];
+#pragma unroll
+    for (int i = 0; i < TM; ++i) a[i] = x.A + min(int64_t(i * 16 + lane % 16), g.M - 1) * g.lda;
+    acc4 acc[TM] = {};
+    // a wave's unit q: 16 bytes at k, of line q / 2 of its own
+    auto at = [&](int64_t q) { return ((q / 2 * waves + wave) * 8 + q % 2 * 4 + lane / 16) * E; };
+    const int64_t lines = (x.K + 8 * E - 1) / (8 * E), mine = lines > wave ? ((lines - wave - 1) / waves + 1) * 2 : 0;
+    const int64_t sure = x.K / (8 * E), whole = sure > wave ? ((sure - wave - 1) / waves + 1) * 2 : 0;      // of lines that end inside the row
+    int64_t q = 0;
+    for (; q + FEW_AHEAD <= whole; q += FEW_AHEAD) {
+        raw16 rw[FEW_AHEAD], ra[FEW_AHEAD][TM];
+#pragma unroll
+        for (int u = 0; u < FEW_AHEAD; ++u) {
+            typedef raw16 raw16_by1 __attribute__((aligned(1)));
+            const int64_t k = at(q + u) * BYTES<DT>;
+            rw[u] = *reinterpret_cast<const raw16_by1 *>(w + k);
+#pragma unroll
+            for (int i = 0; i < TM; ++i) ra[u][i] = *reinterpret_cast<const raw16_by1 *>(a[i] + k);
+        }
+#pragma unroll
+        for (int u = 0; u < FEW_AHEAD; ++u)
+#pragma unroll
+            for (int i = 0; i < TM; ++i) acc[i] = multiply16<DT>(rw[u], ra[u][i], acc[i]);
+    }
+    for (; q < mine; ++q) {
+        const int64_t k = at(q);
+        const raw16 rw = load_unit<DT>(w, k, x.K);
+#pragma unroll
+        for (int i = 0; i < TM; ++i) acc[i] = multiply16<DT>(rw, load_unit<DT>(a[i], k, x.K), acc[i]);
+    }
+#pragma unroll
+    for (int i = 0; i < TM; ++i) sums[wave][i][lane] = acc[i];
+    __syncthreads();
+    for (int i = wave; i < TM; i += waves) {
+        acc4 s = sums[0][i][lane];
+        for (int v = 1; v < waves; ++v) s += sums[v][i][lane];
+        const int64_t row = i * 16 + lane % 16, col = n0 + lane / 16 * 4;
+        const int count = static_cast<int>(min(g.N - col, int64_t(4)));
+        if (row < g.M && count > 0) {
+            float v[4] = {s[0], s[1], s[2], s[3]};
+            if (g.part) st_row<false, 4>(reinterpret_cast<char *>(g.part + (blockIdx.y * g.M + row) * g.part_ld + col), 0, v);
+            else finish<4>(g, row, col, count, v);
+        }
+    }
 }
 
 // ------------------------------------------------------------------ the epilogue's gradient
@@ -530,7 +662,45 @@ template <class F> static void with_types(int dtype, int out_dtype, F f) {
     else o ? f(std::integral_constant<int, CAPGNN_E4M3>(), Y()) : f(std::integral_constant<int, E4M3_FINE>(), N());
 }
 
-extern "C" size_t capgnn_linear_workspace_bytes(int64_t, int64_t, int64_t, int) { return 0; }
+// How a product runs
+struct LinearPlan {
+    int tile;                   // rows and columns of a tile; 0: a few rows
+    int parts;                  // of the reduction
+    int64_t part_k;
+};
+constexpr int FEW_ROWS = 32;
+
+static LinearPlan linear_plan(int64_t M, int64_t N, int64_t K, int es) {
+    LinearPlan p{0, 1, K};
+    auto tiles = [&](int64_t b) { return ((M + b - 1) / b) * ((N + b - 1) / b); };
+    const int64_t lines = (K * es + 127) / 128;         // steps
+    int64_t groups, most;
+    if (M <= FEW_ROWS) {
+        groups = (N + 15) / 16;
+        most = lines / 32;
+    } else {
+        p.tile = tiles(256) >= 200 ? 256 : tiles(128) >= 256 ? 128 : 64;
+        groups = tiles(p.tile);
+        most = p.tile == 64 ? lines / 8 : 1;
+    }
+    const int64_t parts = std::min<int64_t>(std::min<int64_t>(most, (p.tile ? 512 : 256) / groups), 32);
+    if (parts > 1) {
+        const int64_t each = (lines + parts - 1) / parts;
+        p.part_k = each * (128 / es);
+        p.parts = static_cast<int>((lines + each - 1) / each);
+        if (p.parts == 1) p.part_k = K;
+    }
+    return p;
+}
+static int operand_bytes(int dtype) { return dtype == CAPGNN_E4M3 ? 1 : elem_bytes(dtype); }
+static int64_t part_pitch(int64_t N) { return (N + 7) / 8 * 8; }
+
+extern "C" size_t capgnn_linear_workspace_bytes(int64_t M, int64_t N, int64_t K, int dtype) {
+    const int64_t most = int64_t(1) << 31;
+    if (M <= 0 || N <= 0 || K <= 0 || M >= most || N >= most || K >= most || (!is_float_type(dtype) && dtype != CAPGNN_E4M3)) return 0;
+    const LinearPlan p = linear_plan(M, N, K, operand_bytes(dtype));
+    return p.parts > 1 ? align_up(sizeof(float) * p.parts * M * part_pitch(N), 256) : 0;
+}
 
 extern "C" int capgnn_linear(int64_t M, int64_t N, int64_t K, const void *A, int64_t lda, const float *a_scale, const void *W, int64_t ldw,
                              const float *w_scale, int dtype, const float *bias, int act, const void *R, int64_t ldr, void *U, int64_t ldu,
@@ -549,29 +719,53 @@ extern "C" int capgnn_linear(int64_t M, int64_t N, int64_t K, const void *A, int
         CG_FAIL(CAPGNN_EINVAL, "linear: an operand is not aligned to its elements");
     if (Y == U || (R && U == R) || (Y == R && ldy != ldr)) CG_FAIL(CAPGNN_EINVAL, "linear: Y may be R with the same pitch; U is neither");
     if (K > 0 && (Y == A || Y == W || (U && (U == A || U == W)))) CG_FAIL(CAPGNN_EINVAL, "linear: Y and U must not be A or W");
-    const int es = dtype == CAPGNN_E4M3 ? 1 : elem_bytes(dtype), os = elem_bytes(out_dtype);
+    const int es = operand_bytes(dtype), os = elem_bytes(out_dtype);
     if (K * es >= most) CG_FAIL(CAPGNN_EINVAL, "linear: rows of 2^31 bytes and more");
+    const size_t need = capgnn_linear_workspace_bytes(M, N, K, dtype);
+    if (need && (!ws || ws_bytes < need)) CG_FAIL(CAPGNN_ENOMEM, "linear: workspace of %zu bytes needed, %zu given", need, ws ? ws_bytes : size_t(0));
+    if (need && reinterpret_cast<uintptr_t>(ws) & 255u) CG_FAIL(CAPGNN_EINVAL, "linear: workspace must be 256-byte aligned");
+    const LinearPlan p = linear_plan(M, N, K, es);
     const LinearArgs g{M, N, K, static_cast<const char *>(A), static_cast<const char *>(W), lda * es, ldw * es, a_scale, w_scale, bias, act,
                        static_cast<const char *>(R), static_cast<char *>(U), static_cast<char *>(Y), ldr * os, ldu * os, ldy * os,
-                       out_dtype == CAPGNN_BF16};
+                       out_dtype == CAPGNN_BF16, p.parts > 1 ? static_cast<float *>(ws) : nullptr, part_pitch(N), p.part_k};
     hipStream_t st = static_cast<hipStream_t>(stream);
-    (void)ws;
-    (void)ws_bytes;
-    const bool aligned = K > 0 && ((reinterpret_cast<uintptr_t>(A) | reinterpret_cast<uintptr_t>(W) | uintptr_t(g.lda) | uintptr_t(g.ldw)) & 15u) == 0 &&
-                         g.lda < most / 256 && g.ldw < most / 256;
-    if (aligned && M * N >= 256 * 256 * 128) {
-        const unsigned tiles = static_cast<unsigned>((M + 255) / 256 * ((N + 255) / 256));
+    if (p.tile == 0) {
+        // a line of a row per wave and turn
+        const int64_t lines = (p.part_k * es + 127) / 128;
+        const int waves = std::min<int>(FEW_WAVES, pow2_at_least(static_cast<int>(std::min<int64_t>(lines / 4 + 1, FEW_WAVES))));
+        const dim3 grid(static_cast<unsigned>((N + 15) / 16), p.parts);
+        auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(waves * 64), 0, st, g); };
+        if (dtype == CAPGNN_F32) M <= 16 ? go(linear_few_kernel<CAPGNN_F32, 1>) : go(linear_few_kernel<CAPGNN_F32, 2>);
+        else if (dtype == CAPGNN_BF16) M <= 16 ? go(linear_few_kernel<CAPGNN_BF16, 1>) : go(linear_few_kernel<CAPGNN_BF16, 2>);
+        else M <= 16 ? go(linear_few_kernel<E4M3_FINE, 1>) : go(linear_few_kernel<E4M3_FINE, 2>);
+    } else {
+        const bool aligned = ((reinterpret_cast<uintptr_t>(A) | reinterpret_cast<uintptr_t>(W) | uintptr_t(g.lda) | uintptr_t(g.ldw)) & 15u) == 0 &&
+                             g.lda < most / 256 && g.ldw < most / 256 && K > 0;
+        const int tile = !aligned && p.tile == 256 ? 128 : p.tile;
+        const int64_t tiles = (M + tile - 1) / tile * ((N + tile - 1) / tile);
+        if (tiles > int64_t(1) << 22) CG_FAIL(CAPGNN_EUNSUPPORTED, "linear: more than 2^22 tiles of results");
+        const dim3 grid(static_cast<unsigned>(tiles), p.parts);
         with_types(dtype, out_dtype, [&](auto d, auto o) {
-            hipLaunchKernelGGL((linear_direct_kernel<d.value, o.value, 2, 2, 4, 4>), dim3(tiles), dim3(256), 0, st, g);
+            // eight waves of 128 x 64 fill one another's gaps; 8-bit operands, whose matrix instructions run twice as long, do with half the
+            // reads of four waves of 128 x 128 (us, four / eight: 8192^3 bf16 908 / 855, 8192 x 8192 x 16384 e4m3 831 / 858)
+            if (tile == 256) {
+                if constexpr (d.value == CAPGNN_E4M3) hipLaunchKernelGGL((linear_direct_kernel<d.value, o.value, 2, 2, 4, 4>), grid, dim3(256), 0, st, g);
+                else hipLaunchKernelGGL((linear_direct_kernel<d.value, o.value, 2, 4, 4, 2>), grid, dim3(512), 0, st, g);
+            } else if (aligned) {
+                if (tile == 128) hipLaunchKernelGGL((linear_direct_kernel<d.value, o.value, 2, 2, 2, 2>), grid, dim3(256), 0, st, g);
+                else hipLaunchKernelGGL((linear_direct_kernel<d.value, o.value, 2, 2, 1, 1>), grid, dim3(256), 0, st, g);
+            } else {
+                if (tile == 128) hipLaunchKernelGGL((linear_tile_kernel<d.value, o.value, 2, 2, 2, 2>), grid, dim3(256), 0, st, g);
+                else hipLaunchKernelGGL((linear_tile_kernel<d.value, o.value, 2, 2, 1, 1>), grid, dim3(256), 0, st, g);
+            }
         });
-        CG_HIP(hipGetLastError());
-        return CAPGNN_OK;
     }
-    const dim3 grid(static_cast<unsigned>((M + 63) / 64), static_cast<unsigned>((N + 63) / 64));
-    with_types(dtype, out_dtype, [&](auto d, auto o) {
-        hipLaunchKernelGGL((linear_tile_kernel<d.value, o.value, 2, 2, 1, 1>), grid, dim3(256), 0, st, g);
-    });
     CG_HIP(hipGetLastError());
+    if (p.parts > 1) {
+        const int64_t jobs = M * (g.part_ld / 8);
+        hipLaunchKernelGGL(linear_join_kernel, dim3(static_cast<unsigned>((jobs + 255) / 256)), dim3(256), 0, st, g, p.parts);
+        CG_HIP(hipGetLastError());
+    }
     return CAPGNN_OK;
 }
 
