@@ -605,7 +605,7 @@ int capgnn_quantize_rows(int64_t n, int F, const void *X, int64_t ldx, int dtype
  * bias: device float[N] or NULL.  act: CAPGNN_ACT_*.  R: device [M x ldr] or NULL; U: device [M x ldu] or NULL (kept for the backward
  * pass); Y: device [M x ldy]; all of out_dtype (CAPGNN_F32 or CAPGNN_BF16), each rounded once.  Y may be R (same pitch).
  * K = 0: the sums are 0.  M, N, K < 2^31, a row of A or W shorter than 2^31 bytes.
- * Errors: EINVAL, EUNSUPPORTED (more than 2^22 tiles of 128 x 128 results), ENOMEM (workspace too small), EHIP. */
+ * Errors: EINVAL, EUNSUPPORTED (more than 2^22 tiles of 64 x 64 results), ENOMEM (workspace too small), EHIP. */
 size_t capgnn_linear_workspace_bytes(int64_t M, int64_t N, int64_t K, int dtype);
 int capgnn_linear(int64_t M, int64_t N, int64_t K, const void *A, int64_t lda, const float *a_scale, const void *W, int64_t ldw,
                   const float *w_scale, int dtype, const float *bias, int act, const void *R, int64_t ldr, void *U, int64_t ldu, void *Y,

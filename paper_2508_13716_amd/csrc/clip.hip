@@ -17,14 +17,12 @@ namespace capgnn {
 
 struct alignas(16) ClipPiece {
     char *g, *p;
-    uint32_t count;
-    uint8_t g_bf16, p_bf16, unused[2];
-    uint64_t unused2;
+    uint32_t count, g_bf16, p_bf16, unused;
 };
 static_assert(sizeof(ClipPiece) == 32, "two 16-byte loads a piece");
 
-constexpr unsigned CLIP_GROUPS = 2048;      // workgroups of a launch, and sums that the first one leaves
-constexpr int CLIP_LEAST = 2048, CLIP_MOST = 32768;      // elements of a piece
+constexpr unsigned CLIP_GROUPS = 4096;      // workgroups of a launch, and sums that the first one leaves
+constexpr int CLIP_PIECE = 4096;            // elements of a piece (more where a list would have more than 2^22 of them)
 
 // sum over a workgroup of 256, in every thread
 __device__ __forceinline__ double group_sum(double v) {
@@ -42,12 +40,22 @@ template <bool BF16> __device__ __forceinline__ double piece_squares(const char 
 #pragma unroll
     for (int e = 0; e < V; ++e) sum[e] = 0.0;
     int j = threadIdx.x * V;
-#pragma unroll 4
-    for (; j + V <= count; j += 256 * V) {
-        float v[V];
-        ld_row<BF16, V>(g, j, v);
+    auto add = [&](const RawRow<BF16, V> &r) __attribute__((always_inline)) {
 #pragma unroll
-        for (int e = 0; e < V; ++e) sum[e] = fma(static_cast<double>(v[e]), static_cast<double>(v[e]), sum[e]);
+        for (int e = 0; e < V; ++e) sum[e] = fma(static_cast<double>(r.get(e)), static_cast<double>(r.get(e)), sum[e]);
+    };
+    constexpr int U = 4;                // vectors on their way at a time
+    for (; j + (U - 1) * 256 * V + V <= count; j += U * 256 * V) {
+        RawRow<BF16, V> r[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) r[u].load(g, j + u * 256 * V);
+#pragma unroll
+        for (int u = 0; u < U; ++u) add(r[u]);
+    }
+    for (; j + V <= count; j += 256 * V) {
+        RawRow<BF16, V> r;
+        r.load(g, j);
+        add(r);
     }
     for (; j < count; ++j) {            // (one thread's: the others' j is behind the end by now)
         const double x = ld_logit<BF16>(g, j);
@@ -61,8 +69,10 @@ template <bool BF16> __device__ __forceinline__ double piece_squares(const char 
 
 __global__ __launch_bounds__(256) void clip_squares_kernel(const ClipPiece *pieces, unsigned n, double *sums) {
     double sum = 0.0;
+    ClipPiece ahead = pieces[blockIdx.x];
     for (unsigned k = blockIdx.x; k < n; k += gridDim.x) {
-        const ClipPiece q = pieces[k];
+        const ClipPiece q = ahead;
+        ahead = pieces[min(k + gridDim.x, n - 1)];
         sum += q.g_bf16 ? piece_squares<true>(q.g, q.count) : piece_squares<false>(q.g, q.count);
     }
     sum = group_sum(sum);
@@ -114,8 +124,11 @@ template <bool STEP> __global__ __launch_bounds__(256) void clip_apply_kernel(co
     if (!STEP && !clip) return;
     const double c = clip ? static_cast<double>(max_norm) / norm : 1.0;
     const float factor = static_cast<float>(STEP ? static_cast<double>(lr) * c : c);
+    if (blockIdx.x >= n) return;
+    ClipPiece ahead = pieces[n - 1 - blockIdx.x];
     for (unsigned k = blockIdx.x; k < n; k += gridDim.x) {
-        const ClipPiece q = pieces[n - 1 - k];
+        const ClipPiece q = ahead;
+        ahead = pieces[n - 1 - min(k + gridDim.x, n - 1)];
         if constexpr (STEP) {
             if (q.g_bf16) q.p_bf16 ? piece_apply<true, true, true>(q, factor) : piece_apply<true, true, false>(q, factor);
             else q.p_bf16 ? piece_apply<true, false, true>(q, factor) : piece_apply<true, false, false>(q, factor);
@@ -168,9 +181,9 @@ extern "C" int capgnn_tensors_create(capgnn_tensors **t, int count, void *const 
         std::sort(spans.begin(), spans.end(), [](const Span &a, const Span &b) { return a.from < b.from; });
         for (size_t i = 1; i < spans.size(); ++i)
             if (spans[i].from < spans[i - 1].to) CG_FAIL(CAPGNN_EINVAL, "tensors_create: two tensors share memory");
-        // two pieces per workgroup of a launch where there is enough for that
-        int64_t size = CLIP_LEAST;
-        while (size < CLIP_MOST && size * CLIP_GROUPS * 2 < total) size *= 2;
+        // pieces small enough that the workgroups of a launch work on one stretch of memory at a time, and few enough for the list
+        int64_t size = CLIP_PIECE;
+        while (total / size > int64_t(1) << 22) size *= 2;
         for (int i = 0; i < count; ++i)
             for (int64_t at = 0; at < counts[i]; at += size) {
                 ClipPiece q{};

@@ -202,14 +202,7 @@ __global__ __launch_bounds__(SORT_THREADS) void sort_move_kernel(SortPass s) {
     __shared__ uint32_t count[SORT_WAVES][1 << SORT_BITS], start[1 << SORT_BITS], sum[SORT_WAVES];
     if (blockIdx.x >= s.tiles) return fill_share(s.fill, blockIdx.x - s.tiles, gridDim.x - s.tiles);
     const int digits = 1 << s.bits, wave = threadIdx.x / 64;
-    for (int d = threadIdx.x; d < digits; d += SORT_THREADS) {
-        start[d] = s.total[d];
-#pragma unroll
-        for (int w = 0; w < SORT_WAVES; ++w) count[w][d] = 0;
-    }
-    __syncthreads();
-    digit_scan<SORT_WAVES>(start, digits, sum);
-    // a wave has SORT_ITEMS * 64 neighbouring items, 64 at a time
+    // a wave has SORT_ITEMS * 64 neighbouring items, 64 at a time; all that is read is asked for first
     const int64_t first = int64_t(blockIdx.x) * SORT_TILE + wave * (SORT_ITEMS * 64) + (threadIdx.x & 63);
     uint32_t key[SORT_ITEMS], pos[SORT_ITEMS], rank[SORT_ITEMS];
     bool on[SORT_ITEMS];
@@ -220,15 +213,34 @@ __global__ __launch_bounds__(SORT_THREADS) void sort_move_kernel(SortPass s) {
         key[i] = on[i] ? sort_key(s, k) : 0u;
         pos[i] = on[i] ? (s.ids ? static_cast<uint32_t>(k) : s.pos[k]) : 0u;
     }
+    constexpr int EACH = (1 << SORT_BITS) / SORT_THREADS;
+    uint32_t before[EACH];
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) {
+        const int d = i * SORT_THREADS + threadIdx.x;
+        before[i] = 0;
+        if (d < digits) {
+            before[i] = s.count[int64_t(d) * s.tiles + blockIdx.x];
+            start[d] = s.total[d];
+#pragma unroll
+            for (int w = 0; w < SORT_WAVES; ++w) count[w][d] = 0;
+        }
+    }
+    __syncthreads();
+    digit_scan<SORT_WAVES>(start, digits, sum);
     rank_items(key, on, s.shift, s.bits, count[wave], rank);
     __syncthreads();
-    for (int d = threadIdx.x; d < digits; d += SORT_THREADS) {
-        uint32_t at = start[d] + s.count[int64_t(d) * s.tiles + blockIdx.x];
 #pragma unroll
-        for (int w = 0; w < SORT_WAVES; ++w) {
-            const uint32_t c = count[w][d];
-            count[w][d] = at;
-            at += c;
+    for (int i = 0; i < EACH; ++i) {
+        const int d = i * SORT_THREADS + threadIdx.x;
+        if (d < digits) {
+            uint32_t at = start[d] + before[i];
+#pragma unroll
+            for (int w = 0; w < SORT_WAVES; ++w) {
+                const uint32_t c = count[w][d];
+                count[w][d] = at;
+                at += c;
+            }
         }
     }
     __syncthreads();
@@ -333,99 +345,190 @@ template <int V> __device__ __forceinline__ void put_row(const RunArgs &a, uint3
     }
 }
 
-constexpr int RUN_AHEAD = 8;        // rows on their way at a time
+constexpr int RUN_AHEAD = 8;        // rows of a batch: one is on its way while another is added
 
+// A team's next entries are in its lanes, one each, and handed round from there, so that a row's address waits for nothing but its entry's load
+// a whole stretch before.
 template <bool BF16, int V> __global__ __launch_bounds__(256) void run_sums_kernel(RunArgs a) {
     const int lane = threadIdx.x & (a.lanes - 1), teams = 256 / a.lanes;
     const int64_t tile = int64_t(blockIdx.x) * teams + threadIdx.x / a.lanes;
     const int vec = blockIdx.y * a.lanes + lane, j = vec * V;
-    if (tile >= a.tiles || j >= a.F) return;
+    const bool live = tile < a.tiles && j < a.F;
     const int from = min(j, a.F - V), skip = j - from;
-    const int64_t p0 = tile * a.R, p1 = min(p0 + a.R, a.n);
+    const int64_t p0 = min(tile, a.tiles - 1) * a.R, p1 = min(p0 + a.R, a.n);
+    const int count = static_cast<int>(p1 - p0);
+    // (loaded without conditions, so that they are under way together)
     uint32_t cur = a.key[p0];
-    bool head = p0 > 0 && a.key[p0 - 1] == cur;
-    const uint32_t next = p1 < a.n ? a.key[p1] : ~0u;
+    const uint32_t last = a.key[max(p0 - 1, int64_t(0))], after = a.key[min(p1, a.n - 1)];
+    bool head = p0 > 0 && last == cur;
+    const uint32_t next = p1 < a.n ? after : ~0u;
     float *part = a.part + tile * 2 * a.part_ld + vec * V;
     float acc[V];
 #pragma unroll
     for (int e = 0; e < V; ++e) acc[e] = 0.f;
-    for (int64_t p = p0; p < p1; p += RUN_AHEAD) {
-        uint32_t key[RUN_AHEAD];
-        RawRow<BF16, V> row[RUN_AHEAD];
+    uint32_t keys[2][RUN_AHEAD];
+    RawRow<BF16, V> rows[2][RUN_AHEAD];
+    // entries of a team that its lanes hold: [held, held + lanes)
+    int held = 0;
+    uint32_t key_here = 0, pos_here = 0;
+    auto hold = [&](int from_entry) __attribute__((always_inline)) {
+        held = from_entry;
+        const int64_t p = p0 + min(from_entry + lane, count - 1);
+        key_here = a.key[p];
+        pos_here = a.pos[p];
+    };
+    auto fetch = [&](int set, int entry) __attribute__((always_inline)) {
 #pragma unroll
         for (int i = 0; i < RUN_AHEAD; ++i) {
-            const int64_t q = min(p + i, p1 - 1);
-            key[i] = a.key[q];
-            row[i].load(a.dY + int64_t(a.pos[q]) * a.lddy, from);
+            const int at = min(entry + i, count - 1);
+            if (at >= held + a.lanes) hold(at);
+            const int source = (threadIdx.x & 63 & ~(a.lanes - 1)) + at - held;
+            keys[set][i] = static_cast<uint32_t>(__shfl(static_cast<int>(key_here), source));
+            const uint32_t pos = static_cast<uint32_t>(__shfl(static_cast<int>(pos_here), source));
+            rows[set][i].load(a.dY + int64_t(pos) * a.lddy, from);
         }
+    };
+    auto add = [&](int set, int entry) __attribute__((always_inline)) {
 #pragma unroll
         for (int i = 0; i < RUN_AHEAD; ++i) {
-            if (p + i < p1) {
-                if (key[i] != cur) {
-                    if (head) st_row<false, V>(reinterpret_cast<char *>(part), 0, acc);
-                    else put_row<V>(a, cur, from, skip, acc);
+            if (entry + i < count) {
+                if (keys[set][i] != cur) {
+                    if (live) {
+                        if (head) st_row<false, V>(reinterpret_cast<char *>(part), 0, acc);
+                        else if (cur < a.V) put_row<V>(a, cur, from, skip, acc);
+                    }
                     head = false;
-                    cur = key[i];
+                    cur = keys[set][i];
 #pragma unroll
                     for (int e = 0; e < V; ++e) acc[e] = 0.f;
                 }
 #pragma unroll
-                for (int e = 0; e < V; ++e) acc[e] += row[i].get(e);
+                for (int e = 0; e < V; ++e) acc[e] += rows[set][i].get(e);
             }
         }
-        if (cur >= a.V) return;         // (sorted: what follows names no row either)
+    };
+    // (all lanes of a wave walk as many batches: what is behind a tile's end repeats its last entry and is not added)
+    hold(0);
+    fetch(0, 0);
+    for (int p = 0; p < a.R; p += 2 * RUN_AHEAD) {
+        if (p + RUN_AHEAD < a.R) fetch(1, p + RUN_AHEAD);
+        add(0, p);
+        if (p + 2 * RUN_AHEAD < a.R) fetch(0, p + 2 * RUN_AHEAD);
+        if (p + RUN_AHEAD < a.R) add(1, p + RUN_AHEAD);
     }
+    if (!live || cur >= a.V) return;            // (ids outside the table are the last ones)
     if (head) st_row<false, V>(reinterpret_cast<char *>(part), 0, acc);
     else if (cur == next) st_row<false, V>(reinterpret_cast<char *>(part + a.part_ld), 0, acc);
     else put_row<V>(a, cur, from, skip, acc);
 }
 
-// The runs that cross tiles: the workgroup of the tile in which one begins adds its parts, every team those of a stretch of tiles.
-template <int V> __global__ __launch_bounds__(256) void run_join_kernel(RunArgs a) {
-    __shared__ float sums[256 * V];
-    __shared__ int run_end;
-    const int64_t tile = blockIdx.x, p0 = tile * a.R, p1 = p0 + a.R;
-    if (p1 >= a.n) return;
-    const uint32_t id = a.key[p1];
-    if (id >= a.V || a.key[p1 - 1] != id || (a.key[p0] == id && p0 > 0 && a.key[p0 - 1] == id)) return;
-    // tiles tile + 1 .. tile + m begin with this id (so does, by the order, every one between)
-    int64_t m = 1;
-    for (bool more = true; more;) {
-        if (threadIdx.x == 0) run_end = 256;
-        __syncthreads();
-        const int64_t t = tile + 1 + m + threadIdx.x;
-        if (t >= a.tiles || a.key[t * a.R] != id) atomicMin(&run_end, static_cast<int>(threadIdx.x));
-        __syncthreads();
-        m += run_end;
-        more = run_end == 256;
-        __syncthreads();
-    }
-    const int lane = threadIdx.x & (a.lanes - 1), teams = 256 / a.lanes, team = threadIdx.x / a.lanes;
-    const int vec = blockIdx.y * a.lanes + lane, j = vec * V;
+// The runs that cross tiles: where one begins, its parts are added, by the tile's team if they are few, else by the whole workgroup, every team
+// those of a stretch of tiles.
+constexpr int JOIN_THREADS = 1024, JOIN_FEW = 16;
+
+template <int V> __global__ __launch_bounds__(JOIN_THREADS) void run_join_kernel(RunArgs a) {
+    __shared__ float sums[JOIN_THREADS * V];
+    __shared__ int run_end, many[JOIN_THREADS], n_many;
+    __shared__ uint32_t many_id[JOIN_THREADS];
+    const int lane = threadIdx.x & (a.lanes - 1), teams = JOIN_THREADS / a.lanes, team = threadIdx.x / a.lanes;
+    const int vec = blockIdx.y * a.lanes + lane, j = vec * V, from = min(j, a.F - V);
     const bool live = j < a.F;
-    const int64_t each = (m + teams - 1) / teams, first = tile + 1 + min(each * team, m), end = tile + 1 + min(each * (team + 1), m);
-    float acc[V];
+    auto part = [&](int64_t tile, int which) { return reinterpret_cast<const char *>(a.part + (tile * 2 + which) * a.part_ld + vec * V); };
+    if (threadIdx.x == 0) n_many = 0;
+    __syncthreads();
+    {
+        const int64_t tile = int64_t(blockIdx.x) * teams + team, p0 = tile * a.R, p1 = p0 + a.R, last = a.n - 1;
+        // (everything that may be asked is asked for together: a step that waits for memory costs two microseconds here)
+        const uint32_t id = a.key[min(p1, last)], id_end = a.key[min(p1 - 1, last)], id_begin = a.key[min(p0, last)];
+        const uint32_t id_last = a.key[min(max(p0 - 1, int64_t(0)), last)];
+        uint32_t begins[JOIN_FEW];
 #pragma unroll
-    for (int e = 0; e < V; ++e) acc[e] = 0.f;
-    if (live) {
-        if (team == 0) ld_row<false, V>(reinterpret_cast<const char *>(a.part + (tile * 2 + 1) * a.part_ld + vec * V), 0, acc);
+        for (int i = 0; i < JOIN_FEW; ++i) begins[i] = a.key[min(tile + 2 + i, a.tiles - 1) * a.R];
+        // (ids beyond the table are no run; one that came in from the tile before begins elsewhere)
+        if (p1 < a.n && id < a.V && id_end == id && !(id_begin == id && p0 > 0 && id_last == id)) {
+            int m = 1;
+#pragma unroll
+            for (int i = 0; i < JOIN_FEW; ++i)
+                if (m == i + 1 && tile + 2 + i < a.tiles && begins[i] == id) ++m;
+            if (m <= JOIN_FEW) {
+                if (live) {
+                    float acc[V];
+                    ld_row<false, V>(part(tile, 1), 0, acc);
 #pragma unroll 4
-        for (int64_t t = first; t < end; ++t) {
-            float v[V];
-            ld_row<false, V>(reinterpret_cast<const char *>(a.part + t * 2 * a.part_ld + vec * V), 0, v);
+                    for (int t = 1; t <= m; ++t) {
+                        float v[V];
+                        ld_row<false, V>(part(tile + t, 0), 0, v);
 #pragma unroll
-            for (int e = 0; e < V; ++e) acc[e] += v[e];
+                        for (int e = 0; e < V; ++e) acc[e] += v[e];
+                    }
+                    put_row<V>(a, id, from, j - from, acc);
+                }
+            } else if (lane == 0) {
+                const int k = atomicAdd(&n_many, 1);        // (each is added by itself: their order changes nothing)
+                many[k] = team;
+                many_id[k] = id;
+            }
         }
     }
-#pragma unroll
-    for (int e = 0; e < V; ++e) sums[e * 256 + threadIdx.x] = acc[e];
     __syncthreads();
-    if (team == 0 && live) {
-        for (int q = 1; q < teams; ++q)
+    for (int k = 0; k < n_many; ++k) {
+        const int64_t tile = int64_t(blockIdx.x) * teams + many[k];
+        const uint32_t id = many_id[k];
+        int64_t m = JOIN_FEW;               // tiles tile + 1 .. tile + m begin with this id (by the order every one between does)
+        constexpr int PROBES = 4;           // of a thread at a time
+        for (bool more = true; more;) {
+            if (threadIdx.x == 0) run_end = PROBES * JOIN_THREADS;
+            __syncthreads();
+            uint32_t probe[PROBES];
+            const int64_t t = tile + 1 + m + threadIdx.x;
 #pragma unroll
-            for (int e = 0; e < V; ++e) acc[e] += sums[e * 256 + q * a.lanes + lane];
-        const int from = min(j, a.F - V);
-        put_row<V>(a, id, from, j - from, acc);
+            for (int i = 0; i < PROBES; ++i) probe[i] = a.key[min(t + i * JOIN_THREADS, a.tiles - 1) * a.R];
+#pragma unroll
+            for (int i = 0; i < PROBES; ++i) {
+                const uint64_t out = __ballot(t + i * JOIN_THREADS >= a.tiles || probe[i] != id);
+                if (out && (threadIdx.x & 63) == 0) atomicMin(&run_end, static_cast<int>(threadIdx.x) + i * JOIN_THREADS + __ffsll(static_cast<unsigned long long>(out)) - 1);
+            }
+            __syncthreads();
+            m += run_end;
+            more = run_end == PROBES * JOIN_THREADS;
+            __syncthreads();
+        }
+        const int64_t each = (m + teams - 1) / teams, first = tile + 1 + min(each * team, m), end = tile + 1 + min(each * (team + 1), m);
+        float acc[V];
+#pragma unroll
+        for (int e = 0; e < V; ++e) acc[e] = 0.f;
+        if (live) {
+            if (team == 0) ld_row<false, V>(part(tile, 1), 0, acc);
+            constexpr int AHEAD = V == 8 ? 8 : 16;
+            for (int64_t t = first; t < end; t += AHEAD) {
+                float v[AHEAD][V];
+#pragma unroll
+                for (int i = 0; i < AHEAD; ++i) ld_row<false, V>(part(min(t + i, end - 1), 0), 0, v[i]);
+#pragma unroll
+                for (int i = 0; i < AHEAD; ++i)
+                    if (t + i < end) {
+#pragma unroll
+                        for (int e = 0; e < V; ++e) acc[e] += v[i][e];
+                    }
+            }
+        }
+#pragma unroll
+        for (int e = 0; e < V; ++e) sums[e * JOIN_THREADS + threadIdx.x] = acc[e];
+        __syncthreads();
+        // the teams' sums, half of them to the other half, in a fixed order
+        for (int half = teams / 2; half; half /= 2) {
+            if (team < half) {
+#pragma unroll
+                for (int e = 0; e < V; ++e) sums[e * JOIN_THREADS + threadIdx.x] += sums[e * JOIN_THREADS + threadIdx.x + half * a.lanes];
+            }
+            __syncthreads();
+        }
+        if (team == 0 && live) {
+#pragma unroll
+            for (int e = 0; e < V; ++e) acc[e] = sums[e * JOIN_THREADS + threadIdx.x];
+            put_row<V>(a, id, from, j - from, acc);
+        }
+        __syncthreads();
     }
 }
 
@@ -587,7 +690,8 @@ extern "C" int capgnn_embed_bwd(int64_t n, const int64_t *ids, int64_t V, int F,
                     lddy * elem_bytes(dy_dtype), scale, dtable, lddt, accumulate != 0, reinterpret_cast<float *>(base + w.part),
                     (F + e.V - 1) / e.V * e.V};
     const int teams = 256 / e.lanes;
-    const dim3 sums(static_cast<unsigned>((a.tiles + teams - 1) / teams), e.chunks), join(static_cast<unsigned>(a.tiles), e.chunks);
+    const dim3 sums(static_cast<unsigned>((a.tiles + teams - 1) / teams), e.chunks);
+    const dim3 join(static_cast<unsigned>((a.tiles * e.lanes + JOIN_THREADS - 1) / JOIN_THREADS), e.chunks);
     if (bf16) {
         if (e.V == 1) hipLaunchKernelGGL((run_sums_kernel<true, 1>), sums, dim3(256), 0, st, a);
         else hipLaunchKernelGGL((run_sums_kernel<true, 8>), sums, dim3(256), 0, st, a);
@@ -596,9 +700,9 @@ extern "C" int capgnn_embed_bwd(int64_t n, const int64_t *ids, int64_t V, int F,
         else hipLaunchKernelGGL((run_sums_kernel<false, 4>), sums, dim3(256), 0, st, a);
     }
     if (a.tiles > 1) {
-        if (e.V == 1) hipLaunchKernelGGL(run_join_kernel<1>, join, dim3(256), 0, st, a);
-        else if (e.V == 4) hipLaunchKernelGGL(run_join_kernel<4>, join, dim3(256), 0, st, a);
-        else hipLaunchKernelGGL(run_join_kernel<8>, join, dim3(256), 0, st, a);
+        if (e.V == 1) hipLaunchKernelGGL(run_join_kernel<1>, join, dim3(JOIN_THREADS), 0, st, a);
+        else if (e.V == 4) hipLaunchKernelGGL(run_join_kernel<4>, join, dim3(JOIN_THREADS), 0, st, a);
+        else hipLaunchKernelGGL(run_join_kernel<8>, join, dim3(JOIN_THREADS), 0, st, a);
     }
     CG_HIP(hipGetLastError());
     return CAPGNN_OK;

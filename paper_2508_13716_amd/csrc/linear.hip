@@ -398,9 +398,11 @@ template <int MFMAS, int READS, int LOADS> __device__ __forceinline__ void inter
     }
 }
 
-template <int DT, bool OB, int WR, int WC, int TM, int TN> __global__ __launch_bounds__(WR *WC * 64) void linear_direct_kernel(LinearArgs g) {
+// LB: bytes of a lane's load, 16 or (rows that start on any 4 bytes) 4
+template <int DT, bool OB, int WR, int WC, int TM, int TN, int LB> __global__ __launch_bounds__(WR *WC * 64) void linear_direct_kernel(LinearArgs g) {
     constexpr int T = WR * WC * 64, BM = WR * TM * 32, BN = WC * TN * 32, STEP = 128 / BYTES<DT>, S = SLICES<DT>;
-    constexpr int PA = BM * UNITS / T, PB = BN * UNITS / T, TILE = (BM + BN) * UNITS;
+    constexpr int PER_ROW = 128 / LB, ROWS = T / PER_ROW;               // lanes of a row, rows of a load of all waves
+    constexpr int PA = BM / ROWS, PB = BN / ROWS, TILE = (BM + BN) * UNITS;
     static_assert(STAGE_BYTES<WR * WC, TN> <= 2 * TILE * 16, "results leave through the tiles' memory");
     __shared__ raw16 lds[2 * TILE];
     const int wave = threadIdx.x / 64, lane = threadIdx.x & 63, half = lane / 32;
@@ -415,27 +417,34 @@ template <int DT, bool OB, int WR, int WC, int TM, int TN> __global__ __launch_b
     const char *A = x.A + m0 * g.lda, *W = x.W + n0 * g.ldw;
     auto sa = __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(A), 0, (rows_a - 1) * lda + width, 0x00027000);
     auto sb = __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(W), 0, (rows_b - 1) * ldw + width, 0x00027000);
-    // A wave's load fills 8 rows of LDS in order: lane l has place l % 8 of row l / 8, which holds unit (l % 8) ^ (row / 2 % 8).  Rows behind the last
-    // one are the last one again: their results are not stored, and nothing depends on the buffer's bounds.
-    const uint32_t row = threadIdx.x / UNITS, unit = (threadIdx.x % UNITS) ^ (row >> 1 & 7);
+    // A wave's load fills LDS in order (for 16 bytes: lane l has place l % 8 of row l / 8), and place p of a row holds unit p ^ (row / 2 % 8).
+    // Rows behind the last one are the last one again: their results are not stored, and nothing depends on the buffer's bounds.
+    const uint32_t row = threadIdx.x / PER_ROW, byte = threadIdx.x % PER_ROW * LB;
     uint32_t oa[PA], ob[PB];
 #pragma unroll
-    for (int p = 0; p < PA; ++p) oa[p] = min(row + p * (T / UNITS), rows_a - 1u) * lda + unit * 16;
+    for (int p = 0; p < PA; ++p) oa[p] = min(row + p * ROWS, rows_a - 1u) * lda + (byte ^ (row + p * ROWS) / 2 % 8 * 16);
 #pragma unroll
-    for (int p = 0; p < PB; ++p) ob[p] = min(row + p * (T / UNITS), rows_b - 1u) * ldw + unit * 16;
+    for (int p = 0; p < PB; ++p) ob[p] = min(row + p * ROWS, rows_b - 1u) * ldw + (byte ^ (row + p * ROWS) / 2 % 8 * 16);
     const int steps = static_cast<int>(x.K / STEP), all = steps + (x.K % STEP ? 1 : 0);
     auto fill = [&](int t) __attribute__((always_inline)) {
-        raw16 *As = lds + (t & 1) * TILE, *Bs = As + BM * UNITS;
+        char *As = reinterpret_cast<char *>(lds + (t & 1) * TILE) + wave * 64 * LB, *Bs = As + BM * 128;
+        if constexpr (LB == 16) {
 #pragma unroll
-        for (int p = 0; p < PA; ++p) __builtin_amdgcn_raw_ptr_buffer_load_lds(sa, As + p * T + wave * 64, 16, static_cast<int>(oa[p]), t * 128, 0, 0);
+            for (int p = 0; p < PA; ++p) __builtin_amdgcn_raw_ptr_buffer_load_lds(sa, As + p * T * LB, 16, static_cast<int>(oa[p]), t * 128, 0, 0);
 #pragma unroll
-        for (int p = 0; p < PB; ++p) __builtin_amdgcn_raw_ptr_buffer_load_lds(sb, Bs + p * T + wave * 64, 16, static_cast<int>(ob[p]), t * 128, 0, 0);
+            for (int p = 0; p < PB; ++p) __builtin_amdgcn_raw_ptr_buffer_load_lds(sb, Bs + p * T * LB, 16, static_cast<int>(ob[p]), t * 128, 0, 0);
+        } else {
+#pragma unroll
+            for (int p = 0; p < PA; ++p) __builtin_amdgcn_raw_ptr_buffer_load_lds(sa, As + p * T * LB, 4, static_cast<int>(oa[p]), t * 128, 0, 0);
+#pragma unroll
+            for (int p = 0; p < PB; ++p) __builtin_amdgcn_raw_ptr_buffer_load_lds(sb, Bs + p * T * LB, 4, static_cast<int>(ob[p]), t * 128, 0, 0);
+        }
     };
     auto fill_end = [&]() __attribute__((always_inline)) {              // what is left of the reduction, element by element at its end
         raw16 *As = lds + (steps & 1) * TILE;
         const int64_t k = int64_t(steps) * STEP + threadIdx.x % UNITS * (16 / BYTES<DT>);
 #pragma unroll 1
-        for (int r = row; r < BM + BN; r += T / UNITS)
+        for (int r = threadIdx.x / UNITS; r < BM + BN; r += T / UNITS)
             As[unit_at(r, threadIdx.x % UNITS)] = r < BM ? load_unit<DT>(A + int64_t(min(r, rows_a - 1)) * g.lda, k, x.K)
                                                         : load_unit<DT>(W + int64_t(min(r - BM, rows_b - 1)) * g.ldw, k, x.K);
     };
@@ -739,9 +748,9 @@ extern "C" int capgnn_linear(int64_t M, int64_t N, int64_t K, const void *A, int
         else if (dtype == CAPGNN_BF16) M <= 16 ? go(linear_few_kernel<CAPGNN_BF16, 1>) : go(linear_few_kernel<CAPGNN_BF16, 2>);
         else M <= 16 ? go(linear_few_kernel<E4M3_FINE, 1>) : go(linear_few_kernel<E4M3_FINE, 2>);
     } else {
-        const bool aligned = ((reinterpret_cast<uintptr_t>(A) | reinterpret_cast<uintptr_t>(W) | uintptr_t(g.lda) | uintptr_t(g.ldw)) & 15u) == 0 &&
-                             g.lda < most / 256 && g.ldw < most / 256 && K > 0;
-        const int tile = !aligned && p.tile == 256 ? 128 : p.tile;
+        const uintptr_t at = reinterpret_cast<uintptr_t>(A) | reinterpret_cast<uintptr_t>(W) | uintptr_t(g.lda) | uintptr_t(g.ldw);
+        const int unit = K == 0 || at % 4 || g.lda >= most / 256 || g.ldw >= most / 256 ? 1 : at % 16 ? 4 : 16;      // bytes of a load to LDS
+        const int tile = unit == 1 ? 64 : unit == 4 ? std::min(p.tile, 128) : p.tile;
         const int64_t tiles = (M + tile - 1) / tile * ((N + tile - 1) / tile);
         if (tiles > int64_t(1) << 22) CG_FAIL(CAPGNN_EUNSUPPORTED, "linear: more than 2^22 tiles of results");
         const dim3 grid(static_cast<unsigned>(tiles), p.parts);
@@ -749,14 +758,16 @@ extern "C" int capgnn_linear(int64_t M, int64_t N, int64_t K, const void *A, int
             // eight waves of 128 x 64 fill one another's gaps; 8-bit operands, whose matrix instructions run twice as long, do with half the
             // reads of four waves of 128 x 128 (us, four / eight: 8192^3 bf16 908 / 855, 8192 x 8192 x 16384 e4m3 831 / 858)
             if (tile == 256) {
-                if constexpr (d.value == CAPGNN_E4M3) hipLaunchKernelGGL((linear_direct_kernel<d.value, o.value, 2, 2, 4, 4>), grid, dim3(256), 0, st, g);
-                else hipLaunchKernelGGL((linear_direct_kernel<d.value, o.value, 2, 4, 4, 2>), grid, dim3(512), 0, st, g);
-            } else if (aligned) {
-                if (tile == 128) hipLaunchKernelGGL((linear_direct_kernel<d.value, o.value, 2, 2, 2, 2>), grid, dim3(256), 0, st, g);
-                else hipLaunchKernelGGL((linear_direct_kernel<d.value, o.value, 2, 2, 1, 1>), grid, dim3(256), 0, st, g);
+                if constexpr (d.value == CAPGNN_E4M3) hipLaunchKernelGGL((linear_direct_kernel<d.value, o.value, 2, 2, 4, 4, 16>), grid, dim3(256), 0, st, g);
+                else hipLaunchKernelGGL((linear_direct_kernel<d.value, o.value, 2, 4, 4, 2, 16>), grid, dim3(512), 0, st, g);
+            } else if (unit == 16) {
+                if (tile == 128) hipLaunchKernelGGL((linear_direct_kernel<d.value, o.value, 2, 2, 2, 2, 16>), grid, dim3(256), 0, st, g);
+                else hipLaunchKernelGGL((linear_direct_kernel<d.value, o.value, 2, 2, 1, 1, 16>), grid, dim3(256), 0, st, g);
+            } else if (unit == 4) {
+                if (tile == 128) hipLaunchKernelGGL((linear_direct_kernel<d.value, o.value, 2, 2, 2, 2, 4>), grid, dim3(256), 0, st, g);
+                else hipLaunchKernelGGL((linear_direct_kernel<d.value, o.value, 2, 2, 1, 1, 4>), grid, dim3(256), 0, st, g);
             } else {
-                if (tile == 128) hipLaunchKernelGGL((linear_tile_kernel<d.value, o.value, 2, 2, 2, 2>), grid, dim3(256), 0, st, g);
-                else hipLaunchKernelGGL((linear_tile_kernel<d.value, o.value, 2, 2, 1, 1>), grid, dim3(256), 0, st, g);
+                hipLaunchKernelGGL((linear_tile_kernel<d.value, o.value, 2, 2, 1, 1>), grid, dim3(256), 0, st, g);
             }
         });
     }
