@@ -398,13 +398,14 @@ template <int MFMAS, int READS, int LOADS> __device__ __forceinline__ void inter
     }
 }
 
-// LB: bytes of a lane's load, 16 or (rows that start on any 4 bytes) 4
-template <int DT, bool OB, int WR, int WC, int TM, int TN, int LB> __global__ __launch_bounds__(WR *WC * 64) void linear_direct_kernel(LinearArgs g) {
+// LB: bytes of a lane's load, 16 or (rows that start on any 4 bytes) 4; NB: steps that LDS holds
+template <int DT, bool OB, int WR, int WC, int TM, int TN, int LB, int NB> __global__ __launch_bounds__(WR *WC * 64) void linear_direct_kernel(LinearArgs g) {
     constexpr int T = WR * WC * 64, BM = WR * TM * 32, BN = WC * TN * 32, STEP = 128 / BYTES<DT>, S = SLICES<DT>;
     constexpr int PER_ROW = 128 / LB, ROWS = T / PER_ROW;               // lanes of a row, rows of a load of all waves
     constexpr int PA = BM / ROWS, PB = BN / ROWS, TILE = (BM + BN) * UNITS;
-    static_assert(STAGE_BYTES<WR * WC, TN> <= 2 * TILE * 16, "results leave through the tiles' memory");
-    __shared__ raw16 lds[2 * TILE];
+    static_assert(STAGE_BYTES<WR * WC, TN> <= NB * TILE * 16, "results leave through the tiles' memory");
+    static_assert((NB - 2) * (PA + PB) < 64, "loads that a wave can wait for one by one");
+    __shared__ raw16 lds[NB * TILE];
     const int wave = threadIdx.x / 64, lane = threadIdx.x & 63, half = lane / 32;
     const int wm = wave / WC * TM * 32, wn = wave % WC * TN * 32;
     unsigned tm, tn;
@@ -427,7 +428,7 @@ template <int DT, bool OB, int WR, int WC, int TM, int TN, int LB> __global__ __
     for (int p = 0; p < PB; ++p) ob[p] = min(row + p * ROWS, rows_b - 1u) * ldw + (byte ^ (row + p * ROWS) / 2 % 8 * 16);
     const int steps = static_cast<int>(x.K / STEP), all = steps + (x.K % STEP ? 1 : 0);
     auto fill = [&](int t) __attribute__((always_inline)) {
-        char *As = reinterpret_cast<char *>(lds + (t & 1) * TILE) + wave * 64 * LB, *Bs = As + BM * 128;
+        char *As = reinterpret_cast<char *>(lds + t % NB * TILE) + wave * 64 * LB, *Bs = As + BM * 128;
         if constexpr (LB == 16) {
 #pragma unroll
             for (int p = 0; p < PA; ++p) __builtin_amdgcn_raw_ptr_buffer_load_lds(sa, As + p * T * LB, 16, static_cast<int>(oa[p]), t * 128, 0, 0);
@@ -441,7 +442,7 @@ template <int DT, bool OB, int WR, int WC, int TM, int TN, int LB> __global__ __
         }
     };
     auto fill_end = [&]() __attribute__((always_inline)) {              // what is left of the reduction, element by element at its end
-        raw16 *As = lds + (steps & 1) * TILE;
+        raw16 *As = lds + steps % NB * TILE;
         const int64_t k = int64_t(steps) * STEP + threadIdx.x % UNITS * (16 / BYTES<DT>);
 #pragma unroll 1
         for (int r = threadIdx.x / UNITS; r < BM + BN; r += T / UNITS)
@@ -453,14 +454,17 @@ template <int DT, bool OB, int WR, int WC, int TM, int TN, int LB> __global__ __
     Slice<DT, TM> a[2];
     Slice<DT, TN> b[2];
     auto read = [&](int k, int t, int s) {
-        const raw16 *As = lds + (t & 1) * TILE;
+        const raw16 *As = lds + t % NB * TILE;
         a[k].read(As, wm + lane % 32, half, s);
         b[k].read(As + BM * UNITS, wn + lane % 32, half, s);
     };
-    auto arrived = [&]() __attribute__((always_inline)) {               // everyone's loads to LDS are there, and everyone has read what he asked for
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    // everyone's loads to LDS but the last `later` are there, and everyone has read what he asked for
+    auto arrived = [&](auto later) __attribute__((always_inline)) {
+        asm volatile("s_waitcnt vmcnt(%0)" ::"n"(later.value) : "memory");
         __syncthreads();
     };
+    using None = std::integral_constant<int, 0>;
+    using Later = std::integral_constant<int, (NB - 2) * (PA + PB)>;
     auto most = [&](int t) __attribute__((always_inline)) {             // the slices of step t but the last
 #pragma unroll
         for (int s = 0; s + 1 < S; ++s) {
@@ -470,24 +474,24 @@ template <int DT, bool OB, int WR, int WC, int TM, int TN, int LB> __global__ __
         }
     };
 #pragma unroll 1
-    for (int t = 0; t < min(steps, 2); ++t) fill(t);
-    if (steps < 2 && steps < all) fill_end();
-    arrived();
+    for (int t = 0; t < min(steps, NB); ++t) fill(t);
+    if (steps < NB && steps < all) fill_end();
+    arrived(None());
     read(0, 0, 0);
     int t = 0;
-    for (; t + 2 < steps; ++t) {
+    for (; t + NB < steps; ++t) {
         most(t);
-        arrived();
+        arrived(Later());               // step t + 1 is; t + 2 .. t + NB - 1 may be on their way
         read(0, t + 1, 0);
-        fill(t + 2);
+        fill(t + NB);
         multiply_slice<DT, TM, TN>(a[1], b[1], acc);
         interleave<MFMAS, READS, PA + PB>();
     }
     for (; t < all; ++t) {
         most(t);
         if (t + 1 < all) {
-            arrived();
-            if (t + 2 == steps && steps < all) fill_end();
+            arrived(None());
+            if (t + NB == steps && steps < all) fill_end();
             read(0, t + 1, 0);
         }
         multiply_slice<DT, TM, TN>(a[1], b[1], acc);
@@ -533,11 +537,11 @@ template <int DT> __device__ __forceinline__ acc4 multiply16(raw16 w, raw16 a, a
     }
 }
 
-constexpr int FEW_WAVES = 16, FEW_AHEAD = 4;        // waves of a workgroup, at most; units of a row on their way at a time, per lane
+constexpr int FEW_WAVES = 16;           // of a workgroup, at most
 
 // TM: groups of 16 rows of A
 template <int DT, int TM> __global__ __launch_bounds__(FEW_WAVES * 64) void linear_few_kernel(LinearArgs g) {
-    constexpr int E = 16 / BYTES<DT>;
+    constexpr int E = 16 / BYTES<DT>, AHEAD = 8 / TM;           // units of a row on their way at a time, per lane
     __shared__ acc4 sums[FEW_WAVES][TM][64];
     const int wave = threadIdx.x / 64, waves = blockDim.x / 64, lane = threadIdx.x & 63;
     const int64_t n0 = int64_t(blockIdx.x) * 16;
@@ -551,10 +555,10 @@ template <int DT, int TM> __global__ __launch_bounds__(FEW_WAVES * 64) void line
     const int64_t lines = (x.K + 8 * E - 1) / (8 * E), mine = lines > wave ? ((lines - wave - 1) / waves + 1) * 2 : 0;
     const int64_t sure = x.K / (8 * E), whole = sure > wave ? ((sure - wave - 1) / waves + 1) * 2 : 0;      // of lines that end inside the row
     int64_t q = 0;
-    for (; q + FEW_AHEAD <= whole; q += FEW_AHEAD) {
-        raw16 rw[FEW_AHEAD], ra[FEW_AHEAD][TM];
+    for (; q + AHEAD <= whole; q += AHEAD) {
+        raw16 rw[AHEAD], ra[AHEAD][TM];
 #pragma unroll
-        for (int u = 0; u < FEW_AHEAD; ++u) {
+        for (int u = 0; u < AHEAD; ++u) {
             typedef raw16 raw16_by1 __attribute__((aligned(1)));
             const int64_t k = at(q + u) * BYTES<DT>;
             rw[u] = *reinterpret_cast<const raw16_by1 *>(w + k);
@@ -562,7 +566,7 @@ template <int DT, int TM> __global__ __launch_bounds__(FEW_WAVES * 64) void line
             for (int i = 0; i < TM; ++i) ra[u][i] = *reinterpret_cast<const raw16_by1 *>(a[i] + k);
         }
 #pragma unroll
-        for (int u = 0; u < FEW_AHEAD; ++u)
+        for (int u = 0; u < AHEAD; ++u)
 #pragma unroll
             for (int i = 0; i < TM; ++i) acc[i] = multiply16<DT>(rw[u], ra[u][i], acc[i]);
     }
@@ -758,14 +762,14 @@ extern "C" int capgnn_linear(int64_t M, int64_t N, int64_t K, const void *A, int
             // eight waves of 128 x 64 fill one another's gaps; 8-bit operands, whose matrix instructions run twice as long, do with half the
             // reads of four waves of 128 x 128 (us, four / eight: 8192^3 bf16 908 / 855, 8192 x 8192 x 16384 e4m3 831 / 858)
             if (tile == 256) {
-                if constexpr (d.value == CAPGNN_E4M3) hipLaunchKernelGGL((linear_direct_kernel<d.value, o.value, 2, 2, 4, 4, 16>), grid, dim3(256), 0, st, g);
-                else hipLaunchKernelGGL((linear_direct_kernel<d.value, o.value, 2, 4, 4, 2, 16>), grid, dim3(512), 0, st, g);
+                if constexpr (d.value == CAPGNN_E4M3) hipLaunchKernelGGL((linear_direct_kernel<d.value, o.value, 2, 2, 4, 4, 16, 2>), grid, dim3(256), 0, st, g);
+                else hipLaunchKernelGGL((linear_direct_kernel<d.value, o.value, 2, 4, 4, 2, 16, 2>), grid, dim3(512), 0, st, g);
             } else if (unit == 16) {
-                if (tile == 128) hipLaunchKernelGGL((linear_direct_kernel<d.value, o.value, 2, 2, 2, 2, 16>), grid, dim3(256), 0, st, g);
-                else hipLaunchKernelGGL((linear_direct_kernel<d.value, o.value, 2, 2, 1, 1, 16>), grid, dim3(256), 0, st, g);
+                if (tile == 128) hipLaunchKernelGGL((linear_direct_kernel<d.value, o.value, 2, 2, 2, 2, 16, 4>), grid, dim3(256), 0, st, g);
+                else hipLaunchKernelGGL((linear_direct_kernel<d.value, o.value, 2, 2, 1, 1, 16, 3>), grid, dim3(256), 0, st, g);
             } else if (unit == 4) {
-                if (tile == 128) hipLaunchKernelGGL((linear_direct_kernel<d.value, o.value, 2, 2, 2, 2, 4>), grid, dim3(256), 0, st, g);
-                else hipLaunchKernelGGL((linear_direct_kernel<d.value, o.value, 2, 2, 1, 1, 4>), grid, dim3(256), 0, st, g);
+                if (tile == 128) hipLaunchKernelGGL((linear_direct_kernel<d.value, o.value, 2, 2, 2, 2, 4, 3>), grid, dim3(256), 0, st, g);
+                else hipLaunchKernelGGL((linear_direct_kernel<d.value, o.value, 2, 2, 1, 1, 4, 3>), grid, dim3(256), 0, st, g);
             } else {
                 hipLaunchKernelGGL((linear_tile_kernel<d.value, o.value, 2, 2, 1, 1>), grid, dim3(256), 0, st, g);
             }
