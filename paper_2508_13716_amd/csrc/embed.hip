@@ -532,6 +532,98 @@ template <int V> __global__ __launch_bounds__(JOIN_THREADS) void run_join_kernel
     }
 }
 
+// ------------------------------------------------------------------ tables of a few rows
+// A table that fits LDS many times over needs no sorting: a team of lanes has a copy of its own there and adds the rows of dY to it, one
+// after the other, each lane its columns; a workgroup's copies are added at its end, and the workgroups' sums by a second launch, in
+// their order.  (612000 rows of 100 floats into 47: 102 us by sorting, of which the sums alone take 57.)  What nothing was added to is -0,
+// which changes no sum.
+struct TableArgs {
+    int64_t n;
+    int V, F, lanes, chunk;     // a workgroup takes `chunk` vectors of a row (at most 64)
+    const int64_t *ids;
+    const char *dY;
+    int64_t lddy;               // in bytes
+    int64_t rows;               // of a workgroup
+    float *part;                // [workgroups][V][F]
+};
+
+constexpr int TABLE_AHEAD = 16;         // rows of a team on their way
+
+template <bool BF16, int V> __global__ __launch_bounds__(256, 1) void table_sums_kernel(TableArgs a) {
+    extern __shared__ float tables[];
+    const int lane = threadIdx.x & (a.lanes - 1), teams = blockDim.x / a.lanes, team = threadIdx.x / a.lanes;
+    const int vec = blockIdx.y * a.chunk + lane, j = vec * V;
+    const bool live = lane < a.chunk && j < a.F;
+    const int from = min(j, a.F - V), size = a.V * a.chunk * V;         // of a copy
+    for (int i = threadIdx.x; i < teams * size; i += blockDim.x) tables[i] = -0.f;
+    __syncthreads();
+    float *mine = tables + team * size + lane * V;
+    const int64_t first = blockIdx.x * a.rows, end = min(first + a.rows, a.n);
+    if (live && first + team < end) {
+        int64_t id[2][TABLE_AHEAD];
+        RawRow<BF16, V> row[2][TABLE_AHEAD];
+        const int64_t step = int64_t(teams) * TABLE_AHEAD;
+        auto fetch = [&](int set, int64_t i) __attribute__((always_inline)) {
+#pragma unroll
+            for (int u = 0; u < TABLE_AHEAD; ++u) {
+                const int64_t r = min(i + int64_t(u) * teams, end - 1);
+                id[set][u] = a.ids[r];
+                row[set][u].load(a.dY + r * a.lddy, from);
+            }
+        };
+        auto add = [&](int set, int64_t i) __attribute__((always_inline)) {
+#pragma unroll
+            for (int u = 0; u < TABLE_AHEAD; ++u) {
+                if (i + int64_t(u) * teams < end && id[set][u] >= 0 && id[set][u] < a.V) {
+                    float *t = mine + static_cast<int>(id[set][u]) * a.chunk * V;
+                    float v[V];
+#pragma unroll
+                    for (int e = 0; e < V; ++e) v[e] = t[e];
+#pragma unroll
+                    for (int e = 0; e < V; ++e) t[e] = v[e] + row[set][u].get(e);
+                }
+            }
+        };
+        int64_t i = first + team;
+        fetch(0, i);
+        for (; i < end; i += 2 * step) {
+            if (i + step < end) fetch(1, i + step);
+            add(0, i);
+            if (i + 2 * step < end) fetch(0, i + 2 * step);
+            if (i + step < end) add(1, i + step);
+        }
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < size; i += blockDim.x) {
+        float sum = tables[i];
+        for (int q = 1; q < teams; ++q) sum += tables[q * size + i];
+        // entry i: element e of vector k of row r; a row's last vector has its elements from the row's end backwards
+        const int r = i / (a.chunk * V), k = i / V % a.chunk, e = i % V, at = (blockIdx.y * a.chunk + k) * V;
+        if (at < a.F && e >= at - min(at, a.F - V)) a.part[(int64_t(blockIdx.x) * a.V + r) * a.F + min(at, a.F - V) + e] = sum;
+    }
+}
+
+// dtable (+)= scale * the workgroups' sums: 16 columns a workgroup, 16 threads each with every 16th part, then their sums in order
+__global__ __launch_bounds__(256) void table_join_kernel(const float *part, int parts, int64_t size, int F, float scale, float *dtable, int64_t lddt,
+                                                         int accumulate) {
+    __shared__ float s[16][17];
+    const int c = threadIdx.x & 15, q = threadIdx.x / 16;
+    const int64_t j = int64_t(blockIdx.x) * 16 + c;
+    float v = -0.f;
+    if (j < size) {
+#pragma unroll 8
+        for (int p = q; p < parts; p += 16) v += part[p * size + j];
+    }
+    s[q][c] = v;
+    __syncthreads();
+    if (q == 0 && j < size) {
+        for (int i = 1; i < 16; ++i) v += s[i][c];
+        float *out = dtable + j / F * lddt + j % F;
+        if (!accumulate) *out = v * scale + 0.f;
+        else if (__float_as_uint(v) != 0x80000000u) *out += v * scale;
+    }
+}
+
 __global__ __launch_bounds__(256) void fill_kernel(Fill f) { fill_share(f, blockIdx.x, gridDim.x); }
 
 // ------------------------------------------------------------------ host side
@@ -550,6 +642,29 @@ static int run_tile(int64_t n, const EmbedShape &s) {
     const int64_t teams = std::max<int64_t>(int64_t(NUM_CU) * 16 * (64 / s.lanes) / s.chunks, 1);
     const int64_t R = std::min<int64_t>(std::max<int64_t>((n + teams - 1) / teams, 8), 128);
     return static_cast<int>(std::max<int64_t>(R, (n >> 22) + 1));
+}
+
+// A table in LDS: workgroups, threads and LDS of each; 0 workgroups where the table is too large for it
+struct TableShape {
+    int groups, threads, chunk;
+    int64_t rows;
+    size_t lds;
+};
+static TableShape table_shape(int64_t n, int64_t V, const EmbedShape &s, int F) {
+    TableShape t{};
+    const int vectors = (F + s.V - 1) / s.V;
+    t.chunk = std::min(vectors, s.lanes);
+    // copies for 128 lanes at least, so that a compute unit has enough rows on their way (V <= 71 of fp32, 35 of bf16 rows of whole vectors)
+    for (t.threads = 256; t.threads >= 128; t.threads /= 2) {
+        t.lds = size_t(V) * t.chunk * s.V * sizeof(float) * (t.threads / s.lanes);
+        if (t.lds <= 156 * 1024) break;
+    }
+    if (t.threads < 128 || V > 4096) return {};
+    const int64_t teams = t.threads / s.lanes, room = std::min<int64_t>(160 * 1024 / std::max<size_t>(t.lds, 1), 8);
+    const int64_t most = std::max<int64_t>(NUM_CU * room / s.chunks, 64);
+    t.rows = std::max<int64_t>((n + most - 1) / most, teams * TABLE_AHEAD);
+    t.groups = static_cast<int>((n + t.rows - 1) / t.rows);
+    return t;
 }
 
 struct EmbedWork {              // offsets into the workspace
@@ -584,6 +699,10 @@ static EmbedWork embed_work(int64_t n, int64_t V, int F) {
     }
     w.part = take(part);
     w.bytes = at;
+    for (bool bf16 : {false, true}) {
+        const EmbedShape s = embed_shape(F, bf16);
+        w.bytes = std::max(w.bytes, align_up(sizeof(float) * table_shape(n, V, s, F).groups * V * F, 256));
+    }
     return w;
 }
 
@@ -642,6 +761,25 @@ extern "C" int capgnn_embed_bwd(int64_t n, const int64_t *ids, int64_t V, int F,
     const EmbedWork w = embed_work(n, V, F);
     if (!ws || ws_bytes < w.bytes) CG_FAIL(CAPGNN_ENOMEM, "embed_bwd: workspace of %zu bytes needed, %zu given", w.bytes, ws ? ws_bytes : size_t(0));
     if (reinterpret_cast<uintptr_t>(ws) & 255u) CG_FAIL(CAPGNN_EINVAL, "embed_bwd: workspace must be 256-byte aligned");
+    const bool bf16 = dy_dtype == CAPGNN_BF16;
+    const EmbedShape e = embed_shape(F, bf16);
+    if (const TableShape t = table_shape(n, V, e, F); t.groups) {
+        const TableArgs a{n, static_cast<int>(V), F, e.lanes, t.chunk, ids, static_cast<const char *>(dY), lddy * elem_bytes(dy_dtype), t.rows,
+                          static_cast<float *>(ws)};
+        const dim3 grid(t.groups, e.chunks);
+        auto go = [&](auto kernel) {
+            if (t.lds > 64 * 1024) CG_HIP(hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(t.lds)));
+            hipLaunchKernelGGL(kernel, grid, dim3(t.threads), t.lds, st, a);
+            CG_HIP(hipGetLastError());
+            return static_cast<int>(CAPGNN_OK);
+        };
+        if (bf16) CG_TRY(e.V == 1 ? go(table_sums_kernel<true, 1>) : go(table_sums_kernel<true, 8>));
+        else CG_TRY(e.V == 1 ? go(table_sums_kernel<false, 1>) : go(table_sums_kernel<false, 4>));
+        const int64_t size = V * int64_t(F);
+        hipLaunchKernelGGL(table_join_kernel, dim3(static_cast<unsigned>((size + 15) / 16)), dim3(256), 0, st, a.part, t.groups, size, F, scale, dtable, lddt, accumulate != 0);
+        CG_HIP(hipGetLastError());
+        return CAPGNN_OK;
+    }
     char *base = static_cast<char *>(ws);
     auto at = [&](size_t off) { return reinterpret_cast<uint32_t *>(base + off); };
     const bool small = n <= SMALL_TILE;
@@ -683,8 +821,6 @@ extern "C" int capgnn_embed_bwd(int64_t n, const int64_t *ids, int64_t V, int F,
         }
     }
     CG_HIP(hipGetLastError());
-    const bool bf16 = dy_dtype == CAPGNN_BF16;
-    const EmbedShape e = embed_shape(F, bf16);
     const int R = run_tile(n, e);
     const RunArgs a{n, s.V, F, e.lanes, R, (n + R - 1) / R, at(w.key[now]), at(w.pos[now]), static_cast<const char *>(dY),
                     lddy * elem_bytes(dy_dtype), scale, dtable, lddt, accumulate != 0, reinterpret_cast<float *>(base + w.part),

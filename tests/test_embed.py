@@ -142,8 +142,34 @@ def test_gradient(n, V, F, kind, t, accumulate, pad):
 @pytest.mark.gpu
 @pytest.mark.parametrize("n,F,t", [(70_000, 4, "f32"), (33_000, 64, "bf16"), (9000, 300, "f32"), (257, 8, "bf16")])
 @pytest.mark.parametrize("accumulate", [False, True])
-def test_every_row_names_the_same_one(n, F, t, accumulate):
-    check_gradient(n, 5, F, t, 1, "one", accumulate)
+@pytest.mark.parametrize("V", [5, 5000])
+def test_every_row_names_the_same_one(n, F, t, accumulate, V):
+    check_gradient(n, V, F, t, 1, "one", accumulate)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("n", [100, 20_000])
+@pytest.mark.parametrize("V", [1, 2, 31, 36, 40, 41, 71, 72, 73, 120, 305])
+@pytest.mark.parametrize("F,t", [(1, "f32"), (3, "f32"), (9, "bf16"), (64, "f32"), (256, "bf16"), (258, "f32"), (520, "bf16")])
+def test_tables_of_a_few_rows(n, V, F, t):
+    check_gradient(n, V, F, t, 2, "outside", V % 2 == 0)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("V", [7, 900])
+@pytest.mark.parametrize("n", [60, 9000])
+def test_rows_that_no_id_names_keep_their_bits(V, n):
+    """what is added to: signs of zero and NaN among it"""
+    import torch
+    bits = torch.tensor([0x80000000, 0, 0x7FC12345, 0x3F800000, 0xFF800000], dtype=torch.int64).to(torch.int32).repeat(V * 4)[: V * 4]
+    dtable = bits.cuda().view(torch.float32)
+    ids = dev(np.full(n, 2))
+    dY = Mat(np.full((n, 4), 0.25), "f32")
+    ws, size = ws_of(B.embed_bwd_workspace_bytes(n, V, 4))
+    B.embed_bwd(n, ids, V, 4, dY.p, 4, B.F32, -1.0, dtable, 4, 1, ws, size)
+    torch.cuda.synchronize()
+    now = dtable.view(torch.int32).cpu()
+    assert torch.equal(now[:8], bits[:8]) and torch.equal(now[12:], bits[12:])
 
 
 @pytest.mark.gpu
@@ -171,17 +197,19 @@ def test_no_ids_zero_the_table():
 
 
 @pytest.mark.gpu
-def test_a_row_that_is_nan_stays_with_its_id():
+@pytest.mark.parametrize("V", [50, 500])
+def test_a_row_that_is_nan_stays_with_its_id(V):
     import torch
     x = np.ones((9000, 6))
     x[4000] = np.nan
     x[100, 2] = np.inf
     ids = np.arange(9000) % 50
-    dtable = new(50, 6, "f32")
-    ws, size = ws_of(B.embed_bwd_workspace_bytes(9000, 50, 6))
-    B.embed_bwd(9000, dev(ids), 50, 6, Mat(x, "bf16").p, 6, B.BF16, 1.0, dtable.p, 6, 0, ws, size)
+    dtable = new(V, 6, "f32")
+    ws, size = ws_of(B.embed_bwd_workspace_bytes(9000, V, 6))
+    B.embed_bwd(9000, dev(ids), V, 6, Mat(x, "bf16").p, 6, B.BF16, 1.0, dtable.p, 6, 0, ws, size)
     torch.cuda.synchronize()
-    got = dtable.get()
+    assert (dtable.get()[50:] == 0).all()
+    got = dtable.get()[:50]
     want = np.full((50, 6), 180.0)
     want[0] = np.nan
     assert np.isnan(got[0]).all() and (got[1:] == 180.0).all()
