@@ -143,7 +143,10 @@ constexpr int UNITS = 8;                // units of a tile's row
 // beside a bf16 result's rounding, but a hundred times a float's.  So for float results the operands are widened to bf16, exactly, and
 // take the bf16 instruction, at half the rate.
 constexpr int E4M3_FINE = 3;
-template <int DT> constexpr int BYTES = DT == CAPGNN_F32 ? 4 : DT == CAPGNN_BF16 ? 2 : 1;
+// fp32 operands cut into three bf16 numbers each, exactly; the six largest of the nine products go to the bf16 instruction, smallest first, and what
+// is dropped is 2^-23 of a product at most.  Six instructions stand for eight fp32 ones of twice the time.
+constexpr int F32_CUT = 4;
+template <int DT> constexpr int BYTES = DT == CAPGNN_F32 || DT == F32_CUT ? 4 : DT == CAPGNN_BF16 ? 2 : 1;
 
 __device__ __forceinline__ int unit_at(int row, int unit) { return row * UNITS + (unit ^ (row >> 1 & 7)); }
 
@@ -163,18 +166,18 @@ template <int DT> __device__ __forceinline__ raw16 load_unit(const char *row, in
 #pragma unroll
     for (int e = 0; e < E; ++e)
         if (k + e < end) {
-            if constexpr (DT == CAPGNN_F32) r[e] = reinterpret_cast<const uint32_t *>(row)[k + e];
-            else if constexpr (DT == CAPGNN_BF16) r[e / 2] |= uint32_t(reinterpret_cast<const uint16_t *>(row)[k + e]) << (e % 2 * 16);
+            if constexpr (BYTES<DT> == 4) r[e] = reinterpret_cast<const uint32_t *>(row)[k + e];
+            else if constexpr (BYTES<DT> == 2) r[e / 2] |= uint32_t(reinterpret_cast<const uint16_t *>(row)[k + e]) << (e % 2 * 16);
             else r[e / 4] |= uint32_t(reinterpret_cast<const uint8_t *>(row)[k + e]) << (e % 4 * 8);
         }
     return r;
 }
 
 // a step's products are formed a slice of k at a time, one instruction's (of fp32: four) for each pair of tiles
-template <int DT> constexpr int SLICES = DT == CAPGNN_E4M3 ? 2 : 4;
+template <int DT> constexpr int SLICES = DT == CAPGNN_E4M3 || DT == F32_CUT ? 2 : 4;
 
 template <int DT, int T> struct Slice {                                 // a lane's operands of T tiles' rows
-    static constexpr int U = DT == CAPGNN_E4M3 ? 2 : 1;
+    static constexpr int U = 4 / SLICES<DT>;
     raw16 u[T][U];
     __device__ __forceinline__ void read(const raw16 *tile, int row, int half, int s) {
 #pragma unroll
@@ -186,8 +189,49 @@ template <int DT, int T> struct Slice {                                 // a lan
 __device__ __forceinline__ int8v join_units(raw16 lo, raw16 hi) {
     return int8v{int(lo[0]), int(lo[1]), int(lo[2]), int(lo[3]), int(hi[0]), int(hi[1]), int(hi[2]), int(hi[3])};
 }
+// eight floats as three times eight bf16
+struct Cut {
+    half8 p[3];
+    __device__ __forceinline__ void operator()(raw16 lo, raw16 hi) {
+        uint32_t w[3][4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            float x = __uint_as_float(k < 2 ? lo[2 * k] : hi[2 * k - 4]), y = __uint_as_float(k < 2 ? lo[2 * k + 1] : hi[2 * k - 3]);
+#pragma unroll
+            for (int q = 0; q < 3; ++q) {
+                w[q][k] = bf16_two(x, y);
+                x -= __uint_as_float(w[q][k] << 16);
+                y -= __uint_as_float(w[q][k] & 0xffff0000u);
+            }
+        }
+#pragma unroll
+        for (int q = 0; q < 3; ++q) p[q] = __builtin_bit_cast(half8, raw16{w[q][0], w[q][1], w[q][2], w[q][3]});
+    }
+};
+template <int TM, int TN>
+__device__ __forceinline__ void multiply_cut(const Slice<F32_CUT, TM> &a, const Slice<F32_CUT, TN> &b, acc16 (&acc)[TM][TN]) {
+    Cut cb[TN];
+#pragma unroll
+    for (int j = 0; j < TN; ++j) cb[j](b.u[j][0], b.u[j][1]);
+#pragma unroll
+    for (int i = 0; i < TM; ++i) {
+        Cut ca;
+        ca(a.u[i][0], a.u[i][1]);
+#pragma unroll
+        for (int s = 3; s-- > 0;)       // pieces p of A and s - p of W, 2^-8s of the product each
+#pragma unroll
+            for (int p = 0; p < 3; ++p)
+                if (p <= s) {
+#pragma unroll
+                    for (int j = 0; j < TN; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ca.p[p], cb[j].p[s - p], acc[i][j], 0, 0, 0);
+                }
+    }
+}
+
 template <int DT, int TM, int TN>
 __device__ __forceinline__ void multiply_slice(const Slice<DT, TM> &a, const Slice<DT, TN> &b, acc16 (&acc)[TM][TN]) {
+    if constexpr (DT == F32_CUT) return multiply_cut<TM, TN>(a, b, acc);
+    else
 #pragma unroll
     for (int i = 0; i < TM; ++i)
 #pragma unroll
@@ -201,7 +245,7 @@ __device__ __forceinline__ void multiply_slice(const Slice<DT, TM> &a, const Sli
 #pragma unroll
                 for (int e = 0; e < 2; ++e)
                     acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(widen8(a.u[i][0], e), widen8(b.u[j][0], e), acc[i][j], 0, 0, 0);
-            } else {
+            } else if constexpr (DT == CAPGNN_F32) {
 #pragma unroll
                 for (int e = 0; e < 4; ++e)
                     acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(a.u[i][0][e]), __uint_as_float(b.u[j][0][e]), acc[i][j], 0, 0, 0);
@@ -450,7 +494,7 @@ template <int DT, bool OB, int WR, int WC, int TM, int TN, int LB, int NB> __glo
                                                         : load_unit<DT>(W + int64_t(min(r - BM, rows_b - 1)) * g.ldw, k, x.K);
     };
     acc16 acc[TM][TN] = {};
-    constexpr int MFMAS = TM * TN * (DT == CAPGNN_F32 ? 4 : DT == E4M3_FINE ? 2 : 1), READS = (TM + TN) * Slice<DT, TM>::U;
+    constexpr int MFMAS = TM * TN * (DT == CAPGNN_F32 ? 4 : DT == F32_CUT ? 6 : DT == E4M3_FINE ? 2 : 1), READS = (TM + TN) * Slice<DT, TM>::U;
     Slice<DT, TM> a[2];
     Slice<DT, TN> b[2];
     auto read = [&](int k, int t, int s) {
@@ -666,11 +710,12 @@ using namespace capgnn;
 static bool bad_act(int act) { return act < CAPGNN_ACT_NONE || act > CAPGNN_ACT_SILU; }
 
 // f(operands, results in bf16) as compile-time numbers
-template <class F> static void with_types(int dtype, int out_dtype, F f) {
+template <class F> static void with_types(int dtype, int out_dtype, bool cut, F f) {
     using Y = std::true_type;
     using N = std::false_type;
     const bool o = out_dtype == CAPGNN_BF16;
-    if (dtype == CAPGNN_F32) o ? f(std::integral_constant<int, CAPGNN_F32>(), Y()) : f(std::integral_constant<int, CAPGNN_F32>(), N());
+    if (cut) o ? f(std::integral_constant<int, F32_CUT>(), Y()) : f(std::integral_constant<int, F32_CUT>(), N());
+    else if (dtype == CAPGNN_F32) o ? f(std::integral_constant<int, CAPGNN_F32>(), Y()) : f(std::integral_constant<int, CAPGNN_F32>(), N());
     else if (dtype == CAPGNN_BF16) o ? f(std::integral_constant<int, CAPGNN_BF16>(), Y()) : f(std::integral_constant<int, CAPGNN_BF16>(), N());
     else o ? f(std::integral_constant<int, CAPGNN_E4M3>(), Y()) : f(std::integral_constant<int, E4M3_FINE>(), N());
 }
@@ -683,6 +728,8 @@ struct LinearPlan {
 };
 constexpr int FEW_ROWS = 32;
 
+static bool cut_pays(int64_t M, int64_t N, int64_t K) { return M * N >= ((int64_t(1) << 28) + K - 1) / std::max<int64_t>(K, 1); }
+
 static LinearPlan linear_plan(int64_t M, int64_t N, int64_t K, int es) {
     LinearPlan p{0, 1, K};
     auto tiles = [&](int64_t b) { return ((M + b - 1) / b) * ((N + b - 1) / b); };
@@ -692,7 +739,7 @@ static LinearPlan linear_plan(int64_t M, int64_t N, int64_t K, int es) {
         groups = (N + 15) / 16;
         most = lines / 32;
     } else {
-        p.tile = tiles(256) >= 200 ? 256 : tiles(128) >= 256 ? 128 : 64;
+        p.tile = tiles(256) >= 200 ? 256 : tiles(128) >= (es == 4 && cut_pays(M, N, K) ? 96 : 256) ? 128 : 64;
         groups = tiles(p.tile);
         most = p.tile == 64 ? lines / 8 : 1;
     }
@@ -754,24 +801,32 @@ extern "C" int capgnn_linear(int64_t M, int64_t N, int64_t K, const void *A, int
     } else {
         const uintptr_t at = reinterpret_cast<uintptr_t>(A) | reinterpret_cast<uintptr_t>(W) | uintptr_t(g.lda) | uintptr_t(g.ldw);
         const int unit = K == 0 || at % 4 || g.lda >= most / 256 || g.ldw >= most / 256 ? 1 : at % 16 ? 4 : 16;      // bytes of a load to LDS
-        const int tile = unit == 1 ? 64 : unit == 4 ? std::min(p.tile, 128) : p.tile;
+        const int tile = unit == 1 || (dtype == CAPGNN_F32 && !cut_pays(M, N, K)) ? 64 : unit == 4 ? std::min(p.tile, 128) : p.tile;
         const int64_t tiles = (M + tile - 1) / tile * ((N + tile - 1) / tile);
         if (tiles > int64_t(1) << 22) CG_FAIL(CAPGNN_EUNSUPPORTED, "linear: more than 2^22 tiles of results");
         const dim3 grid(static_cast<unsigned>(tiles), p.parts);
-        with_types(dtype, out_dtype, [&](auto d, auto o) {
-            // eight waves of 128 x 64 fill one another's gaps; 8-bit operands, whose matrix instructions run twice as long, do with half the
-            // reads of four waves of 128 x 128 (us, four / eight: 8192^3 bf16 908 / 855, 8192 x 8192 x 16384 e4m3 831 / 858)
+        const bool cut = dtype == CAPGNN_F32 && tile > 64 && cut_pays(M, N, K);
+        with_types(dtype, out_dtype, cut, [&](auto d, auto o) {
+            auto direct = [&](auto wr, auto wc, auto tm, auto tn, auto lb, auto nb) {
+                hipLaunchKernelGGL((linear_direct_kernel<d.value, o.value, wr.value, wc.value, tm.value, tn.value, lb.value, nb.value>), grid,
+                                   dim3(wr.value * wc.value * 64), 0, st, g);
+            };
+            constexpr std::integral_constant<int, 1> I1;
+            constexpr std::integral_constant<int, 2> I2;
+            constexpr std::integral_constant<int, 3> I3;
+            constexpr std::integral_constant<int, 4> I4;
+            constexpr std::integral_constant<int, 16> I16;
+            // Eight waves of 128 x 64 fill one another's gaps; 8-bit operands, whose matrix instructions run twice as long, and fp32 ones, which
+            // are cut on their way, do with half the reads of four waves of 128 x 128 (us, four / eight: 8192^3 bf16 908 / 855,
+            // 8192 x 8192 x 16384 e4m3 831 / 858)
             if (tile == 256) {
-                if constexpr (d.value == CAPGNN_E4M3) hipLaunchKernelGGL((linear_direct_kernel<d.value, o.value, 2, 2, 4, 4, 16, 2>), grid, dim3(256), 0, st, g);
-                else hipLaunchKernelGGL((linear_direct_kernel<d.value, o.value, 2, 4, 4, 2, 16, 2>), grid, dim3(512), 0, st, g);
-            } else if (unit == 16) {
-                if (tile == 128) hipLaunchKernelGGL((linear_direct_kernel<d.value, o.value, 2, 2, 2, 2, 16, 4>), grid, dim3(256), 0, st, g);
-                else hipLaunchKernelGGL((linear_direct_kernel<d.value, o.value, 2, 2, 1, 1, 16, 3>), grid, dim3(256), 0, st, g);
-            } else if (unit == 4) {
-                if (tile == 128) hipLaunchKernelGGL((linear_direct_kernel<d.value, o.value, 2, 2, 2, 2, 4, 3>), grid, dim3(256), 0, st, g);
-                else hipLaunchKernelGGL((linear_direct_kernel<d.value, o.value, 2, 2, 1, 1, 4, 3>), grid, dim3(256), 0, st, g);
-            } else {
-                hipLaunchKernelGGL((linear_tile_kernel<d.value, o.value, 2, 2, 1, 1>), grid, dim3(256), 0, st, g);
+                if constexpr (d.value == CAPGNN_E4M3 || d.value == F32_CUT) direct(I2, I2, I4, I4, I16, I2);
+                else if constexpr (d.value != CAPGNN_F32) direct(I2, I4, I4, I2, I16, I2);
+            } else if (tile == 128) {
+                if constexpr (d.value != CAPGNN_F32) unit == 16 ? direct(I2, I2, I2, I2, I16, I4) : direct(I2, I2, I2, I2, I4, I3);
+            } else if constexpr (d.value != F32_CUT) {
+                if (unit == 1) hipLaunchKernelGGL((linear_tile_kernel<d.value, o.value, 2, 2, 1, 1>), grid, dim3(256), 0, st, g);
+                else unit == 16 ? direct(I2, I2, I1, I1, I16, I3) : direct(I2, I2, I1, I1, I4, I3);
             }
         });
     }

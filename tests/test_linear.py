@@ -159,7 +159,8 @@ def test_variants(M, N, K, t):
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("M,N,K,t", [(1000, 1100, 700, "bf16"), (513, 2049, 384, "e4m3"), (700, 600, 513, "f32"), (2100, 515, 2048, "bf16"), (1030, 1030, 1024, "e4m3"),
-                                     (1500, 47, 256, "f32"), (2600, 2600, 128, "bf16"), (2570, 2590, 256, "f32")])
+                                     (1500, 47, 256, "f32"), (2600, 2600, 128, "bf16"), (2570, 2590, 256, "f32"), (4000, 3700, 50, "f32"), (3600, 3700, 97, "bf16"),
+                                     (3650, 3600, 200, "e4m3"), (1500, 1100, 602, "f32"), (1290, 1300, 161, "f32")])
 def test_large_tiles(M, N, K, t):
     check(M, N, K, t, "f32", "none")
     check(M, N, K, t, "bf16", "gelu", residual=True, save=True, pad=8)
