@@ -581,58 +581,54 @@ template <int DT> __device__ __forceinline__ acc4 multiply16(raw16 w, raw16 a, a
     }
 }
 
-constexpr int FEW_WAVES = 16;           // of a workgroup, at most
+constexpr int FEW_WAVES = 16, FEW_AHEAD = 8;        // waves of a workgroup, at most; units of a row on their way at a time, per lane
 
-// TM: groups of 16 rows of A
-template <int DT, int TM> __global__ __launch_bounds__(FEW_WAVES * 64) void linear_few_kernel(LinearArgs g) {
-    constexpr int E = 16 / BYTES<DT>, AHEAD = 8 / TM;           // units of a row on their way at a time, per lane
-    __shared__ acc4 sums[FEW_WAVES][TM][64];
+template <int DT> __global__ __launch_bounds__(FEW_WAVES * 64) void linear_few_kernel(LinearArgs g) {
+    constexpr int E = 16 / BYTES<DT>;
+    __shared__ acc4 sums[FEW_WAVES][64];
     const int wave = threadIdx.x / 64, waves = blockDim.x / 64, lane = threadIdx.x & 63;
     const int64_t n0 = int64_t(blockIdx.x) * 16;
     const Stretch x = stretch_of<BYTES<DT>>(g);
-    const char *w = x.W + min(n0 + lane % 16, g.N - 1) * g.ldw, *a[TM];
-#pragma unroll
-    for (int i = 0; i < TM; ++i) a[i] = x.A + min(int64_t(i * 16 + lane % 16), g.M - 1) * g.lda;
-    acc4 acc[TM] = {};
+    const char *w = x.W + min(n0 + lane % 16, g.N - 1) * g.ldw, *a = x.A + min(int64_t(lane % 16), g.M - 1) * g.lda;
+    acc4 acc = {};
     // a wave's unit q: 16 bytes at k, of line q / 2 of its own
     auto at = [&](int64_t q) { return ((q / 2 * waves + wave) * 8 + q % 2 * 4 + lane / 16) * E; };
     const int64_t lines = (x.K + 8 * E - 1) / (8 * E), mine = lines > wave ? ((lines - wave - 1) / waves + 1) * 2 : 0;
     const int64_t sure = x.K / (8 * E), whole = sure > wave ? ((sure - wave - 1) / waves + 1) * 2 : 0;      // of lines that end inside the row
     int64_t q = 0;
-    for (; q + AHEAD <= whole; q += AHEAD) {
-        raw16 rw[AHEAD], ra[AHEAD][TM];
+    for (; q + FEW_AHEAD <= whole; q += FEW_AHEAD) {
+        raw16 rw[FEW_AHEAD], ra[FEW_AHEAD];
 #pragma unroll
-        for (int u = 0; u < AHEAD; ++u) {
+        for (int u = 0; u < FEW_AHEAD; ++u) {
             typedef raw16 raw16_by1 __attribute__((aligned(1)));
             const int64_t k = at(q + u) * BYTES<DT>;
             rw[u] = *reinterpret_cast<const raw16_by1 *>(w + k);
-#pragma unroll
-            for (int i = 0; i < TM; ++i) ra[u][i] = *reinterpret_cast<const raw16_by1 *>(a[i] + k);
+            ra[u] = *reinterpret_cast<const raw16_by1 *>(a + k);
         }
 #pragma unroll
-        for (int u = 0; u < AHEAD; ++u)
-#pragma unroll
-            for (int i = 0; i < TM; ++i) acc[i] = multiply16<DT>(rw[u], ra[u][i], acc[i]);
+        for (int u = 0; u < FEW_AHEAD; ++u) acc = multiply16<DT>(rw[u], ra[u], acc);
     }
-    for (; q < mine; ++q) {
-        const int64_t k = at(q);
-        const raw16 rw = load_unit<DT>(w, k, x.K);
+    for (; q < mine; q += 2) {              // a line at a time, its end checked
+        raw16 rw[2], ra[2];
 #pragma unroll
-        for (int i = 0; i < TM; ++i) acc[i] = multiply16<DT>(rw, load_unit<DT>(a[i], k, x.K), acc[i]);
+        for (int u = 0; u < 2; ++u) {
+            rw[u] = load_unit<DT>(w, at(q + u), x.K);
+            ra[u] = load_unit<DT>(a, at(q + u), x.K);
+        }
+#pragma unroll
+        for (int u = 0; u < 2; ++u) acc = multiply16<DT>(rw[u], ra[u], acc);
     }
-#pragma unroll
-    for (int i = 0; i < TM; ++i) sums[wave][i][lane] = acc[i];
+    sums[wave][lane] = acc;
     __syncthreads();
-    for (int i = wave; i < TM; i += waves) {
-        acc4 s = sums[0][i][lane];
-        for (int v = 1; v < waves; ++v) s += sums[v][i][lane];
-        const int64_t row = i * 16 + lane % 16, col = n0 + lane / 16 * 4;
-        const int count = static_cast<int>(min(g.N - col, int64_t(4)));
-        if (row < g.M && count > 0) {
-            float v[4] = {s[0], s[1], s[2], s[3]};
-            if (g.part) st_row<false, 4>(reinterpret_cast<char *>(g.part + (blockIdx.y * g.M + row) * g.part_ld + col), 0, v);
-            else finish<4>(g, row, col, count, v);
-        }
+    if (wave) return;
+    acc4 s = sums[0][lane];
+    for (int v = 1; v < waves; ++v) s += sums[v][lane];
+    const int64_t row = lane % 16, col = n0 + lane / 16 * 4;
+    const int count = static_cast<int>(min(g.N - col, int64_t(4)));
+    if (row < g.M && count > 0) {
+        float v[4] = {s[0], s[1], s[2], s[3]};
+        if (g.part) st_row<false, 4>(reinterpret_cast<char *>(g.part + (blockIdx.y * g.M + row) * g.part_ld + col), 0, v);
+        else finish<4>(g, row, col, count, v);
     }
 }
 
@@ -698,7 +694,7 @@ int launch_column_join(const float *part, int parts, int64_t F, float *sums, hip
 
 static int act_parts(int64_t M, int64_t N, int64_t *rows) {
     const int64_t across = (N + 255) / 256;         // workgroups side by side, at least
-    const int64_t parts = std::max<int64_t>(1, std::min<int64_t>((M + 15) / 16, 2048 / std::min<int64_t>(across, 2048)));
+    const int64_t parts = M <= 32 ? 1 : std::max<int64_t>(1, std::min<int64_t>((M + 15) / 16, 2048 / std::min<int64_t>(across, 2048)));
     *rows = (M + parts - 1) / parts;
     return static_cast<int>((M + *rows - 1) / *rows);
 }
@@ -726,7 +722,7 @@ struct LinearPlan {
     int parts;                  // of the reduction
     int64_t part_k;
 };
-constexpr int FEW_ROWS = 32;
+constexpr int FEW_ROWS = 16;            // (32 by two such groups: 32 x 4096 x 4096 bf16 15.3 us, 33 rows by tiles of 64 in parts 13.5)
 
 static bool cut_pays(int64_t M, int64_t N, int64_t K) { return M * N >= ((int64_t(1) << 28) + K - 1) / std::max<int64_t>(K, 1); }
 
@@ -739,10 +735,17 @@ static LinearPlan linear_plan(int64_t M, int64_t N, int64_t K, int es) {
         groups = (N + 15) / 16;
         most = lines / 32;
     } else {
-        p.tile = tiles(256) >= 200 ? 256 : tiles(128) >= (es == 4 && cut_pays(M, N, K) ? 96 : 256) ? 128 : 64;
+        // Large tiles read their operands less often, where there are enough of them for the compute units, little of them lies beyond the matrix
+        // and the reduction is long enough for what a workgroup alone on its compute unit cannot overlap: its first loads and its results.
+        // us, tiles of 256 / 128 / 64: 8192 x 8192 x 2048 bf16 298 / 329 / 463, x 1024 206 / 208 / 272, x 256 133 / 111 / 147; x 1024 fp32
+        // 647 / 717 / 1047, x 256 222 / 215 / 305; x 1024 e4m3 166 / 145 / 187, x 2048 216 / 204 / 266; 612000 x 47 x 256 bf16 274 / 157 / 107,
+        // fp32 660 / 296 / 233; 3000^3 bf16 (144 tiles of 256) 123 with them, 105 / 117 with the others.
+        auto wide = [&](int64_t b) { return tiles(b) * b * b * 4 <= tiles(b / 2) * (b / 2) * (b / 2) * 5; };
+        p.tile = tiles(256) >= 200 && wide(256) && lines >= (es == 1 ? 32 : 16) ? 256 : tiles(128) >= 256 && wide(128) ? 128 : 64;
         groups = tiles(p.tile);
         most = p.tile == 64 ? lines / 8 : 1;
     }
+    // (enough workgroups for the chip, parts of 8 steps or more; of a few rows 32)
     const int64_t parts = std::min<int64_t>(std::min<int64_t>(most, (p.tile ? 512 : 256) / groups), 32);
     if (parts > 1) {
         const int64_t each = (lines + parts - 1) / parts;
@@ -795,9 +798,9 @@ extern "C" int capgnn_linear(int64_t M, int64_t N, int64_t K, const void *A, int
         const int waves = std::min<int>(FEW_WAVES, pow2_at_least(static_cast<int>(std::min<int64_t>(lines / 4 + 1, FEW_WAVES))));
         const dim3 grid(static_cast<unsigned>((N + 15) / 16), p.parts);
         auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(waves * 64), 0, st, g); };
-        if (dtype == CAPGNN_F32) M <= 16 ? go(linear_few_kernel<CAPGNN_F32, 1>) : go(linear_few_kernel<CAPGNN_F32, 2>);
-        else if (dtype == CAPGNN_BF16) M <= 16 ? go(linear_few_kernel<CAPGNN_BF16, 1>) : go(linear_few_kernel<CAPGNN_BF16, 2>);
-        else M <= 16 ? go(linear_few_kernel<E4M3_FINE, 1>) : go(linear_few_kernel<E4M3_FINE, 2>);
+        if (dtype == CAPGNN_F32) go(linear_few_kernel<CAPGNN_F32>);
+        else if (dtype == CAPGNN_BF16) go(linear_few_kernel<CAPGNN_BF16>);
+        else go(linear_few_kernel<E4M3_FINE>);
     } else {
         const uintptr_t at = reinterpret_cast<uintptr_t>(A) | reinterpret_cast<uintptr_t>(W) | uintptr_t(g.lda) | uintptr_t(g.ldw);
         const int unit = K == 0 || at % 4 || g.lda >= most / 256 || g.ldw >= most / 256 ? 1 : at % 16 ? 4 : 16;      // bytes of a load to LDS
@@ -805,7 +808,7 @@ extern "C" int capgnn_linear(int64_t M, int64_t N, int64_t K, const void *A, int
         const int64_t tiles = (M + tile - 1) / tile * ((N + tile - 1) / tile);
         if (tiles > int64_t(1) << 22) CG_FAIL(CAPGNN_EUNSUPPORTED, "linear: more than 2^22 tiles of results");
         const dim3 grid(static_cast<unsigned>(tiles), p.parts);
-        const bool cut = dtype == CAPGNN_F32 && tile > 64 && cut_pays(M, N, K);
+        const bool cut = dtype == CAPGNN_F32 && unit > 1 && cut_pays(M, N, K);
         with_types(dtype, out_dtype, cut, [&](auto d, auto o) {
             auto direct = [&](auto wr, auto wc, auto tm, auto tn, auto lb, auto nb) {
                 hipLaunchKernelGGL((linear_direct_kernel<d.value, o.value, wr.value, wc.value, tm.value, tn.value, lb.value, nb.value>), grid,
@@ -823,10 +826,13 @@ extern "C" int capgnn_linear(int64_t M, int64_t N, int64_t K, const void *A, int
                 if constexpr (d.value == CAPGNN_E4M3 || d.value == F32_CUT) direct(I2, I2, I4, I4, I16, I2);
                 else if constexpr (d.value != CAPGNN_F32) direct(I2, I4, I4, I2, I16, I2);
             } else if (tile == 128) {
-                if constexpr (d.value != CAPGNN_F32) unit == 16 ? direct(I2, I2, I2, I2, I16, I4) : direct(I2, I2, I2, I2, I4, I3);
-            } else if constexpr (d.value != F32_CUT) {
-                if (unit == 1) hipLaunchKernelGGL((linear_tile_kernel<d.value, o.value, 2, 2, 1, 1>), grid, dim3(256), 0, st, g);
-                else unit == 16 ? direct(I2, I2, I1, I1, I16, I3) : direct(I2, I2, I1, I1, I4, I3);
+                if constexpr (d.value != CAPGNN_F32) unit == 16 ? direct(I2, I2, I2, I2, I16, I2) : direct(I2, I2, I2, I2, I4, I2);
+            } else {
+                if constexpr (d.value != F32_CUT) {
+                    if (unit == 1) hipLaunchKernelGGL((linear_tile_kernel<d.value, o.value, 2, 2, 1, 1>), grid, dim3(256), 0, st, g);
+                }
+                if (unit == 1) return;
+                unit == 16 ? direct(I2, I2, I1, I1, I16, I3) : direct(I2, I2, I1, I1, I4, I3);
             }
         });
     }
@@ -842,7 +848,8 @@ extern "C" int capgnn_linear(int64_t M, int64_t N, int64_t K, const void *A, int
 extern "C" size_t capgnn_linear_act_bwd_workspace_bytes(int64_t M, int64_t N) {
     if (M <= 0 || N <= 0) return 0;
     int64_t rows;
-    return align_up(sizeof(float) * N * act_parts(M, N, &rows), 256);
+    const int parts = act_parts(M, N, &rows);
+    return parts > 1 ? align_up(sizeof(float) * N * parts, 256) : 0;
 }
 
 extern "C" int capgnn_linear_act_bwd(int64_t M, int64_t N, const void *dY, int64_t lddy, const void *U, int64_t ldu, int dtype, int act, void *dU,
@@ -869,12 +876,12 @@ extern "C" int capgnn_linear_act_bwd(int64_t M, int64_t N, const void *dY, int64
     int64_t rows;
     const int parts = act_parts(M, N, &rows);
     const ActGradArgs a{M, N, static_cast<const char *>(dY), static_cast<const char *>(U), static_cast<char *>(dU), lddy * es, ldu * es,
-                        lddu * es, dbias ? static_cast<float *>(ws) : nullptr, rows};
+                        lddu * es, dbias && parts > 1 ? static_cast<float *>(ws) : dbias, rows};
     const dim3 grid(static_cast<unsigned>((N + 64 * V - 1) / (64 * V)), parts);
     with_act(act, [&](auto k) {
         if (bf16) hipLaunchKernelGGL((act_grad_kernel<true, k.value>), grid, dim3(256), 0, st, a);
         else hipLaunchKernelGGL((act_grad_kernel<false, k.value>), grid, dim3(256), 0, st, a);
     });
     CG_HIP(hipGetLastError());
-    return dbias ? launch_column_join(a.part, parts, N, dbias, st) : CAPGNN_OK;
+    return dbias && parts > 1 ? launch_column_join(a.part, parts, N, dbias, st) : CAPGNN_OK;
 }

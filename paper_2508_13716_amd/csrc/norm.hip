@@ -399,7 +399,8 @@ extern "C" int capgnn_quantize_rows(int64_t n, int F, const void *X, int64_t ldx
 
 extern "C" size_t capgnn_rmsnorm_bwd_workspace_bytes(int64_t n, int F) {
     if (n <= 0 || F <= 0 || F > CAPGNN_NORM_MAX) return 0;
-    return align_up(sizeof(float) * F * std::max(grad_groups(n, F, false), grad_groups(n, F, true)), 256);
+    const int groups = std::max(grad_groups(n, F, false), grad_groups(n, F, true));
+    return groups > 1 ? align_up(sizeof(float) * F * groups, 256) : 0;
 }
 
 extern "C" int capgnn_rmsnorm_bwd(int64_t n, int F, const void *dY, int64_t lddy, int dy_dtype, const void *H, int64_t ldh, int dtype,
@@ -429,10 +430,10 @@ extern "C" int capgnn_rmsnorm_bwd(int64_t n, int F, const void *dY, int64_t lddy
     const int es = elem_bytes(dtype);
     const NormGradArgs a{n, F, s.lanes, dy_dtype == CAPGNN_BF16, static_cast<const char *>(dY), static_cast<const char *>(H),
                          static_cast<const char *>(dH), lddy * elem_bytes(dy_dtype), ldh * es, lddh * es, w, rstd, static_cast<char *>(dX),
-                         lddx * es, 1.f / static_cast<float>(F), dw ? static_cast<float *>(ws) : nullptr};
+                         lddx * es, 1.f / static_cast<float>(F), dw && groups > 1 ? static_cast<float *>(ws) : dw};
     with_shape(s, bf16, [&](auto t, auto v, auto k, auto th) {
         hipLaunchKernelGGL((rmsnorm_grad_kernel<t.value, v.value, k.value, th.value>), dim3(groups), dim3(th.value == 64 ? 256 : th.value), 0, st, a);
     });
     CG_HIP(hipGetLastError());
-    return dw ? launch_column_join(a.part, groups, F, dw, st) : CAPGNN_OK;
+    return dw && groups > 1 ? launch_column_join(a.part, groups, F, dw, st) : CAPGNN_OK;
 }

@@ -53,14 +53,14 @@ def bwd_args(**kw):
 
 @pytest.mark.parametrize("bad", [dict(M=-1), dict(N=-1), dict(dtype=2), dict(act=4), dict(dY=None), dict(U=None), dict(lddy=7), dict(ldu=7), dict(lddu=7),
                                  dict(dY=FAKE + 2), dict(U=FAKE + 2), dict(dU=FAKE + 1, dtype=B.BF16), dict(dbias=FAKE + 2), dict(dU=FAKE, lddu=9),
-                                 dict(dU=2 * FAKE, lddu=9), dict(ws=FAKE + 16)])
+                                 dict(dU=2 * FAKE, lddu=9), dict(M=400, ws=FAKE + 16)])
 def test_linear_act_bwd_refuses(bad):
     refuse(B.EINVAL, B.linear_act_bwd, **bwd_args(**bad))
 
 
 def test_little_workspace_and_no_work():
-    refuse(B.ENOMEM, B.linear_act_bwd, **bwd_args(ws_bytes=B.linear_act_bwd_workspace_bytes(4, 8) - 1))
-    refuse(B.ENOMEM, B.linear_act_bwd, **bwd_args(ws=None))
+    refuse(B.ENOMEM, B.linear_act_bwd, **bwd_args(M=400, ws_bytes=B.linear_act_bwd_workspace_bytes(400, 8) - 1))
+    refuse(B.ENOMEM, B.linear_act_bwd, **bwd_args(M=400, ws=None))
     B.linear(**fwd_args(M=0, A=None, Y=None))
     B.linear(**fwd_args(N=0, W=None, Y=None))
     B.linear_act_bwd(**bwd_args(M=0, dY=None, U=None, dU=None, dbias=None, ws=None, ws_bytes=0))

@@ -41,7 +41,7 @@ def bwd_args(**kw):
 @pytest.mark.parametrize("bad", [
     dict(n=-1), dict(F=0), dict(dtype=2), dict(dy_dtype=2), dict(dY=None), dict(H=None), dict(rstd=None), dict(dX=None), dict(lddy=7), dict(ldh=7), dict(lddh=7),
     dict(lddx=7), dict(dY=FAKE + 2), dict(dX=FAKE + 1, dtype=B.BF16), dict(dw=FAKE + 2), dict(dX=FAKE, lddx=9), dict(dX=FAKE, dtype=B.BF16), dict(dX=2 * FAKE, lddx=9),
-    dict(dX=3 * FAKE, lddx=9), dict(ws=FAKE + 16)])
+    dict(dX=3 * FAKE, lddx=9), dict(n=4000, ws=FAKE + 16)])
 def test_rmsnorm_bwd_refuses(bad):
     refuse(B.EINVAL, B.rmsnorm_bwd, **bwd_args(**bad))
 
@@ -59,9 +59,9 @@ def test_too_wide_and_too_little_are_refused():
     refuse(B.EUNSUPPORTED, B.rmsnorm, **fwd_args(F=wide, ldx=wide, ldr=wide, ldh=wide, ldy=wide))
     refuse(B.EUNSUPPORTED, B.rmsnorm_bwd, **bwd_args(F=wide, lddy=wide, ldh=wide, lddh=wide, lddx=wide))
     refuse(B.EUNSUPPORTED, B.quantize_rows, 1, wide, FAKE, wide, B.F32, 2 * FAKE, wide, FAKE)
-    need = B.rmsnorm_bwd_workspace_bytes(4, 8)
-    refuse(B.ENOMEM, B.rmsnorm_bwd, **bwd_args(ws_bytes=need - 1))
-    refuse(B.ENOMEM, B.rmsnorm_bwd, **bwd_args(ws=None))
+    need = B.rmsnorm_bwd_workspace_bytes(4000, 8)
+    refuse(B.ENOMEM, B.rmsnorm_bwd, **bwd_args(n=4000, ws_bytes=need - 1))
+    refuse(B.ENOMEM, B.rmsnorm_bwd, **bwd_args(n=4000, ws=None))
     B.rmsnorm(**fwd_args(n=0, X=None, Y=None))
     B.quantize_rows(0, 8, None, 8, B.F32, None, 8, None)
     B.rmsnorm_bwd(**bwd_args(n=0, dY=None, H=None, dX=None, rstd=None, dw=None, ws=None, ws_bytes=0))
