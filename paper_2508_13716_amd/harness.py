@@ -161,17 +161,37 @@ class DeviceProblem:
         if self.ws_bytes == 0:
             raise B.CapgnnError(B.EINVAL, B.last_error())
         self.ws = torch.empty(self.ws_bytes, dtype=torch.uint8, device="cuda")
+        self._list = None
         torch.cuda.synchronize()
 
     def resolved_orders(self) -> List[int]:
         return [B.layer_order(self.graph, l, i > 0) for i, l in enumerate(self.layers)]
 
-    def run_epoch(self, lr: float = 0.0, want_loss: bool = True, want_times: bool = False, mask=True, teacher=None):
+    def run_epoch(self, lr: float = 0.0, want_loss: bool = True, want_times: bool = False, mask=True, teacher=None,
+                  max_norm: Optional[float] = None):
+        """One epoch.  With max_norm the update W <- W - lr dW is a call of its own behind the epoch (capgnn_clipped_step), of gradients brought
+        to a global norm of max_norm at most, and for bf16 weights too; self.grad_norm (a device float) holds the norm before that."""
+        if max_norm is not None:
+            out = self.run_epoch(0.0, want_loss, want_times, mask, teacher)
+            t = self.tensor_list()
+            B.clipped_step(t, lr, max_norm, self.grad_norm, self.step_ws, self.step_ws.numel(), stream=self.stream)
+            return out
         return B.epoch(self.graph, self.cache, self.layers, self.X0, self.ld0, self.labels,
                        self.mask if mask else None, 0.0, self.logits, self.dW,
                        self.dW_self if any(t is not None for t in self.dW_self) else None, self.dbias, lr,
                        self.ws, self.ws_bytes, self.stream, self.side, want_loss=want_loss, want_times=want_times,
                        targets=self.targets, ldt=0 if self.targets is None else self.targets.shape[1], teacher=teacher)
+
+    def tensor_list(self) -> B.TensorList:
+        """Every weight and bias with its gradient, made on first use."""
+        if self._list is None:
+            torch = _torch()
+            pairs = [(g, p) for g, p in zip(self.dW + self.dW_self + self.dbias, self.W + self.W_self + self.bias) if p is not None]
+            self._list = B.TensorList([g for g, _ in pairs], [p for _, p in pairs], stream=self.stream)
+            self.grad_norm = torch.zeros(1, dtype=torch.float32, device="cuda")
+            self.step_ws = torch.empty(B.grad_workspace_bytes(self._list), dtype=torch.uint8, device="cuda")
+            torch.cuda.synchronize()
+        return self._list
 
     def capture_epoch(self, lr: float = 0.0, mask=True, two_streams: bool = False):
         """The epoch as a HIP graph on this problem's buffers; returns (graph, device float the replays write the loss to).
@@ -205,6 +225,9 @@ class DeviceProblem:
 
     def close(self):
         _torch().cuda.synchronize()     # a pipelined epoch may have left a prefetch into the workspace in flight
+        if self._list is not None:
+            self._list.close()
+            self._list = None
         if self.cache is not None:
             self.cache.close()
         self.graph.close()
