@@ -604,6 +604,7 @@ int capgnn_quantize_rows(int64_t n, int F, const void *X, int64_t ldx, int dtype
  * lies below 2^-13 of the largest (some 1e-5 of a sum's size; with a float result nothing is dropped).
  * bias: device float[N] or NULL.  act: CAPGNN_ACT_*.  R: device [M x ldr] or NULL; U: device [M x ldu] or NULL (kept for the backward
  * pass); Y: device [M x ldy]; all of out_dtype (CAPGNN_F32 or CAPGNN_BF16), each rounded once.  Y may be R (same pitch).
+ * fp32 products of 2^28 multiply-adds and more are formed as CAPGNN_F32_PRODUCT_SPLIT forms them (above 3.38e38 a number counts as not finite).
  * K = 0: the sums are 0.  M, N, K < 2^31, a row of A or W shorter than 2^31 bytes.
  * Errors: EINVAL, EUNSUPPORTED (more than 2^22 tiles of 64 x 64 results), ENOMEM (workspace too small), EHIP. */
 size_t capgnn_linear_workspace_bytes(int64_t M, int64_t N, int64_t K, int dtype);

@@ -9,6 +9,7 @@
 #include "rows.h"
 
 #include <algorithm>
+#include <type_traits>
 
 namespace capgnn {
 
@@ -275,44 +276,50 @@ int launch_column_join(const float *part, int parts, int64_t F, float *sums, hip
     return CAPGNN_OK;
 }
 
-// Team of a row: threads (64: lanes of a wave) and vectors per lane.
+// Team of a row: threads (64: lanes of a wave) and vectors per lane.  `held`: elements per lane, at most; of the widest team's 32.
 struct NormShape {
     int V, K, T, lanes;
 };
-static NormShape norm_shape(int F, bool bf16, int held = 32) {      // held: elements per lane, at most, where the widest team leaves the choice
+constexpr int NORM_HELD = 32, GRAD_HELD = 16;   // (the gradient holds h, dY, dH and the sums of dw)
+static NormShape norm_shape(int F, bool bf16, int held) {
     const int V = bf16 ? ROW_V<true> : ROW_V<false>;
     if (F < V) return {1, 1, 64, pow2_at_least(F)};
     const int vectors = (F + V - 1) / V, most = (vectors <= 1024 * (held / V) ? held : 32) / V;
-    const int T = vectors <= 64 * most ? 64 : vectors <= 256 * most ? 256 : 1024;
+    const int T = vectors <= 64 * (held / V) ? 64 : vectors <= 256 * (held / V) ? 256 : 1024;
     int K = 1;
     while (K < most && vectors > T * K) K *= 2;
     return {V, K, T, T == 64 ? std::min(64, pow2_at_least((vectors + K - 1) / K)) : T};
 }
+// whether norm_shape gives a row of vectors of V elements K of them per lane of T
+template <int HELD> constexpr bool has_shape(int V, int K, int T) {
+    if (V == 1) return K == 1 && T == 64;
+    const int most = HELD / V, narrower = T == 64 ? 0 : T == 256 ? 64 * most : 256 * most;      // vectors of the next narrower team
+    return T * K > narrower && (K <= most || (T == 1024 && K * V == 32));
+}
 
 // f(type, V, K, T) as compile-time numbers
-template <class G> static void with_shape(const NormShape &s, bool bf16, G f) {
+template <int HELD, class G> static void with_shape(const NormShape &s, bool bf16, G f) {
+    auto one = [&](auto b, auto v, auto k, auto t) {
+        if constexpr (has_shape<HELD>(v.value, k.value, t.value)) f(b, v, k, t);
+    };
     auto threads = [&](auto b, auto v, auto k) {
-        if (s.T == 64) f(b, v, k, std::integral_constant<int, 64>());
-        else if (s.T == 256) f(b, v, k, std::integral_constant<int, 256>());
-        else f(b, v, k, std::integral_constant<int, 1024>());
+        if (s.T == 64) one(b, v, k, std::integral_constant<int, 64>());
+        else if (s.T == 256) one(b, v, k, std::integral_constant<int, 256>());
+        else one(b, v, k, std::integral_constant<int, 1024>());
     };
     using I1 = std::integral_constant<int, 1>;
     using I2 = std::integral_constant<int, 2>;
     using I4 = std::integral_constant<int, 4>;
     using I8 = std::integral_constant<int, 8>;
-    if (s.V == 1) {
-        if (bf16) f(std::true_type(), I1(), I1(), std::integral_constant<int, 64>());
-        else f(std::false_type(), I1(), I1(), std::integral_constant<int, 64>());
-    } else if (bf16) {
-        s.K == 1 ? threads(std::true_type(), I8(), I1()) : s.K == 2 ? threads(std::true_type(), I8(), I2()) : threads(std::true_type(), I8(), I4());
-    } else {
+    if (s.V == 1) bf16 ? threads(std::true_type(), I1(), I1()) : threads(std::false_type(), I1(), I1());
+    else if (bf16) s.K == 1 ? threads(std::true_type(), I8(), I1()) : s.K == 2 ? threads(std::true_type(), I8(), I2()) : threads(std::true_type(), I8(), I4());
+    else
         s.K == 1 ? threads(std::false_type(), I4(), I1()) : s.K == 2 ? threads(std::false_type(), I4(), I2())
         : s.K == 4 ? threads(std::false_type(), I4(), I4()) : threads(std::false_type(), I4(), I8());
-    }
 }
 
 static int launch_norm(NormArgs a, bool bf16, hipStream_t st) {
-    const NormShape s = norm_shape(a.F, bf16);
+    const NormShape s = norm_shape(a.F, bf16, NORM_HELD);
     a.lanes = s.lanes;
     const int64_t rows = s.T == 64 ? 4 * (64 / s.lanes) : 1;
     const int64_t most = int64_t(1) << 20;      // workgroups of a launch (fewer than 2^32 threads)
@@ -326,15 +333,13 @@ static int launch_norm(NormArgs a, bool bf16, hipStream_t st) {
         if (b.y_scale) b.y_scale += done;
         if (b.rstd) b.rstd += done;
         const unsigned grid = static_cast<unsigned>((b.n + rows - 1) / rows);
-        with_shape(s, bf16, [&](auto t, auto v, auto k, auto th) {
+        with_shape<NORM_HELD>(s, bf16, [&](auto t, auto v, auto k, auto th) {
             hipLaunchKernelGGL((rmsnorm_kernel<t.value, v.value, k.value, th.value>), dim3(grid), dim3(th.value == 64 ? 256 : th.value), 0, st, b);
         });
         CG_HIP(hipGetLastError());
     }
     return CAPGNN_OK;
 }
-
-constexpr int GRAD_HELD = 16;   // (h, dY, dH and the sums of dw are all held)
 
 // workgroups of the gradient: each has a part of dw
 static int grad_groups(int64_t n, int F, bool bf16) {
@@ -431,7 +436,7 @@ extern "C" int capgnn_rmsnorm_bwd(int64_t n, int F, const void *dY, int64_t lddy
     const NormGradArgs a{n, F, s.lanes, dy_dtype == CAPGNN_BF16, static_cast<const char *>(dY), static_cast<const char *>(H),
                          static_cast<const char *>(dH), lddy * elem_bytes(dy_dtype), ldh * es, lddh * es, w, rstd, static_cast<char *>(dX),
                          lddx * es, 1.f / static_cast<float>(F), dw && groups > 1 ? static_cast<float *>(ws) : dw};
-    with_shape(s, bf16, [&](auto t, auto v, auto k, auto th) {
+    with_shape<GRAD_HELD>(s, bf16, [&](auto t, auto v, auto k, auto th) {
         hipLaunchKernelGGL((rmsnorm_grad_kernel<t.value, v.value, k.value, th.value>), dim3(groups), dim3(th.value == 64 ? 256 : th.value), 0, st, a);
     });
     CG_HIP(hipGetLastError());

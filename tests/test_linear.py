@@ -200,6 +200,35 @@ def test_what_is_not_finite_stays_in_its_row_and_column(M, N, K, t):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("pad", [0, 1])
+def test_what_is_not_finite_in_a_large_fp32_product(pad):
+    """in three pieces (2^28 multiply-adds and more): an infinity's row may be NaN, no other one"""
+    import torch
+    M, N, K = 1030, 520, 513
+    a, w = np.ones((M, K)), np.ones((N, K))
+    a[3, 500] = np.inf
+    a[1029, 512] = np.nan
+    Y = new(M, N, "f32")
+    B.linear(M, N, K, Mat(a, "f32", K + pad).p, K + pad, None, Mat(w, "f32", K + pad).p, K + pad, None, B.F32, None, B.ACT_NONE, None, 0, None, 0, Y.p, N, B.F32,
+             *ws_of(B.linear_workspace_bytes(M, N, K, B.F32)))
+    torch.cuda.synchronize()
+    y = Y.get()
+    assert not np.isfinite(y[3]).any() and np.isnan(y[1029]).all()
+    y[3] = y[1029] = K
+    assert (y == K).all()
+
+
+@pytest.mark.gpu
+def test_no_rows():
+    import torch
+    for N in (1, 70, 1009):
+        db = Mat(np.full((1, N), 7.0), "f32")
+        B.linear_act_bwd(0, N, None, N, None, N, B.F32, B.ACT_GELU, None, N, db.p, None, 0)
+        torch.cuda.synchronize()
+        assert (db.get() == 0).all()
+
+
+@pytest.mark.gpu
 def test_operands_beyond_32_bit_offsets():
     import torch
     M, K = 4_200_000, 1030                           # A has more than 2^32 elements

@@ -293,3 +293,13 @@ def test_rows_beyond_32_bit_offsets():
     torch.cuda.synchronize()
     assert float(H[-1, -1]) == 6.0 and float(H[0, 0]) == 4.0 and float(out[-1, 0]) == 1.0 and float(out[0, -1]) == 1.0
     assert int(torch.count_nonzero(out[:, 5])) == 2
+
+
+@pytest.mark.gpu
+def test_the_gradient_of_no_rows_is_zero():
+    import torch
+    for F in (1, 41, 602):
+        dw = Mat(np.full((1, F), 7.0), "f32")
+        B.rmsnorm_bwd(0, F, None, F, B.F32, None, F, B.F32, None, None, None, 0, None, F, dw.p, None, 0)
+        torch.cuda.synchronize()
+        assert (dw.get() == 0).all()
