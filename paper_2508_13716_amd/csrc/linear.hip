@@ -420,7 +420,7 @@ template <int DT, bool OB, int WR, int WC, int TM, int TN> __global__ __launch_b
     store_tile<OB, WR, WC, TM, TN>(g, lds, m0 + wm, n0 + wn, acc);
 }
 
-// The same for aligned operands (16 bytes) that need no check but at the last step: loads go straight to LDS, one step ahead, and the operands
+// The same for operands whose rows start on 4 bytes (what a load to LDS asks for) and need no check but at the last step: loads go straight to LDS, steps ahead, and the operands
 // of a slice (half or a quarter of a step) are read while the one before is multiplied, across the barrier too: behind the last slice's
 // reads the other buffer's loads are waited for, this one's are free to start, and the next step's first slice is read.
 // The order of a slice: reads of the next one's operands, then loads to LDS, between its matrix instructions.  (Asked for all at once they
@@ -442,10 +442,10 @@ template <int MFMAS, int READS, int LOADS> __device__ __forceinline__ void inter
     }
 }
 
-// LB: bytes of a lane's load, 16 or (rows that start on any 4 bytes) 4; NB: steps that LDS holds
-template <int DT, bool OB, int WR, int WC, int TM, int TN, int LB, int NB> __global__ __launch_bounds__(WR *WC * 64) void linear_direct_kernel(LinearArgs g) {
+// NB: steps that LDS holds
+template <int DT, bool OB, int WR, int WC, int TM, int TN, int NB> __global__ __launch_bounds__(WR *WC * 64) void linear_direct_kernel(LinearArgs g) {
     constexpr int T = WR * WC * 64, BM = WR * TM * 32, BN = WC * TN * 32, STEP = 128 / BYTES<DT>, S = SLICES<DT>;
-    constexpr int PER_ROW = 128 / LB, ROWS = T / PER_ROW;               // lanes of a row, rows of a load of all waves
+    constexpr int ROWS = T / UNITS;                                     // of a load of all waves
     constexpr int PA = BM / ROWS, PB = BN / ROWS, TILE = (BM + BN) * UNITS;
     static_assert(STAGE_BYTES<WR * WC, TN> <= NB * TILE * 16, "results leave through the tiles' memory");
     static_assert((NB - 2) * (PA + PB) < 64, "loads that a wave can wait for one by one");
@@ -462,9 +462,9 @@ template <int DT, bool OB, int WR, int WC, int TM, int TN, int LB, int NB> __glo
     const char *A = x.A + m0 * g.lda, *W = x.W + n0 * g.ldw;
     auto sa = __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(A), 0, (rows_a - 1) * lda + width, 0x00027000);
     auto sb = __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(W), 0, (rows_b - 1) * ldw + width, 0x00027000);
-    // A wave's load fills LDS in order (for 16 bytes: lane l has place l % 8 of row l / 8), and place p of a row holds unit p ^ (row / 2 % 8).
+    // A wave's load fills LDS in order (lane l has place l % 8 of row l / 8), and place p of a row holds unit p ^ (row / 2 % 8).
     // Rows behind the last one are the last one again: their results are not stored, and nothing depends on the buffer's bounds.
-    const uint32_t row = threadIdx.x / PER_ROW, byte = threadIdx.x % PER_ROW * LB;
+    const uint32_t row = threadIdx.x / UNITS, byte = threadIdx.x % UNITS * 16;
     uint32_t oa[PA], ob[PB];
 #pragma unroll
     for (int p = 0; p < PA; ++p) oa[p] = min(row + p * ROWS, rows_a - 1u) * lda + (byte ^ (row + p * ROWS) / 2 % 8 * 16);
@@ -472,18 +472,11 @@ template <int DT, bool OB, int WR, int WC, int TM, int TN, int LB, int NB> __glo
     for (int p = 0; p < PB; ++p) ob[p] = min(row + p * ROWS, rows_b - 1u) * ldw + (byte ^ (row + p * ROWS) / 2 % 8 * 16);
     const int steps = static_cast<int>(x.K / STEP), all = steps + (x.K % STEP ? 1 : 0);
     auto fill = [&](int t) __attribute__((always_inline)) {
-        char *As = reinterpret_cast<char *>(lds + t % NB * TILE) + wave * 64 * LB, *Bs = As + BM * 128;
-        if constexpr (LB == 16) {
+        raw16 *As = lds + t % NB * TILE + wave * 64, *Bs = As + BM * UNITS;
 #pragma unroll
-            for (int p = 0; p < PA; ++p) __builtin_amdgcn_raw_ptr_buffer_load_lds(sa, As + p * T * LB, 16, static_cast<int>(oa[p]), t * 128, 0, 0);
+        for (int p = 0; p < PA; ++p) __builtin_amdgcn_raw_ptr_buffer_load_lds(sa, As + p * T, 16, static_cast<int>(oa[p]), t * 128, 0, 0);
 #pragma unroll
-            for (int p = 0; p < PB; ++p) __builtin_amdgcn_raw_ptr_buffer_load_lds(sb, Bs + p * T * LB, 16, static_cast<int>(ob[p]), t * 128, 0, 0);
-        } else {
-#pragma unroll
-            for (int p = 0; p < PA; ++p) __builtin_amdgcn_raw_ptr_buffer_load_lds(sa, As + p * T * LB, 4, static_cast<int>(oa[p]), t * 128, 0, 0);
-#pragma unroll
-            for (int p = 0; p < PB; ++p) __builtin_amdgcn_raw_ptr_buffer_load_lds(sb, Bs + p * T * LB, 4, static_cast<int>(ob[p]), t * 128, 0, 0);
-        }
+        for (int p = 0; p < PB; ++p) __builtin_amdgcn_raw_ptr_buffer_load_lds(sb, Bs + p * T, 16, static_cast<int>(ob[p]), t * 128, 0, 0);
     };
     auto fill_end = [&]() __attribute__((always_inline)) {              // what is left of the reduction, element by element at its end
         raw16 *As = lds + steps % NB * TILE;
@@ -803,36 +796,34 @@ extern "C" int capgnn_linear(int64_t M, int64_t N, int64_t K, const void *A, int
         else go(linear_few_kernel<E4M3_FINE>);
     } else {
         const uintptr_t at = reinterpret_cast<uintptr_t>(A) | reinterpret_cast<uintptr_t>(W) | uintptr_t(g.lda) | uintptr_t(g.ldw);
-        const int unit = K == 0 || at % 4 || g.lda >= most / 256 || g.ldw >= most / 256 ? 1 : at % 16 ? 4 : 16;      // bytes of a load to LDS
-        const int tile = unit == 1 || (dtype == CAPGNN_F32 && !cut_pays(M, N, K)) ? 64 : unit == 4 ? std::min(p.tile, 128) : p.tile;
+        const bool direct_rows = K > 0 && at % 4 == 0 && g.lda < most / 256 && g.ldw < most / 256;
+        const bool cut = dtype == CAPGNN_F32 && direct_rows && cut_pays(M, N, K);
+        const int tile = !direct_rows || (dtype == CAPGNN_F32 && !cut) ? 64 : p.tile;
         const int64_t tiles = (M + tile - 1) / tile * ((N + tile - 1) / tile);
         if (tiles > int64_t(1) << 22) CG_FAIL(CAPGNN_EUNSUPPORTED, "linear: more than 2^22 tiles of results");
         const dim3 grid(static_cast<unsigned>(tiles), p.parts);
-        const bool cut = dtype == CAPGNN_F32 && unit > 1 && cut_pays(M, N, K);
         with_types(dtype, out_dtype, cut, [&](auto d, auto o) {
-            auto direct = [&](auto wr, auto wc, auto tm, auto tn, auto lb, auto nb) {
-                hipLaunchKernelGGL((linear_direct_kernel<d.value, o.value, wr.value, wc.value, tm.value, tn.value, lb.value, nb.value>), grid,
+            auto direct = [&](auto wr, auto wc, auto tm, auto tn, auto nb) {
+                hipLaunchKernelGGL((linear_direct_kernel<d.value, o.value, wr.value, wc.value, tm.value, tn.value, nb.value>), grid,
                                    dim3(wr.value * wc.value * 64), 0, st, g);
             };
             constexpr std::integral_constant<int, 1> I1;
             constexpr std::integral_constant<int, 2> I2;
             constexpr std::integral_constant<int, 3> I3;
             constexpr std::integral_constant<int, 4> I4;
-            constexpr std::integral_constant<int, 16> I16;
             // Eight waves of 128 x 64 fill one another's gaps; 8-bit operands, whose matrix instructions run twice as long, and fp32 ones, which
             // are cut on their way, do with half the reads of four waves of 128 x 128 (us, four / eight: 8192^3 bf16 908 / 855,
-            // 8192 x 8192 x 16384 e4m3 831 / 858)
+            // 8192 x 8192 x 16384 e4m3 831 / 858).  Tiles of 128 leave room for two workgroups a compute unit, those of 64 for three.
             if (tile == 256) {
-                if constexpr (d.value == CAPGNN_E4M3 || d.value == F32_CUT) direct(I2, I2, I4, I4, I16, I2);
-                else if constexpr (d.value != CAPGNN_F32) direct(I2, I4, I4, I2, I16, I2);
+                if constexpr (d.value == CAPGNN_E4M3 || d.value == F32_CUT) direct(I2, I2, I4, I4, I2);
+                else if constexpr (d.value != CAPGNN_F32) direct(I2, I4, I4, I2, I2);
             } else if (tile == 128) {
-                if constexpr (d.value != CAPGNN_F32) unit == 16 ? direct(I2, I2, I2, I2, I16, I2) : direct(I2, I2, I2, I2, I4, I2);
+                if constexpr (d.value != CAPGNN_F32) direct(I2, I2, I2, I2, I2);
             } else {
                 if constexpr (d.value != F32_CUT) {
-                    if (unit == 1) hipLaunchKernelGGL((linear_tile_kernel<d.value, o.value, 2, 2, 1, 1>), grid, dim3(256), 0, st, g);
+                    if (!direct_rows) hipLaunchKernelGGL((linear_tile_kernel<d.value, o.value, 2, 2, 1, 1>), grid, dim3(256), 0, st, g);
                 }
-                if (unit == 1) return;
-                unit == 16 ? direct(I2, I2, I1, I1, I16, I3) : direct(I2, I2, I1, I1, I4, I3);
+                if (direct_rows) direct(I2, I2, I1, I1, I3);
             }
         });
     }
