@@ -5,6 +5,9 @@
 // and sum runs of equal ids in registers.  A run inside a tile goes straight to the table; one that crosses tiles leaves a part per tile,
 // and one workgroup a run adds its parts in order.  Rows that no id names are zeroed first; that is shared out over the sort's launches,
 // which wait for memory more than they use it.
+// us: 300001 bf16 rows of 256 into 500009 fp32 ones (0.67 GB) 212, of them 118 for six launches that sort and zero 512 MB (the zeros shared out
+// over four of them; over all six 123: the moves have room for three workgroups a compute unit), 82 for the sums (rows of 512 bytes
+// from everywhere), 17 for the joins; 64 rows of 1024 looked up 3.2.
 #include "rows.h"
 #include "grid.h"
 
@@ -82,9 +85,9 @@ __device__ __forceinline__ void fill_share(const Fill &f, int64_t group, int64_t
 // Keys are ids in 32 bits, V for an id outside the table (the last ones then, and no run of theirs is summed).  A pass sorts by `bits` bits of
 // the key from `shift` on, keeping the order of equal digits: counts of every digit per tile, their prefix along the tiles (a wave per
 // digit), and the move.
-constexpr int SORT_THREADS = 256, SORT_WAVES = SORT_THREADS / 64, SORT_ITEMS = 8, SORT_TILE = SORT_THREADS * SORT_ITEMS;
+constexpr int SORT_THREADS = 256, SORT_WAVES = SORT_THREADS / 64, SORT_ITEMS = 4, SORT_TILE = SORT_THREADS * SORT_ITEMS;
 constexpr int SORT_BITS = 11;               // of a digit, at most
-constexpr int SMALL_THREADS = 1024, SMALL_WAVES = SMALL_THREADS / 64, SMALL_TILE = SMALL_THREADS * SORT_ITEMS, SMALL_BITS = 8;
+constexpr int SMALL_THREADS = 1024, SMALL_WAVES = SMALL_THREADS / 64, SMALL_ITEMS = 8, SMALL_TILE = SMALL_THREADS * SMALL_ITEMS, SMALL_BITS = 8;
 
 struct SortPass {
     int64_t n;
@@ -160,10 +163,11 @@ __device__ __forceinline__ void same_digit(uint32_t digit, bool on, int bits, in
 }
 
 // Ranks of a wave's items among its own of the same digit; count[digit] (the wave's, zero before) is their number afterwards.
-__device__ __forceinline__ void rank_items(const uint32_t (&key)[SORT_ITEMS], const bool (&on)[SORT_ITEMS], int shift, int bits,
-                                           volatile uint32_t *count, uint32_t (&rank)[SORT_ITEMS]) {
+template <int ITEMS>
+__device__ __forceinline__ void rank_items(const uint32_t (&key)[ITEMS], const bool (&on)[ITEMS], int shift, int bits, volatile uint32_t *count,
+                                           uint32_t (&rank)[ITEMS]) {
 #pragma unroll
-    for (int i = 0; i < SORT_ITEMS; ++i) {
+    for (int i = 0; i < ITEMS; ++i) {
         const uint32_t digit = (key[i] >> shift) & ((1u << bits) - 1);
         int before, all;
         same_digit(digit, on[i], bits, &before, &all);
@@ -200,7 +204,6 @@ template <int W> __device__ __forceinline__ void digit_scan(uint32_t *v, int dig
 
 __global__ __launch_bounds__(SORT_THREADS) void sort_move_kernel(SortPass s) {
     __shared__ uint32_t count[SORT_WAVES][1 << SORT_BITS], start[1 << SORT_BITS], sum[SORT_WAVES];
-    if (blockIdx.x >= s.tiles) return fill_share(s.fill, blockIdx.x - s.tiles, gridDim.x - s.tiles);
     const int digits = 1 << s.bits, wave = threadIdx.x / 64;
     // a wave has SORT_ITEMS * 64 neighbouring items, 64 at a time; all that is read is asked for first
     const int64_t first = int64_t(blockIdx.x) * SORT_TILE + wave * (SORT_ITEMS * 64) + (threadIdx.x & 63);
@@ -258,11 +261,11 @@ __global__ __launch_bounds__(SMALL_THREADS) void sort_small_kernel(SortPass s) {
     __shared__ uint32_t count[SMALL_WAVES][1 << SMALL_BITS], start[1 << SMALL_BITS], sum[SMALL_WAVES], keys[SMALL_TILE], poss[SMALL_TILE];
     if (blockIdx.x >= 1) return fill_share(s.fill, blockIdx.x - 1, gridDim.x - 1);
     const int n = static_cast<int>(s.n), wave = threadIdx.x / 64, digits = 1 << SMALL_BITS;
-    const int first = wave * (SORT_ITEMS * 64) + (threadIdx.x & 63);
-    uint32_t key[SORT_ITEMS], pos[SORT_ITEMS], rank[SORT_ITEMS];
-    bool on[SORT_ITEMS];
+    const int first = wave * (SMALL_ITEMS * 64) + (threadIdx.x & 63);
+    uint32_t key[SMALL_ITEMS], pos[SMALL_ITEMS], rank[SMALL_ITEMS];
+    bool on[SMALL_ITEMS];
 #pragma unroll
-    for (int i = 0; i < SORT_ITEMS; ++i) {
+    for (int i = 0; i < SMALL_ITEMS; ++i) {
         const int k = first + i * 64;
         on[i] = k < n;
         key[i] = on[i] ? sort_key(s, k) : 0u;
@@ -285,7 +288,7 @@ __global__ __launch_bounds__(SMALL_THREADS) void sort_small_kernel(SortPass s) {
         __syncthreads();
         digit_scan<SMALL_WAVES>(start, digits, sum);
 #pragma unroll
-        for (int i = 0; i < SORT_ITEMS; ++i)
+        for (int i = 0; i < SMALL_ITEMS; ++i)
             if (on[i]) {
                 const uint32_t d = (key[i] >> shift) & (digits - 1), to = start[d] + count[wave][d] + rank[i];
                 keys[to] = key[i];
@@ -293,7 +296,7 @@ __global__ __launch_bounds__(SMALL_THREADS) void sort_small_kernel(SortPass s) {
             }
         __syncthreads();
 #pragma unroll
-        for (int i = 0; i < SORT_ITEMS; ++i)
+        for (int i = 0; i < SMALL_ITEMS; ++i)
             if (on[i]) {
                 key[i] = keys[first + i * 64];
                 pos[i] = poss[first + i * 64];
@@ -301,7 +304,7 @@ __global__ __launch_bounds__(SMALL_THREADS) void sort_small_kernel(SortPass s) {
         __syncthreads();
     }
 #pragma unroll
-    for (int i = 0; i < SORT_ITEMS; ++i)
+    for (int i = 0; i < SMALL_ITEMS; ++i)
         if (on[i]) {
             s.key_out[first + i * 64] = key[i];
             s.pos_out[first + i * 64] = pos[i];
@@ -452,14 +455,17 @@ template <int V> __global__ __launch_bounds__(JOIN_THREADS) void run_join_kernel
                 if (m == i + 1 && tile + 2 + i < a.tiles && begins[i] == id) ++m;
             if (m <= JOIN_FEW) {
                 if (live) {
-                    float acc[V];
+                    float acc[V], v[4][V];
                     ld_row<false, V>(part(tile, 1), 0, acc);
-#pragma unroll 4
-                    for (int t = 1; t <= m; ++t) {
-                        float v[V];
-                        ld_row<false, V>(part(tile + t, 0), 0, v);
+                    for (int t = 1; t <= m; t += 4) {
 #pragma unroll
-                        for (int e = 0; e < V; ++e) acc[e] += v[e];
+                        for (int i = 0; i < 4; ++i) ld_row<false, V>(part(tile + min(t + i, m), 0), 0, v[i]);
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)
+                            if (t + i <= m) {
+#pragma unroll
+                                for (int e = 0; e < V; ++e) acc[e] += v[i][e];
+                            }
                     }
                     put_row<V>(a, id, from, j - from, acc);
                 }
@@ -535,7 +541,8 @@ template <int V> __global__ __launch_bounds__(JOIN_THREADS) void run_join_kernel
 // ------------------------------------------------------------------ tables of a few rows
 // A table that fits LDS many times over needs no sorting: a team of lanes has a copy of its own there and adds the rows of dY to it, one
 // after the other, each lane its columns; a workgroup's copies are added at its end, and the workgroups' sums by a second launch, in
-// their order.  (612000 rows of 100 floats into 47: 102 us by sorting, of which the sums alone take 57.)  What nothing was added to is -0,
+// their order.  (612000 rows of 100 floats into 47: 102 us by sorting, of which the sums alone take 57; here 64, 3.9 TB/s, and 5 for the
+// join; with one batch of rows on its way instead of two 80.)  What nothing was added to is -0,
 // which changes no sum.
 struct TableArgs {
     int64_t n;
@@ -790,7 +797,7 @@ extern "C" int capgnn_embed_bwd(int64_t n, const int64_t *ids, int64_t V, int F,
     s.count = at(w.count);
     s.total = at(w.total);
     s.fill = fill;
-    s.fill.parts = small ? 1 : 3 * w.passes;
+    s.fill.parts = small ? 1 : 2 * w.passes;
     auto fill_groups = [&](int threads) {           // workgroups that a launch has for its share of the zeros
         return s.fill.p ? static_cast<unsigned>(std::min<int64_t>(std::max<int64_t>(fill_jobs * 256 / threads / s.fill.parts, 1), 4096)) : 0u;
     };
@@ -816,8 +823,7 @@ extern "C" int capgnn_embed_bwd(int64_t n, const int64_t *ids, int64_t V, int F,
             ++s.fill.part;
             hipLaunchKernelGGL(sort_prefix_kernel, dim3(((1u << s.bits) + SORT_WAVES - 1) / SORT_WAVES + more), dim3(SORT_THREADS), 0, st, s);
             ++s.fill.part;
-            hipLaunchKernelGGL(sort_move_kernel, dim3(s.tiles + more), dim3(SORT_THREADS), 0, st, s);
-            ++s.fill.part;
+            hipLaunchKernelGGL(sort_move_kernel, dim3(s.tiles), dim3(SORT_THREADS), 0, st, s);
         }
     }
     CG_HIP(hipGetLastError());

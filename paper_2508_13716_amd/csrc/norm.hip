@@ -6,6 +6,9 @@
 // lanes of a wave as it has vectors of 16 bytes (a power of two), up to 64, or a workgroup for wide rows.  Where a row is no whole number
 // of vectors its last lane takes the row's last V elements: those that the lane before it has, too, are left out of the sums and stored
 // twice with the same value.  Every sum has a fixed order.
+// us (of the bytes a pass cannot do without): 180000 x 602 fp32 with the residual 331 (5.2 TB/s), 16384 x 4096 bf16 gradient with dH and dw
+// 112, and 7 for the join of dw's parts (4.5 TB/s), one row of 4096 into 8 bits 3.4.  More than 16 elements per lane of the gradient at
+// 1024 threads (rows above 16384) do not fit the registers: up to 540 bytes of scratch memory a thread there.
 #include "rows.h"
 
 #include <algorithm>
@@ -154,6 +157,8 @@ struct NormGradArgs {
     float *part;                // [workgroups][F] parts of dw, or null
 };
 
+// A workgroup strides over the rows and keeps its part of dw in registers.  All of a row is asked for before its sum, dH too, which is
+// used behind it.
 template <bool BF16, int V, int K, int T> __global__ __launch_bounds__(T == 64 ? 256 : T) void rmsnorm_grad_kernel(NormGradArgs a) {
     constexpr bool WIDE = T > 64;
     __shared__ float part[WIDE ? 2 * (T / 64) : 4 * 64 * V * K];
