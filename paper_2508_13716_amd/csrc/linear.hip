@@ -741,9 +741,13 @@ static LinearPlan linear_plan(int64_t M, int64_t N, int64_t K, int es) {
         // 647 / 717 / 1047, x 256 222 / 215 / 305; x 1024 e4m3 166 / 145 / 187, x 2048 216 / 204 / 266; 612000 x 47 x 256 bf16 274 / 157 / 107,
         // fp32 660 / 296 / 233; 3000^3 bf16 (144 tiles of 256) 123 with them, 105 / 117 with the others.
         auto wide = [&](int64_t b) { return tiles(b) * b * b * 4 <= tiles(b / 2) * (b / 2) * (b / 2) * 5; };
-        p.tile = tiles(256) >= 200 && wide(256) && lines >= (es == 1 ? 32 : 16) ? 256 : tiles(128) >= 256 && wide(128) ? 128 : 64;
+        // Tiles of 128 in parts of 32 steps and more, where that gives every compute unit one: 6095 x 376 x 5188 fp32 177, tiles of 64 281;
+        // 1500 x 1500 x 6000 bf16 60 / 84; 100 x 8192 x 8192 bf16 45.5 / 44.3, 300 x 4096 x 8192 37.6 / 47.6 (with parts of 16, 2048 x 1024 x 2048
+        // bf16 23.8 / 17.7).
+        const int64_t split = tiles(128) < 256 ? std::min<int64_t>(std::min<int64_t>(lines / 32, 512 / tiles(128)), 32) : 1;
+        p.tile = tiles(256) >= 200 && wide(256) && lines >= (es == 1 ? 32 : 16) ? 256 : tiles(128) * split >= 256 && wide(128) ? 128 : 64;
         groups = tiles(p.tile);
-        most = p.tile == 64 ? lines / 8 : 1;
+        most = p.tile == 64 ? lines / 8 : p.tile == 128 ? split : 1;
     }
     // (enough workgroups for the chip, parts of 8 steps or more; of a few rows 32)
     const int64_t parts = std::min<int64_t>(std::min<int64_t>(most, (p.tile ? 512 : 256) / groups), 32);

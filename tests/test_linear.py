@@ -168,6 +168,14 @@ def test_large_tiles(M, N, K, t):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("M,N,K,t", [(700, 900, 14_000, "bf16"), (1500, 1100, 3300, "f32"), (1000, 1000, 16_500, "e4m3"), (520, 600, 24_500, "bf16"), (600, 640, 12_001, "f32")])
+def test_long_reductions(M, N, K, t):
+    """large tiles whose reduction is split, rows on 4 bytes and rows that are not"""
+    check(M, N, K, t, "f32", "none")
+    check(M, N, K, t, "bf16", "gelu", residual=True, save=True, pad=3)
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("M", [1, 20, 200])
 def test_no_reduction(M):
     """K = 0: the epilogue of zeros"""
