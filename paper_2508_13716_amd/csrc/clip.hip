@@ -7,7 +7,7 @@
 // added in double: a float's square does not overflow there, and the sum's rounding is far below the result's; at one fused operation per
 // 4 bytes that is a twentieth of the card's rate.  Every workgroup adds the first launch's sums itself, in one order: two launches in all.
 // The second one takes the pieces from the last to the first: what the first has read last is what the caches still hold.
-// us: 120 million fp32 gradients of bf16 weights in 300 tensors 270 (1.44 GB, 5.3 TB/s), the norm alone 86 (5.6 TB/s); pieces of 32768
+// us: 120 million fp32 gradients of bf16 weights in 300 tensors 273 (1.44 GB, 5.3 TB/s), 111 of them the norm; pieces of 32768
 // elements 299, of 8192 272; 165 thousand in four tensors 3 and 4.4.
 #include "rows.h"
 

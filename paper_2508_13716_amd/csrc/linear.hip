@@ -7,10 +7,10 @@
 //
 // D layout of the 32 x 32 instructions: register r of lane l holds row 8 (r / 4) + 4 (l / 32) + r % 4, column l % 32.
 //
-// us (TFLOP/s), epilogue of activation and residual included: 8192^3 bf16 897 (1226; a library product alone reaches 1350), 8192 x 8192 x 4096
-// e4m3 314 (1750; 2740), fp32 2403 (229; 154), 4096^3 bf16 111 (1240).  The matrix cores bound the wide ones, at the clock that power
-// leaves them (8192^3 bf16: busy 61 % of the cycles at 1.7 GHz with four waves a tile; without loads to LDS a quarter faster); the
-// 8-bit one spends a quarter of its time on results, whose arithmetic no other workgroup on the compute unit hides.
+// us (TFLOP/s), epilogue of activation and residual included: 8192^3 bf16 903 (1218; a library product alone reaches 1350), 8192 x 8192 x 4096
+// e4m3 316 (1740; 2740), fp32 2403 (229; 154), 4096^3 bf16 111 (1240).  The matrix cores bound the wide ones, at the clock that power
+// leaves them (8192^3 bf16: busy 68 % of the cycles, at 1.6 GHz); the 8-bit one spends a quarter of its time on results, whose
+// arithmetic no other workgroup on the compute unit hides (busy 37 %, at 2.0 GHz).
 #include "rows.h"
 #include "grid.h"
 
