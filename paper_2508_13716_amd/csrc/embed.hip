@@ -39,9 +39,11 @@ template <bool BF16, int V> __global__ __launch_bounds__(256) void embed_kernel(
             float v[V];
 #pragma unroll
             for (int e = 0; e < V; ++e) v[e] = 0.f;
-            if (inside) ld_row<BF16, V>(src, from, v);
+            if (inside) {
+                ld_row<BF16, V>(src, from, v);
 #pragma unroll
-            for (int e = 0; e < V; ++e) v[e] *= a.scale;
+                for (int e = 0; e < V; ++e) v[e] *= a.scale;
+            }
             st_row_of<V>(a.out_bf16, dst, from, v);
         }
     }
@@ -666,9 +668,9 @@ static TableShape table_shape(int64_t n, int64_t V, const EmbedShape &s, int F) 
         t.lds = size_t(V) * t.chunk * s.V * sizeof(float) * (t.threads / s.lanes);
         if (t.lds <= 156 * 1024) break;
     }
-    if (t.threads < 128 || V > 4096) return {};
+    if (t.threads < 128 || V > 4096 || V * F > int64_t(1) << 27) return {};      // (the join's grid: fewer than 2^32 threads)
     const int64_t teams = t.threads / s.lanes, room = std::min<int64_t>(160 * 1024 / std::max<size_t>(t.lds, 1), 8);
-    const int64_t most = std::max<int64_t>(NUM_CU * room / s.chunks, 64);
+    const int64_t most = std::max<int64_t>(NUM_CU * room / s.chunks, 1);
     t.rows = std::max<int64_t>((n + most - 1) / most, teams * TABLE_AHEAD);
     t.groups = static_cast<int>((n + t.rows - 1) / t.rows);
     return t;

@@ -156,6 +156,22 @@ def test_tables_of_a_few_rows(n, V, F, t):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("n,V,F,t", [(2000, 3, 20_001, "f32"), (2000, 70, 20_001, "bf16"), (400, 2, 100_000, "f32")])
+def test_tables_of_a_few_wide_rows(n, V, F, t):
+    check_gradient(n, V, F, t, 1, "outside", V == 3)
+
+
+@pytest.mark.gpu
+def test_an_infinite_scale_leaves_rows_of_zeros():
+    import torch
+    x = Mat(np.full((4, 40), 0.5), "f32")
+    out = new(3, 40, "f32")
+    B.embed(3, dev(np.array([-1, 2, 4])), 4, 40, x.p, 40, B.F32, float("inf"), out.p, 40, B.F32)
+    torch.cuda.synchronize()
+    assert (out.get() == np.array([[0.0], [np.inf], [0.0]])).all()
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("V", [7, 900])
 @pytest.mark.parametrize("n", [60, 9000])
 def test_rows_that_no_id_names_keep_their_bits(V, n):
