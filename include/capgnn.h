@@ -606,7 +606,7 @@ int capgnn_quantize_rows(int64_t n, int F, const void *X, int64_t ldx, int dtype
  * pass); Y: device [M x ldy]; all of out_dtype (CAPGNN_F32 or CAPGNN_BF16), each rounded once.  Y may be R (same pitch).
  * fp32 products of 2^28 multiply-adds and more are formed as CAPGNN_F32_PRODUCT_SPLIT forms them (above 3.38e38 a number counts as not finite).
  * K = 0: the sums are 0.  M, N, K < 2^31, a row of A or W shorter than 2^31 bytes.
- * Errors: EINVAL, EUNSUPPORTED (more than 2^22 tiles of 64 x 64 results), ENOMEM (workspace too small), EHIP. */
+ * Errors: EINVAL, EUNSUPPORTED (more than 2^22 tiles of 64 x 64 results; N > 2^26 where M <= 16), ENOMEM (workspace too small), EHIP. */
 size_t capgnn_linear_workspace_bytes(int64_t M, int64_t N, int64_t K, int dtype);
 int capgnn_linear(int64_t M, int64_t N, int64_t K, const void *A, int64_t lda, const float *a_scale, const void *W, int64_t ldw,
                   const float *w_scale, int dtype, const float *bias, int act, const void *R, int64_t ldr, void *U, int64_t ldu, void *Y,
@@ -634,7 +634,8 @@ int capgnn_tensors_destroy(capgnn_tensors *t);
  *   capgnn_grad_norm:    writes the norm.
  *   capgnn_grad_clip:    and multiplies every gradient by c = min(1, max_norm / norm).
  *   capgnn_clipped_step: and updates param <- param - lr * c * g (in float, rounded once to the param's type); the gradients stay.
- * max_norm >= 0 (infinity: c = 1).  A norm that is not finite (a gradient holds infinity or NaN) changes no gradient and no param.  No handle
+ * max_norm >= 0 (infinity: c = 1).  A norm that is not finite (a gradient holds infinity or NaN, or it exceeds a float) changes no
+ * gradient and no param.  No handle
  * state changes: calls on one list may be recorded, and may overlap if they write different memory and have workspaces of their own.
  * Errors: EINVAL (no params in the list), ENOMEM (workspace too small), EHIP. */
 size_t capgnn_grad_workspace_bytes(const capgnn_tensors *t);

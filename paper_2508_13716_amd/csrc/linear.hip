@@ -341,9 +341,13 @@ __device__ __forceinline__ void store_tile(const LinearArgs &g, raw16 *lds, int6
                     if (row >= g.M) continue;
                     float v[8];
                     ld_row<false, 8>(reinterpret_cast<const char *>(mine + p * ROWS * PITCH), 0, v);
-                    const float s = g.a_scale ? g.a_scale[row] : 1.f;
+                    if (g.a_scale) {                    // (one after the other: the scales' product may leave float's range where the result does not)
+                        const float s = g.a_scale[row];
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) v[e] = fmaf(v[e], s * scale[e], bias[e]);
+                        for (int e = 0; e < 8; ++e) v[e] *= s;
+                    }
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) v[e] = fmaf(v[e], scale[e], bias[e]);
                     if (g.U) st_row<OB, 8>(g.U + row * g.ldu + col * ES, 0, v);
 #pragma unroll
                     for (int e = 0; e < 8; ++e) {
@@ -800,6 +804,7 @@ extern "C" int capgnn_linear(int64_t M, int64_t N, int64_t K, const void *A, int
         // a line of a row per wave and turn
         const int64_t lines = (p.part_k * es + 127) / 128;
         const int waves = std::min<int>(FEW_WAVES, pow2_at_least(static_cast<int>(std::min<int64_t>(lines / 4 + 1, FEW_WAVES))));
+        if (N > int64_t(1) << 26) CG_FAIL(CAPGNN_EUNSUPPORTED, "linear: more than 2^26 results of a few rows");
         const dim3 grid(static_cast<unsigned>((N + 15) / 16), p.parts);
         auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(waves * 64), 0, st, g); };
         if (dtype == CAPGNN_F32) go(linear_few_kernel<CAPGNN_F32>);

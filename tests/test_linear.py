@@ -34,6 +34,12 @@ def test_linear_refuses(bad):
     refuse(B.EINVAL, B.linear, **fwd_args(**bad))
 
 
+@pytest.mark.parametrize("big", [dict(M=16, N=(1 << 26) + 1, K=8), dict(M=1, N=(1 << 31) - 1, K=1), dict(M=1 << 20, N=1 << 20, K=8)])
+def test_more_results_than_a_launch_has(big):
+    n = big["N"]
+    refuse(B.EUNSUPPORTED, B.linear, **fwd_args(**big, lda=8, ldw=8, R=None, U=None, ldy=n))
+
+
 def test_linear_workspace():
     for M, N, K, t in ((1, 16, 65_536, B.BF16), (100, 100, 16_384, B.F32), (40, 8, 40_000, B.E4M3)):
         need = B.linear_workspace_bytes(M, N, K, t)
@@ -173,6 +179,25 @@ def test_long_reductions(M, N, K, t):
     """large tiles whose reduction is split, rows on 4 bytes and rows that are not"""
     check(M, N, K, t, "f32", "none")
     check(M, N, K, t, "bf16", "gelu", residual=True, save=True, pad=3)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("M", [3, 70])
+@pytest.mark.parametrize("down,up", [(1e-30, 1e-13), (1e30, 1e9)])
+def test_scales_whose_product_leaves_floats_range(M, down, up):
+    """row scales of 8-bit operands: their product is below float's normal range, or above it, where the results are not"""
+    import torch
+    rng = np.random.default_rng(M)
+    N, K = 72, 512
+    big = 448.0 if down < 1 else 2.0 ** -9          # operands of the largest or of the smallest magnitude
+    a = big * rng.choice([-1.0, 1.0], (M, K))
+    w = big * rng.choice([-1.0, 1.0], (N, K))
+    sa, sw = held(np.full((1, M), down), "f32"), held(np.full((1, N), up), "f32")
+    A, W, sad, swd, Y = Mat(a, "e4m3"), Mat(w, "e4m3"), vec(sa), vec(sw), new(M, N, "f32")
+    B.linear(M, N, K, A.p, K, sad.p, W.p, K, swd.p, B.E4M3, None, B.ACT_NONE, None, 0, None, 0, Y.p, N, B.F32, *ws_of(B.linear_workspace_bytes(M, N, K, B.E4M3)))
+    torch.cuda.synchronize()
+    both = sa.T @ sw
+    close(Y.get(), a @ w.T * both, np.abs(a) @ np.abs(w).T * both * (K + 12) * EPS * 1.001, "Y")
 
 
 @pytest.mark.gpu
