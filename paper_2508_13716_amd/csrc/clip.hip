@@ -120,8 +120,9 @@ template <bool STEP, bool GB, bool PB> __device__ __forceinline__ void piece_app
 template <bool STEP> __global__ __launch_bounds__(256) void clip_apply_kernel(const ClipPiece *pieces, unsigned n, const double *sums,
                                                                               unsigned groups, float lr, float max_norm, float *norm_dev) {
     const double norm = whole_norm(sums, groups);
-    if (blockIdx.x == 0 && threadIdx.x == 0) *norm_dev = static_cast<float>(norm);
-    if (!(norm <= 1.7976931348623157e308)) return;           // infinity or NaN: nothing changes
+    const float shown = static_cast<float>(norm);
+    if (blockIdx.x == 0 && threadIdx.x == 0) *norm_dev = shown;
+    if (!(shown <= 3.402823466e38f)) return;                 // infinity or NaN: nothing changes
     const bool clip = norm > static_cast<double>(max_norm);
     if (!STEP && !clip) return;
     const double c = clip ? static_cast<double>(max_norm) / norm : 1.0;

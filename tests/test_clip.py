@@ -147,6 +147,19 @@ def test_a_norm_that_is_not_finite_changes_nothing(bad):
 
 
 @pytest.mark.gpu
+def test_a_norm_beyond_a_float_changes_nothing():
+    import torch
+    m = Model([100, 5000, 3], "f32", "f32", 1, seed=1)
+    for at in (m.at[0][0], m.at[1][0], m.at[1][0] + 77):
+        m.G[at] = 3e38                               # (each is a float; the norm, 5.2e38, is none)
+    g, q = m.G.clone(), m.P.clone()
+    B.clipped_step(m.list, 0.1, 1.0, m.norm, m.ws, m.size)
+    B.grad_clip(m.list, 1.0, m.norm, m.ws, m.size)
+    torch.cuda.synchronize()
+    assert torch.equal(m.G, g) and torch.equal(m.P, q) and m.norm.item() == np.inf
+
+
+@pytest.mark.gpu
 def test_squares_beyond_a_float_and_far_below_it():
     import torch
     for spread in (1e30, 1e-30):
