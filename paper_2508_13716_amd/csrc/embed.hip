@@ -12,6 +12,7 @@
 #include "grid.h"
 
 #include <algorithm>
+#include <type_traits>
 
 namespace capgnn {
 
@@ -427,9 +428,10 @@ template <bool BF16, int V> __global__ __launch_bounds__(256) void run_sums_kern
     else put_row<V>(a, cur, from, skip, acc);
 }
 
-// The runs that cross tiles: where one begins, its parts are added, by the tile's team if they are few, else by the whole workgroup, every team
-// those of a stretch of tiles.
-constexpr int JOIN_THREADS = 1024, JOIN_FEW = 16;
+// The runs that cross tiles: where one begins, its parts are added, by the tile's team if they are few, by a wave if its teams have a few batches
+// each of them, else by the whole workgroup, every team those of a stretch of tiles.  (us of the whole gradient, without the waves / with them:
+// 117176 rows of 2 into 1660 57 / 38, 60000 of 8 into 1000 66 / 33, 500000 of 8 into 5000 100 / 73, 300001 of 256 into 500009 no other.)
+constexpr int JOIN_THREADS = 1024, JOIN_FEW = 8, JOIN_STEPS = 4;
 
 template <int V> __global__ __launch_bounds__(JOIN_THREADS) void run_join_kernel(RunArgs a) {
     __shared__ float sums[JOIN_THREADS * V];
@@ -479,11 +481,68 @@ template <int V> __global__ __launch_bounds__(JOIN_THREADS) void run_join_kernel
         }
     }
     __syncthreads();
+    constexpr int PROBES = 4;           // of a thread at a time
+    using Few = std::integral_constant<int, V == 1 ? 16 : 8>;           // parts of a team on their way at a time
+    using Many = std::integral_constant<int, V == 8 ? 8 : 16>;
+    // what a team adds up of a run's parts: of tiles [first, end), behind what acc has
+    auto add_parts = [&](auto ahead, int64_t first, int64_t end, float (&acc)[V]) __attribute__((always_inline)) {
+        constexpr int AHEAD = ahead.value;
+        for (int64_t t = first; t < end; t += AHEAD) {
+            float v[AHEAD][V];
+#pragma unroll
+            for (int i = 0; i < AHEAD; ++i) ld_row<false, V>(part(min(t + i, end - 1), 0), 0, v[i]);
+#pragma unroll
+            for (int i = 0; i < AHEAD; ++i)
+                if (t + i < end) {
+#pragma unroll
+                    for (int e = 0; e < V; ++e) acc[e] += v[i][e];
+                }
+        }
+    };
+    {
+        // (of narrow rows many such runs begin in one workgroup)
+        const int wave = threadIdx.x / 64, own = 64 / a.lanes, mine = (threadIdx.x & 63) / a.lanes;
+        const int64_t most = int64_t(own) * Few::value * JOIN_STEPS;
+        for (int k = wave; own > 1 && k < n_many; k += JOIN_THREADS / 64) {
+            const int64_t tile = int64_t(blockIdx.x) * teams + many[k];
+            const uint32_t id = many_id[k];
+            int64_t m = JOIN_FEW;
+            for (bool more = true; more && m <= most;) {
+                const int64_t t = tile + 1 + m + (threadIdx.x & 63);
+                uint32_t probe[PROBES];
+#pragma unroll
+                for (int i = 0; i < PROBES; ++i) probe[i] = a.key[min(t + i * 64, a.tiles - 1) * a.R];
+#pragma unroll
+                for (int i = 0; i < PROBES; ++i)
+                    if (more) {
+                        const uint64_t out = __ballot(t + i * 64 >= a.tiles || probe[i] != id);
+                        m += out ? __ffsll(static_cast<unsigned long long>(out)) - 1 : 64;
+                        more = out == 0;
+                    }
+            }
+            if (m > most) continue;
+            const int64_t each = (m + own - 1) / own;
+            float acc[V];
+#pragma unroll
+            for (int e = 0; e < V; ++e) acc[e] = 0.f;
+            if (live) {
+                if (mine == 0) ld_row<false, V>(part(tile, 1), 0, acc);
+                add_parts(Few(), tile + 1 + min(each * mine, m), tile + 1 + min(each * (mine + 1), m), acc);
+            }
+            for (int half = own / 2; half; half /= 2) {
+#pragma unroll
+                for (int e = 0; e < V; ++e) acc[e] += __shfl_down(acc[e], half * a.lanes);
+            }
+            if (mine == 0 && live) put_row<V>(a, id, from, j - from, acc);
+            if ((threadIdx.x & 63) == 0) many[k] = -1;
+        }
+    }
+    __syncthreads();
     for (int k = 0; k < n_many; ++k) {
+        if (many[k] < 0) continue;
         const int64_t tile = int64_t(blockIdx.x) * teams + many[k];
         const uint32_t id = many_id[k];
         int64_t m = JOIN_FEW;               // tiles tile + 1 .. tile + m begin with this id (by the order every one between does)
-        constexpr int PROBES = 4;           // of a thread at a time
         for (bool more = true; more;) {
             if (threadIdx.x == 0) run_end = PROBES * JOIN_THREADS;
             __syncthreads();
@@ -507,18 +566,7 @@ template <int V> __global__ __launch_bounds__(JOIN_THREADS) void run_join_kernel
         for (int e = 0; e < V; ++e) acc[e] = 0.f;
         if (live) {
             if (team == 0) ld_row<false, V>(part(tile, 1), 0, acc);
-            constexpr int AHEAD = V == 8 ? 8 : 16;
-            for (int64_t t = first; t < end; t += AHEAD) {
-                float v[AHEAD][V];
-#pragma unroll
-                for (int i = 0; i < AHEAD; ++i) ld_row<false, V>(part(min(t + i, end - 1), 0), 0, v[i]);
-#pragma unroll
-                for (int i = 0; i < AHEAD; ++i)
-                    if (t + i < end) {
-#pragma unroll
-                        for (int e = 0; e < V; ++e) acc[e] += v[i][e];
-                    }
-            }
+            add_parts(Many(), first, end, acc);
         }
 #pragma unroll
         for (int e = 0; e < V; ++e) sums[e * JOIN_THREADS + threadIdx.x] = acc[e];

@@ -162,6 +162,14 @@ def test_tables_of_a_few_wide_rows(n, V, F, t):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("n,V,F", [(120_000, 1660, 2), (60_000, 1000, 8), (200_000, 900, 1), (150_000, 400, 40), (40_000, 300, 200)])
+@pytest.mark.parametrize("t", ["f32", "bf16"])
+def test_runs_of_every_length(n, V, F, t):
+    """narrow rows drawn by a power law: runs inside a tile, over a few, over what a wave adds, over more"""
+    check_gradient(n, V, F, t, 1, "power", F == 8)
+
+
+@pytest.mark.gpu
 def test_an_infinite_scale_leaves_rows_of_zeros():
     import torch
     x = Mat(np.full((4, 40), 0.5), "f32")
