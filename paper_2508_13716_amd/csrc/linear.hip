@@ -812,8 +812,12 @@ extern "C" int capgnn_linear(int64_t M, int64_t N, int64_t K, const void *A, int
         else go(linear_few_kernel<E4M3_FINE>);
     } else {
         const uintptr_t at = reinterpret_cast<uintptr_t>(A) | reinterpret_cast<uintptr_t>(W) | uintptr_t(g.lda) | uintptr_t(g.ldw);
-        const bool direct_rows = K > 0 && at % 4 == 0 && g.lda < most / 256 && g.ldw < most / 256;
-        const bool cut = dtype == CAPGNN_F32 && direct_rows && cut_pays(M, N, K);
+        const bool rows_of_4 = K > 0 && at % 4 == 0 && g.lda < most / 256 && g.ldw < most / 256;
+        const bool cut = dtype == CAPGNN_F32 && rows_of_4 && cut_pays(M, N, K);
+        // One or two steps pay for no loads ahead: through registers more workgroups share a compute unit (us, to LDS / through registers:
+        // 612000 x 47 x 100 bf16 104 / 80, x 128 82 / 65, 100000 x 256 x 100 44 / 37, 8192 x 4096 x 64 48 / 44, 16311 x 2503 x 2 fp32 74 / 63;
+        // two whole steps of larger tiles, 8192 x 4096 x 128 28.2 / 30.6; three steps and more the same or less).
+        const bool direct_rows = cut || (rows_of_4 && K * es >= (p.tile == 64 ? 257 : 256));
         const int tile = !direct_rows || (dtype == CAPGNN_F32 && !cut) ? 64 : p.tile;
         const int64_t tiles = (M + tile - 1) / tile * ((N + tile - 1) / tile);
         if (tiles > int64_t(1) << 22) CG_FAIL(CAPGNN_EUNSUPPORTED, "linear: more than 2^22 tiles of results");
