@@ -90,7 +90,7 @@ __device__ __forceinline__ void fill_share(const Fill &f, int64_t group, int64_t
 // digit), and the move.
 constexpr int SORT_THREADS = 256, SORT_WAVES = SORT_THREADS / 64, SORT_ITEMS = 4, SORT_TILE = SORT_THREADS * SORT_ITEMS;
 constexpr int SORT_BITS = 11;               // of a digit, at most
-constexpr int SMALL_THREADS = 1024, SMALL_WAVES = SMALL_THREADS / 64, SMALL_ITEMS = 8, SMALL_TILE = SMALL_THREADS * SMALL_ITEMS, SMALL_BITS = 8;
+constexpr int SMALL_THREADS = 1024, SMALL_WAVES = SMALL_THREADS / 64, SMALL_ITEMS = 8, SMALL_TILE = SMALL_THREADS * SMALL_ITEMS, SMALL_BITS = 8, SMALL_COUNT = 128;
 
 struct SortPass {
     int64_t n;
@@ -264,6 +264,24 @@ __global__ __launch_bounds__(SMALL_THREADS) void sort_small_kernel(SortPass s) {
     __shared__ uint32_t count[SMALL_WAVES][1 << SMALL_BITS], start[1 << SMALL_BITS], sum[SMALL_WAVES], keys[SMALL_TILE], poss[SMALL_TILE];
     if (blockIdx.x >= 1) return fill_share(s.fill, blockIdx.x - 1, gridDim.x - 1);
     const int n = static_cast<int>(s.n), wave = threadIdx.x / 64, digits = 1 << SMALL_BITS;
+    if (n <= SMALL_COUNT) {             // a key's place is the number of keys before it
+        const int t = threadIdx.x;
+        const uint32_t mine = t < n ? sort_key(s, t) : ~0u;
+        if (t < SMALL_COUNT) keys[t] = mine;
+        __syncthreads();
+        if (t >= n) return;
+        int to = 0;
+        for (int j = 0; j < n; j += 8) {
+            uint32_t k[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) k[e] = keys[j + e];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) to += k[e] < mine || (k[e] == mine && j + e < t);
+        }
+        s.key_out[to] = mine;
+        s.pos_out[to] = t;
+        return;
+    }
     const int first = wave * (SMALL_ITEMS * 64) + (threadIdx.x & 63);
     uint32_t key[SMALL_ITEMS], pos[SMALL_ITEMS], rank[SMALL_ITEMS];
     bool on[SMALL_ITEMS];
@@ -604,15 +622,15 @@ struct TableArgs {
     float *part;                // [workgroups][V][F]
 };
 
-constexpr int TABLE_AHEAD = 16;         // rows of a team on their way
+constexpr int TABLE_THREADS = 256, TABLE_AHEAD = 16;         // rows of a team on their way
 
-template <bool BF16, int V> __global__ __launch_bounds__(256, 1) void table_sums_kernel(TableArgs a) {
+template <bool BF16, int V> __global__ __launch_bounds__(TABLE_THREADS, 1) void table_sums_kernel(TableArgs a) {
     extern __shared__ float tables[];
-    const int lane = threadIdx.x & (a.lanes - 1), teams = blockDim.x / a.lanes, team = threadIdx.x / a.lanes;
+    const int lane = threadIdx.x & (a.lanes - 1), teams = TABLE_THREADS / a.lanes, team = threadIdx.x / a.lanes;
     const int vec = blockIdx.y * a.chunk + lane, j = vec * V;
     const bool live = lane < a.chunk && j < a.F;
     const int from = min(j, a.F - V), size = a.V * a.chunk * V;         // of a copy
-    for (int i = threadIdx.x; i < teams * size; i += blockDim.x) tables[i] = -0.f;
+    for (int i = threadIdx.x; i < teams * size; i += TABLE_THREADS) tables[i] = -0.f;
     __syncthreads();
     float *mine = tables + team * size + lane * V;
     const int64_t first = blockIdx.x * a.rows, end = min(first + a.rows, a.n);
@@ -651,7 +669,7 @@ template <bool BF16, int V> __global__ __launch_bounds__(256, 1) void table_sums
         }
     }
     __syncthreads();
-    for (int i = threadIdx.x; i < size; i += blockDim.x) {
+    for (int i = threadIdx.x; i < size; i += TABLE_THREADS) {
         float sum = tables[i];
         for (int q = 1; q < teams; ++q) sum += tables[q * size + i];
         // entry i: element e of vector k of row r; a row's last vector has its elements from the row's end backwards
@@ -701,24 +719,23 @@ static int run_tile(int64_t n, const EmbedShape &s) {
     return static_cast<int>(std::max<int64_t>(R, (n >> 22) + 1));
 }
 
-// A table in LDS: workgroups, threads and LDS of each; 0 workgroups where the table is too large for it
+// A table in LDS: workgroups and LDS of each; 0 workgroups where sorting is the shorter way.  What it costs at any n grows with the copies of
+// all teams, which are cleared and added up; bf16 rows in several stretches read twice as many places of LDS per byte.  (us, LDS / sorted: 100000
+// fp32 rows of 250 into 35 47 / 60, 3000 into 35 25 / 21, into 18 17 / 23, 200 rows of 64 into 40 20 / 16, into 20 12 / 14; bf16 rows of 1000
+// into 4: 9000 25 / 36, 30000 45 / 52, 300000 277 / 227; 100000 fp32 rows of 250 into 70, two teams of 64 lanes a workgroup, 89 / 56.)
 struct TableShape {
-    int groups, threads, chunk;
+    int groups, chunk;
     int64_t rows;
     size_t lds;
 };
 static TableShape table_shape(int64_t n, int64_t V, const EmbedShape &s, int F) {
     TableShape t{};
-    const int vectors = (F + s.V - 1) / s.V;
-    t.chunk = std::min(vectors, s.lanes);
-    // copies for 128 lanes at least, so that a compute unit has enough rows on their way (V <= 71 of fp32, 35 of bf16 rows of whole vectors)
-    for (t.threads = 256; t.threads >= 128; t.threads /= 2) {
-        t.lds = size_t(V) * t.chunk * s.V * sizeof(float) * (t.threads / s.lanes);
-        if (t.lds <= 156 * 1024) break;
-    }
-    if (t.threads < 128 || V > 4096 || V * F > int64_t(1) << 27) return {};      // (the join's grid: fewer than 2^32 threads)
-    const int64_t teams = t.threads / s.lanes, room = std::min<int64_t>(160 * 1024 / std::max<size_t>(t.lds, 1), 8);
-    const int64_t most = std::max<int64_t>(NUM_CU * room / s.chunks, 1);
+    const int64_t vectors = (F + s.V - 1) / s.V, teams = TABLE_THREADS / s.lanes;
+    t.chunk = static_cast<int>(std::min<int64_t>(vectors, s.lanes));
+    t.lds = size_t(V) * t.chunk * s.V * sizeof(float) * teams;
+    if (t.lds > size_t(n <= SMALL_TILE ? 80 : 156) * 1024 || (s.V == 8 && s.chunks > 1 && n > 32768)) return {};
+    if (V * F > int64_t(1) << 27) return {};        // (the join's grid: fewer than 2^32 threads)
+    const int64_t room = std::min<int64_t>(160 * 1024 / t.lds, 8), most = std::max<int64_t>(NUM_CU * room / s.chunks, 1);
     t.rows = std::max<int64_t>((n + most - 1) / most, teams * TABLE_AHEAD);
     t.groups = static_cast<int>((n + t.rows - 1) / t.rows);
     return t;
@@ -826,7 +843,7 @@ extern "C" int capgnn_embed_bwd(int64_t n, const int64_t *ids, int64_t V, int F,
         const dim3 grid(t.groups, e.chunks);
         auto go = [&](auto kernel) {
             if (t.lds > 64 * 1024) CG_HIP(hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(t.lds)));
-            hipLaunchKernelGGL(kernel, grid, dim3(t.threads), t.lds, st, a);
+            hipLaunchKernelGGL(kernel, grid, dim3(TABLE_THREADS), t.lds, st, a);
             CG_HIP(hipGetLastError());
             return static_cast<int>(CAPGNN_OK);
         };

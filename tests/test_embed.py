@@ -162,6 +162,21 @@ def test_tables_of_a_few_wide_rows(n, V, F, t):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("n,V,F,t", [(8192, 20, 64, "f32"), (8192, 21, 64, "f32"), (8193, 39, 64, "f32"), (8193, 40, 64, "f32"), (9000, 156, 1, "f32"), (9000, 157, 1, "f32"),
+                                     (50, 80, 1, "f32"), (50, 81, 1, "f32"), (32_768, 3, 520, "bf16"), (32_769, 3, 520, "bf16"), (9000, 18, 250, "bf16"), (9000, 20, 250, "bf16")])
+def test_tables_at_the_borders_of_a_workgroups_memory(n, V, F, t):
+    check_gradient(n, V, F, t, 1, "outside", False)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("n", [1, 2, 63, 64, 65, 127, 128, 129, 130, 1025])
+@pytest.mark.parametrize("V", [200, 3_000_000])
+def test_a_few_ids(n, V):
+    check_gradient(n, V, 9, "f32", 1, "outside", V > 200)
+    check_gradient(n, V, 9, "bf16", 0, "one", True)
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("n,V,F", [(120_000, 1660, 2), (60_000, 1000, 8), (200_000, 900, 1), (150_000, 400, 40), (40_000, 300, 200)])
 @pytest.mark.parametrize("t", ["f32", "bf16"])
 def test_runs_of_every_length(n, V, F, t):
