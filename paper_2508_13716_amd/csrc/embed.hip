@@ -3,7 +3,7 @@
 // Both move memory and compute next to nothing.  The gradient's sums have to be the same every time, so no float is added atomically:
 // positions are sorted by id (a stable radix sort of our own), and teams of lanes, 16 bytes of a row each, walk tiles of the sorted list
 // and sum runs of equal ids in registers.  A run inside a tile goes straight to the table; one that crosses tiles leaves a part per tile,
-// and one workgroup a run adds its parts in order.  Rows that no id names are zeroed first; that is shared out over the sort's launches,
+// added in their order by a team, a wave or a workgroup.  Rows that no id names are zeroed first; that is shared out over the sort's launches,
 // which wait for memory more than they use it.
 // us: 300001 bf16 rows of 256 into 500009 fp32 ones (0.67 GB) 212, of them 118 for six launches that sort and zero 512 MB (the zeros shared out
 // over four of them; over all six 123: the moves have room for three workgroups a compute unit), 82 for the sums (rows of 512 bytes
