@@ -4,8 +4,8 @@
 //
 // Memory bounds them: a row is read once, held in registers through its sums and written once.  A row belongs to a team: as many
 // lanes of a wave as it has vectors of 16 bytes (a power of two), up to 64, or a workgroup for wide rows.  Where a row is no whole number
-// of vectors its last lane takes the row's last V elements: those that the lane before it has, too, are left out of the sums and stored
-// twice with the same value.  Every sum has a fixed order.
+// of vectors its last lane takes the row's last V elements: those that the lane before it has, too, are left out of the sums (passed over, not
+// multiplied by 0: one may be an infinity) and stored twice with the same value.  Every sum has a fixed order.
 // us (of the bytes a pass cannot do without): 180000 x 602 fp32 with the residual 331 (5.2 TB/s), 16384 x 4096 bf16 gradient with dH and dw
 // 112, and 7 for the join of dw's parts (4.5 TB/s), one row of 4096 into 8 bits 3.4.  More than 16 elements per lane of the gradient at
 // 1024 threads (rows above 16384) do not fit the registers: up to 540 bytes of scratch memory a thread there.
@@ -83,7 +83,7 @@ template <bool BF16, int V, int K, int T> __global__ __launch_bounds__(T == 64 ?
 #pragma unroll
         for (int i = 0; i < K; ++i)
 #pragma unroll
-            for (int e = 0; e < V; ++e) sum = fmaf(e < s.skip[i] ? 0.f : h[i][e], h[i][e], sum);
+            for (int e = 0; e < V; ++e) sum = e < s.skip[i] ? sum : fmaf(h[i][e], h[i][e], sum);
         sum = team_sum(sum, WIDE ? 64 : lanes);
         if constexpr (WIDE) {
             if ((threadIdx.x & 63) == 0) part[wave] = sum;
@@ -204,7 +204,7 @@ template <bool BF16, int V, int K, int T> __global__ __launch_bounds__(T == 64 ?
                 acc[i][e] = fmaf(g[i][e], hat, acc[i][e]);
                 g[i][e] *= w[e];
                 h[i][e] = hat;
-                sum = fmaf(e < s.skip[i] ? 0.f : g[i][e], hat, sum);
+                sum = e < s.skip[i] ? sum : fmaf(g[i][e], hat, sum);
             }
         }
         sum = team_sum(sum, WIDE ? 64 : lanes);

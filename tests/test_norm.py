@@ -303,3 +303,32 @@ def test_the_gradient_of_no_rows_is_zero():
         B.rmsnorm_bwd(0, F, None, F, B.F32, None, F, B.F32, None, None, None, 0, None, F, dw.p, None, 0)
         torch.cuda.synchronize()
         assert (dw.get() == 0).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("F", [5, 6, 9, 41, 100, 602, 2049, 8193, 32_767])
+@pytest.mark.parametrize("t", ["f32", "bf16"])
+@pytest.mark.parametrize("way", ["X", "R", "sum"])
+def test_an_infinity_among_elements_that_two_vectors_share(F, t, way):
+    """a row's last vector ends where the row does and repeats elements of the one before: an infinity at each of its places"""
+    import torch
+    places = list(range(max(F - 8, 0), F)) + [0]
+    n = len(places)
+    rows, sign = np.arange(n), np.where(np.arange(n) % 2, -1.0, 1.0)
+    x, r = np.ones((n, F)), np.zeros((n, F))
+    if way == "sum":                                 # (two numbers whose sum is none)
+        x[rows, places] = r[rows, places] = sign * 3e38
+    else:
+        (x if way == "X" else r)[rows, places] = sign * np.inf
+    X, R, H, out, rstd = Mat(x, t), Mat(r, t), new(n, F, t), new(n, F, "f32"), new(1, n, "f32")
+    q, s = new(n, F, "e4m3"), new(1, n, "f32")
+    B.rmsnorm(n, F, X.p, F, R.p, F, H.p, F, CODE[t], None, 1e-6, out.p, F, B.F32, None, rstd.p)
+    B.rmsnorm(n, F, X.p, F, R.p, F, None, 0, CODE[t], None, 1e-6, q.p, F, B.E4M3, s.p)
+    torch.cuda.synchronize()
+    there = np.zeros((n, F), bool)
+    there[rows, places] = True
+    y = out.get()
+    assert (rstd.get()[0] == 0).all()
+    assert np.isnan(y[there]).all() and (y[~there] == 0).all()          # infinity * 0, and 1 * 0
+    assert np.array_equal(H.get()[there], sign[np.nonzero(there)[0]] * np.inf) and (H.get()[~there] == 1).all()
+    assert np.isnan(s.get()).all() and np.isnan(q.get()).all()
