@@ -611,7 +611,7 @@ template <int V> __global__ __launch_bounds__(JOIN_THREADS) void run_join_kernel
 // after the other, each lane its columns; a workgroup's copies are added at its end, and the workgroups' sums by a second launch, in
 // their order.  (612000 rows of 100 floats into 47: 102 us by sorting, of which the sums alone take 57; here 64, 3.9 TB/s, and 5 for the
 // join; with one batch of rows on its way instead of two 80.)  What nothing was added to is -0,
-// which changes no sum.
+// which changes no sum and is none: a -0 of dY is added as 0.
 struct TableArgs {
     int64_t n;
     int V, F, lanes, chunk;     // a workgroup takes `chunk` vectors of a row (at most 64)
@@ -655,7 +655,7 @@ template <bool BF16, int V> __global__ __launch_bounds__(TABLE_THREADS, 1) void 
 #pragma unroll
                     for (int e = 0; e < V; ++e) v[e] = t[e];
 #pragma unroll
-                    for (int e = 0; e < V; ++e) t[e] = v[e] + row[set][u].get(e);
+                    for (int e = 0; e < V; ++e) t[e] = v[e] + (row[set][u].get(e) + 0.f);        // (no -0: that is the mark)
                 }
             }
         };
@@ -694,8 +694,9 @@ __global__ __launch_bounds__(256) void table_join_kernel(const float *part, int 
     if (q == 0 && j < size) {
         for (int i = 1; i < 16; ++i) v += s[i][c];
         float *out = dtable + j / F * lddt + j % F;
-        if (!accumulate) *out = v * scale + 0.f;
-        else if (__float_as_uint(v) != 0x80000000u) *out += v * scale;
+        const bool added = __float_as_uint(v) != 0x80000000u;       // (nothing stays nothing at a scale that is infinite or NaN, too)
+        if (!accumulate) *out = added ? v * scale + 0.f : 0.f;
+        else if (added) *out += v * scale;
     }
 }
 

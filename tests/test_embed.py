@@ -318,3 +318,27 @@ def test_two_streams_with_a_workspace_each():
         np.add.at(want, ids, x)
         np.add.at(mass, ids, np.abs(x))
         close(dtable.get(), want, mass * (np.bincount(ids, minlength=V)[:, None] + 2) * EPS + np.abs(want) * 2 * EPS)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("scale", [np.inf, -np.inf, np.nan])
+@pytest.mark.parametrize("n,V", [(60, 7), (60, 900), (9000, 7), (9000, 900), (300_000, 7)])
+@pytest.mark.parametrize("F,t", [(3, "f32"), (40, "f32"), (41, "bf16")])
+@pytest.mark.parametrize("accumulate", [0, 1])
+def test_a_scale_that_is_not_finite_leaves_the_gradient_of_rows_that_no_id_names(scale, n, V, F, t, accumulate):
+    """tables in LDS and sorted ids alike: such rows are zeros, or what they were; a sum of zeros, -0 among them, is 0 * scale"""
+    import torch
+    ids = np.arange(n) % 5                           # 0: a sum above 0, 1: one of -0, 2: one that cancels, 3 and 4: no row
+    ids = np.where(ids == 3, -1, np.where(ids == 4, V, ids))
+    x = np.full((n, F), 0.5)
+    x[ids == 1] = -0.0
+    x[np.flatnonzero(ids == 2)[::2]] = -0.5
+    assert (ids == 2).sum() % 2 == 0
+    dtable = Mat(np.full((V, F), 3.0), "f32", F + 1)
+    ws, size = ws_of(B.embed_bwd_workspace_bytes(n, V, F))
+    B.embed_bwd(n, dev(ids), V, F, Mat(x, t).p, F, CODE[t], scale, dtable.p, F + 1, accumulate, ws, size)
+    torch.cuda.synchronize()
+    got = dtable.get()
+    assert (got[3:] == (3.0 if accumulate else 0.0)).all()
+    assert np.isnan(got[1:3]).all()
+    assert np.isnan(got[0]).all() if np.isnan(scale) else (got[0] == scale).all()
