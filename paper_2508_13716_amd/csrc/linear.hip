@@ -12,7 +12,7 @@
 // leaves them (8192^3 bf16: busy 68 % of the cycles, at 1.6 GHz); the 8-bit one spends a quarter of its time on results, whose
 // arithmetic no other workgroup on the compute unit hides (busy 37 %, at 2.0 GHz).
 #include "rows.h"
-#include "grid.h"
+#include "linear_plan.h"
 
 #include <algorithm>
 #include <type_traits>
@@ -584,7 +584,7 @@ template <int DT> __device__ __forceinline__ acc4 multiply16(raw16 w, raw16 a, a
     }
 }
 
-constexpr int FEW_WAVES = 16, FEW_AHEAD = 8;        // waves of a workgroup, at most; units of a row on their way at a time, per lane
+constexpr int FEW_AHEAD = 8;            // units of a row on their way at a time, per lane
 
 template <int DT> __global__ __launch_bounds__(FEW_WAVES * 64) void linear_few_kernel(LinearArgs g) {
     constexpr int E = 16 / BYTES<DT>;
@@ -720,49 +720,6 @@ template <class F> static void with_types(int dtype, int out_dtype, bool cut, F 
     else o ? f(std::integral_constant<int, CAPGNN_E4M3>(), Y()) : f(std::integral_constant<int, E4M3_FINE>(), N());
 }
 
-// How a product runs
-struct LinearPlan {
-    int tile;                   // rows and columns of a tile; 0: a few rows
-    int parts;                  // of the reduction
-    int64_t part_k;
-};
-constexpr int FEW_ROWS = 16;            // (32 by two such groups: 32 x 4096 x 4096 bf16 15.3 us, 33 rows by tiles of 64 in parts 13.5)
-
-static bool cut_pays(int64_t M, int64_t N, int64_t K) { return M * N >= ((int64_t(1) << 28) + K - 1) / std::max<int64_t>(K, 1); }
-
-static LinearPlan linear_plan(int64_t M, int64_t N, int64_t K, int es) {
-    LinearPlan p{0, 1, K};
-    auto tiles = [&](int64_t b) { return ((M + b - 1) / b) * ((N + b - 1) / b); };
-    const int64_t lines = (K * es + 127) / 128;         // steps
-    int64_t groups, most;
-    if (M <= FEW_ROWS) {
-        groups = (N + 15) / 16;
-        most = lines / 32;
-    } else {
-        // Large tiles read their operands less often, where there are enough of them for the compute units, little of them lies beyond the matrix
-        // and the reduction is long enough for what a workgroup alone on its compute unit cannot overlap: its first loads and its results.
-        // us, tiles of 256 / 128 / 64: 8192 x 8192 x 2048 bf16 298 / 329 / 463, x 1024 206 / 208 / 272, x 256 133 / 111 / 147; x 1024 fp32
-        // 647 / 717 / 1047, x 256 222 / 215 / 305; x 1024 e4m3 166 / 145 / 187, x 2048 216 / 204 / 266; 612000 x 47 x 256 bf16 274 / 157 / 107,
-        // fp32 660 / 296 / 233; 3000^3 bf16 (144 tiles of 256) 123 with them, 105 / 117 with the others.
-        auto wide = [&](int64_t b) { return tiles(b) * b * b * 4 <= tiles(b / 2) * (b / 2) * (b / 2) * 5; };
-        // Tiles of 128 in parts of 32 steps and more, where that gives every compute unit one: 6095 x 376 x 5188 fp32 177, tiles of 64 281;
-        // 1500 x 1500 x 6000 bf16 60 / 84; 100 x 8192 x 8192 bf16 45.5 / 44.3, 300 x 4096 x 8192 37.6 / 47.6 (with parts of 16, 2048 x 1024 x 2048
-        // bf16 23.8 / 17.7).
-        const int64_t split = tiles(128) < 256 ? std::min<int64_t>(std::min<int64_t>(lines / 32, 512 / tiles(128)), 32) : 1;
-        p.tile = tiles(256) >= 200 && wide(256) && lines >= (es == 1 ? 32 : 16) ? 256 : tiles(128) * split >= 256 && wide(128) ? 128 : 64;
-        groups = tiles(p.tile);
-        most = p.tile == 64 ? lines / 8 : p.tile == 128 ? split : 1;
-    }
-    // (enough workgroups for the chip, parts of 8 steps or more; of a few rows 32)
-    const int64_t parts = std::min<int64_t>(std::min<int64_t>(most, (p.tile ? 512 : 256) / groups), 32);
-    if (parts > 1) {
-        const int64_t each = (lines + parts - 1) / parts;
-        p.part_k = each * (128 / es);
-        p.parts = static_cast<int>((lines + each - 1) / each);
-        if (p.parts == 1) p.part_k = K;
-    }
-    return p;
-}
 static int operand_bytes(int dtype) { return dtype == CAPGNN_E4M3 ? 1 : elem_bytes(dtype); }
 static int64_t part_pitch(int64_t N) { return (N + 7) / 8 * 8; }
 
@@ -800,29 +757,21 @@ extern "C" int capgnn_linear(int64_t M, int64_t N, int64_t K, const void *A, int
                        static_cast<const char *>(R), static_cast<char *>(U), static_cast<char *>(Y), ldr * os, ldu * os, ldy * os,
                        out_dtype == CAPGNN_BF16, p.parts > 1 ? static_cast<float *>(ws) : nullptr, part_pitch(N), p.part_k};
     hipStream_t st = static_cast<hipStream_t>(stream);
-    if (p.tile == 0) {
-        // a line of a row per wave and turn
-        const int64_t lines = (p.part_k * es + 127) / 128;
-        const int waves = std::min<int>(FEW_WAVES, pow2_at_least(static_cast<int>(std::min<int64_t>(lines / 4 + 1, FEW_WAVES))));
+    const uintptr_t at = reinterpret_cast<uintptr_t>(A) | reinterpret_cast<uintptr_t>(W) | uintptr_t(g.lda) | uintptr_t(g.ldw);
+    const LinearWay way = linear_way(p, M, N, K, es, K > 0 && at % 4 == 0 && g.lda < most / 256 && g.ldw < most / 256);
+    if (way.tile == 0) {
         if (N > int64_t(1) << 26) CG_FAIL(CAPGNN_EUNSUPPORTED, "linear: more than 2^26 results of a few rows");
         const dim3 grid(static_cast<unsigned>((N + 15) / 16), p.parts);
-        auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(waves * 64), 0, st, g); };
+        auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(way.waves * 64), 0, st, g); };
         if (dtype == CAPGNN_F32) go(linear_few_kernel<CAPGNN_F32>);
         else if (dtype == CAPGNN_BF16) go(linear_few_kernel<CAPGNN_BF16>);
         else go(linear_few_kernel<E4M3_FINE>);
     } else {
-        const uintptr_t at = reinterpret_cast<uintptr_t>(A) | reinterpret_cast<uintptr_t>(W) | uintptr_t(g.lda) | uintptr_t(g.ldw);
-        const bool rows_of_4 = K > 0 && at % 4 == 0 && g.lda < most / 256 && g.ldw < most / 256;
-        const bool cut = dtype == CAPGNN_F32 && rows_of_4 && cut_pays(M, N, K);
-        // One or two steps pay for no loads ahead: through registers more workgroups share a compute unit (us, to LDS / through registers:
-        // 612000 x 47 x 100 bf16 104 / 80, x 128 82 / 65, 100000 x 256 x 100 44 / 37, 8192 x 4096 x 64 48 / 44, 16311 x 2503 x 2 fp32 74 / 63;
-        // two whole steps of larger tiles, 8192 x 4096 x 128 28.2 / 30.6; three steps and more the same or less).
-        const bool direct_rows = cut || (rows_of_4 && K * es >= (p.tile == 64 ? 257 : 256));
-        const int tile = !direct_rows || (dtype == CAPGNN_F32 && !cut) ? 64 : p.tile;
+        const int tile = way.tile;
         const int64_t tiles = (M + tile - 1) / tile * ((N + tile - 1) / tile);
         if (tiles > int64_t(1) << 22) CG_FAIL(CAPGNN_EUNSUPPORTED, "linear: more than 2^22 tiles of results");
         const dim3 grid(static_cast<unsigned>(tiles), p.parts);
-        with_types(dtype, out_dtype, cut, [&](auto d, auto o) {
+        with_types(dtype, out_dtype, way.cut, [&](auto d, auto o) {
             auto direct = [&](auto wr, auto wc, auto tm, auto tn, auto nb) {
                 hipLaunchKernelGGL((linear_direct_kernel<d.value, o.value, wr.value, wc.value, tm.value, tn.value, nb.value>), grid,
                                    dim3(wr.value * wc.value * 64), 0, st, g);
@@ -841,9 +790,9 @@ extern "C" int capgnn_linear(int64_t M, int64_t N, int64_t K, const void *A, int
                 if constexpr (d.value != CAPGNN_F32) direct(I2, I2, I2, I2, I2);
             } else {
                 if constexpr (d.value != F32_CUT) {
-                    if (!direct_rows) hipLaunchKernelGGL((linear_tile_kernel<d.value, o.value, 2, 2, 1, 1>), grid, dim3(256), 0, st, g);
+                    if (!way.direct) hipLaunchKernelGGL((linear_tile_kernel<d.value, o.value, 2, 2, 1, 1>), grid, dim3(256), 0, st, g);
                 }
-                if (direct_rows) direct(I2, I2, I1, I1, I3);
+                if (way.direct) direct(I2, I2, I1, I1, I3);
             }
         });
     }
