@@ -604,7 +604,8 @@ int capgnn_quantize_rows(int64_t n, int F, const void *X, int64_t ldx, int dtype
  * lies below 2^-13 of the largest (some 1e-5 of a sum's size; with a float result nothing is dropped).
  * bias: device float[N] or NULL.  act: CAPGNN_ACT_*.  R: device [M x ldr] or NULL; U: device [M x ldu] or NULL (kept for the backward
  * pass); Y: device [M x ldy]; all of out_dtype (CAPGNN_F32 or CAPGNN_BF16), each rounded once.  Y may be R (same pitch).
- * fp32 products of 2^28 multiply-adds and more are formed as CAPGNN_F32_PRODUCT_SPLIT forms them (above 3.38e38 a number counts as not finite).
+ * fp32 products of 2^28 multiply-adds and more with M > 16 are formed as CAPGNN_F32_PRODUCT_SPLIT forms them (what is not finite, and what lies
+ * above 3.38e38, makes NaN there).  Every activation lets NaN through, ReLU too (the layers' ReLU and capgnn_gemm's make 0 of it).
  * K = 0: the sums are 0.  M, N, K < 2^31, a row of A or W shorter than 2^31 bytes.
  * Errors: EINVAL, EUNSUPPORTED (more than 2^22 tiles of 64 x 64 results; N > 2^26 where M <= 16), ENOMEM (workspace too small), EHIP. */
 size_t capgnn_linear_workspace_bytes(int64_t M, int64_t N, int64_t K, int dtype);
@@ -615,7 +616,7 @@ int capgnn_linear(int64_t M, int64_t N, int64_t K, const void *A, int64_t lda, c
 /* The epilogue's gradient: dU = dY * act'(U), dbias[j] = sum_i dU[i,j] (of the unrounded dU, in a fixed order).  (R's gradient is dY.  What
  * is left are capgnn_gemm's products of dU: dA = dU W, capgnn_gemm(0, 0, M, K, N, dU, W); dW = dU^T A, capgnn_gemm(1, 0, N, K, M, dU, A).)
  * dY, U, dU: device [M x lddy / ldu / lddu] of `dtype` (CAPGNN_F32 or CAPGNN_BF16); U may be NULL for CAPGNN_ACT_NONE; dU may be dY or U
- * (same pitch), or NULL; dbias: device float[N] or NULL.  The slope of ReLU at 0 is 0. */
+ * (same pitch), or NULL; dbias: device float[N] or NULL.  The slope of ReLU at 0 is 0, every slope at NaN is NaN. */
 size_t capgnn_linear_act_bwd_workspace_bytes(int64_t M, int64_t N);
 int capgnn_linear_act_bwd(int64_t M, int64_t N, const void *dY, int64_t lddy, const void *U, int64_t ldu, int dtype, int act, void *dU,
                           int64_t lddu, float *dbias, void *ws, size_t ws_bytes, void *stream);

@@ -68,13 +68,13 @@ __device__ __forceinline__ float normal(float u, float *bell) {
 }
 template <int ACT> __device__ __forceinline__ float act_of(float u) {
     float bell;
-    if constexpr (ACT == CAPGNN_ACT_RELU) return u > 0.f ? u : 0.f;
+    if constexpr (ACT == CAPGNN_ACT_RELU) return u <= 0.f ? 0.f : u;           // (a NaN stays one)
     else if constexpr (ACT == CAPGNN_ACT_GELU) return u * normal(u, &bell);
     else if constexpr (ACT == CAPGNN_ACT_SILU) return u * logistic(u);
     else return u;
 }
 template <int ACT> __device__ __forceinline__ float act_slope(float u) {
-    if constexpr (ACT == CAPGNN_ACT_RELU) return u > 0.f ? 1.f : 0.f;
+    if constexpr (ACT == CAPGNN_ACT_RELU) return u > 0.f ? 1.f : u <= 0.f ? 0.f : u;
     else if constexpr (ACT == CAPGNN_ACT_GELU) {
         float bell;
         const float phi = normal(u, &bell);

@@ -252,6 +252,54 @@ def test_what_is_not_finite_in_a_large_fp32_product(pad):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("kind", ["none", "relu", "gelu", "silu"])
+@pytest.mark.parametrize("M,N,K,t", [(2, 40, 100, "bf16"), (30, 50, 130, "f32"), (30, 50, 2, "e4m3"), (300, 400, 200, "bf16"), (1030, 520, 513, "f32")])
+def test_every_activation_lets_nan_through(M, N, K, t, kind):
+    """a few rows, tiles through registers and straight to LDS, fp32 in three pieces (where an infinity may count as NaN, too)"""
+    import torch
+    a, w = np.ones((M, K)), np.ones((N, K))
+    a[M - 1, K - 1] = np.nan
+    w[N - 1, 0] = np.nan
+    if t != "e4m3":
+        a[0, K // 2] = np.inf
+    for residual in (False, True):
+        for to in ("f32", "bf16"):
+            Y, U, R = new(M, N, to), new(M, N, to), Mat(np.ones((M, N)), to) if residual else None
+            B.linear(M, N, K, Mat(a, t).p, K, None, Mat(w, t).p, K, None, CODE[t], None, ACTS[kind], p(R), N, U.p, N, Y.p, N, CODE[to],
+                     *ws_of(B.linear_workspace_bytes(M, N, K, CODE[t])))
+            torch.cuda.synchronize()
+            y, u, add = Y.get(), U.get(), 1.0 if residual else 0.0
+            assert np.array_equal(np.isnan(u), np.isnan(y))
+            assert np.isnan(y[M - 1]).all() and np.isnan(y[:, N - 1]).all()
+            first = 1 if t != "e4m3" else 0
+            assert first == 0 or not np.isfinite(y[0]).any()
+            rest = y[first:M - 1, :N - 1]
+            want = held(act(kind, np.full_like(rest, K)) + add, to)
+            close(rest, want, np.abs(want) * (16 * EPS + 2 * HALF[to]), kind)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("t", ["f32", "bf16"])
+@pytest.mark.parametrize("kind", ["relu", "gelu", "silu"])
+@pytest.mark.parametrize("M,N", [(3, 5), (40, 260)])
+def test_the_slope_at_nan_is_nan(M, N, t, kind):
+    import torch
+    u = np.ones((M, N))
+    u[0, 0], u[M - 1, 3], u[1, 1] = np.nan, np.nan, -np.inf
+    if kind != "relu":
+        u[1, 1] = -1.0
+    dU, db = new(M, N, t), new(1, N, "f32")
+    B.linear_act_bwd(M, N, Mat(np.ones((M, N)), t).p, N, Mat(u, t).p, N, CODE[t], ACTS[kind], dU.p, N, db.p, *ws_of(B.linear_act_bwd_workspace_bytes(M, N)))
+    torch.cuda.synchronize()
+    want = slope(kind, u)
+    want[np.isnan(u)] = np.nan
+    if kind == "relu":
+        want[1, 1] = 0.0
+    close(dU.get(), want, 1.001 * (16 * EPS * (1 + np.abs(np.where(np.isfinite(u), u, 0))) + np.abs(want) * HALF[t]), "dU")
+    assert np.isnan(db.get()[0, [0, 3]]).all() and np.isfinite(np.delete(db.get()[0], [0, 3])).all()
+
+
+@pytest.mark.gpu
 def test_no_rows():
     import torch
     for N in (1, 70, 1009):
