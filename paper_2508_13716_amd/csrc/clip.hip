@@ -117,6 +117,23 @@ template <bool STEP, bool GB, bool PB> __device__ __forceinline__ void piece_app
     }
 }
 
+// The same where a float has fewer bits of the factor, or none (a norm of 1e37 and a small limit): its product with a gradient of that size is
+// an ordinary number.  Formed in double, rounded to float, then to the tensor's type.
+template <bool STEP> __device__ __forceinline__ void piece_apply_small(const ClipPiece &q, double factor) {
+    const int count = static_cast<int>(q.count);
+    for (int j = threadIdx.x; j < count; j += 256) {
+        const double g = q.g_bf16 ? ld_logit<true>(q.g, j) : ld_logit<false>(q.g, j);
+        if constexpr (STEP) {
+            const double p = q.p_bf16 ? ld_logit<true>(q.p, j) : ld_logit<false>(q.p, j);
+            const float v = static_cast<float>(fma(-factor, g, p));
+            q.p_bf16 ? st_grad<true>(q.p, j, v) : st_grad<false>(q.p, j, v);
+        } else {
+            const float v = static_cast<float>(factor * g);
+            q.g_bf16 ? st_grad<true>(q.g, j, v) : st_grad<false>(q.g, j, v);
+        }
+    }
+}
+
 template <bool STEP> __global__ __launch_bounds__(256) void clip_apply_kernel(const ClipPiece *pieces, unsigned n, const double *sums,
                                                                               unsigned groups, float lr, float max_norm, float *norm_dev) {
     const double norm = whole_norm(sums, groups);
@@ -126,13 +143,16 @@ template <bool STEP> __global__ __launch_bounds__(256) void clip_apply_kernel(co
     const bool clip = norm > static_cast<double>(max_norm);
     if (!STEP && !clip) return;
     const double c = clip ? static_cast<double>(max_norm) / norm : 1.0;
-    const float factor = static_cast<float>(STEP ? static_cast<double>(lr) * c : c);
+    const double whole = STEP ? static_cast<double>(lr) * c : c;
+    const float factor = static_cast<float>(whole);
+    const bool small = whole != 0.0 && fabs(whole) < 0x1p-126;
     if (blockIdx.x >= n) return;
     ClipPiece ahead = pieces[n - 1 - blockIdx.x];
     for (unsigned k = blockIdx.x; k < n; k += gridDim.x) {
         const ClipPiece q = ahead;
         ahead = pieces[n - 1 - min(k + gridDim.x, n - 1)];
-        if constexpr (STEP) {
+        if (small) piece_apply_small<STEP>(q, whole);
+        else if constexpr (STEP) {
             if (q.g_bf16) q.p_bf16 ? piece_apply<true, true, true>(q, factor) : piece_apply<true, true, false>(q, factor);
             else q.p_bf16 ? piece_apply<true, false, true>(q, factor) : piece_apply<true, false, false>(q, factor);
         } else {

@@ -227,3 +227,29 @@ def test_a_tensor_beyond_32_bit_offsets():
     B.clipped_step(t, 1.0, 10.0, norm, *ws_of(B.grad_workspace_bytes(t)))
     torch.cuda.synchronize()
     assert norm.item() == 5.0 and float(P[0]) == -3.0 and float(P[-1]) == -4.0 and float(P[1]) == 0.0
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("gt,pt", [("f32", "f32"), ("bf16", "bf16"), ("f32", "bf16"), ("bf16", "f32")])
+@pytest.mark.parametrize("top,limit,lr", [(3e36, 1e-3, 1e-6), (3e36, 1e-3, -1e-2), (1e36, 1e-5, 1.0), (3e36, 1e-36, 1e5), (1e30, 1e-9, 1e-30), (1e36, 1e38, 1e-43)])
+def test_factors_below_floats_normal_range(gt, pt, top, limit, lr):
+    """norms that are large but finite: the factor has few bits as a float, or none, its product with a gradient all of them.  A product far
+    below the least normal float is off by a step there at most"""
+    import torch
+    m = Model([5000, 1, 33], gt, pt, 1, seed=5, spread=top)
+    m.p *= 0.0
+    m.P.zero_()
+    want = m.want()
+    limit, lr = float(np.float32(limit)), float(np.float32(lr))
+    c = min(1.0, limit / want)
+    step = 2.0 ** -149 if "f32" == pt else 2.0 ** -133
+    B.clipped_step(m.list, lr, limit, m.norm, m.ws, m.size)
+    torch.cuda.synchronize()
+    assert abs(m.norm.item() - want) <= want * EPS * 1.01
+    to = np.where(m.inside, -lr * c * m.g, 0.0)
+    close(m.P.double().cpu().numpy(), to, np.where(m.inside, np.abs(to) * (2 * EPS + HALF[pt]) * 1.001 + 2.0 ** -149 + step, 0.0), "step")
+    step = 2.0 ** -149 if "f32" == gt else 2.0 ** -133
+    B.grad_clip(m.list, limit, m.norm, m.ws, m.size)
+    torch.cuda.synchronize()
+    to = np.where(m.inside, m.g * c, m.g)
+    close(m.G.double().cpu().numpy(), to, np.where(m.inside & (c < 1), np.abs(to) * (2 * EPS + HALF[gt]) * 1.001 + 2.0 ** -149 + step, 0.0), "clip")
