@@ -648,7 +648,7 @@ def linear_act_bwd(M: int, N: int, dY, lddy: int, U, ldu: int, dtype: int, act: 
 
 
 class TensorList:
-    """capgnn_tensors_create on dense tensors (float32 or bfloat16): gradients, and what they belong to (None: gradients alone).  Keeps
+    """capgnn_tensors_create on dense tensors on the GPU (float32 or bfloat16): gradients, and what they belong to (None: gradients alone).  Keeps
     references to the tensors: the list holds their addresses."""
 
     def __init__(self, grads: Sequence, params: Optional[Sequence] = None, stream=None):
@@ -659,6 +659,8 @@ class TensorList:
         kinds = {"torch.float32": F32, "torch.bfloat16": BF16}
         if any(str(t.dtype) not in kinds or not t.is_contiguous() for t in both):
             raise ValueError("dense float32 or bfloat16 tensors are expected")
+        if not all(t.is_cuda for t in both):
+            raise ValueError("tensors on the GPU are expected")
         arrays = lambda ts: ((C.c_void_p * n)(*[t.data_ptr() or None for t in ts]), (C.c_int32 * n)(*[kinds[str(t.dtype)] for t in ts]))
         pg, tg = arrays(grads)
         pp, tp = arrays(params) if params is not None else (None, None)

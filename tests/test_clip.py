@@ -72,6 +72,27 @@ def test_the_list_takes_dense_float_tensors_alone():
         B.TensorList([torch.zeros(4)], [torch.zeros(5)])
 
 
+def test_the_list_takes_tensors_on_the_gpu_alone():
+    """a host address would reach the kernels"""
+    import torch
+    for t in (torch.float32, torch.bfloat16):
+        with pytest.raises(ValueError, match="GPU"):
+            B.TensorList([torch.zeros(4, dtype=t)])
+        with pytest.raises(ValueError, match="GPU"):
+            B.TensorList([torch.zeros(4, dtype=t)], [torch.zeros(4, dtype=t)])
+    with pytest.raises(ValueError, match="GPU"):
+        B.TensorList([torch.zeros(4, device="meta")])
+
+
+@pytest.mark.gpu
+def test_the_list_takes_no_host_tensor_among_others():
+    import torch
+    on = torch.zeros(4, device="cuda")
+    for grads, params in (([on, torch.zeros(4)], None), ([on], [torch.zeros(4)]), ([torch.zeros(4).pin_memory()], [on])):
+        with pytest.raises(ValueError, match="GPU"):
+            B.TensorList(grads, params)
+
+
 # ----------------------------------------------------------------------------- the GPU
 class Model:
     """tensors of given sizes, one after the other in one allocation, each `gap` elements after the last"""
