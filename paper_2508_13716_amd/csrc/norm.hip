@@ -258,26 +258,32 @@ template <bool BF16, int V, int K, int T> __global__ __launch_bounds__(T == 64 ?
     }
 }
 
-// sums[j] = sum over the parts of column j: 16 columns a workgroup, 16 threads each with every 16th part, then their sums in order
-__global__ __launch_bounds__(256) void column_join_kernel(const float *part, int parts, int64_t F, float *sums) {
+// sums[j] = sum over the parts of column j: 16 columns a workgroup, 16 threads each with every 16th part, then their sums in order.
+// Of rows of F columns it takes `columns`.
+__global__ __launch_bounds__(256) void column_join_kernel(const float *part, int parts, int64_t F, int64_t columns, float *sums) {
     __shared__ float s[16][17];
     const int c = threadIdx.x & 15, q = threadIdx.x / 16;
     const int64_t j = int64_t(blockIdx.x) * 16 + c;
     float v = 0.f;
-    if (j < F) {
+    if (j < columns) {
 #pragma unroll 8
         for (int p = q; p < parts; p += 16) v += part[p * F + j];
     }
     s[q][c] = v;
     __syncthreads();
-    if (q == 0 && j < F) {
+    if (q == 0 && j < columns) {
         for (int i = 1; i < 16; ++i) v += s[i][c];
         sums[j] = v;
     }
 }
 int launch_column_join(const float *part, int parts, int64_t F, float *sums, hipStream_t st) {
-    hipLaunchKernelGGL(column_join_kernel, dim3(static_cast<unsigned>((F + 15) / 16)), dim3(256), 0, st, part, parts, F, sums);
-    CG_HIP(hipGetLastError());
+    constexpr int64_t most = int64_t(1) << 27;      // columns of a launch (fewer than 2^32 threads)
+    for (int64_t j = 0; j < F; j += most) {
+        const int64_t columns = std::min(F - j, most);
+        hipLaunchKernelGGL(column_join_kernel, dim3(static_cast<unsigned>((columns + 15) / 16)), dim3(256), 0, st, part ? part + j : nullptr, parts, F, columns,
+                           sums + j);
+        CG_HIP(hipGetLastError());
+    }
     return CAPGNN_OK;
 }
 

@@ -310,6 +310,17 @@ def test_no_rows():
 
 
 @pytest.mark.gpu
+def test_no_rows_of_more_columns_than_a_launch_has_threads_for():
+    """16 threads a column: 2^28 columns and more are several launches"""
+    import torch
+    N = (1 << 28) + 5
+    db = torch.full((N + 3,), 7.0, device="cuda")
+    B.linear_act_bwd(0, N, None, N, None, N, B.F32, B.ACT_GELU, None, N, db, None, 0)
+    torch.cuda.synchronize()
+    assert int(torch.count_nonzero(db)) == 3 and db[N:].tolist() == [7.0] * 3
+
+
+@pytest.mark.gpu
 def test_operands_beyond_32_bit_offsets():
     import torch
     M, K = 4_200_000, 1030                           # A has more than 2^32 elements
