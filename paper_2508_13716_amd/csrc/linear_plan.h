@@ -64,6 +64,7 @@ inline LinearWay linear_way(const LinearPlan &p, int64_t M, int64_t N, int64_t K
     if (p.tile == 0) {
         const int64_t lines = (p.part_k * es + 127) / 128;          // a line of a row per wave and turn
         while (w.waves < FEW_WAVES && w.waves < lines / 4 + 1) w.waves *= 2;
+        while ((N + 15) / 16 * w.waves * 64 >= int64_t(1) << 32 && w.waves > 1) w.waves /= 2;      // (of a launch: fewer than 2^32 threads)
         return w;
     }
     w.cut = es == 4 && rows_of_4 && cut_pays(M, N, K);

@@ -59,6 +59,12 @@ def test_sizes_take_the_tiles_they_are_here_for(ways):
     assert all(w[:3] == (64, 0, 0) for w in ways([(M, N, K, t, False) for M, N, K, t, _ in LARGE]))
 
 
+def test_a_few_rows_by_many_results_are_fewer_threads_than_a_launch_has(ways):
+    sizes = [(M, N, K, t, True) for M in (1, 16) for N in (1, (1 << 25) + 1, (1 << 26) - 16, (1 << 26) - 15, 1 << 26) for K in (1, 1000, 4096) for t in BYTES]
+    for (M, N, K, t, _), w in zip(sizes, ways(sizes)):
+        assert w[0] == 0 and 1 <= w[4] <= 16 and -(-N // 16) * w[4] * 64 < 1 << 32, (M, N, K, t, w)
+
+
 def act(kind, u):
     import torch
     if kind == "gelu":
