@@ -342,3 +342,22 @@ def test_a_scale_that_is_not_finite_leaves_the_gradient_of_rows_that_no_id_names
     assert (got[3:] == (3.0 if accumulate else 0.0)).all()
     assert np.isnan(got[1:3]).all()
     assert np.isnan(got[0]).all() if np.isnan(scale) else (got[0] == scale).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("n,V,F,t", [(9000, 30, 64, "f32"), (200, 20, 16, "f32"), (20_000, 7, 200, "bf16")])
+def test_tables_recorded_and_replayed(n, V, F, t):
+    """tables in LDS, more and less of it than a launch has by itself"""
+    rng = np.random.default_rng(11)
+    ids = dev(some_ids(n, V, rng, "outside"))
+    dY, dtable, more = Mat(rng.standard_normal((n, F)), t), new(V, F, "f32"), Mat(rng.standard_normal((V, F)), "f32")
+    start = more.bits.clone()
+    ws, size = ws_of(B.embed_bwd_workspace_bytes(n, V, F))
+
+    def run(st):
+        import torch
+        with torch.cuda.stream(st):
+            more.bits.copy_(start)
+        B.embed_bwd(n, ids, V, F, dY.p, F, CODE[t], 2.0, dtable.p, F, 0, ws, size, stream=st)
+        B.embed_bwd(n, ids, V, F, dY.p, F, CODE[t], 2.0, more.p, F, 1, ws, size, stream=st)
+    replayed(run, lambda: [dtable.raw(), more.raw()])
