@@ -579,8 +579,9 @@ int capgnn_embed_bwd(int64_t n, const int64_t *ids, int64_t V, int F, const void
  * w: device float[F] or NULL (= 1).  rstd: device float[n] (what the backward pass reads) or NULL.  Y: device [n x ldy] of y_dtype, may be
  * X or R if type and pitch are the same too (and H is not); y comes from the unrounded h.  Everything is formed in float.
  * y_dtype CAPGNN_F32 or CAPGNN_BF16: Y = y, y_scale NULL.  CAPGNN_E4M3: y_scale (device float[n]) = max(max_j |y_j|, 2^-100) / 448 and
- * Y = y / y_scale[i] rounded to nearest even (bytes); a row that holds NaN has a scale of NaN.
- * eps >= 0, finite (with eps = 0 a row of zeros is 0 * infinity = NaN).  F <= CAPGNN_NORM_MAX.  Errors: EINVAL, EUNSUPPORTED (wider rows), EHIP. */
+ * Y = y / y_scale[i] (formed as y * (1 / y_scale[i])) rounded to nearest even (bytes); a row that holds NaN or an infinity has a y of NaN and
+ * with it a scale of NaN.
+ * eps >= 0, finite (with eps = 0 a row of zeros is 0 * infinity = NaN).  A row that holds an infinity has rstd = 0: y is NaN there, 0 elsewhere.  F <= CAPGNN_NORM_MAX.  Errors: EINVAL, EUNSUPPORTED (wider rows), EHIP. */
 int capgnn_rmsnorm(int64_t n, int F, const void *X, int64_t ldx, const void *R, int64_t ldr, void *H, int64_t ldh, int dtype, const float *w,
                    float eps, void *Y, int64_t ldy, int y_dtype, float *y_scale, float *rstd, void *stream);
 
@@ -601,7 +602,8 @@ int capgnn_quantize_rows(int64_t n, int F, const void *X, int64_t ldx, int dtype
  * A: device [M x lda], W: device [N x ldw] (a row of weights per output, so that both run along K), both of `dtype`: CAPGNN_F32, CAPGNN_BF16,
  * or CAPGNN_E4M3 with a_scale (device float[M]) and w_scale (device float[N]), NULL = 1 (NULL for the other types).  Sums in float;
  * with 8-bit operands and a bf16 result the matrix instruction adds eight neighbouring products with a common exponent first, dropping what
- * lies below 2^-13 of the largest (some 1e-5 of a sum's size; with a float result nothing is dropped).
+ * lies below 2^-13 of the largest (less than 7 * 2^-13 of the largest of each eight terms, some 1e-5 of the sum's size where the terms are alike;
+ * where large terms cancel that can be seen: ask for a float result, with which nothing is dropped).
  * bias: device float[N] or NULL.  act: CAPGNN_ACT_*.  R: device [M x ldr] or NULL; U: device [M x ldu] or NULL (kept for the backward
  * pass); Y: device [M x ldy]; all of out_dtype (CAPGNN_F32 or CAPGNN_BF16), each rounded once.  Y may be R (same pitch).
  * fp32 products of 2^28 multiply-adds and more with M > 16 are formed as CAPGNN_F32_PRODUCT_SPLIT forms them (what is not finite, and what lies
@@ -615,6 +617,7 @@ int capgnn_linear(int64_t M, int64_t N, int64_t K, const void *A, int64_t lda, c
 
 /* The epilogue's gradient: dU = dY * act'(U), dbias[j] = sum_i dU[i,j] (of the unrounded dU, in a fixed order).  (R's gradient is dY.  What
  * is left are capgnn_gemm's products of dU: dA = dU W, capgnn_gemm(0, 0, M, K, N, dU, W); dW = dU^T A, capgnn_gemm(1, 0, N, K, M, dU, A).)
+ * GELU's Phi is off by 0.75e-7 at most, here and above.
  * dY, U, dU: device [M x lddy / ldu / lddu] of `dtype` (CAPGNN_F32 or CAPGNN_BF16); U may be NULL for CAPGNN_ACT_NONE; dU may be dY or U
  * (same pitch), or NULL; dbias: device float[N] or NULL.  The slope of ReLU at 0 is 0, every slope at NaN is NaN. */
 size_t capgnn_linear_act_bwd_workspace_bytes(int64_t M, int64_t N);
@@ -625,7 +628,7 @@ int capgnn_linear_act_bwd(int64_t M, int64_t N, const void *dY, int64_t lddy, co
  * (params NULL: a list of gradients alone); counts: host int64[count], elements of each (0 allowed); grad_dtype, param_dtype: host
  * int32[count], CAPGNN_F32 or CAPGNN_BF16 each.  Tensors are dense and aligned to their elements; no tensor that is written may overlap
  * another of the list (EINVAL: two gradients, two params, or a param and a gradient that share memory).  The list holds addresses: the
- * tensors stay allocated while it is used.  Synchronises `stream`.  Errors: EINVAL, ENOMEM, EHIP. */
+ * tensors stay allocated while it is used, and a list that a HIP graph recorded stays until the graph is gone.  Synchronises `stream`.  Errors: EINVAL, ENOMEM, EHIP. */
 typedef struct capgnn_tensors capgnn_tensors;
 int capgnn_tensors_create(capgnn_tensors **t, int count, void *const *grads, const int32_t *grad_dtype, void *const *params,
                           const int32_t *param_dtype, const int64_t *counts, void *stream);
@@ -635,7 +638,7 @@ int capgnn_tensors_destroy(capgnn_tensors *t);
  *   capgnn_grad_norm:    writes the norm.
  *   capgnn_grad_clip:    and multiplies every gradient by c = min(1, max_norm / norm).
  *   capgnn_clipped_step: and updates param <- param - lr * c * g (in float, rounded once to the param's type); the gradients stay.
- * max_norm >= 0 (infinity: c = 1).  A norm that is not finite (a gradient holds infinity or NaN, or it exceeds a float) changes no
+ * max_norm >= 0 (infinity: c = 1).  c and lr * c are formed in double, also where they lie below float's range.  A norm that is not finite (a gradient holds infinity or NaN, or it exceeds a float) changes no
  * gradient and no param.  No handle
  * state changes: calls on one list may be recorded, and may overlap if they write different memory and have workspaces of their own.
  * Errors: EINVAL (no params in the list), ENOMEM (workspace too small), EHIP. */

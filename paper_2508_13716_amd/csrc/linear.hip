@@ -144,9 +144,10 @@ template <int V> __device__ __forceinline__ void finish(const LinearArgs &g, int
 constexpr int UNITS = 8;                // units of a tile's row
 
 // e4m3 operands of a float result.  The 8-bit matrix instructions add the products of eight neighbouring k at a time and drop, toward zero,
-// what lies below 2^-13 of the largest one's power of two (groups of eight are then added in float): 1.3e-5 of a sum's size, nothing
-// beside a bf16 result's rounding, but a hundred times a float's.  So for float results the operands are widened to bf16, exactly, and
-// take the bf16 instruction, at half the rate.
+// what lies below 2^-13 of the largest one's power of two (groups of eight are then added in float): less than 7 * 2^-13 of each group's largest
+// product, 1.3e-5 of a sum's size with normally distributed operands.  Beside a bf16 result's rounding that is nothing (8192 x 8192 x 4096: 1.669e-3
+// off float64, root mean square, with it and without; one result in 190 is rounded the other way), but a hundred times a float's.  So for float
+// results the operands are widened to bf16, exactly, and take the bf16 instruction, at half the rate.
 constexpr int E4M3_FINE = 3;
 // fp32 operands cut into three bf16 numbers each, exactly; the six largest of the nine products go to the bf16 instruction, smallest first, and what
 // is dropped is 2^-23 of a product at most.  Six instructions stand for eight fp32 ones of twice the time.
@@ -783,6 +784,8 @@ extern "C" int capgnn_linear(int64_t M, int64_t N, int64_t K, const void *A, int
             // Eight waves of 128 x 64 fill one another's gaps; 8-bit operands, whose matrix instructions run twice as long, and fp32 ones, which
             // are cut on their way, do with half the reads of four waves of 128 x 128 (us, four / eight: 8192^3 bf16 908 / 855,
             // 8192 x 8192 x 16384 e4m3 831 / 858).  Tiles of 128 leave room for two workgroups a compute unit, those of 64 for three.
+            // A load to LDS takes rows that start on 4 bytes; others go through registers, one step in LDS, in tiles of 64 alone (the row's pitch one
+            // element more: 8192^3 bf16 831 -> 2713, 4096^3 110 -> 327, 8192 x 8192 x 4096 e4m3 245 -> 740).
             if (tile == 256) {
                 if constexpr (d.value == CAPGNN_E4M3 || d.value == F32_CUT) direct(I2, I2, I4, I4, I2);
                 else if constexpr (d.value != CAPGNN_F32) direct(I2, I4, I4, I2, I2);

@@ -69,8 +69,10 @@ inline LinearWay linear_way(const LinearPlan &p, int64_t M, int64_t N, int64_t K
     }
     w.cut = es == 4 && rows_of_4 && cut_pays(M, N, K);
     // One or two steps pay for no loads ahead: through registers more workgroups share a compute unit (us, to LDS / through registers:
-    // 612000 x 47 x 100 bf16 104 / 80, x 128 82 / 65, 100000 x 256 x 100 44 / 37, 8192 x 4096 x 64 48 / 44, 16311 x 2503 x 2 fp32 74 / 63;
-    // two whole steps of larger tiles, 8192 x 4096 x 128 28.2 / 30.6; three steps and more the same or less).
+    // 612000 x 47 x 100 bf16 104 / 80, x 128 82 / 65, 100000 x 256 x 100 44 / 37, 16311 x 2503 x 2 fp32 74 / 63; two whole steps of larger
+    // tiles, 8192 x 4096 x 128 28.2 / 30.6; three steps and more the same or less).  Below 256 bytes larger tiles straight to LDS and those of 64
+    // through registers are near one another: 8192 x 4096 x 64 bf16 25.0 / 26.4, 8192 x 8192 x 64 45 / 48, 180000 x 256 x 64 30.6 / 30.8,
+    // 612000 x 256 x 100 213 / 225, 100000 x 256 x 100 42 / 36, 8192 x 4096 x 16 34.6 / 30.5.
     w.direct = w.cut || (rows_of_4 && K * es >= (p.tile == 64 ? 257 : 256));
     w.tile = !w.direct || (es == 4 && !w.cut) ? 64 : p.tile;
     return w;

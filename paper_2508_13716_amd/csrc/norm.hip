@@ -7,8 +7,9 @@
 // of vectors its last lane takes the row's last V elements: those that the lane before it has, too, are left out of the sums (passed over, not
 // multiplied by 0: one may be an infinity) and stored twice with the same value.  Every sum has a fixed order.
 // us (of the bytes a pass cannot do without): 180000 x 602 fp32 with the residual 331 (5.2 TB/s), 16384 x 4096 bf16 gradient with dH and dw
-// 112, and 7 for the join of dw's parts (4.5 TB/s), one row of 4096 into 8 bits 3.4.  More than 16 elements per lane of the gradient at
-// 1024 threads (rows above 16384) do not fit the registers: up to 540 bytes of scratch memory a thread there.
+// 112, and 7 for the join of dw's parts (4.5 TB/s), one row of 4096 into 8 bits 3.4.  16 elements per lane of the gradient at 1024
+// threads and more (fp32 rows above 8192, bf16 rows above 16384) do not fit the registers: 36 bytes of scratch memory a thread for fp32 rows up to
+// 16384, above that 536 (bf16 368).
 #include "rows.h"
 
 #include <algorithm>
